@@ -264,8 +264,8 @@ def run(state):
         Wq = ctx.group_unscale(s["Zq"], S, s["group"])
         dZq, dS = ctx.group_unscale_backward(s["dWq"], s["Zq"], S, s["group"])
         return {"S": S, "Z": Z, "Wq": Wq, "dZq": dZq, "dS": dS, "dW": ctx.group_scale_backward(Z, S, s["group"], s["dZ"], dS)}
-    loss, lse = ctx.distill(s["logits"], s["index"], s["teacher"], s["tau"])
-    return {"loss": loss, "lse": lse, "dlogits": ctx.distill_backward(s["logits"], s["index"], s["teacher"], s["tau"], lse, s["dloss"])}
+    loss, lse, dlogits = ctx.distill(s["logits"], s["index"], s["teacher"], s["tau"], s["dloss"])
+    return {"loss": loss, "lse": lse, "dlogits": dlogits}
 
 
 # ------------------------------------------------------------------------------------------------ work and values
