@@ -246,6 +246,89 @@ idkm_status idkm_unpack_quantize(idkm_ctx* ctx, const uint32_t* words, int64_t m
                                  float* Wh_out, void* hip_stream);
 
 /*
+ * Products with a layer in its stored form.  The codes of the rows of a [rows, cols] weight matrix, row after row, make the
+ * stream (cols is a multiple of d; idkm_pack_codes of an assign of rows cols / d values).  Weight (r, c) is
+ *   w[r,c] = S[r, c div group] C[code of sub-vector (r cols + c) div d, c mod d]
+ * with S left out where it is NULL.  A code >= k makes its weights NaN, as in idkm_unpack_quantize.
+ * Activations, outputs and the codebook are of one type, dtype; scales, dC and dS are float32.  All sums are float32; results
+ * are rounded once.  Two things are rounded to 16 bits on the way, with 16-bit types and scales only: the product S C where the
+ * layer is written out as a matrix for the matrix cores (many tokens, and dX), to the type, as a stored 16-bit weight is.
+ *
+ *   idkm_codes_linear           Y[t,r] = sum_c X[t,c] w[r,c] for n tokens (n = 0 is a no-op)
+ *   idkm_codes_linear_backward  from dY [n, rows]:  dX[t,c] = sum_r dY[t,r] w[r,c];  with P[r,c] = sum_t dY[t,r] X[t,c],
+ *       dS[r,g] = sum over the group's columns of P[r,c] C[code, c mod d],  dC[j,i] = the sum of S P over the components
+ *       i of all sub-vectors with code j.  dX, dC, dS may each be NULL (not wanted); X may be NULL if dC and dS are.  The
+ *       codes stay as they are.  n = 0 writes zeros to dC and dS.  Results do not depend on the order in which workgroups run.
+ *   ldx, ldy, ...  elements between consecutive rows; pointers are aligned to their element type.  Outputs overlap nothing.
+ *   workspace      device, 16-byte aligned, of at least the number of bytes that the _workspace function of the call gives
+ *       (-1 for arguments that the call refuses; 0: may be NULL).  Its contents mean nothing between calls; calls that may
+ *       run at the same time need one each, and so does every captured graph that may be replayed beside other work.
+ *   Both enqueue on hip_stream, do not wait, allocate nothing and can be captured into a graph.
+ * Limits: 1 <= k <= 1024, 1 <= d <= 64; a group shorter than a row is a multiple of 32 and of d (any group >= cols: one scale
+ * a row); rows, cols, n <= 4,000,000, rows cols <= 2^36.  Fast for up to 64 tokens: k <= 256 with d in {1, 2, 4, 8}.
+ */
+typedef enum { IDKM_F32 = 0, IDKM_F16 = 1, IDKM_BF16 = 2 } idkm_dtype;
+typedef struct {
+    const uint32_t* words; /* device, idkm_code_words(rows * cols / d, k) words */
+    int64_t rows, cols;
+    const void* C; /* device [k,d], dtype */
+    int32_t k, d;
+    const float* S; /* device [rows, ceil(cols / group)], or NULL */
+    int32_t group;
+    int32_t dtype; /* idkm_dtype of C, X, Y, dX, dY */
+} idkm_codes_desc;
+int64_t idkm_codes_linear_workspace(const idkm_codes_desc* w, int64_t n);
+idkm_status idkm_codes_linear(idkm_ctx* ctx, const idkm_codes_desc* w, const void* X, int64_t n, int64_t ldx, void* Y,
+                              int64_t ldy, void* workspace, int64_t workspace_bytes, void* hip_stream);
+int64_t idkm_codes_linear_backward_workspace(const idkm_codes_desc* w, int64_t n);
+idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, const void* X, int64_t ldx, const void* dY,
+                                       int64_t lddy, int64_t n, void* dX, int64_t lddx, float* dC, float* dS,
+                                       void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/*
+ * Scales of groups: a layer whose rows or parts of rows differ in size is divided by the root mean square of each group of
+ * `group` consecutive weights of a row (the last one of a row may be shorter) before it is clustered, so that one codebook and one
+ * temperature serve all of it, and multiplied by it afterwards.  All tensors float32, contiguous: W, Z, Zq [rows, cols],
+ * S [rows, ceil(cols / group)].
+ *   idkm_group_scale             S = sqrt(mean of W^2 over the group),  Z = W / S   (0 in a group of zeros)
+ *   idkm_group_unscale           Wq = S Zq
+ *   idkm_group_unscale_backward  dZq = S dWq,  dS = sum over the group of dWq Zq
+ *   idkm_group_scale_backward    dW = dZ / S + Z / count (dS - sum over the group of dZ Z / S)   (0 in a group of zeros);
+ *                                dS NULL: zero
+ * The [rows, cols] output may be the call's first [rows, cols] input (dZ in the last one).  Enqueue on hip_stream, do not wait;
+ * rows = 0 is a no-op.  rows cols <= 2^36.
+ */
+idkm_status idkm_group_scale(idkm_ctx* ctx, const float* W, int64_t rows, int64_t cols, int64_t group, float* S_out,
+                             float* Z_out, void* hip_stream);
+idkm_status idkm_group_unscale(idkm_ctx* ctx, const float* Zq, const float* S, int64_t rows, int64_t cols, int64_t group,
+                               float* Wq_out, void* hip_stream);
+idkm_status idkm_group_unscale_backward(idkm_ctx* ctx, const float* dWq, const float* Zq, const float* S, int64_t rows,
+                                        int64_t cols, int64_t group, float* dZq_out, float* dS_out, void* hip_stream);
+idkm_status idkm_group_scale_backward(idkm_ctx* ctx, const float* Z, const float* S, const float* dZ, const float* dS,
+                                      int64_t rows, int64_t cols, int64_t group, float* dW_out, void* hip_stream);
+
+/*
+ * Loss of a quantised network against the network it was made from: Kullback-Leibler divergence of the student's softmax from
+ * the softmax of the teacher's largest logits, and its gradient.  For each of n rows of logits z (V of them, rows ldz
+ * elements apart, type dtype) the teacher's list holds up to `top` pairs (index, value); an entry with a negative index is none.
+ *   p = softmax(teacher / tau) over the row's entries (entries of one index add up),  q = softmax(z / tau) over all V
+ *   loss_out[t] = sum p (log p - log q),   lse_out[t] = log sum exp(z / tau)
+ *   dlogits_out[t,v] = weight[t] / tau (q_v - p_v): the gradient of sum_t weight[t] loss[t]
+ * A row without entries, or whose entries are all -inf, has loss 0 and gradient 0, whatever its logits are; an index >= V or a
+ * NaN in a row's list makes its loss and gradient NaN.  Logits of -inf have q = 0.
+ *   weight, dlogits_out  device [n] float32 and [n,V] (rows ldd apart), both or neither NULL (neither: loss and lse only).
+ *                        dlogits_out may be logits itself, with ldd = ldz.
+ *   index, teacher       device [n,top] int32 and float32, 1 <= top <= 1024.
+ *   workspace            as for idkm_codes_linear, of idkm_distill_workspace bytes.
+ * Enqueues on hip_stream, does not wait; n = 0 is a no-op.  Logits and gradient are aligned to their element type.
+ */
+int64_t idkm_distill_workspace(int64_t n, int64_t V, int32_t top, int32_t dtype);
+idkm_status idkm_distill(idkm_ctx* ctx, const void* logits, int64_t n, int64_t V, int64_t ldz, idkm_dtype dtype,
+                         const int32_t* index, const float* teacher, int32_t top, float tau, const float* weight,
+                         float* loss_out, float* lse_out, void* dlogits_out, int64_t ldd, void* workspace,
+                         int64_t workspace_bytes, void* hip_stream);
+
+/*
  * Batched calls for the per-layer loops of Algorithm 2 ("for all layers: find C*(W)" and the matching backward
  * loop).  The layers are independent problems.  A batch owns one context per layer; layers that the persistent
  * path serves and that share a kernel shape (k, d, dist) are solved by ONE launch in which every layer has its own

@@ -24,6 +24,9 @@ PATH_AUTO, PATH_STREAM, PATH_PERSISTENT = 0, 1, 2
 EXPORTS = ["idkm_version", "idkm_limits", "idkm_status_string", "idkm_create", "idkm_destroy", "idkm_last_error",
            "idkm_set_path", "idkm_set_matrix_cores", "idkm_set_tile_limit", "idkm_set_spin_limit", "idkm_set_kernel_timing", "idkm_last_kernel_ms", "idkm_set_gmres_basis", "idkm_advance_sequence", "idkm_forward", "idkm_backward", "idkm_step_F", "idkm_step_JCT", "idkm_get_cotangents", "idkm_forward_noalloc", "idkm_noalloc_last_error",
            "idkm_calibrate", "idkm_code_bits", "idkm_code_words", "idkm_pack_codes", "idkm_unpack_quantize",
+           "idkm_codes_linear_workspace", "idkm_codes_linear", "idkm_codes_linear_backward_workspace",
+           "idkm_codes_linear_backward", "idkm_group_scale", "idkm_group_unscale", "idkm_group_unscale_backward",
+           "idkm_group_scale_backward", "idkm_distill_workspace", "idkm_distill",
            "idkm_batch_create", "idkm_batch_destroy", "idkm_batch_last_error", "idkm_batch_launches",
            "idkm_batch_context", "idkm_batch_forward", "idkm_batch_backward"]
 
@@ -42,6 +45,11 @@ class IdkmFwdDesc(C.Structure):
 class IdkmBwdDesc(C.Structure):
     _fields_ = [("dWq", C.c_void_p), ("mode", C.c_int32), ("tol", C.c_float), ("max_iter", C.c_int32),
                 ("alpha", C.c_float), ("dW_out", C.c_void_p)]
+
+
+class IdkmCodesDesc(C.Structure):
+    _fields_ = [("words", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("C", C.c_void_p), ("k", C.c_int32),
+                ("d", C.c_int32), ("S", C.c_void_p), ("group", C.c_int32), ("dtype", C.c_int32)]
 
 
 class IdkmLimits(C.Structure):
@@ -121,6 +129,27 @@ def load_library():
     lib.idkm_pack_codes.restype = C.c_int
     lib.idkm_unpack_quantize.argtypes = [vp, vp, C.c_int64, f32p, C.c_int32, C.c_int32, f32p, vp]
     lib.idkm_unpack_quantize.restype = C.c_int
+    i64, i32, desc = C.c_int64, C.c_int32, C.POINTER(IdkmCodesDesc)
+    lib.idkm_codes_linear_workspace.argtypes = [desc, i64]
+    lib.idkm_codes_linear_workspace.restype = i64
+    lib.idkm_codes_linear.argtypes = [vp, desc, vp, i64, i64, vp, i64, vp, i64, vp]
+    lib.idkm_codes_linear.restype = C.c_int
+    lib.idkm_codes_linear_backward_workspace.argtypes = [desc, i64]
+    lib.idkm_codes_linear_backward_workspace.restype = i64
+    lib.idkm_codes_linear_backward.argtypes = [vp, desc, vp, i64, vp, i64, i64, vp, i64, vp, vp, vp, i64, vp]
+    lib.idkm_codes_linear_backward.restype = C.c_int
+    lib.idkm_group_scale.argtypes = [vp, vp, i64, i64, i64, vp, vp, vp]
+    lib.idkm_group_scale.restype = C.c_int
+    lib.idkm_group_unscale.argtypes = [vp, vp, vp, i64, i64, i64, vp, vp]
+    lib.idkm_group_unscale.restype = C.c_int
+    lib.idkm_group_unscale_backward.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, vp, vp]
+    lib.idkm_group_unscale_backward.restype = C.c_int
+    lib.idkm_group_scale_backward.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, vp, vp]
+    lib.idkm_group_scale_backward.restype = C.c_int
+    lib.idkm_distill_workspace.argtypes = [i64, i64, i32, i32]
+    lib.idkm_distill_workspace.restype = i64
+    lib.idkm_distill.argtypes = [vp, vp, i64, i64, i64, C.c_int, vp, vp, i32, C.c_float, vp, vp, vp, vp, i64, vp, i64, vp]
+    lib.idkm_distill.restype = C.c_int
     lib.idkm_batch_create.argtypes = [C.POINTER(vp), C.c_int, C.c_int32]
     lib.idkm_batch_create.restype = C.c_int
     lib.idkm_batch_destroy.argtypes = [vp]
@@ -168,6 +197,75 @@ def _ptr(t, dtype, shape, name):
 def _stream():
     import torch
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+F32, F16, BF16 = 0, 1, 2
+
+
+def _dtype(t, name):
+    import torch
+    code = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32, float16 or bfloat16, got {t.dtype}")
+    return code
+
+
+def _rows(t, dtype, width, device, name):
+    """Checks a matrix [n, width] on `device` whose rows may lie further apart than their length; elements between rows."""
+    if not t.is_cuda or t.device.index != device:
+        raise TypeError(f"{name} must be in the memory of device {device}")
+    if t.dtype != dtype or t.dim() != 2 or t.shape[1] != width:
+        raise TypeError(f"{name} must be {dtype} of shape (n, {width}), got {t.dtype} {tuple(t.shape)}")
+    n, ld = t.shape[0], t.stride(0)
+    if (width > 1 and t.stride(1) != 1) or (n > 1 and ld < width):
+        raise TypeError(f"{name} must have contiguous rows that do not overlap")
+    return ld if n > 1 else width
+
+
+class CodesLayer:
+    """A [rows, cols] layer in its stored form: `words` of Context.pack_codes of its rows' codes, one row after another, the
+    codebook C [k,d] in the type of the activations, and optionally float32 scales S [rows, ceil(cols / group)] of groups of
+    `group` weights of a row.  Holds the tensors; they may be changed in place between calls (not `words`' meaning)."""
+
+    def __init__(self, words, rows, cols, Cb, S=None, group=0):
+        import torch
+        k, d = Cb.shape
+        rows, cols, group = int(rows), int(cols), int(group)
+        if cols < 1 or rows < 1 or cols % d:
+            raise ValueError(f"rows and cols must be at least 1 and cols a multiple of d = {d}, got {rows} x {cols}")
+        if (S is None) != (group == 0) or group < 0:
+            raise ValueError("scales and their group go together")
+        if S is not None and group < cols and (group % 32 or group % d):
+            raise ValueError("a group shorter than a row must be a multiple of 32 and of d")
+        self.dtype, self.code = Cb.dtype, _dtype(Cb, "C")
+        self.device = Cb.device.index
+        p = _ptr(Cb, Cb.dtype, (k, d), "C")
+        nwords = code_words(rows * cols // d, k)
+        if nwords < 0:
+            raise ValueError(f"a codebook of {k} codewords is not supported")
+        w = _ptr(words, torch.int32, (nwords,), "words")
+        groups = -(-cols // group) if group else 0
+        s = _ptr(S, torch.float32, (rows, groups), "S")
+        for t in (words, S):
+            if t is not None and t.device.index != self.device:
+                raise TypeError("words, C and S must be on one device")
+        self.rows, self.cols, self.k, self.d, self.group, self.groups = rows, cols, k, d, group, groups
+        self.words, self.C, self.S = words, Cb, S
+        self._desc = IdkmCodesDesc(w, rows, cols, p, k, d, s, min(group, 2**31 - 1), self.code)
+        self._at = C.byref(self._desc)
+        self._bytes = {}  # workspace sizes by (call, tokens)
+
+    def workspace_bytes(self, n, backward=False):
+        """Bytes that codes_linear (or codes_linear_backward) of n tokens works in; raises for a layer it refuses."""
+        key = (n, backward)
+        b = self._bytes.get(key)
+        if b is None:
+            lib = load_library()
+            b = (lib.idkm_codes_linear_backward_workspace if backward else lib.idkm_codes_linear_workspace)(self._at, n)
+            if len(self._bytes) > 4096:
+                self._bytes.clear()
+            self._bytes[key] = b
+        return b
 
 
 class Context:
@@ -306,6 +404,149 @@ class Context:
                                             _ptr(out, torch.float32, (m, d), "Wh_out"), _stream())
         self._check(st)
         return out
+
+    def _on(self, *named):
+        """Checks that tensors are contiguous float32 matrices or vectors on this context's device."""
+        import torch
+        for name, t, shape in named:
+            if t is None:
+                continue
+            _ptr(t, torch.float32, shape, name)
+            if t.device.index != self.device:
+                raise TypeError(f"{name} must be in the memory of device {self.device}")
+
+    def _stream(self):
+        import torch
+        return torch._C._cuda_getCurrentRawStream(self.device)
+
+    def codes_linear(self, layer, X, out=None):
+        """idkm_codes_linear: X [n, cols] in the layer's type -> X w^T [n, rows].  Rows of X and `out` may lie apart."""
+        import torch
+        if layer.device != self.device:
+            raise TypeError(f"the layer must be in the memory of device {self.device}")
+        ldx = _rows(X, layer.dtype, layer.cols, self.device, "X")
+        n = X.shape[0]
+        if out is None:
+            out = torch.empty((n, layer.rows), dtype=layer.dtype, device=X.device)
+            ldy = layer.rows
+        else:
+            ldy = _rows(out, layer.dtype, layer.rows, self.device, "out")
+            if out.shape[0] != n:
+                raise TypeError(f"out must have {n} rows")
+        need = layer.workspace_bytes(n)
+        ws = torch.empty((need,), dtype=torch.uint8, device=X.device) if need > 0 else None
+        self._check(self._lib.idkm_codes_linear(self._h, layer._at, X.data_ptr(), n, ldx, out.data_ptr(), ldy,
+                                                ws.data_ptr() if need > 0 else None, need, self._stream()))
+        return out
+
+    def codes_linear_backward(self, layer, X, dY, want_dX=True, want_dC=True, want_dS=True):
+        """idkm_codes_linear_backward: dict of dX [n, cols] in the layer's type and float32 dC [k, d] and, for a layer with
+        scales, dS [rows, groups].  X may be None if only dX is wanted."""
+        import torch
+        if layer.device != self.device:
+            raise TypeError(f"the layer must be in the memory of device {self.device}")
+        ldy = _rows(dY, layer.dtype, layer.rows, self.device, "dY")
+        n = dY.shape[0]
+        want_dS = want_dS and layer.S is not None
+        ldx = 0
+        if X is not None:
+            ldx = _rows(X, layer.dtype, layer.cols, self.device, "X")
+            if X.shape[0] != n:
+                raise TypeError(f"X must have {n} rows")
+        elif want_dC or want_dS:
+            raise TypeError("X is needed for dC and dS")
+        res = {}
+        if want_dX:
+            res["dX"] = torch.empty((n, layer.cols), dtype=layer.dtype, device=dY.device)
+        if want_dC:
+            res["dC"] = torch.empty((layer.k, layer.d), dtype=torch.float32, device=dY.device)
+        if want_dS:
+            res["dS"] = torch.empty((layer.rows, layer.groups), dtype=torch.float32, device=dY.device)
+        need = layer.workspace_bytes(n, True)
+        ws = torch.empty((need,), dtype=torch.uint8, device=dY.device) if need > 0 else None
+        at = {key: t.data_ptr() for key, t in res.items()}
+        self._check(self._lib.idkm_codes_linear_backward(
+            self._h, layer._at, X.data_ptr() if X is not None else None, ldx, dY.data_ptr(), ldy, n, at.get("dX"), layer.cols,
+            at.get("dC"), at.get("dS"), ws.data_ptr() if need > 0 else None, need, self._stream()))
+        return res
+
+    def group_scale(self, W, group):
+        """idkm_group_scale: W [rows, cols] float32 -> (S [rows, ceil(cols / group)], Z = W / S)."""
+        import torch
+        rows, cols = W.shape
+        self._on(("W", W, (rows, cols)))
+        group = max(int(group), 0)
+        S = torch.empty((rows, -(-cols // max(group, 1))), dtype=torch.float32, device=W.device)
+        Z = torch.empty_like(W)
+        self._check(self._lib.idkm_group_scale(self._h, W.data_ptr(), rows, cols, group, S.data_ptr(), Z.data_ptr(), self._stream()))
+        return S, Z
+
+    def group_unscale(self, Zq, S, group):
+        """idkm_group_unscale: S Zq."""
+        import torch
+        rows, cols = Zq.shape
+        self._on(("Zq", Zq, (rows, cols)), ("S", S, (rows, -(-cols // max(int(group), 1)))))
+        Wq = torch.empty_like(Zq)
+        self._check(self._lib.idkm_group_unscale(self._h, Zq.data_ptr(), S.data_ptr(), rows, cols, int(group), Wq.data_ptr(),
+                                                 self._stream()))
+        return Wq
+
+    def group_unscale_backward(self, dWq, Zq, S, group):
+        """idkm_group_unscale_backward: (dZq, dS)."""
+        import torch
+        rows, cols = Zq.shape
+        self._on(("dWq", dWq, (rows, cols)), ("Zq", Zq, (rows, cols)), ("S", S, (rows, -(-cols // max(int(group), 1)))))
+        dZq, dS = torch.empty_like(Zq), torch.empty_like(S)
+        self._check(self._lib.idkm_group_unscale_backward(self._h, dWq.data_ptr(), Zq.data_ptr(), S.data_ptr(), rows, cols, int(group),
+                                                          dZq.data_ptr(), dS.data_ptr(), self._stream()))
+        return dZq, dS
+
+    def group_scale_backward(self, Z, S, group, dZ, dS=None):
+        """idkm_group_scale_backward: dW from the gradients of Z and, optionally, of S."""
+        import torch
+        rows, cols = Z.shape
+        shape = (rows, -(-cols // max(int(group), 1)))
+        self._on(("Z", Z, (rows, cols)), ("dZ", dZ, (rows, cols)), ("S", S, shape), ("dS", dS, shape))
+        dW = torch.empty_like(Z)
+        self._check(self._lib.idkm_group_scale_backward(self._h, Z.data_ptr(), S.data_ptr(), dZ.data_ptr(),
+                                                        dS.data_ptr() if dS is not None else None, rows, cols, int(group),
+                                                        dW.data_ptr(), self._stream()))
+        return dW
+
+    def distill(self, logits, index, teacher, tau, weight=None, out=None):
+        """idkm_distill: (loss [n], lse [n]) of logits [n, V] against the teacher's list (index int32, teacher float32, both
+        [n, top]; a negative index is no entry), and with weight [n] also the gradient of (weight * loss).sum() in the
+        logits; `out` (which may be the logits themselves) receives it."""
+        import torch
+        code = _dtype(logits, "logits")
+        if logits.dim() != 2 or index.dim() != 2:
+            raise TypeError("logits and index must be matrices")
+        n, V = logits.shape
+        top = index.shape[1]
+        ldz = _rows(logits, logits.dtype, V, self.device, "logits")
+        self._on(("teacher", teacher, (n, top)), ("weight", weight, (n,)))
+        _ptr(index, torch.int32, (n, top), "index")
+        if index.device.index != self.device:
+            raise TypeError(f"index must be in the memory of device {self.device}")
+        loss = torch.empty((n,), dtype=torch.float32, device=logits.device)
+        lse = torch.empty((n,), dtype=torch.float32, device=logits.device)
+        ldd = V
+        if weight is None:
+            if out is not None:
+                raise TypeError("the gradient needs weights")
+        elif out is None:
+            out = torch.empty((n, V), dtype=logits.dtype, device=logits.device)
+        else:
+            ldd = _rows(out, logits.dtype, V, self.device, "out")
+            if out.shape[0] != n:
+                raise TypeError(f"out must have {n} rows")
+        need = self._lib.idkm_distill_workspace(n, V, top, code)
+        ws = torch.empty((need,), dtype=torch.uint8, device=logits.device) if need > 0 else None
+        self._check(self._lib.idkm_distill(self._h, logits.data_ptr(), n, V, ldz, code, index.data_ptr(), teacher.data_ptr(), top,
+                                           float(tau), weight.data_ptr() if weight is not None else None, loss.data_ptr(),
+                                           lse.data_ptr(), out.data_ptr() if out is not None else None, ldd,
+                                           ws.data_ptr() if need > 0 else None, need, self._stream()))
+        return (loss, lse) if weight is None else (loss, lse, out)
 
     def step_F(self, W, Cb, tau, dist):
         """idkm_step_F: one evaluation of F at Cb.  Returns (C+ [k,d], n [k])."""

@@ -1471,6 +1471,17 @@ idkm_status idkm_unpack_quantize(idkm_ctx* ctx, const uint32_t* words, int64_t m
     return IDKM_OK;
 }
 
+}  // extern "C"
+
+namespace idkm {
+
+int context_device(const idkm_ctx* ctx) { return ctx->device; }
+void context_error(idkm_ctx* ctx, const char* msg) { ctx->err = msg; }
+
+}  // namespace idkm
+
+extern "C" {
+
 #ifdef IDKM_TRACE
 // development builds only: device buffer of 2*64*8 int64 clock stamps filled by the persistent forward kernel
 idkm_status idkm_debug_trace(idkm_ctx* ctx, long long* dev_buf) {

@@ -1,0 +1,65 @@
+// Host-side lookup of the kernels for coded layers, group scales and the loss against a teacher, and their arguments.
+#pragma once
+#include "codes_gradient.hpp"
+#include "codes_product.hpp"
+#include "tile_product.hpp"
+
+namespace idkm {
+
+// Few tokens, straight from the codes.  B bits a code, d in {1, 2, 4, 8}, L weights of a row to a lane at a time (8, 32),
+// NT in {1, 4}; aligned: every run of codes begins with a word.  nullptr if not instantiated.
+typedef void (*ProductFn)(const ProductArgs);
+ProductFn codes_product_kernel(int dtype, int B, int d, int L, int NT, bool aligned);
+int codes_product_table_bytes(int dtype, int B, int d);
+
+struct TileShape {
+    int bm, bn, threads;
+    size_t lds;
+    void (*fn)(const TileArgs);
+};
+constexpr int TILE_SHAPES = 4;
+// The shapes of a type's tile product, largest first.
+TileShape tile_shape(int dtype, int which);
+
+void launch_dense_rows(int dtype, const DenseArgs& a, hipStream_t s);
+void launch_dense_cols(int dtype, const DenseArgs& a, hipStream_t s);
+void launch_pad_rows(int dtype, const void* in, int64_t ldi, int64_t M, int64_t N, void* out, int64_t pad, hipStream_t s);
+void launch_transpose(int dtype, const void* in, int64_t ldi, int64_t M, int64_t N, void* out, int64_t pad, hipStream_t s);
+void launch_join_parts(int dtype, const float* parts, int nz, int64_t M, int64_t N, void* out, int64_t ldo, hipStream_t s);
+void launch_codes_bins(int dtype, const BinArgs& a, int grid, int waves, hipStream_t s);
+void launch_fill_zero(float* out, int64_t n, hipStream_t s);
+void launch_join_bins(const float* bins, int nwg, int kd, float* dC, hipStream_t s);
+
+constexpr int SCALE_FWD = 0, UNSCALE_FWD = 1, UNSCALE_BWD = 2, SCALE_BWD = 3;
+struct ScaleArgs {
+    int64_t rows, cols, group, groups;
+    const float* x;   // W, Zq, dWq, dZ
+    const float* y;   // UNSCALE_BWD: Zq, SCALE_BWD: Z
+    const float* S;   // all but SCALE_FWD
+    const float* dS;  // SCALE_BWD, or null
+    float* out;       // Z, Wq, dZq, dW
+    float* s_out;     // SCALE_FWD: S, UNSCALE_BWD: dS
+};
+void launch_group_scale(int op, const ScaleArgs& a, hipStream_t s);
+
+struct DistillArgs {
+    const void* logits;  // T [n, ldz]
+    int64_t n, V, ldz;
+    const int32_t* index;  // [n, top]
+    const float* teacher;  // [n, top]
+    int top;
+    float tau;
+    const float* weight;  // [n] or null
+    float* loss;          // [n]
+    float* lse;           // [n]
+    void* dlogits;        // T [n, ldd] or null
+    int64_t ldd;
+    int64_t part;   // columns of a part
+    int parts;      // workgroups that share a row; 0: a row stays in one
+    float* stats;   // [n, parts, 2]
+    float* listed;  // [n, top]
+};
+void distill_plan(int64_t n, int64_t V, int esize, int64_t* part, int* parts);
+void launch_distill(int dtype, const DistillArgs& a, hipStream_t s);
+
+}  // namespace idkm

@@ -1,0 +1,583 @@
+// C entry points of the operators on coded layers (products and their gradients), group scales and the loss against a
+// teacher: checks of arguments, choice of kernels, layout of the caller's workspace.
+#include <climits>
+#include <cmath>
+#include <cstdint>
+#include <cstdio>
+#include <exception>
+#include <new>
+
+#include "../../include/idkm.h"
+#include "layers.h"
+
+namespace idkm {
+
+int context_device(const idkm_ctx* ctx);
+void context_error(idkm_ctx* ctx, const char* msg);
+
+ProductFn codes_product_kernel_1(int, int, int, int, bool);
+ProductFn codes_product_kernel_2(int, int, int, int, bool);
+ProductFn codes_product_kernel_3(int, int, int, int, bool);
+ProductFn codes_product_kernel_4(int, int, int, int, bool);
+ProductFn codes_product_kernel_5(int, int, int, int, bool);
+ProductFn codes_product_kernel_6(int, int, int, int, bool);
+ProductFn codes_product_kernel_7(int, int, int, int, bool);
+ProductFn codes_product_kernel_8(int, int, int, int, bool);
+
+ProductFn codes_product_kernel(int dtype, int B, int d, int L, int NT, bool aligned) {
+    static ProductFn (*const by_bits[8])(int, int, int, int, bool) = {
+        codes_product_kernel_1, codes_product_kernel_2, codes_product_kernel_3, codes_product_kernel_4,
+        codes_product_kernel_5, codes_product_kernel_6, codes_product_kernel_7, codes_product_kernel_8};
+    return B >= 1 && B <= 8 ? by_bits[B - 1](dtype, d, L, NT, aligned) : nullptr;
+}
+
+int codes_product_table_bytes(int dtype, int B, int d) {
+    const int c = codes_at_once(B, d);
+    return (1 << (c * B)) * c * d * (dtype == IDKM_F32 ? 4 : 2);
+}
+
+}  // namespace idkm
+
+using namespace idkm;
+
+namespace {
+
+constexpr int64_t MAX_SIDE = 4000000;      // rows, columns, tokens: 64 of them to a workgroup fit one grid dimension
+constexpr int64_t PANEL = (int64_t)1 << 26;  // weights of a layer that are written out at a time
+
+idkm_status refuse(idkm_ctx* ctx, idkm_status s, const char* msg) {
+    if (ctx) context_error(ctx, msg);
+    return s;
+}
+
+// The context's device is the current one inside; the caller's is again after it.
+struct OnDevice {
+    int before = -1;
+    bool ok = false;
+    explicit OnDevice(int device) {
+        if (hipGetDevice(&before) != hipSuccess) return;
+        ok = before == device || hipSetDevice(device) == hipSuccess;
+        if (before == device) before = -1;
+    }
+    ~OnDevice() {
+        if (ok && before >= 0) (void)hipSetDevice(before);
+    }
+};
+
+// Runs body() on the context's device; no exception leaves a C entry point.
+template <class Body>
+idkm_status entry(idkm_ctx* ctx, Body body) noexcept {
+    if (!ctx) return IDKM_ERR_INVALID_ARG;
+    try {
+        context_error(ctx, "");
+        return body();
+    } catch (const std::bad_alloc&) {
+        return IDKM_ERR_ALLOC;
+    } catch (...) {
+        return IDKM_ERR_DEVICE;
+    }
+}
+
+template <class Launches>
+idkm_status launched(idkm_ctx* ctx, Launches launches) {
+    OnDevice on(context_device(ctx));
+    if (!on.ok) {
+        (void)hipGetLastError();
+        return refuse(ctx, IDKM_ERR_DEVICE, "the context's device cannot be made current");
+    }
+    launches();
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? IDKM_OK : refuse(ctx, IDKM_ERR_DEVICE, hipGetErrorString(e));
+}
+
+int64_t up_to(int64_t x, int64_t unit) { return (x + unit - 1) / unit * unit; }
+int esize_of(int dtype) { return dtype == IDKM_F32 ? 4 : 2; }
+bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+const char* wrong_layer(const idkm_codes_desc* w, idkm_status* st) {
+    *st = IDKM_ERR_INVALID_ARG;
+    if (!w) return "the layer must be non-NULL";
+    if (!w->words || !w->C) return "words and C must be non-NULL";
+    if (w->dtype != IDKM_F32 && w->dtype != IDKM_F16 && w->dtype != IDKM_BF16) return "dtype must be an idkm_dtype";
+    if (w->rows < 1 || w->cols < 1) return "rows and cols must be >= 1";
+    if (w->k < 1 || w->k > 1024 || w->d < 1 || w->d > 64) return "need 1 <= k <= 1024 and 1 <= d <= 64";
+    if (w->cols % w->d != 0) return "cols must be a multiple of d";
+    if (w->S) {
+        if (w->group < 1) return "group must be >= 1 where there are scales";
+        if (w->group < w->cols && (w->group % 32 != 0 || w->group % w->d != 0))
+            return "a group shorter than a row must be a multiple of 32 and of d";
+        if (!aligned_to(w->S, 4)) return "S must be aligned to its type";
+    }
+    if (!aligned_to(w->words, 4) || !aligned_to(w->C, esize_of(w->dtype))) return "words and C must be aligned to their types";
+    *st = IDKM_ERR_UNSUPPORTED;
+    if (w->rows > MAX_SIDE || w->cols > MAX_SIDE || w->rows * w->cols > ((int64_t)1 << 36)) return "the layer is too large";
+    return nullptr;
+}
+
+int groups_of(const idkm_codes_desc& w) { return w.S ? (int)((w.cols + w.group - 1) / w.group) : 0; }
+
+// ---- few tokens
+
+struct FewPlan {
+    ProductFn fn = nullptr;
+    int NT, waves;
+    dim3 grid;
+    size_t lds;
+};
+
+// Up to 64 tokens are computed straight from the codes.
+constexpr int64_t FEW_TOKENS = 64;
+
+FewPlan few_plan(const idkm_codes_desc& w, int64_t n) {
+    FewPlan p;
+    const int bits = idkm_code_bits(w.k);
+    if (n > FEW_TOKENS || bits > 8 || (w.d != 1 && w.d != 2 && w.d != 4 && w.d != 8)) return p;
+    // a chunk of four runs has to lie in one group
+    const int L = !w.S || w.group >= w.cols || w.group % 128 == 0 ? 32 : 8;
+    const bool aligned = (w.cols / w.d * bits) % 32 == 0 && (32 / w.d * bits) % 32 == 0;
+    p.NT = n <= 16 ? 1 : 4;
+    p.fn = codes_product_kernel(w.dtype, bits, w.d, L, p.NT, aligned);
+    const int64_t chunks = (w.cols + 4 * L - 1) / (4 * L);
+    p.waves = chunks < 8 ? (int)chunks : 8;
+    p.grid = dim3((unsigned)((w.rows + 15) / 16), (unsigned)((n + 16 * p.NT - 1) / (16 * p.NT)));
+    p.lds = codes_product_table_bytes(w.dtype, bits, w.d);
+    if (p.lds < (size_t)p.waves * p.NT * 1024) p.lds = (size_t)p.waves * p.NT * 1024;
+    return p;
+}
+
+// ---- tile products
+
+struct TilePlan {
+    int which, parts;
+};
+
+// The largest tile that gives most of the 256 compute units one; the smallest splits the sum where there are few of them.
+TilePlan tile_plan(int64_t M, int64_t N, int64_t steps, int dtype) {
+    for (int s = 0; s < TILE_SHAPES; ++s) {
+        const TileShape t = tile_shape(dtype, s);
+        const int64_t tiles = ((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn);
+        if (tiles >= 200) return TilePlan{s, 1};
+        if (s + 1 == TILE_SHAPES) {
+            int64_t parts = (256 + tiles - 1) / tiles;
+            if (parts > steps / 4) parts = steps / 4;
+            if (parts > 16) parts = 16;
+            return TilePlan{s, parts < 1 ? 1 : (int)parts};
+        }
+    }
+    return TilePlan{0, 1};
+}
+
+void run_tile(int dtype, const TilePlan& p, const TileArgs& args, hipStream_t s) {
+    const TileShape t = tile_shape(dtype, p.which);
+    TileArgs a = args;
+    a.tiles_m = (int)((a.M + t.bm - 1) / t.bm);
+    a.tiles_n = (int)((a.N + t.bn - 1) / t.bn);
+    if (t.lds > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(t.fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)t.lds);
+    hipLaunchKernelGGL(t.fn, dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)p.parts), dim3((unsigned)t.threads), t.lds, s, a);
+}
+
+// Bytes of a buffer in the workspace.
+int64_t buffer(int64_t elements, int esize) { return up_to(elements * esize, 256); }
+
+// out[M, N] in T (rows ldo apart): in one part, or in several that are joined.
+void run_product(int dtype, const TilePlan& p, TileArgs a, void* out, int64_t ldo, float* parts, hipStream_t s) {
+    a.wide = p.parts > 1;
+    a.out = a.wide ? (void*)parts : out;
+    a.ldo = a.wide ? a.N : ldo;
+    run_tile(dtype, p, a, s);
+    if (p.parts > 1) launch_join_parts(dtype, parts, p.parts, a.M, a.N, out, ldo, s);
+}
+
+int64_t panel_of(int64_t lines, int64_t length) {
+    int64_t p = PANEL / length / 256 * 256;
+    if (p < 256) p = 256;
+    return p < lines ? p : lines;
+}
+
+DenseArgs dense_of(const idkm_codes_desc& w) {
+    DenseArgs a{};
+    a.words = w.words;
+    a.nwords = idkm_code_words(w.rows * w.cols / w.d, w.k);
+    a.rows = w.rows;
+    a.cols = w.cols;
+    a.C = w.C;
+    a.k = w.k;
+    a.d = w.d;
+    a.bits = idkm_code_bits(w.k);
+    a.S = w.S;
+    a.group = w.S ? (w.group < w.cols ? w.group : (int)w.cols) : 1;
+    a.groups = groups_of(w);
+    return a;
+}
+
+// Layout of the workspace of a product: operand rows brought to whole steps, the layer's panel, parts.
+struct ProductLayout {
+    int64_t pad, panel, operand, matrix, parts, bytes;
+    TilePlan plan;
+};
+
+// lines: the layer's rows (product) or columns (dX); sum: the other side.
+ProductLayout product_layout(int dtype, int64_t n, int64_t lines, int64_t sum) {
+    const int es = esize_of(dtype);
+    ProductLayout l;
+    l.pad = up_to(sum, TP_STEP / es);
+    l.panel = panel_of(lines, l.pad);
+    l.plan = tile_plan(n, l.panel, l.pad * es / TP_STEP, dtype);
+    l.operand = 0;
+    l.matrix = buffer(n * l.pad, es);
+    l.parts = l.matrix + buffer(l.panel * l.pad, es);
+    l.bytes = l.parts + (l.plan.parts > 1 ? buffer(n * l.panel * l.plan.parts, 4) : 0);
+    return l;
+}
+
+// The operand as the tile product takes it: itself, or a copy with whole steps.
+void operand_of(int dtype, const void* in, int64_t ldi, int64_t n, int64_t sum, const ProductLayout& l, unsigned char* ws, TileArgs* a,
+                hipStream_t s) {
+    const int es = esize_of(dtype);
+    if (sum == l.pad && ldi * es % 16 == 0 && aligned_to(in, 16)) {
+        a->A = in;
+        a->lda = ldi;
+    } else {
+        launch_pad_rows(dtype, in, ldi, n, sum, ws + l.operand, l.pad, s);
+        a->A = ws + l.operand;
+        a->lda = l.pad;
+    }
+    a->M = n;
+    a->ldb = l.pad;
+    a->B = ws + l.matrix;
+    a->steps = (int)(l.pad * es / TP_STEP);
+}
+
+// Gradients of the layer itself.
+struct LayerGradLayout {
+    int64_t pad, panel, panels, dy, x, p, bins, bytes;
+    TilePlan plan;
+    int group, groups, lanes, waves, codes, grid;
+};
+
+LayerGradLayout layer_grad_layout(const idkm_codes_desc& w, int64_t n) {
+    const int es = esize_of(w.dtype);
+    LayerGradLayout l;
+    l.pad = up_to(n, TP_STEP / es);
+    l.panel = panel_of(w.rows, w.cols);
+    l.panels = (w.rows + l.panel - 1) / l.panel;
+    l.plan = tile_plan(l.panel, w.cols, l.pad * es / TP_STEP, w.dtype);
+    // a wavefront takes a group of a row at a time; without scales, some hundred columns
+    l.group = w.S ? (int)(w.group < w.cols ? w.group : w.cols) : (int)(w.cols < 512 ? w.cols : 512 / w.d * w.d);
+    l.groups = (int)((w.cols + l.group - 1) / l.group);
+    l.lanes = 64 / w.d * w.d;
+    l.codes = w.k < 512 ? w.k : 512;  // bins of 512 codewords fill 128 KB
+    l.waves = (128 * 1024) / (l.codes * 256);
+    if (l.waves > 4) l.waves = 4;
+    int64_t grid = (l.panel * l.groups + l.waves - 1) / l.waves;
+    const int64_t most = l.codes * 256 * l.waves > 32 * 1024 ? 512 : 2048;
+    l.grid = (int)(grid < most ? grid : most);
+    l.dy = 0;
+    l.x = buffer(w.rows * l.pad, es);
+    l.p = l.x + buffer(w.cols * l.pad, es);
+    l.bins = l.p + buffer(l.panel * w.cols * l.plan.parts, 4);
+    l.bytes = l.bins + buffer(l.panels * l.grid * w.k * w.d, 4);
+    return l;
+}
+
+const char* wrong_workspace(const void* ws, int64_t have, int64_t need) {
+    if (need == 0) return nullptr;
+    if (!ws || have < need) return "the workspace is smaller than the size asked for";
+    if (!aligned_to(ws, 16)) return "the workspace must be 16-byte aligned";
+    return nullptr;
+}
+
+const char* wrong_scale_shape(int64_t rows, int64_t cols, int64_t group) {
+    if (rows < 0 || cols < 1) return "need rows >= 0 and cols >= 1";
+    if (group < 1) return "group must be >= 1";
+    if (rows > ((int64_t)1 << 36) || cols > INT_MAX || (rows > 0 && cols > ((int64_t)1 << 36) / rows)) return "the matrix is too large";
+    return nullptr;
+}
+
+ScaleArgs scale_args(int64_t rows, int64_t cols, int64_t group) {
+    ScaleArgs a{};
+    a.rows = rows;
+    a.cols = cols;
+    a.group = group < cols ? group : cols;
+    a.groups = (cols + a.group - 1) / a.group;
+    return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t idkm_codes_linear_workspace(const idkm_codes_desc* w, int64_t n) {
+    idkm_status st;
+    if (wrong_layer(w, &st) || n < 0 || n > MAX_SIDE) return -1;
+    if (n == 0 || few_plan(*w, n).fn) return 0;
+    return product_layout(w->dtype, n, w->rows, w->cols).bytes;
+}
+
+idkm_status idkm_codes_linear(idkm_ctx* ctx, const idkm_codes_desc* w, const void* X, int64_t n, int64_t ldx, void* Y, int64_t ldy,
+                              void* workspace, int64_t workspace_bytes, void* hip_stream) {
+    return entry(ctx, [&]() -> idkm_status {
+        idkm_status st;
+        if (const char* e = wrong_layer(w, &st)) return refuse(ctx, st, e);
+        if (n < 0) return refuse(ctx, IDKM_ERR_INVALID_ARG, "n must be >= 0");
+        if (n > MAX_SIDE) return refuse(ctx, IDKM_ERR_UNSUPPORTED, "too many tokens");
+        if (n == 0) return IDKM_OK;
+        const int es = esize_of(w->dtype);
+        if (!X || !Y) return refuse(ctx, IDKM_ERR_INVALID_ARG, "X and Y must be non-NULL");
+        if (ldx < w->cols || ldy < w->rows) return refuse(ctx, IDKM_ERR_INVALID_ARG, "ldx must be >= cols and ldy >= rows");
+        if (!aligned_to(X, es) || !aligned_to(Y, es)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "X and Y must be aligned to their type");
+        hipStream_t s = (hipStream_t)hip_stream;
+        const FewPlan few = few_plan(*w, n);
+        if (few.fn) {
+            ProductArgs a{};
+            a.words = w->words;
+            a.nwords = idkm_code_words(w->rows * w->cols / w->d, w->k);
+            a.rows = w->rows;
+            a.cols = w->cols;
+            a.C = w->C;
+            a.k = w->k;
+            a.S = w->S;
+            a.group = w->S ? (w->group < w->cols ? w->group : (int)w->cols) : 1;
+            a.groups = groups_of(*w);
+            a.X = X;
+            a.ldx = ldx;
+            a.Y = Y;
+            a.ldy = ldy;
+            a.n = n;
+            return launched(ctx, [&] { hipLaunchKernelGGL(few.fn, few.grid, dim3((unsigned)few.waves * 64), few.lds, s, a); });
+        }
+        const ProductLayout l = product_layout(w->dtype, n, w->rows, w->cols);
+        if (const char* e = wrong_workspace(workspace, workspace_bytes, l.bytes)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
+        unsigned char* ws = static_cast<unsigned char*>(workspace);
+        return launched(ctx, [&] {
+            TileArgs t{};
+            operand_of(w->dtype, X, ldx, n, w->cols, l, ws, &t, s);
+            for (int64_t r = 0; r < w->rows; r += l.panel) {
+                DenseArgs a = dense_of(*w);
+                a.first = r;
+                a.count = w->rows - r < l.panel ? w->rows - r : l.panel;
+                a.pad = l.pad;
+                a.out = ws + l.matrix;
+                launch_dense_rows(w->dtype, a, s);
+                t.N = a.count;
+                run_product(w->dtype, l.plan, t, static_cast<unsigned char*>(Y) + r * es, ldy, reinterpret_cast<float*>(ws + l.parts), s);
+            }
+        });
+    });
+}
+
+int64_t idkm_codes_linear_backward_workspace(const idkm_codes_desc* w, int64_t n) {
+    idkm_status st;
+    if (wrong_layer(w, &st) || n < 0 || n > MAX_SIDE) return -1;
+    if (n == 0) return 0;
+    const int64_t a = product_layout(w->dtype, n, w->cols, w->rows).bytes, b = layer_grad_layout(*w, n).bytes;
+    return a > b ? a : b;
+}
+
+idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, const void* X, int64_t ldx, const void* dY, int64_t lddy,
+                                       int64_t n, void* dX, int64_t lddx, float* dC, float* dS, void* workspace, int64_t workspace_bytes,
+                                       void* hip_stream) {
+    return entry(ctx, [&]() -> idkm_status {
+        idkm_status st;
+        if (const char* e = wrong_layer(w, &st)) return refuse(ctx, st, e);
+        if (n < 0) return refuse(ctx, IDKM_ERR_INVALID_ARG, "n must be >= 0");
+        if (n > MAX_SIDE) return refuse(ctx, IDKM_ERR_UNSUPPORTED, "too many tokens");
+        if (dS && !w->S) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dS of a layer without scales");
+        if (!aligned_to(dC, 4) || !aligned_to(dS, 4)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dC and dS must be aligned to their type");
+        hipStream_t s = (hipStream_t)hip_stream;
+        const int es = esize_of(w->dtype), groups = groups_of(*w);
+        if (n == 0)
+            return launched(ctx, [&] {
+                if (dC) launch_fill_zero(dC, (int64_t)w->k * w->d, s);
+                if (dS) launch_fill_zero(dS, w->rows * groups, s);
+            });
+        const bool layer = dC || dS;
+        if (!dX && !layer) return IDKM_OK;
+        if (!dY || lddy < w->rows) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dY must be non-NULL and lddy >= rows");
+        if (layer && (!X || ldx < w->cols)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "X must be non-NULL and ldx >= cols");
+        if (dX && lddx < w->cols) return refuse(ctx, IDKM_ERR_INVALID_ARG, "lddx must be >= cols");
+        if (!aligned_to(dY, es) || !aligned_to(X, es) || !aligned_to(dX, es))
+            return refuse(ctx, IDKM_ERR_INVALID_ARG, "X, dY and dX must be aligned to their type");
+        const int64_t need = idkm_codes_linear_backward_workspace(w, n);
+        if (const char* e = wrong_workspace(workspace, workspace_bytes, need)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
+        unsigned char* ws = static_cast<unsigned char*>(workspace);
+        return launched(ctx, [&] {
+            if (dX) {
+                const ProductLayout l = product_layout(w->dtype, n, w->cols, w->rows);
+                TileArgs t{};
+                operand_of(w->dtype, dY, lddy, n, w->rows, l, ws, &t, s);
+                for (int64_t c = 0; c < w->cols; c += l.panel) {
+                    DenseArgs a = dense_of(*w);
+                    a.first = c;
+                    a.count = w->cols - c < l.panel ? w->cols - c : l.panel;
+                    a.pad = l.pad;
+                    a.out = ws + l.matrix;
+                    launch_dense_cols(w->dtype, a, s);
+                    t.N = a.count;
+                    run_product(w->dtype, l.plan, t, static_cast<unsigned char*>(dX) + c * es, lddx, reinterpret_cast<float*>(ws + l.parts), s);
+                }
+            }
+            if (!layer) return;
+            const LayerGradLayout l = layer_grad_layout(*w, n);
+            launch_transpose(w->dtype, dY, lddy, n, w->rows, ws + l.dy, l.pad, s);
+            launch_transpose(w->dtype, X, ldx, n, w->cols, ws + l.x, l.pad, s);
+            float* bins = reinterpret_cast<float*>(ws + l.bins);
+            int64_t written = 0;
+            for (int64_t r = 0; r < w->rows; r += l.panel) {
+                const int64_t count = w->rows - r < l.panel ? w->rows - r : l.panel;
+                TileArgs t{};
+                t.A = ws + l.dy + r * l.pad * es;
+                t.lda = l.pad;
+                t.M = count;
+                t.B = ws + l.x;
+                t.ldb = l.pad;
+                t.N = w->cols;
+                t.steps = (int)(l.pad * es / TP_STEP);
+                t.wide = 1;
+                t.out = ws + l.p;
+                t.ldo = w->cols;
+                run_tile(w->dtype, l.plan, t, s);
+                BinArgs b{};
+                b.words = w->words;
+                b.nwords = idkm_code_words(w->rows * w->cols / w->d, w->k);
+                b.rows = w->rows;
+                b.cols = w->cols;
+                b.C = w->C;
+                b.k = w->k;
+                b.d = w->d;
+                b.bits = idkm_code_bits(w->k);
+                b.S = w->S;
+                b.group = l.group;
+                b.groups = l.groups;
+                b.P = reinterpret_cast<const float*>(ws + l.p);
+                b.parts = l.plan.parts;
+                b.ldp = w->cols;
+                b.first = r;
+                b.count = count;
+                b.lanes = l.lanes;
+                for (int c0 = 0; c0 < (dC ? w->k : 1); c0 += l.codes) {
+                    b.dS = c0 == 0 ? dS : nullptr;
+                    b.bins = dC ? bins + written * w->k * w->d : nullptr;
+                    b.code0 = c0;
+                    b.codes = l.codes;
+                    launch_codes_bins(w->dtype, b, l.grid, l.waves, s);
+                }
+                written += l.grid;
+            }
+            if (dC) launch_join_bins(bins, (int)written, w->k * w->d, dC, s);
+        });
+    });
+}
+
+idkm_status idkm_group_scale(idkm_ctx* ctx, const float* W, int64_t rows, int64_t cols, int64_t group, float* S_out, float* Z_out,
+                             void* hip_stream) {
+    return entry(ctx, [&]() -> idkm_status {
+        if (const char* e = wrong_scale_shape(rows, cols, group)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
+        if (rows == 0) return IDKM_OK;
+        if (!W || !S_out || !Z_out) return refuse(ctx, IDKM_ERR_INVALID_ARG, "W, S_out and Z_out must be non-NULL");
+        ScaleArgs a = scale_args(rows, cols, group);
+        a.x = W;
+        a.out = Z_out;
+        a.s_out = S_out;
+        return launched(ctx, [&] { launch_group_scale(SCALE_FWD, a, (hipStream_t)hip_stream); });
+    });
+}
+
+idkm_status idkm_group_unscale(idkm_ctx* ctx, const float* Zq, const float* S, int64_t rows, int64_t cols, int64_t group, float* Wq_out,
+                               void* hip_stream) {
+    return entry(ctx, [&]() -> idkm_status {
+        if (const char* e = wrong_scale_shape(rows, cols, group)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
+        if (rows == 0) return IDKM_OK;
+        if (!Zq || !S || !Wq_out) return refuse(ctx, IDKM_ERR_INVALID_ARG, "Zq, S and Wq_out must be non-NULL");
+        ScaleArgs a = scale_args(rows, cols, group);
+        a.x = Zq;
+        a.S = S;
+        a.out = Wq_out;
+        return launched(ctx, [&] { launch_group_scale(UNSCALE_FWD, a, (hipStream_t)hip_stream); });
+    });
+}
+
+idkm_status idkm_group_unscale_backward(idkm_ctx* ctx, const float* dWq, const float* Zq, const float* S, int64_t rows, int64_t cols,
+                                        int64_t group, float* dZq_out, float* dS_out, void* hip_stream) {
+    return entry(ctx, [&]() -> idkm_status {
+        if (const char* e = wrong_scale_shape(rows, cols, group)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
+        if (rows == 0) return IDKM_OK;
+        if (!dWq || !Zq || !S || !dZq_out || !dS_out)
+            return refuse(ctx, IDKM_ERR_INVALID_ARG, "dWq, Zq, S, dZq_out and dS_out must be non-NULL");
+        ScaleArgs a = scale_args(rows, cols, group);
+        a.x = dWq;
+        a.y = Zq;
+        a.S = S;
+        a.out = dZq_out;
+        a.s_out = dS_out;
+        return launched(ctx, [&] { launch_group_scale(UNSCALE_BWD, a, (hipStream_t)hip_stream); });
+    });
+}
+
+idkm_status idkm_group_scale_backward(idkm_ctx* ctx, const float* Z, const float* S, const float* dZ, const float* dS, int64_t rows,
+                                      int64_t cols, int64_t group, float* dW_out, void* hip_stream) {
+    return entry(ctx, [&]() -> idkm_status {
+        if (const char* e = wrong_scale_shape(rows, cols, group)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
+        if (rows == 0) return IDKM_OK;
+        if (!Z || !S || !dZ || !dW_out) return refuse(ctx, IDKM_ERR_INVALID_ARG, "Z, S, dZ and dW_out must be non-NULL");
+        ScaleArgs a = scale_args(rows, cols, group);
+        a.x = dZ;
+        a.y = Z;
+        a.S = S;
+        a.dS = dS;
+        a.out = dW_out;
+        return launched(ctx, [&] { launch_group_scale(SCALE_BWD, a, (hipStream_t)hip_stream); });
+    });
+}
+
+int64_t idkm_distill_workspace(int64_t n, int64_t V, int32_t top, int32_t dtype) {
+    if (n < 0 || V < 1 || top < 1 || top > 1024 || dtype < 0 || dtype > 2 || n > INT_MAX || V > INT_MAX) return -1;
+    if (n == 0) return 0;
+    int64_t part;
+    int parts;
+    distill_plan(n, V, esize_of(dtype), &part, &parts);
+    return parts == 0 ? 0 : buffer(n * parts * 2, 4) + buffer(n * top, 4);
+}
+
+idkm_status idkm_distill(idkm_ctx* ctx, const void* logits, int64_t n, int64_t V, int64_t ldz, idkm_dtype dtype, const int32_t* index,
+                         const float* teacher, int32_t top, float tau, const float* weight, float* loss_out, float* lse_out,
+                         void* dlogits_out, int64_t ldd, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+    return entry(ctx, [&]() -> idkm_status {
+        if (dtype != IDKM_F32 && dtype != IDKM_F16 && dtype != IDKM_BF16) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dtype must be an idkm_dtype");
+        if (n < 0 || V < 1 || n > INT_MAX || V > INT_MAX) return refuse(ctx, IDKM_ERR_INVALID_ARG, "need n >= 0 and V >= 1, below 2^31");
+        if (top < 1 || top > 1024) return refuse(ctx, IDKM_ERR_INVALID_ARG, "need 1 <= top <= 1024");
+        if (!(tau > 0.f) || !std::isfinite(tau)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "tau must be finite and > 0");
+        if ((weight != nullptr) != (dlogits_out != nullptr))
+            return refuse(ctx, IDKM_ERR_INVALID_ARG, "weight and dlogits_out go together");
+        if (n == 0) return IDKM_OK;
+        if (!logits || !index || !teacher || !loss_out || !lse_out)
+            return refuse(ctx, IDKM_ERR_INVALID_ARG, "logits, index, teacher, loss_out and lse_out must be non-NULL");
+        if (ldz < V || (dlogits_out && ldd < V)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "ldz and ldd must be >= V");
+        const int es = esize_of(dtype);
+        if (!aligned_to(logits, es) || !aligned_to(dlogits_out, es))
+            return refuse(ctx, IDKM_ERR_INVALID_ARG, "logits and dlogits_out must be aligned to their type");
+        if (dlogits_out == logits && ldd != ldz) return refuse(ctx, IDKM_ERR_INVALID_ARG, "in place, ldd must be ldz");
+        DistillArgs a{};
+        a.logits = logits;
+        a.n = n;
+        a.V = V;
+        a.ldz = ldz;
+        a.index = index;
+        a.teacher = teacher;
+        a.top = top;
+        a.tau = tau;
+        a.weight = weight;
+        a.loss = loss_out;
+        a.lse = lse_out;
+        a.dlogits = dlogits_out;
+        a.ldd = ldd;
+        distill_plan(n, V, es, &a.part, &a.parts);
+        if (const char* e = wrong_workspace(workspace, workspace_bytes, idkm_distill_workspace(n, V, top, dtype)))
+            return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
+        a.stats = static_cast<float*>(workspace);
+        if (a.parts > 0) a.listed = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + buffer(n * a.parts * 2, 4));
+        return launched(ctx, [&] { launch_distill(dtype, a, (hipStream_t)hip_stream); });
+    });
+}
+
+}  // extern "C"

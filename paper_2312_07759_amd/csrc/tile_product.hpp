@@ -1,0 +1,144 @@
+// out[m, n] = sum_c A[m, c] B[n, c]: the product of two matrices whose rows lie along the sum, on the matrix cores.
+//
+// A workgroup of WM x WN wavefronts computes a BM x BN tile.  128 bytes of every row of A and B (64 elements of 16 bits, 32
+// of float) make a step; ST steps are in flight, each copied from memory straight into LDS.  Row r's 16-byte pieces lie in
+// the order c ^ (r mod 8), so that the eight lanes that LDS serves together read eight different bank groups.
+// Operands are padded: a row's elements up to the next whole step are there (and zero in one of the two), rows begin at
+// multiples of 16 bytes.  Rows behind the last one are read from the last one and not stored.
+#pragma once
+#include "elem.hpp"
+
+namespace idkm {
+
+struct TileArgs {
+    const void* A;
+    const void* B;
+    int64_t lda, ldb;  // elements between rows
+    int64_t M, N;
+    int steps;         // steps of 128 bytes along the sum
+    void* out;         // T [M, ldo], or float when `wide`
+    int64_t ldo;
+    int wide;          // 1: float32 sums; the z-th of gridDim.y parts of the sum goes to out + z M ldo
+    int tiles_m, tiles_n;
+};
+
+constexpr int TP_STEP = 128;  // bytes
+
+template <typename T, int BM, int BN, int WM, int WN, int ST>
+__global__ __launch_bounds__(64 * WM* WN) void k_tile_product(const TileArgs a) {
+    constexpr int NW = WM * WN;
+    constexpr int PIECES = (BM + BN) / 8;      // 8 rows of 128 bytes: what a wavefront copies at once
+    constexpr int PPW = PIECES / NW;
+    static_assert(PIECES % NW == 0 && BM % (16 * WM) == 0 && BN % (16 * WN) == 0, "tile and wavefronts");
+    constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
+    constexpr int STAGE = (BM + BN) * TP_STEP;
+    extern __shared__ __align__(1024) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // Workgroups go to the eight dies in turn: a die gets a run of neighbouring tiles, which share rows of A and B in its
+    // cache.  Inside a run tiles go down strips of eight rows of tiles.
+    const int total = a.tiles_m * a.tiles_n;
+    int t = blockIdx.x;
+    {
+        const int die = t & 7, at = t >> 3, whole = total >> 3, rest = total & 7;
+        t = die * whole + (die < rest ? die : rest) + at;
+    }
+    const int strip = 8 * a.tiles_n, s0 = t / strip, in = t - s0 * strip;
+    const int high = min(8, a.tiles_m - s0 * 8);
+    const int tm = s0 * 8 + in % high, tn = in / high;
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    // this workgroup's part of the sum
+    const int parts = gridDim.y, z = blockIdx.y;
+    const int each = (a.steps + parts - 1) / parts;
+    const int first = min(a.steps, z * each), last = min(a.steps, first + each);
+
+    const unsigned char* src[PPW];
+#pragma unroll
+    for (int p = 0; p < PPW; ++p) {
+        const int r = (wave * PPW + p) * 8 + (lane >> 3);
+        const int c = (lane & 7) ^ (lane >> 3);
+        const bool of_a = r < BM;  // uniform over the piece: BM is a multiple of 8
+        const int64_t row = of_a ? min(m0 + r, a.M - 1) : min(n0 + (r - BM), a.N - 1);
+        src[p] = static_cast<const unsigned char*>(of_a ? a.A : a.B) + row * ((of_a ? a.lda : a.ldb) * (int64_t)sizeof(T)) + c * 16;
+    }
+    auto fetch = [&](int step, int slot) {
+        // behind the last step the last one is fetched again, into a slot that nobody reads: the count of copies in flight stays the same
+        const int64_t off = (int64_t)min(step, last - 1) * TP_STEP;
+#pragma unroll
+        for (int p = 0; p < PPW; ++p)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src[p] + off),
+                                             (__attribute__((address_space(3))) void*)(lds + slot * STAGE + (wave * PPW + p) * 1024), 16, 0, 0);
+    };
+    floatx4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+    const int wm = wave / WN, wn = wave % WN;
+    const int li = lane & 15, q = lane >> 4;
+    const int row_a = wm * (BM / WM) + li, row_b = BM + wn * (BN / WN) + li;
+    if (first < last) {
+#pragma unroll
+        for (int s = 0; s < ST - 1; ++s) fetch(first + s, s);
+        int slot = 0;
+        for (int step = first; step < last; ++step) {
+            // all but the newest ST - 2 steps' copies of this wavefront are there; after the barrier everybody's are, and
+            // everybody has read the slot that is fetched into next
+            // (vmcnt: ST - 2 steps' copies; lgkmcnt 0: this wavefront's own reads of that slot have returned)
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0x0070 | ((PPW * (ST - 2)) & 15) | (((PPW * (ST - 2)) >> 4) << 14));
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            const int next = slot == 0 ? ST - 1 : slot - 1;
+            fetch(step + ST - 1, next);
+            const unsigned char* base = lds + slot * STAGE;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32x4 fa[TM], fb[TN];
+                const int c = (((h << 2) | q) ^ (li & 7)) << 4;
+#pragma unroll
+                for (int i = 0; i < TM; ++i) fa[i] = *reinterpret_cast<const u32x4*>(base + (row_a + i * 16) * TP_STEP + c);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) fb[j] = *reinterpret_cast<const u32x4*>(base + (row_b + j * 16) * TP_STEP + c);
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) mma16<T>(acc[i][j], fb[j], fa[i]);
+            }
+            slot = slot + 1 == ST ? 0 : slot + 1;
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // nothing may still be written into this LDS when it is given to others
+    }
+    // lane: row m = .. + li, columns n = .. + 4 q + r
+    const bool quad = (a.ldo & 3) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15) == 0;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int64_t m = m0 + wm * (BM / WM) + i * 16 + li;
+        if (m >= a.M) continue;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int64_t n = n0 + wn * (BN / WN) + j * 16 + q * 4;
+            if (n >= a.N) continue;
+            if (a.wide) {
+                float* o = static_cast<float*>(a.out) + ((int64_t)z * a.M + m) * a.ldo + n;
+                if (quad && n + 4 <= a.N) {
+                    *reinterpret_cast<floatx4*>(o) = acc[i][j];
+                } else {
+                    for (int r = 0; r < 4 && n + r < a.N; ++r) o[r] = acc[i][j][r];
+                }
+            } else {
+                T* o = static_cast<T*>(a.out) + m * a.ldo + n;
+                if (quad && n + 4 <= a.N) {
+                    struct alignas(4 * sizeof(T)) Quad { T v[4]; } w;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) w.v[r] = Elem<T>::down(acc[i][j][r]);
+                    *reinterpret_cast<Quad*>(o) = w;
+                } else {
+                    for (int r = 0; r < 4 && n + r < a.N; ++r) o[r] = Elem<T>::down(acc[i][j][r]);
+                }
+            }
+        }
+    }
+}
+
+}  // namespace idkm
