@@ -202,24 +202,52 @@ def _stream():
 F32, F16, BF16 = 0, 1, 2
 
 
+_torch = None
+
+
+def _t():
+    """The torch module; this package loads without it."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 def _dtype(t, name):
-    import torch
-    code = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}.get(t.dtype)
-    if code is None:
-        raise TypeError(f"{name} must be float32, float16 or bfloat16, got {t.dtype}")
-    return code
+    torch = _t()
+    dt = t.dtype
+    if dt is torch.bfloat16:
+        return BF16
+    if dt is torch.float32:
+        return F32
+    if dt is torch.float16:
+        return F16
+    raise TypeError(f"{name} must be float32, float16 or bfloat16, got {dt}")
 
 
 def _rows(t, dtype, width, device, name):
     """Checks a matrix [n, width] on `device` whose rows may lie further apart than their length; elements between rows."""
-    if not t.is_cuda or t.device.index != device:
+    if not isinstance(t, _t().Tensor) or t.get_device() != device:
         raise TypeError(f"{name} must be in the memory of device {device}")
-    if t.dtype != dtype or t.dim() != 2 or t.shape[1] != width:
-        raise TypeError(f"{name} must be {dtype} of shape (n, {width}), got {t.dtype} {tuple(t.shape)}")
-    n, ld = t.shape[0], t.stride(0)
-    if (width > 1 and t.stride(1) != 1) or (n > 1 and ld < width):
+    shape = t.shape
+    if t.dtype is not dtype or len(shape) != 2 or shape[1] != width:
+        raise TypeError(f"{name} must be {dtype} of shape (n, {width}), got {t.dtype} {tuple(shape)}")
+    ld, step = t.stride()
+    if shape[0] < 2:
+        ld = width
+    if (width > 1 and step != 1) or ld < width:
         raise TypeError(f"{name} must have contiguous rows that do not overlap")
-    return ld if n > 1 else width
+    return ld
+
+
+def _flat(t, dtype, shape, device, name):
+    """Address of a contiguous tensor of this type and shape on `device`."""
+    if not isinstance(t, _t().Tensor) or t.get_device() != device:
+        raise TypeError(f"{name} must be in the memory of device {device}")
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise TypeError(f"{name} must be contiguous {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
 
 
 class CodesLayer:
@@ -238,7 +266,7 @@ class CodesLayer:
         if S is not None and group < cols and (group % 32 or group % d):
             raise ValueError("a group shorter than a row must be a multiple of 32 and of d")
         self.dtype, self.code = Cb.dtype, _dtype(Cb, "C")
-        self.device = Cb.device.index
+        self.device = Cb.get_device()
         p = _ptr(Cb, Cb.dtype, (k, d), "C")
         nwords = code_words(rows * cols // d, k)
         if nwords < 0:
@@ -405,147 +433,146 @@ class Context:
         self._check(st)
         return out
 
-    def _on(self, *named):
-        """Checks that tensors are contiguous float32 matrices or vectors on this context's device."""
-        import torch
-        for name, t, shape in named:
-            if t is None:
-                continue
-            _ptr(t, torch.float32, shape, name)
-            if t.device.index != self.device:
-                raise TypeError(f"{name} must be in the memory of device {self.device}")
-
-    def _stream(self):
-        import torch
-        return torch._C._cuda_getCurrentRawStream(self.device)
+    def _raw_stream(self):
+        """The current stream of this context's device, which need not be the current device."""
+        return _t()._C._cuda_getCurrentRawStream(self.device)
 
     def codes_linear(self, layer, X, out=None):
         """idkm_codes_linear: X [n, cols] in the layer's type -> X w^T [n, rows].  Rows of X and `out` may lie apart."""
-        import torch
-        if layer.device != self.device:
-            raise TypeError(f"the layer must be in the memory of device {self.device}")
-        ldx = _rows(X, layer.dtype, layer.cols, self.device, "X")
+        dev = self.device
+        if layer.device != dev:
+            raise TypeError(f"the layer must be in the memory of device {dev}")
+        ldx = _rows(X, layer.dtype, layer.cols, dev, "X")
         n = X.shape[0]
         if out is None:
-            out = torch.empty((n, layer.rows), dtype=layer.dtype, device=X.device)
+            out = X.new_empty((n, layer.rows))
             ldy = layer.rows
         else:
-            ldy = _rows(out, layer.dtype, layer.rows, self.device, "out")
+            ldy = _rows(out, layer.dtype, layer.rows, dev, "out")
             if out.shape[0] != n:
                 raise TypeError(f"out must have {n} rows")
         need = layer.workspace_bytes(n)
-        ws = torch.empty((need,), dtype=torch.uint8, device=X.device) if need > 0 else None
-        self._check(self._lib.idkm_codes_linear(self._h, layer._at, X.data_ptr(), n, ldx, out.data_ptr(), ldy,
-                                                ws.data_ptr() if need > 0 else None, need, self._stream()))
+        ws = X.new_empty((need,), dtype=_t().uint8) if need > 0 else None
+        st = self._lib.idkm_codes_linear(self._h, layer._at, X.data_ptr(), n, ldx, out.data_ptr(), ldy,
+                                         ws.data_ptr() if need > 0 else None, need, self._raw_stream())
+        if st:
+            self._check(st)
         return out
 
     def codes_linear_backward(self, layer, X, dY, want_dX=True, want_dC=True, want_dS=True):
         """idkm_codes_linear_backward: dict of dX [n, cols] in the layer's type and float32 dC [k, d] and, for a layer with
         scales, dS [rows, groups].  X may be None if only dX is wanted."""
-        import torch
-        if layer.device != self.device:
-            raise TypeError(f"the layer must be in the memory of device {self.device}")
-        ldy = _rows(dY, layer.dtype, layer.rows, self.device, "dY")
+        torch, dev = _t(), self.device
+        if layer.device != dev:
+            raise TypeError(f"the layer must be in the memory of device {dev}")
+        ldy = _rows(dY, layer.dtype, layer.rows, dev, "dY")
         n = dY.shape[0]
         want_dS = want_dS and layer.S is not None
         ldx = 0
         if X is not None:
-            ldx = _rows(X, layer.dtype, layer.cols, self.device, "X")
+            ldx = _rows(X, layer.dtype, layer.cols, dev, "X")
             if X.shape[0] != n:
                 raise TypeError(f"X must have {n} rows")
         elif want_dC or want_dS:
             raise TypeError("X is needed for dC and dS")
         res = {}
         if want_dX:
-            res["dX"] = torch.empty((n, layer.cols), dtype=layer.dtype, device=dY.device)
+            res["dX"] = dY.new_empty((n, layer.cols))
         if want_dC:
-            res["dC"] = torch.empty((layer.k, layer.d), dtype=torch.float32, device=dY.device)
+            res["dC"] = dY.new_empty((layer.k, layer.d), dtype=torch.float32)
         if want_dS:
-            res["dS"] = torch.empty((layer.rows, layer.groups), dtype=torch.float32, device=dY.device)
+            res["dS"] = dY.new_empty((layer.rows, layer.groups), dtype=torch.float32)
         need = layer.workspace_bytes(n, True)
-        ws = torch.empty((need,), dtype=torch.uint8, device=dY.device) if need > 0 else None
+        ws = dY.new_empty((need,), dtype=torch.uint8) if need > 0 else None
         at = {key: t.data_ptr() for key, t in res.items()}
         self._check(self._lib.idkm_codes_linear_backward(
             self._h, layer._at, X.data_ptr() if X is not None else None, ldx, dY.data_ptr(), ldy, n, at.get("dX"), layer.cols,
-            at.get("dC"), at.get("dS"), ws.data_ptr() if need > 0 else None, need, self._stream()))
+            at.get("dC"), at.get("dS"), ws.data_ptr() if need > 0 else None, need, self._raw_stream()))
         return res
+
+    def _grouped(self, t, group, name):
+        """Address of a float32 [rows, cols] tensor, and the shape of its groups' scales."""
+        shape = t.shape
+        if len(shape) != 2:
+            raise TypeError(f"{name} must be a matrix, got {tuple(shape)}")
+        rows, cols = shape
+        return _flat(t, _t().float32, shape, self.device, name), rows, cols, (rows, -(-cols // group) if group > 0 else 0)
 
     def group_scale(self, W, group):
         """idkm_group_scale: W [rows, cols] float32 -> (S [rows, ceil(cols / group)], Z = W / S)."""
-        import torch
-        rows, cols = W.shape
-        self._on(("W", W, (rows, cols)))
-        group = max(int(group), 0)
-        S = torch.empty((rows, -(-cols // max(group, 1))), dtype=torch.float32, device=W.device)
-        Z = torch.empty_like(W)
-        self._check(self._lib.idkm_group_scale(self._h, W.data_ptr(), rows, cols, group, S.data_ptr(), Z.data_ptr(), self._stream()))
+        w, rows, cols, scales = self._grouped(W, group, "W")
+        S, Z = W.new_empty(scales), W.new_empty((rows, cols))
+        st = self._lib.idkm_group_scale(self._h, w, rows, cols, group, S.data_ptr(), Z.data_ptr(), self._raw_stream())
+        if st:
+            self._check(st)
         return S, Z
 
     def group_unscale(self, Zq, S, group):
         """idkm_group_unscale: S Zq."""
-        import torch
-        rows, cols = Zq.shape
-        self._on(("Zq", Zq, (rows, cols)), ("S", S, (rows, -(-cols // max(int(group), 1)))))
-        Wq = torch.empty_like(Zq)
-        self._check(self._lib.idkm_group_unscale(self._h, Zq.data_ptr(), S.data_ptr(), rows, cols, int(group), Wq.data_ptr(),
-                                                 self._stream()))
+        z, rows, cols, scales = self._grouped(Zq, group, "Zq")
+        s = _flat(S, Zq.dtype, scales, self.device, "S")
+        Wq = Zq.new_empty((rows, cols))
+        st = self._lib.idkm_group_unscale(self._h, z, s, rows, cols, group, Wq.data_ptr(), self._raw_stream())
+        if st:
+            self._check(st)
         return Wq
 
     def group_unscale_backward(self, dWq, Zq, S, group):
         """idkm_group_unscale_backward: (dZq, dS)."""
-        import torch
-        rows, cols = Zq.shape
-        self._on(("dWq", dWq, (rows, cols)), ("Zq", Zq, (rows, cols)), ("S", S, (rows, -(-cols // max(int(group), 1)))))
-        dZq, dS = torch.empty_like(Zq), torch.empty_like(S)
-        self._check(self._lib.idkm_group_unscale_backward(self._h, dWq.data_ptr(), Zq.data_ptr(), S.data_ptr(), rows, cols, int(group),
-                                                          dZq.data_ptr(), dS.data_ptr(), self._stream()))
+        z, rows, cols, scales = self._grouped(Zq, group, "Zq")
+        g = _flat(dWq, Zq.dtype, Zq.shape, self.device, "dWq")
+        s = _flat(S, Zq.dtype, scales, self.device, "S")
+        dZq, dS = Zq.new_empty((rows, cols)), Zq.new_empty(scales)
+        st = self._lib.idkm_group_unscale_backward(self._h, g, z, s, rows, cols, group, dZq.data_ptr(), dS.data_ptr(),
+                                                   self._raw_stream())
+        if st:
+            self._check(st)
         return dZq, dS
 
     def group_scale_backward(self, Z, S, group, dZ, dS=None):
         """idkm_group_scale_backward: dW from the gradients of Z and, optionally, of S."""
-        import torch
-        rows, cols = Z.shape
-        shape = (rows, -(-cols // max(int(group), 1)))
-        self._on(("Z", Z, (rows, cols)), ("dZ", dZ, (rows, cols)), ("S", S, shape), ("dS", dS, shape))
-        dW = torch.empty_like(Z)
-        self._check(self._lib.idkm_group_scale_backward(self._h, Z.data_ptr(), S.data_ptr(), dZ.data_ptr(),
-                                                        dS.data_ptr() if dS is not None else None, rows, cols, int(group),
-                                                        dW.data_ptr(), self._stream()))
+        z, rows, cols, scales = self._grouped(Z, group, "Z")
+        g = _flat(dZ, Z.dtype, Z.shape, self.device, "dZ")
+        s = _flat(S, Z.dtype, scales, self.device, "S")
+        ds = _flat(dS, Z.dtype, scales, self.device, "dS") if dS is not None else None
+        dW = Z.new_empty((rows, cols))
+        st = self._lib.idkm_group_scale_backward(self._h, z, s, g, ds, rows, cols, group, dW.data_ptr(), self._raw_stream())
+        if st:
+            self._check(st)
         return dW
 
     def distill(self, logits, index, teacher, tau, weight=None, out=None):
         """idkm_distill: (loss [n], lse [n]) of logits [n, V] against the teacher's list (index int32, teacher float32, both
         [n, top]; a negative index is no entry), and with weight [n] also the gradient of (weight * loss).sum() in the
         logits; `out` (which may be the logits themselves) receives it."""
-        import torch
+        torch, dev = _t(), self.device
         code = _dtype(logits, "logits")
         if logits.dim() != 2 or index.dim() != 2:
             raise TypeError("logits and index must be matrices")
         n, V = logits.shape
         top = index.shape[1]
-        ldz = _rows(logits, logits.dtype, V, self.device, "logits")
-        self._on(("teacher", teacher, (n, top)), ("weight", weight, (n,)))
-        _ptr(index, torch.int32, (n, top), "index")
-        if index.device.index != self.device:
-            raise TypeError(f"index must be in the memory of device {self.device}")
-        loss = torch.empty((n,), dtype=torch.float32, device=logits.device)
-        lse = torch.empty((n,), dtype=torch.float32, device=logits.device)
+        ldz = _rows(logits, logits.dtype, V, dev, "logits")
+        t = _flat(teacher, torch.float32, (n, top), dev, "teacher")
+        i = _flat(index, torch.int32, (n, top), dev, "index")
+        w = _flat(weight, torch.float32, (n,), dev, "weight") if weight is not None else None
+        loss, lse = teacher.new_empty((n,)), teacher.new_empty((n,))
         ldd = V
         if weight is None:
             if out is not None:
                 raise TypeError("the gradient needs weights")
         elif out is None:
-            out = torch.empty((n, V), dtype=logits.dtype, device=logits.device)
+            out = logits.new_empty((n, V))
         else:
-            ldd = _rows(out, logits.dtype, V, self.device, "out")
+            ldd = _rows(out, logits.dtype, V, dev, "out")
             if out.shape[0] != n:
                 raise TypeError(f"out must have {n} rows")
         need = self._lib.idkm_distill_workspace(n, V, top, code)
-        ws = torch.empty((need,), dtype=torch.uint8, device=logits.device) if need > 0 else None
-        self._check(self._lib.idkm_distill(self._h, logits.data_ptr(), n, V, ldz, code, index.data_ptr(), teacher.data_ptr(), top,
-                                           float(tau), weight.data_ptr() if weight is not None else None, loss.data_ptr(),
-                                           lse.data_ptr(), out.data_ptr() if out is not None else None, ldd,
-                                           ws.data_ptr() if need > 0 else None, need, self._stream()))
+        ws = logits.new_empty((need,), dtype=torch.uint8) if need > 0 else None
+        st = self._lib.idkm_distill(self._h, logits.data_ptr(), n, V, ldz, code, i, t, top, tau, w, loss.data_ptr(), lse.data_ptr(),
+                                    out.data_ptr() if out is not None else None, ldd, ws.data_ptr() if need > 0 else None, need,
+                                    self._raw_stream())
+        if st:
+            self._check(st)
         return (loss, lse) if weight is None else (loss, lse, out)
 
     def step_F(self, W, Cb, tau, dist):

@@ -1,10 +1,9 @@
 // Y[t, n] = sum_c X[t, c] w[n, c] for few tokens, straight from the packed codes: w[n, c] = S[n, c / group] C[code, c % d].
 //
-// Bound by reading the codes once.  They go from memory into registers in the layout in which the matrix instruction takes
-// them (lane l: layer row l % 16, a run of L consecutive weights for each quarter l / 16), so the codes need no LDS and the
-// multiplications no vector instructions; up to 16 NT tokens share one decoding.  A code becomes a weight by reading a table
-// in LDS.  Several codes of few bits are looked up at once: the table is indexed by up to 8 bits of the stream and holds their
-// 2 .. 8 weights, which costs one LDS read and two vector instructions for all of them.
+// Codes go from memory into registers in the layout in which the matrix instruction takes them (lane l: layer row l % 16, a
+// run of L consecutive weights for each quarter l / 16), so they need no LDS and the multiplications no vector instructions.
+// A code becomes a weight by reading a table in LDS.  Several codes of few bits are looked up at once: the table is indexed by
+// up to 8 bits of the stream and holds their up to 8 weights, which costs one LDS read and two vector instructions for all.
 // The table holds the codewords in X's type, as they are given; a group's scale multiplies the float32 sum over its part
 // of the row, so nothing is rounded but the result.
 // The wavefronts of a workgroup share 16 rows of the layer and split the sum; their partial sums meet in LDS, in order.
@@ -20,9 +19,11 @@ struct ProductArgs {
     int64_t nwords;
     int64_t rows, cols;
     const void* C;  // T [k, d]
-    int k;
-    const float* S;  // [rows, groups] or null
-    int group, groups;
+    int k, B, D;        // B bits a code, D weights a codeword
+    int64_t row_bits;   // of the stream
+    const float* S;     // [rows, groups], or groups = 0
+    int groups;
+    unsigned group_magic;  // ceil(2^31 / chunks of a group): its high product with twice a chunk is the chunk's group
     const void* X;  // T [n, ldx]
     int64_t ldx;
     void* Y;  // T [n, ldy]
@@ -37,19 +38,76 @@ constexpr int codes_at_once(int B, int D) {
     return c;
 }
 
+// The table in LDS: entry e holds the W weights of the codes in the IB bits e, the first code in the low bits.  A thread's first
+// entry is asked for by the constructor, so that the wait for it can come later.
+template <typename T, int IB, int W>
+struct Table {
+    struct alignas(W * sizeof(T) > 16 ? 16 : W * sizeof(T)) Entry { T v[W]; };
+    T first[W];
+    unsigned none;  // bit i: first[i] belongs to a code that is none
+    static __device__ __forceinline__ unsigned ask(T* v, unsigned e, const void* codebook, int k, int B, int D) {
+        const T* C = static_cast<const T*>(codebook);
+        unsigned none = 0;
+        int code = 0, part = D;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            if (part == D) {
+                part = 0;
+                code = (int)(e & ((1u << B) - 1u));
+                e >>= B;
+            }
+            v[i] = C[min(code, k - 1) * D + part];
+            none |= code < k ? 0u : 1u << i;
+            ++part;
+        }
+        return none;
+    }
+    static __device__ __forceinline__ void put(T* table, unsigned e, const T* v, unsigned none) {
+        Entry x;
+#pragma unroll
+        for (int i = 0; i < W; ++i) x.v[i] = none >> i & 1 ? Elem<T>::nan() : v[i];
+        *reinterpret_cast<Entry*>(table + e * W) = x;
+    }
+    __device__ __forceinline__ Table(const void* codebook, int k, int B, int D) {
+        none = ask(first, threadIdx.x & ((1u << IB) - 1u), codebook, k, B, D);
+    }
+    __device__ __forceinline__ void build(T* table, const void* codebook, int k, int B, int D) const {
+        if (threadIdx.x < (1u << IB)) put(table, threadIdx.x, first, none);
+        for (unsigned e = threadIdx.x + blockDim.x; e < (1u << IB); e += blockDim.x) {
+            T v[W];
+            const unsigned n = ask(v, e, codebook, k, B, D);
+            put(table, e, v, n);
+        }
+    }
+};
+
 // The run of code bits that begins `bit` bits into the stream, NB of them, in (NB + 31) / 32 words.  Words behind the
 // stream's last are read as that one; what the caller does not use may lie there.  ALIGNED: runs begin with a word.
+// NEAR_END false: the caller knows that SPAN words from the run's first one on belong to the stream.
 template <int NB>
 struct CodeRun {
     static constexpr int NWORDS = (NB + 31) / 32;
+    static constexpr int SPAN = (NB + 31 + 31) / 32;  // words that NB bits may touch
     uint32_t w[NWORDS];
-    template <bool ALIGNED>
+    template <bool ALIGNED, bool NEAR_END>
     __device__ __forceinline__ void load(const uint32_t* words, int64_t nwords, int64_t bit) {
-        constexpr int RAW = ALIGNED ? NWORDS : (NB + 31 + 31) / 32;  // words that NB bits may touch
+        constexpr int RAW = ALIGNED ? NWORDS : SPAN;
         const int64_t at = bit >> 5;
         uint32_t raw[RAW + 1];
-        if (at + RAW <= nwords) {
-            __builtin_memcpy(raw, words + at, RAW * 4);
+        if (!NEAR_END || at + RAW <= nwords) {
+            constexpr int Q = RAW / 4 * 4;
+#pragma unroll
+            for (int i = 0; i < Q; i += 4) {
+                const u32x4 v = *reinterpret_cast<const u32x4_word*>(words + at + i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) raw[i + e] = v[e];
+            }
+            if constexpr (RAW - Q >= 2) {
+                const u32x2 v = *reinterpret_cast<const u32x2_word*>(words + at + Q);
+                raw[Q] = v[0];
+                raw[Q + 1] = v[1];
+            }
+            if constexpr (RAW % 2 == 1) raw[RAW - 1] = words[at + RAW - 1];
         } else {
 #pragma unroll
             for (int i = 0; i < RAW; ++i) raw[i] = words[min(at + i, nwords - 1)];
@@ -67,145 +125,143 @@ struct CodeRun {
     }
 };
 
-// B bits a code, D weights a codeword, L consecutive weights of a row to a lane at a time (a chunk: 4 L), 16 NT tokens.
-template <typename T, int B, int D, int L, int NT, bool ALIGNED>
+// Eight weights from the run's looked-up codes s * 8 / W ...
+template <typename T, int IB, int W, int NB>
+__device__ __forceinline__ void eight_weights(u32x4* out, const CodeRun<NB>& run, int s, const T* table) {
+    struct alignas(16) Eight { T v[8]; } w;
+#pragma unroll
+    for (int e = 0; e < 8 / W; ++e) {
+        const uint32_t idx = run.bits((s * 8 / W + e) * IB, IB);
+        struct alignas(W * sizeof(T) > 16 ? 16 : W * sizeof(T)) Entry { T v[W]; };
+        const Entry x = *reinterpret_cast<const Entry*>(table + idx * W);
+#pragma unroll
+        for (int i = 0; i < W; ++i) w.v[e * W + i] = x.v[i];
+    }
+    __builtin_memcpy(out, &w, sizeof(w));
+}
+
+// Eight elements of a row from column c on, zero behind its end.
+template <typename T>
+__device__ __forceinline__ void eight_of_row(u32x4* out, const T* row, int64_t c, int64_t cols, bool whole) {
+    if (whole) {
+#pragma unroll
+        for (int f = 0; f < 8 / Elem<T>::PER16; ++f) out[f] = reinterpret_cast<const u32x4_any*>(row + c)[f];
+    } else {
+        struct alignas(16) Eight { T v[8]; } y;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y.v[i] = c + i < cols ? row[c + i] : (T)0.f;
+        __builtin_memcpy(out, &y, sizeof(y));
+    }
+}
+
+// Zeros in the place of weights behind column cols: what a row's last run holds there belongs to the next row.
+template <typename T>
+__device__ __forceinline__ void cut_weights(u32x4* w, int64_t c, int64_t cols) {
+    struct alignas(16) Eight { T v[8]; } y;
+    __builtin_memcpy(&y, w, sizeof(y));
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c + i >= cols) y.v[i] = (T)0.f;
+    __builtin_memcpy(w, &y, sizeof(y));
+}
+
+// Up to 16 tokens.  IB bits looked up at once give W weights; L consecutive weights of a row to a lane at a time: four runs make
+// a chunk of 4 L columns, which lies in one group.  Everything that a batch of chunks needs (codes, activations, scales) is
+// asked for before the first of it is used, the first batch before the table is built.
+template <typename T, int IB, int W, int L, bool ALIGNED>
 __global__ __launch_bounds__(512) void k_codes_product(const ProductArgs a) {
-    constexpr int CO = codes_at_once(B, D), IB = CO * B, W = CO * D;  // a table entry: CO codes, IB bits, W weights
-    constexpr int NB = L / D * B;
+    constexpr int NB = L / W * IB;
     constexpr int FR = 8 / Elem<T>::PER16;  // 16-byte fragments in 8 weights
     constexpr int SUB = L / 8;
+    constexpr int U = 16 / (SUB * FR);  // chunks of a batch: 64 registers of activations
     extern __shared__ __align__(16) unsigned char lds[];
     T* table = reinterpret_cast<T*>(lds);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
     const int li = lane & 15, q = lane >> 4;
     const int64_t n0 = (int64_t)blockIdx.x * 16;
-    const int64_t row = min(n0 + li, a.rows - 1);
-    const int64_t t0 = (int64_t)blockIdx.y * (16 * NT);
+    const int64_t row = min(n0 + li, a.rows - 1);  // rows and tokens behind the last one: computed from it, not stored
+    const T* X = static_cast<const T*>(a.X) + min((int64_t)li, a.n - 1) * a.ldx;
 
     const int chunks = (int)((a.cols + 4 * L - 1) / (4 * L));
     const int each = (chunks + nw - 1) / nw;
     const int first = min(chunks, wave * each), last = min(chunks, first + each);
-    const int64_t row_bit = row * (a.cols / D * B);
+    const int full = min(last, (int)(a.cols / (4 * L)));  // chunks before this one are whole
+    const int64_t row_bit = row * a.row_bits + q * NB;
+    const int64_t row_bit_last = min(n0 + 15, a.rows - 1) * a.row_bits + 3 * NB;  // of this workgroup's last lane
 
-    // the table
-    {
-        const T* C = static_cast<const T*>(a.C);
-        for (int e = threadIdx.x; e < (1 << IB) * W; e += blockDim.x) {
-            const int entry = e / W, x = e % W;
-            const int code = (entry >> (x / D * B)) & ((1 << B) - 1);
-            table[e] = code < a.k ? C[code * D + x % D] : Elem<T>::nan();
-        }
-    }
-    __syncthreads();
-
-    floatx4 acc[NT], part[NT];
+    const Table<T, IB, W> entries(a.C, a.k, a.B, a.D);
+    CodeRun<NB> run[U];
+    float scale[U];
+    u32x4 xf[U][SUB][FR];
+    // without scales some word is read in their place, so that there is no branch between the loads
+    const bool scaled = a.groups > 0;
+    const float* S = scaled ? a.S + row * a.groups : reinterpret_cast<const float*>(a.words);
+    auto ask = [&](int u, int ch, auto whole) {
+        run[u].template load<ALIGNED, !decltype(whole)::value>(a.words, a.nwords, row_bit + (int64_t)ch * (4 * NB));
+        scale[u] = S[__umulhi(2u * (unsigned)ch, a.group_magic)];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) acc[j] = part[j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    int g_now = first * (4 * L) / max(a.group, 1);
-    // the scales of the four rows that this lane holds sums of
-    auto close_group = [&](int g) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int64_t n = min(n0 + q * 4 + r, a.rows - 1);
-            const float s = a.S[n * a.groups + g];
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                acc[j][r] += s * part[j][r];
-                part[j][r] = 0.f;
-            }
-        }
+        for (int s = 0; s < SUB; ++s) eight_of_row(xf[u][s], X, (int64_t)ch * (4 * L) + q * L + s * 8, a.cols, decltype(whole)::value);
     };
-    // tokens behind the last one are computed from its activations and not stored
-    const T* X[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) X[j] = static_cast<const T*>(a.X) + min(t0 + j * 16 + li, a.n - 1) * a.ldx;
-    auto chunk = [&](int ch, const CodeRun<NB>& run, auto whole_) {
-        constexpr bool whole = decltype(whole_)::value;  // all of the chunk's weights belong to the row
-        const int64_t c0 = (int64_t)ch * (4 * L) + q * L;
-        if (a.S) {  // a chunk lies in one group
-            const int g = (int)((int64_t)ch * (4 * L) / a.group);
-            if (g != g_now) {
-                close_group(g_now);
-                g_now = g;
-            }
-        }
-        u32x4 xf[SUB][NT][FR];
-#pragma unroll
-        for (int s = 0; s < SUB; ++s)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const T* x = X[j] + c0 + s * 8;
-                if constexpr (whole) {
-#pragma unroll
-                    for (int f = 0; f < FR; ++f) xf[s][j][f] = reinterpret_cast<const u32x4_any*>(x)[f];
-                } else {
-                    struct alignas(16) Eight { T v[8]; } y;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) y.v[i] = c0 + s * 8 + i < a.cols ? x[i] : (T)0.f;
-                    __builtin_memcpy(xf[s][j], &y, sizeof(y));
-                }
-            }
+    floatx4 acc{0.f, 0.f, 0.f, 0.f};
+    auto use = [&](int u, int ch, auto whole) {
+        floatx4 part{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < SUB; ++s) {
-            struct alignas(16) Eight { T v[8]; } w;
-#pragma unroll
-            for (int e = 0; e < 8 / W; ++e) {
-                const uint32_t idx = run.bits((s * 8 / W + e) * IB, IB);
-                struct alignas(W * sizeof(T) > 16 ? 16 : W * sizeof(T)) Entry { T v[W]; };
-                const Entry x = *reinterpret_cast<const Entry*>(table + idx * W);
-#pragma unroll
-                for (int i = 0; i < W; ++i) w.v[e * W + i] = x.v[i];
-            }
-            if constexpr (!whole) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (c0 + s * 8 + i >= a.cols) w.v[i] = (T)0.f;
-            }
             u32x4 wf[FR];
-            __builtin_memcpy(wf, &w, sizeof(wf));
+            eight_weights<T, IB, W, NB>(wf, run[u], s, table);
+            if (!decltype(whole)::value) cut_weights<T>(wf, (int64_t)ch * (4 * L) + q * L + s * 8, a.cols);
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int f = 0; f < FR; ++f) mma16<T>(part[j], wf[f], xf[s][j][f]);
+            for (int f = 0; f < FR; ++f) mma16<T>(part, xf[u][s][f], wf[f]);
         }
+        const float by = scaled ? scale[u] : 1.f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[r] = fmaf(by, part[r], acc[r]);
     };
-    auto load = [&](int ch, CodeRun<NB>& run) {
-        run.template load<ALIGNED>(a.words, a.nwords, row_bit + ((int64_t)ch * (4 * L) + q * L) / D * B);
-    };
-    const int full = (int)min((int64_t)last, a.cols / (4 * L));  // chunks before this one are whole
-    constexpr int U = NT > 1 ? 2 : 4;  // chunks whose codes are asked for together
+    const std::true_type whole;
+    const std::false_type broken;
+    // chunks before this one are whole, and the words that their runs may touch are all there
+    const int64_t room = a.nwords * 32 - 32 * (ALIGNED ? CodeRun<NB>::NWORDS : CodeRun<NB>::SPAN) - row_bit_last;
+    const int safe = room < 0 ? first : (int)max((int64_t)first, min((int64_t)full, room / (4 * NB) + 1));
     int ch = first;
-    for (; ch + U <= full; ch += U) {
-        CodeRun<NB> run[U];
+    bool built = false;
+    if (ch + U <= safe) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) load(ch + u, run[u]);
+        for (int u = 0; u < U; ++u) ask(u, ch + u, whole);
+        entries.build(table, a.C, a.k, a.B, a.D);
+        __syncthreads();
+        built = true;
+        for (;;) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) chunk(ch + u, run[u], std::true_type());
+            for (int u = 0; u < U; ++u) use(u, ch + u, whole);
+            ch += U;
+            if (ch + U > safe) break;
+#pragma unroll
+            for (int u = 0; u < U; ++u) ask(u, ch + u, whole);
+        }
+    }
+    if (!built) {
+        entries.build(table, a.C, a.k, a.B, a.D);
+        __syncthreads();
     }
     for (; ch < last; ++ch) {
-        CodeRun<NB> run;
-        load(ch, run);
-        if (ch < full)
-            chunk(ch, run, std::true_type());
-        else
-            chunk(ch, run, std::false_type());
+        if (ch < safe) {
+            ask(0, ch, whole);
+            use(0, ch, whole);
+        } else {
+            ask(0, ch, broken);
+            use(0, ch, broken);
+        }
     }
-    if (a.S) {
-        if (first < last) close_group(g_now);
-    } else {
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[j] = part[j];
-    }
-    // the wavefronts' sums: [wave][token of 16 NT][row of 16]
+    // the wavefronts' sums: [wave][token][row]
     __syncthreads();
     float* red = reinterpret_cast<float*>(lds);
 #pragma unroll
-    for (int j = 0; j < NT; ++j) *reinterpret_cast<floatx4*>(red + ((wave * NT + j) * 16 + li) * 16 + q * 4) = acc[j];
+    for (int r = 0; r < 4; ++r) red[(wave * 16 + q * 4 + r) * 16 + li] = acc[r];
     __syncthreads();
-    for (int e = threadIdx.x; e < 256 * NT; e += blockDim.x) {
+    for (int e = threadIdx.x; e < 256; e += blockDim.x) {
         float sum = 0.f;
-        for (int w = 0; w < nw; ++w) sum += red[w * 256 * NT + e];
-        const int64_t t = t0 + (e >> 4), n = n0 + (e & 15);
+        for (int w = 0; w < nw; ++w) sum += red[w * 256 + e];
+        const int64_t t = e >> 4, n = n0 + (e & 15);
         if (t < a.n && n < a.rows) static_cast<T*>(a.Y)[t * a.ldy + n] = Elem<T>::down(sum);
     }
 }

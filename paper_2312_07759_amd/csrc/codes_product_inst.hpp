@@ -1,35 +1,38 @@
-// Instantiations of the product of few tokens with codes of CODE_BITS bits; included by one source file for each.
+// Instantiations of the product of few tokens with codes of which CODE_BITS bits are looked up at once; included by one source
+// file for each.
 #include "layers.h"
 
 namespace idkm {
 
-template <typename T, int D, int NT>
+template <typename T, int W>
 static ProductFn for_run(int L, bool aligned) {
-    constexpr int B = CODE_BITS;
-    if (L == 8) return &k_codes_product<T, B, D, 8, NT, false>;
-    if constexpr (32 / D * B % 32 == 0) {
-        if (aligned) return &k_codes_product<T, B, D, 32, NT, true>;
+    constexpr int IB = CODE_BITS;
+    if (L == 8) return &k_codes_product<T, IB, W, 8, false>;
+    if (L == 16) return &k_codes_product<T, IB, W, 16, false>;
+    if constexpr (32 / W * IB % 32 == 0) {
+        if (aligned) return &k_codes_product<T, IB, W, 32, true>;
     }
-    return &k_codes_product<T, B, D, 32, NT, false>;
+    return &k_codes_product<T, IB, W, 32, false>;
 }
 
 template <typename T>
-static ProductFn for_type(int d, int L, int NT, bool aligned) {
-    switch (d) {
-        case 1: return NT == 1 ? for_run<T, 1, 1>(L, aligned) : for_run<T, 1, 4>(L, aligned);
-        case 2: return NT == 1 ? for_run<T, 2, 1>(L, aligned) : for_run<T, 2, 4>(L, aligned);
-        case 4: return NT == 1 ? for_run<T, 4, 1>(L, aligned) : for_run<T, 4, 4>(L, aligned);
-        case 8: return NT == 1 ? for_run<T, 8, 1>(L, aligned) : for_run<T, 8, 4>(L, aligned);
+static ProductFn for_type(int W, int L, bool aligned) {
+    // codes of one to four bits are looked up together until they are eight weights or five bits and more
+    switch (W) {
+        case 1: if constexpr (CODE_BITS >= 5) return for_run<T, 1>(L, aligned); break;
+        case 2: if constexpr (CODE_BITS >= 5) return for_run<T, 2>(L, aligned); break;
+        case 4: if constexpr (CODE_BITS >= 5) return for_run<T, 4>(L, aligned); break;
+        case 8: return for_run<T, 8>(L, aligned);
     }
     return nullptr;
 }
 
 #define CODES_PRODUCT_NAME2(b) codes_product_kernel_##b
 #define CODES_PRODUCT_NAME(b) CODES_PRODUCT_NAME2(b)
-ProductFn CODES_PRODUCT_NAME(CODE_BITS)(int dtype, int d, int L, int NT, bool aligned) {
-    if (dtype == 0) return for_type<float>(d, L, NT, aligned);
-    if (dtype == 1) return for_type<f16>(d, L, NT, aligned);
-    return for_type<bf16>(d, L, NT, aligned);
+ProductFn CODES_PRODUCT_NAME(CODE_BITS)(int dtype, int W, int L, bool aligned) {
+    if (dtype == 0) return for_type<float>(W, L, aligned);
+    if (dtype == 1) return for_type<f16>(W, L, aligned);
+    return for_type<bf16>(W, L, aligned);
 }
 
 }  // namespace idkm

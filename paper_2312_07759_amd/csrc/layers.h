@@ -6,11 +6,10 @@
 
 namespace idkm {
 
-// Few tokens, straight from the codes.  B bits a code, d in {1, 2, 4, 8}, L weights of a row to a lane at a time (8, 32),
-// NT in {1, 4}; aligned: every run of codes begins with a word.  nullptr if not instantiated.
+// Up to 16 tokens, straight from the codes.  IB bits looked up at once give W weights (see codes_at_once), L weights of a row to a
+// lane at a time (8, 16, 32); aligned: every run of codes begins with a word.  nullptr if not instantiated.
 typedef void (*ProductFn)(const ProductArgs);
-ProductFn codes_product_kernel(int dtype, int B, int d, int L, int NT, bool aligned);
-int codes_product_table_bytes(int dtype, int B, int d);
+ProductFn codes_product_kernel(int dtype, int IB, int W, int L, bool aligned);
 
 struct TileShape {
     int bm, bn, threads;

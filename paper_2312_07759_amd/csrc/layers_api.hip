@@ -15,25 +15,20 @@ namespace idkm {
 int context_device(const idkm_ctx* ctx);
 void context_error(idkm_ctx* ctx, const char* msg);
 
-ProductFn codes_product_kernel_1(int, int, int, int, bool);
-ProductFn codes_product_kernel_2(int, int, int, int, bool);
-ProductFn codes_product_kernel_3(int, int, int, int, bool);
-ProductFn codes_product_kernel_4(int, int, int, int, bool);
-ProductFn codes_product_kernel_5(int, int, int, int, bool);
-ProductFn codes_product_kernel_6(int, int, int, int, bool);
-ProductFn codes_product_kernel_7(int, int, int, int, bool);
-ProductFn codes_product_kernel_8(int, int, int, int, bool);
+ProductFn codes_product_kernel_1(int, int, int, bool);
+ProductFn codes_product_kernel_2(int, int, int, bool);
+ProductFn codes_product_kernel_3(int, int, int, bool);
+ProductFn codes_product_kernel_4(int, int, int, bool);
+ProductFn codes_product_kernel_5(int, int, int, bool);
+ProductFn codes_product_kernel_6(int, int, int, bool);
+ProductFn codes_product_kernel_7(int, int, int, bool);
+ProductFn codes_product_kernel_8(int, int, int, bool);
 
-ProductFn codes_product_kernel(int dtype, int B, int d, int L, int NT, bool aligned) {
-    static ProductFn (*const by_bits[8])(int, int, int, int, bool) = {
+ProductFn codes_product_kernel(int dtype, int IB, int W, int L, bool aligned) {
+    static ProductFn (*const by_bits[8])(int, int, int, bool) = {
         codes_product_kernel_1, codes_product_kernel_2, codes_product_kernel_3, codes_product_kernel_4,
         codes_product_kernel_5, codes_product_kernel_6, codes_product_kernel_7, codes_product_kernel_8};
-    return B >= 1 && B <= 8 ? by_bits[B - 1](dtype, d, L, NT, aligned) : nullptr;
-}
-
-int codes_product_table_bytes(int dtype, int B, int d) {
-    const int c = codes_at_once(B, d);
-    return (1 << (c * B)) * c * d * (dtype == IDKM_F32 ? 4 : 2);
+    return IB >= 1 && IB <= 8 ? by_bits[IB - 1](dtype, W, L, aligned) : nullptr;
 }
 
 }  // namespace idkm
@@ -120,28 +115,33 @@ int groups_of(const idkm_codes_desc& w) { return w.S ? (int)((w.cols + w.group -
 
 struct FewPlan {
     ProductFn fn = nullptr;
-    int NT, waves;
+    unsigned group_magic = 0;
+    int waves;
     dim3 grid;
     size_t lds;
 };
 
-// Up to 64 tokens are computed straight from the codes.
-constexpr int64_t FEW_TOKENS = 64;
+constexpr int64_t FEW_TOKENS = 16;
 
 FewPlan few_plan(const idkm_codes_desc& w, int64_t n) {
     FewPlan p;
     const int bits = idkm_code_bits(w.k);
     if (n > FEW_TOKENS || bits > 8 || (w.d != 1 && w.d != 2 && w.d != 4 && w.d != 8)) return p;
     // a chunk of four runs has to lie in one group
-    const int L = !w.S || w.group >= w.cols || w.group % 128 == 0 ? 32 : 8;
-    const bool aligned = (w.cols / w.d * bits) % 32 == 0 && (32 / w.d * bits) % 32 == 0;
-    p.NT = n <= 16 ? 1 : 4;
-    p.fn = codes_product_kernel(w.dtype, bits, w.d, L, p.NT, aligned);
+    const int L = !w.S || w.group >= w.cols || w.group % 128 == 0 ? 32 : w.group % 64 == 0 ? 16 : 8;
+    const int at_once = codes_at_once(bits, w.d), IB = at_once * bits, W = at_once * w.d;
+    const bool aligned = (w.cols / w.d * bits) % 32 == 0 && (32 / W * IB) % 32 == 0;
     const int64_t chunks = (w.cols + 4 * L - 1) / (4 * L);
+    if (w.S && w.group < w.cols) {  // exact while chunks (chunks of a group) < 2^31
+        const int64_t of_group = w.group / (4 * L);
+        if (chunks * of_group >= ((int64_t)1 << 31)) return p;
+        p.group_magic = (unsigned)((((int64_t)1 << 31) + of_group - 1) / of_group);
+    }
+    p.fn = codes_product_kernel(w.dtype, IB, W, L, aligned);
     p.waves = chunks < 8 ? (int)chunks : 8;
-    p.grid = dim3((unsigned)((w.rows + 15) / 16), (unsigned)((n + 16 * p.NT - 1) / (16 * p.NT)));
-    p.lds = codes_product_table_bytes(w.dtype, bits, w.d);
-    if (p.lds < (size_t)p.waves * p.NT * 1024) p.lds = (size_t)p.waves * p.NT * 1024;
+    p.grid = dim3((unsigned)((w.rows + 15) / 16));
+    const size_t table = (size_t)(W << IB) * esize_of(w.dtype), sums = (size_t)p.waves * 1024;
+    p.lds = table > sums ? table : sums;
     return p;
 }
 
@@ -336,9 +336,12 @@ idkm_status idkm_codes_linear(idkm_ctx* ctx, const idkm_codes_desc* w, const voi
             a.cols = w->cols;
             a.C = w->C;
             a.k = w->k;
+            a.B = idkm_code_bits(w->k);
+            a.D = w->d;
+            a.row_bits = w->cols / w->d * a.B;
             a.S = w->S;
-            a.group = w->S ? (w->group < w->cols ? w->group : (int)w->cols) : 1;
             a.groups = groups_of(*w);
+            a.group_magic = few.group_magic;
             a.X = X;
             a.ldx = ldx;
             a.Y = Y;
