@@ -29,6 +29,10 @@ struct ProductArgs {
     void* Y;  // T [n, ldy]
     int64_t ldy;
     int64_t n;
+    // more than 16 tokens
+    int steps;       // of 128 columns
+    int x_pieces;    // rows of X begin at multiples of 16 bytes
+    float* sums;     // [gridDim.z][n][rows] where several workgroups share a row's sum
 };
 
 // Codes looked up at once: c codes of B bits and D weights each, c a power of two, at most 8 bits and 8 weights together.
@@ -264,6 +268,177 @@ __global__ __launch_bounds__(512) void k_codes_product(const ProductArgs a) {
         const int64_t t = e >> 4, n = n0 + (e & 15);
         if (t < a.n && n < a.rows) static_cast<T*>(a.Y)[t * a.ldy + n] = Elem<T>::down(sum);
     }
+}
+
+// More than 16 tokens: 16 NT of them and 64 rows of the layer to a workgroup, whose four pairs of wavefronts take 16 rows each; one
+// of a pair takes the even steps of 128 columns and one the odd ones.  The codes go the same way as above.  The activations, which
+// all four pairs need, come through LDS: up to ST - 1 steps ahead, copied there without passing registers, 16-byte pieces of row r in the
+// order c ^ (r mod 8).  gridDim.z workgroups share the columns; every one of them reads all tokens' activations of its columns, so that a
+// compute unit reads its share of X instead of all of it (64 tokens of 4096 columns are 512 KB).
+template <typename T, int NT>
+struct TileOfTokens {
+    static constexpr int ROW = 128 * (int)sizeof(T);  // bytes of a token's step
+    static constexpr int STAGE = NT * 16 * ROW;
+    static constexpr int FIT = 128 * 1024 / (2 * STAGE);
+    static constexpr int ST = FIT < 4 ? FIT : 4;
+    static constexpr int TABLE = 8192;
+    static constexpr int LDS = TABLE + 2 * ST * STAGE;
+    static_assert(ST >= 2, "stages");
+};
+
+template <typename T, int IB, int W, int L, int NT>
+__global__ __launch_bounds__(512) void k_codes_tile(const ProductArgs a) {
+    typedef TileOfTokens<T, NT> Tile;
+    constexpr int NB = L / W * IB;
+    constexpr int PER = Elem<T>::PER16, FR = 8 / PER, SUB = L / 8, CC = 32 / L;
+    constexpr int ROW = Tile::ROW, PIECES_ROW = ROW / 16, ST = Tile::ST;
+    constexpr int PP = Tile::STAGE / 1024 / 4;  // copies of a wavefront for a step
+    static_assert((W << IB) * (int)sizeof(T) <= Tile::TABLE, "table");
+    extern __shared__ __align__(1024) unsigned char lds[];
+    T* table = reinterpret_cast<T*>(lds);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int li = lane & 15, q = lane >> 4, rw = wave & 3, half = wave >> 2;
+    unsigned char* stage = lds + Tile::TABLE + half * ST * Tile::STAGE;
+    const int64_t n0 = (int64_t)blockIdx.x * 64 + rw * 16;
+    const int64_t row = min(n0 + li, a.rows - 1);
+    const int64_t t0 = (int64_t)blockIdx.y * (16 * NT);
+    const int each = (a.steps + gridDim.z - 1) / gridDim.z;
+    const int first = min(a.steps, (int)blockIdx.z * each), last = min(a.steps, first + each);
+    const int turns = (last - first + 1) / 2;  // steps first + 2 i + half; the last may be missing for the odd half
+    const int copied = a.x_pieces ? min(last, (int)(a.cols / 128)) : first;  // steps before this one are copied straight to LDS
+    const int64_t row_bit = row * a.row_bits + q * NB;
+    const int64_t room = a.nwords * 32 - 32 * CodeRun<NB>::SPAN - (min(n0 + 15, a.rows - 1) * a.row_bits + 3 * NB);
+    const int64_t safe = room < 0 ? 0 : room / (4 * NB) + 1;  // chunks before this one have all words that their runs may touch
+
+    const Table<T, IB, W> entries(a.C, a.k, a.B, a.D);
+    const T* X = static_cast<const T*>(a.X);
+    auto fetch = [&](int i, int slot) {
+        const int step = first + 2 * i + half;
+        if (step >= last) return;
+#pragma unroll
+        for (int p = 0; p < PP; ++p) {
+            const int at = (rw * PP + p) * 64 + lane, r = at / PIECES_ROW, c = (at % PIECES_ROW) ^ (r & 7);
+            const T* src = X + min(t0 + r, a.n - 1) * a.ldx;
+            const int64_t col = (int64_t)step * 128 + c * PER;
+            unsigned char* dst = stage + slot * Tile::STAGE + (rw * PP + p) * 1024;
+            if (step < copied) {
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + col),
+                                                 (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+            } else {
+                struct alignas(16) Piece { T v[PER]; } y;
+                if (col + PER <= a.cols) {
+                    const u32x4 v = *reinterpret_cast<const u32x4_any*>(src + col);
+                    __builtin_memcpy(&y, &v, 16);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) y.v[e] = col + e < a.cols ? src[col + e] : (T)0.f;
+                }
+                *reinterpret_cast<Piece*>(dst + lane * 16) = y;
+            }
+        }
+    };
+    CodeRun<NB> run[ST][CC];
+    float scale[ST][CC];
+    const bool scaled = a.groups > 0;
+    const float* S = scaled ? a.S + row * a.groups : reinterpret_cast<const float*>(a.words);
+    const int last_group = scaled ? a.groups - 1 : 0;
+    auto ask = [&](int i, int slot) {
+        const int step = first + 2 * i + half;
+        if (step >= last) return;
+        if ((int64_t)(step + 1) * CC <= safe) {
+#pragma unroll
+            for (int c = 0; c < CC; ++c) run[slot][c].template load<false, false>(a.words, a.nwords, row_bit + (int64_t)(step * CC + c) * (4 * NB));
+        } else {
+#pragma unroll
+            for (int c = 0; c < CC; ++c) run[slot][c].template load<false, true>(a.words, a.nwords, row_bit + (int64_t)(step * CC + c) * (4 * NB));
+        }
+#pragma unroll
+        for (int c = 0; c < CC; ++c) scale[slot][c] = S[min((int)__umulhi(2u * (unsigned)(step * CC + c), a.group_magic), last_group)];
+    };
+    floatx4 acc[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    auto use = [&](int i, int slot) {
+        const int step = first + 2 * i + half;
+        if (step >= last) return;
+        const bool whole = (int64_t)(step + 1) * 128 <= a.cols;
+        const unsigned char* x = stage + slot * Tile::STAGE + li * ROW;
+#pragma unroll
+        for (int c = 0; c < CC; ++c) {
+            floatx4 part[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) part[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < SUB; ++s) {
+                u32x4 wf[FR];
+                eight_weights<T, IB, W, NB>(wf, run[slot][c], s, table);
+                const int k = c * 4 * L + q * L + s * 8;
+                if (!whole) cut_weights<T>(wf, (int64_t)step * 128 + k, a.cols);
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int f = 0; f < FR; ++f) {
+                        const u32x4 xf = *reinterpret_cast<const u32x4*>(x + j * 16 * ROW + (((k / PER + f) ^ (li & 7)) << 4));
+                        mma16<T>(part[j], xf, wf[f]);
+                    }
+            }
+            const float by = scaled ? scale[slot][c] : 1.f;
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[j][r] = fmaf(by, part[j][r], acc[j][r]);
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < ST - 1; ++u)
+        if (u < turns) {
+            ask(u, u);
+            fetch(u, u);
+        }
+    entries.build(table, a.C, a.k, a.B, a.D);
+    for (int i0 = 0; i0 < turns; i0 += ST) {
+#pragma unroll
+        for (int u = 0; u < ST; ++u) {
+            const int i = i0 + u;
+            if (i < turns) {
+                // this step's copies are there: of all loads at most those of the ST - 2 steps behind it may be missing; where
+                // some of these were not copied, none
+                asm volatile("" ::: "memory");
+                if (first + 2 * (i + ST - 2) + half < copied)
+                    __builtin_amdgcn_s_waitcnt(0x0070 | ((PP * (ST - 2)) & 15) | (((PP * (ST - 2)) >> 4) << 14));
+                else
+                    __builtin_amdgcn_s_waitcnt(0x0070);
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                if (i + ST - 1 < turns) {
+                    ask(i + ST - 1, (u + ST - 1) % ST);
+                    fetch(i + ST - 1, (u + ST - 1) % ST);
+                }
+                use(i, u);
+            }
+        }
+    }
+    // the odd steps' sums join the even ones'
+    __syncthreads();
+    float* red = reinterpret_cast<float*>(lds + Tile::TABLE) + rw * (NT * 256) + lane;
+    if (half == 1) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) red[(j * 4 + r) * 64] = acc[j][r];
+    }
+    __syncthreads();
+    if (half == 1 || n0 + li >= a.rows) return;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int64_t t = t0 + j * 16 + q * 4 + r;
+            const float sum = acc[j][r] + red[(j * 4 + r) * 64];
+            if (t >= a.n) continue;
+            if (gridDim.z > 1) a.sums[((int64_t)blockIdx.z * a.n + t) * a.rows + row] = sum;
+            else static_cast<T*>(a.Y)[t * a.ldy + row] = Elem<T>::down(sum);
+        }
 }
 
 }  // namespace idkm

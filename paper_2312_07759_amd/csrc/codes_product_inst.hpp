@@ -27,12 +27,38 @@ static ProductFn for_type(int W, int L, bool aligned) {
     return nullptr;
 }
 
+template <typename T, int W>
+static ProductFn tile_for_run(int L, int NT) {
+    constexpr int IB = CODE_BITS;
+    if (NT == 2) return L == 8 ? &k_codes_tile<T, IB, W, 8, 2> : L == 16 ? &k_codes_tile<T, IB, W, 16, 2> : &k_codes_tile<T, IB, W, 32, 2>;
+    return L == 8 ? &k_codes_tile<T, IB, W, 8, 4> : L == 16 ? &k_codes_tile<T, IB, W, 16, 4> : &k_codes_tile<T, IB, W, 32, 4>;
+}
+
+template <typename T>
+static ProductFn tile_for_type(int W, int L, int NT) {
+    switch (W) {
+        case 1: if constexpr (CODE_BITS >= 5) return tile_for_run<T, 1>(L, NT); break;
+        case 2: if constexpr (CODE_BITS >= 5) return tile_for_run<T, 2>(L, NT); break;
+        case 4: if constexpr (CODE_BITS >= 5) return tile_for_run<T, 4>(L, NT); break;
+        case 8: return tile_for_run<T, 8>(L, NT);
+    }
+    return nullptr;
+}
+
 #define CODES_PRODUCT_NAME2(b) codes_product_kernel_##b
 #define CODES_PRODUCT_NAME(b) CODES_PRODUCT_NAME2(b)
 ProductFn CODES_PRODUCT_NAME(CODE_BITS)(int dtype, int W, int L, bool aligned) {
     if (dtype == 0) return for_type<float>(W, L, aligned);
     if (dtype == 1) return for_type<f16>(W, L, aligned);
     return for_type<bf16>(W, L, aligned);
+}
+
+#define CODES_TILE_NAME2(b) codes_tile_kernel_##b
+#define CODES_TILE_NAME(b) CODES_TILE_NAME2(b)
+ProductFn CODES_TILE_NAME(CODE_BITS)(int dtype, int W, int L, int NT) {
+    if (dtype == 0) return tile_for_type<float>(W, L, NT);
+    if (dtype == 1) return tile_for_type<f16>(W, L, NT);
+    return tile_for_type<bf16>(W, L, NT);
 }
 
 }  // namespace idkm

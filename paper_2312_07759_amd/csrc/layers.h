@@ -10,6 +10,8 @@ namespace idkm {
 // lane at a time (8, 16, 32); aligned: every run of codes begins with a word.  nullptr if not instantiated.
 typedef void (*ProductFn)(const ProductArgs);
 ProductFn codes_product_kernel(int dtype, int IB, int W, int L, bool aligned);
+// 17 tokens and more, 16 NT of them at a time (NT in {2, 4}).
+ProductFn codes_tile_kernel(int dtype, int IB, int W, int L, int NT);
 
 struct TileShape {
     int bm, bn, threads;

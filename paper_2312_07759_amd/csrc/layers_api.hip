@@ -24,6 +24,22 @@ ProductFn codes_product_kernel_6(int, int, int, bool);
 ProductFn codes_product_kernel_7(int, int, int, bool);
 ProductFn codes_product_kernel_8(int, int, int, bool);
 
+ProductFn codes_tile_kernel_1(int, int, int, int);
+ProductFn codes_tile_kernel_2(int, int, int, int);
+ProductFn codes_tile_kernel_3(int, int, int, int);
+ProductFn codes_tile_kernel_4(int, int, int, int);
+ProductFn codes_tile_kernel_5(int, int, int, int);
+ProductFn codes_tile_kernel_6(int, int, int, int);
+ProductFn codes_tile_kernel_7(int, int, int, int);
+ProductFn codes_tile_kernel_8(int, int, int, int);
+
+ProductFn codes_tile_kernel(int dtype, int IB, int W, int L, int NT) {
+    static ProductFn (*const by_bits[8])(int, int, int, int) = {
+        codes_tile_kernel_1, codes_tile_kernel_2, codes_tile_kernel_3, codes_tile_kernel_4,
+        codes_tile_kernel_5, codes_tile_kernel_6, codes_tile_kernel_7, codes_tile_kernel_8};
+    return IB >= 1 && IB <= 8 ? by_bits[IB - 1](dtype, W, L, NT) : nullptr;
+}
+
 ProductFn codes_product_kernel(int dtype, int IB, int W, int L, bool aligned) {
     static ProductFn (*const by_bits[8])(int, int, int, bool) = {
         codes_product_kernel_1, codes_product_kernel_2, codes_product_kernel_3, codes_product_kernel_4,
@@ -111,17 +127,19 @@ const char* wrong_layer(const idkm_codes_desc* w, idkm_status* st) {
 
 int groups_of(const idkm_codes_desc& w) { return w.S ? (int)((w.cols + w.group - 1) / w.group) : 0; }
 
-// ---- few tokens
+// ---- straight from the codes
 
 struct FewPlan {
     ProductFn fn = nullptr;
     unsigned group_magic = 0;
-    int waves;
+    int threads, steps = 0;
+    int parts = 1;  // workgroups that share a row's sum
     dim3 grid;
     size_t lds;
 };
 
-constexpr int64_t FEW_TOKENS = 16;
+// The matrix-vector form takes up to 16 tokens, the tiles of 32 or 64 the rest.
+constexpr int64_t VECTOR_TOKENS = 16, FEW_TOKENS = 256;
 
 FewPlan few_plan(const idkm_codes_desc& w, int64_t n) {
     FewPlan p;
@@ -130,19 +148,39 @@ FewPlan few_plan(const idkm_codes_desc& w, int64_t n) {
     // a chunk of four runs has to lie in one group
     const int L = !w.S || w.group >= w.cols || w.group % 128 == 0 ? 32 : w.group % 64 == 0 ? 16 : 8;
     const int at_once = codes_at_once(bits, w.d), IB = at_once * bits, W = at_once * w.d;
-    const bool aligned = (w.cols / w.d * bits) % 32 == 0 && (32 / W * IB) % 32 == 0;
     const int64_t chunks = (w.cols + 4 * L - 1) / (4 * L);
     if (w.S && w.group < w.cols) {  // exact while chunks (chunks of a group) < 2^31
         const int64_t of_group = w.group / (4 * L);
         if (chunks * of_group >= ((int64_t)1 << 31)) return p;
         p.group_magic = (unsigned)((((int64_t)1 << 31) + of_group - 1) / of_group);
     }
-    p.fn = codes_product_kernel(w.dtype, IB, W, L, aligned);
-    p.waves = chunks < 8 ? (int)chunks : 8;
-    p.grid = dim3((unsigned)((w.rows + 15) / 16));
-    const size_t table = (size_t)(W << IB) * esize_of(w.dtype), sums = (size_t)p.waves * 1024;
-    p.lds = table > sums ? table : sums;
+    if (n <= VECTOR_TOKENS) {
+        const bool aligned = (w.cols / w.d * bits) % 32 == 0 && (32 / W * IB) % 32 == 0;
+        p.fn = codes_product_kernel(w.dtype, IB, W, L, aligned);
+        const int waves = chunks < 8 ? (int)chunks : 8;
+        p.threads = waves * 64;
+        p.grid = dim3((unsigned)((w.rows + 15) / 16));
+        const size_t table = (size_t)(W << IB) * esize_of(w.dtype), sums = (size_t)waves * 1024;
+        p.lds = table > sums ? table : sums;
+        return p;
+    }
+    const int NT = n <= 32 ? 2 : 4;
+    p.fn = codes_tile_kernel(w.dtype, IB, W, L, NT);
+    p.threads = 512;
+    p.steps = (int)((w.cols + 127) / 128);
+    const int64_t blocks = (w.rows + 63) / 64, tokens = (n + 16 * NT - 1) / (16 * NT);
+    int64_t parts = 256 / (blocks * tokens);
+    if (parts > p.steps / 4) parts = p.steps / 4;
+    if (parts > 16) parts = 16;
+    p.parts = parts < 1 ? 1 : (int)parts;
+    p.grid = dim3((unsigned)blocks, (unsigned)tokens, (unsigned)p.parts);
+    p.lds = w.dtype == IDKM_F32 ? (NT == 2 ? TileOfTokens<float, 2>::LDS : TileOfTokens<float, 4>::LDS)
+                                : (NT == 2 ? TileOfTokens<bf16, 2>::LDS : TileOfTokens<bf16, 4>::LDS);
     return p;
+}
+
+int64_t few_bytes(const FewPlan& p, const idkm_codes_desc& w, int64_t n) {
+    return p.parts > 1 ? up_to(4 * p.parts * n * w.rows, 256) : 0;
 }
 
 // ---- tile products
@@ -310,7 +348,9 @@ extern "C" {
 int64_t idkm_codes_linear_workspace(const idkm_codes_desc* w, int64_t n) {
     idkm_status st;
     if (wrong_layer(w, &st) || n < 0 || n > MAX_SIDE) return -1;
-    if (n == 0 || few_plan(*w, n).fn) return 0;
+    if (n == 0) return 0;
+    const FewPlan few = few_plan(*w, n);
+    if (few.fn) return few_bytes(few, *w, n);
     return product_layout(w->dtype, n, w->rows, w->cols).bytes;
 }
 
@@ -347,7 +387,17 @@ idkm_status idkm_codes_linear(idkm_ctx* ctx, const idkm_codes_desc* w, const voi
             a.Y = Y;
             a.ldy = ldy;
             a.n = n;
-            return launched(ctx, [&] { hipLaunchKernelGGL(few.fn, few.grid, dim3((unsigned)few.waves * 64), few.lds, s, a); });
+            a.steps = few.steps;
+            a.x_pieces = ldx * es % 16 == 0 && aligned_to(X, 16);
+            if (const char* e = wrong_workspace(workspace, workspace_bytes, few_bytes(few, *w, n)))
+                return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
+            a.sums = static_cast<float*>(workspace);
+            return launched(ctx, [&] {
+                if (few.lds > 64 * 1024)
+                    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(few.fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)few.lds);
+                hipLaunchKernelGGL(few.fn, few.grid, dim3((unsigned)few.threads), few.lds, s, a);
+                if (few.parts > 1) launch_join_parts(w->dtype, a.sums, few.parts, n, w->rows, Y, ldy, s);
+            });
         }
         const ProductLayout l = product_layout(w->dtype, n, w->rows, w->cols);
         if (const char* e = wrong_workspace(workspace, workspace_bytes, l.bytes)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);

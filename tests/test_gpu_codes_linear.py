@@ -238,10 +238,10 @@ def test_refusals(ctx):
     with pytest.raises(TypeError):
         ctx.codes_linear_backward(g, None, torch.zeros(2, 16, device="cuda"))
     lib = ctx._lib
-    many = torch.zeros(200, 64, device="cuda")
-    Y = torch.zeros(200, 16, device="cuda")
-    call = lambda ws, size: lib.idkm_codes_linear(ctx._h, g._at, many.data_ptr(), 200, 64, Y.data_ptr(), 16, ws, size, None)  # noqa: E731
-    need = lib.idkm_codes_linear_workspace(g._at, 200)
+    n = 4000
+    many, Y = torch.zeros(n, 64, device="cuda"), torch.zeros(n, 16, device="cuda")
+    call = lambda ws, size: lib.idkm_codes_linear(ctx._h, g._at, many.data_ptr(), n, 64, Y.data_ptr(), 16, ws, size, None)  # noqa: E731
+    need = lib.idkm_codes_linear_workspace(g._at, n)
     ws = torch.empty(need + 16, dtype=torch.uint8, device="cuda")
     assert need > 0 and call(None, need) == 1 and call(ws.data_ptr(), need - 1) == 1 and call(ws.data_ptr() + 4, need) == 1
     assert b"workspace" in lib.idkm_last_error(ctx._h)
