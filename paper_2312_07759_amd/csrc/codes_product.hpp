@@ -30,8 +30,6 @@ struct ProductArgs {
     int64_t ldy;
     int64_t n;
     // more than 16 tokens
-    int steps;       // of 128 columns
-    int x_pieces;    // rows of X begin at multiples of 16 bytes
     float* sums;     // [gridDim.z][n][rows] where several workgroups share a row's sum
 };
 
@@ -42,11 +40,15 @@ constexpr int codes_at_once(int B, int D) {
     return c;
 }
 
-// The table in LDS: entry e holds the W weights of the codes in the IB bits e, the first code in the low bits.  A thread's first
-// entry is asked for by the constructor, so that the wait for it can come later.
+// The table in LDS: entry e holds the W weights of the codes in the IB bits e, the first code in the low bits.  It has 128 bytes,
+// all 32 banks, filled with copies; a lane reads the copy in its own banks, so that no lane waits for another (with one copy, 32
+// lanes at random places of 32 banks took 3.5 turns instead of one, and the lookups bounded the product of a single token).
+// A thread's first entry is asked for by the constructor, so that the wait for it can come later.
 template <typename T, int IB, int W>
 struct Table {
-    struct alignas(W * sizeof(T) > 16 ? 16 : W * sizeof(T)) Entry { T v[W]; };
+    static constexpr int ENTRIES = 1 << IB, BYTES = 128 * ENTRIES;
+    static constexpr int WIDTH = W * (int)sizeof(T), STRIDE = WIDTH < 4 ? 4 : WIDTH, COPIES = 128 / STRIDE;
+    struct alignas(WIDTH > 16 ? 16 : WIDTH) Entry { T v[W]; };
     T first[W];
     unsigned none;  // bit i: first[i] belongs to a code that is none
     static __device__ __forceinline__ unsigned ask(T* v, unsigned e, const void* codebook, int k, int B, int D) {
@@ -66,22 +68,42 @@ struct Table {
         }
         return none;
     }
-    static __device__ __forceinline__ void put(T* table, unsigned e, const T* v, unsigned none) {
-        Entry x;
+    // 16-byte pieces h, h + step, .. of entry e, from a place on that depends on the lane: neighbours write to different banks
+    static __device__ __forceinline__ void put(unsigned char* lds, unsigned e, const T* v, unsigned none, int h, int step) {
+        constexpr int N = WIDTH > 16 ? 2 : 1;  // different pieces
+        u32x4 piece[N];
+        T x[N * 16 / sizeof(T)];
 #pragma unroll
-        for (int i = 0; i < W; ++i) x.v[i] = none >> i & 1 ? Elem<T>::nan() : v[i];
-        *reinterpret_cast<Entry*>(table + e * W) = x;
+        for (int i = 0; i < N * 16 / (int)sizeof(T); ++i) {
+            const int w = i % W;
+            x[i] = none >> w & 1 ? Elem<T>::nan() : v[w];
+        }
+        __builtin_memcpy(piece, x, sizeof(piece));
+        for (int j = h; j < 8; j += step) {
+            const int at = (j + threadIdx.x) & 7;
+            *reinterpret_cast<u32x4*>(lds + e * 128 + at * 16) = N > 1 && (at & 1) ? piece[N - 1] : piece[0];
+        }
     }
     __device__ __forceinline__ Table(const void* codebook, int k, int B, int D) {
-        none = ask(first, threadIdx.x & ((1u << IB) - 1u), codebook, k, B, D);
+        none = ask(first, threadIdx.x & (ENTRIES - 1), codebook, k, B, D);
     }
-    __device__ __forceinline__ void build(T* table, const void* codebook, int k, int B, int D) const {
-        if (threadIdx.x < (1u << IB)) put(table, threadIdx.x, first, none);
-        for (unsigned e = threadIdx.x + blockDim.x; e < (1u << IB); e += blockDim.x) {
-            T v[W];
-            const unsigned n = ask(v, e, codebook, k, B, D);
-            put(table, e, v, n);
+    __device__ __forceinline__ void build(unsigned char* lds, const void* codebook, int k, int B, int D) const {
+        const unsigned team = blockDim.x >> IB;  // threads to an entry
+        if (team >= 1) {
+            const int step = team >= 8 ? 8 : team >= 4 ? 4 : team >= 2 ? 2 : 1;
+            if ((int)(threadIdx.x >> IB) < step) put(lds, threadIdx.x & (ENTRIES - 1), first, none, (int)(threadIdx.x >> IB), step);
+        } else {
+            put(lds, threadIdx.x, first, none, 0, 1);
+            for (unsigned e = threadIdx.x + blockDim.x; e < ENTRIES; e += blockDim.x) {
+                T v[W];
+                const unsigned n = ask(v, e, codebook, k, B, D);
+                put(lds, e, v, n, 0, 1);
+            }
         }
+    }
+    // where this lane's copies begin
+    static __device__ __forceinline__ const unsigned char* own(const unsigned char* lds) {
+        return lds + (threadIdx.x % COPIES) * STRIDE;
     }
 };
 
@@ -121,6 +143,40 @@ struct CodeRun {
 #pragma unroll
         for (int i = 0; i < NWORDS; ++i) w[i] = ALIGNED ? raw[i] : __builtin_amdgcn_alignbit(raw[i + 1], raw[i], sh);
     }
+    // The same without a branch, for a run that lies in the stream as a whole (which has at least SPAN words): near its end the
+    // words are taken from one further ahead.  `bit` counts from `words` on; no window begins behind word `limit`.
+    template <bool ALIGNED>
+    __device__ __forceinline__ void load_inside(const uint32_t* words, int limit, unsigned bit) {
+        constexpr int RAW = ALIGNED ? NWORDS : SPAN;
+        const int at = (int)(bit >> 5);
+        const unsigned from = ALIGNED ? (unsigned)at : (unsigned)min(at, limit);
+        uint32_t raw[RAW + 2];
+        constexpr int Q = RAW / 4 * 4;
+#pragma unroll
+        for (int i = 0; i < Q; i += 4) {
+            const u32x4 v = *reinterpret_cast<const u32x4_word*>(words + from + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) raw[i + e] = v[e];
+        }
+        if constexpr (RAW - Q >= 2) {
+            const u32x2 v = *reinterpret_cast<const u32x2_word*>(words + from + Q);
+            raw[Q] = v[0];
+            raw[Q + 1] = v[1];
+        }
+        if constexpr (RAW % 2 == 1) raw[RAW - 1] = words[from + RAW - 1];
+        raw[RAW] = raw[RAW + 1] = 0;
+        const int sh = (int)(bit & 31);
+        const bool ahead = SPAN > NWORDS && at != (int)from;
+#pragma unroll
+        for (int i = 0; i < NWORDS; ++i) {
+            if constexpr (ALIGNED) {
+                w[i] = raw[i];
+            } else {
+                const uint32_t lo = ahead ? raw[i + 1] : raw[i], hi = ahead ? raw[i + 2] : raw[i + 1];
+                w[i] = __builtin_amdgcn_alignbit(hi, lo, sh);
+            }
+        }
+    }
     // bits [at, at + n), n <= 8, at known to the compiler
     __device__ __forceinline__ uint32_t bits(int at, int n) const {
         const int i = at >> 5, sh = at & 31;
@@ -131,13 +187,12 @@ struct CodeRun {
 
 // Eight weights from the run's looked-up codes s * 8 / W ...
 template <typename T, int IB, int W, int NB>
-__device__ __forceinline__ void eight_weights(u32x4* out, const CodeRun<NB>& run, int s, const T* table) {
+__device__ __forceinline__ void eight_weights(u32x4* out, const CodeRun<NB>& run, int s, const unsigned char* own) {
     struct alignas(16) Eight { T v[8]; } w;
 #pragma unroll
     for (int e = 0; e < 8 / W; ++e) {
         const uint32_t idx = run.bits((s * 8 / W + e) * IB, IB);
-        struct alignas(W * sizeof(T) > 16 ? 16 : W * sizeof(T)) Entry { T v[W]; };
-        const Entry x = *reinterpret_cast<const Entry*>(table + idx * W);
+        const auto x = *reinterpret_cast<const typename Table<T, IB, W>::Entry*>(own + idx * 128);
 #pragma unroll
         for (int i = 0; i < W; ++i) w.v[e * W + i] = x.v[i];
     }
@@ -178,8 +233,8 @@ __global__ __launch_bounds__(512) void k_codes_product(const ProductArgs a) {
     constexpr int FR = 8 / Elem<T>::PER16;  // 16-byte fragments in 8 weights
     constexpr int SUB = L / 8;
     constexpr int U = 16 / (SUB * FR);  // chunks of a batch: 64 registers of activations
-    extern __shared__ __align__(16) unsigned char lds[];
-    T* table = reinterpret_cast<T*>(lds);
+    extern __shared__ __align__(128) unsigned char lds[];
+    const unsigned char* table = Table<T, IB, W>::own(lds);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
     const int li = lane & 15, q = lane >> 4;
     const int64_t n0 = (int64_t)blockIdx.x * 16;
@@ -231,7 +286,7 @@ __global__ __launch_bounds__(512) void k_codes_product(const ProductArgs a) {
     if (ch + U <= safe) {
 #pragma unroll
         for (int u = 0; u < U; ++u) ask(u, ch + u, whole);
-        entries.build(table, a.C, a.k, a.B, a.D);
+        entries.build(lds, a.C, a.k, a.B, a.D);
         __syncthreads();
         built = true;
         for (;;) {
@@ -244,7 +299,7 @@ __global__ __launch_bounds__(512) void k_codes_product(const ProductArgs a) {
         }
     }
     if (!built) {
-        entries.build(table, a.C, a.k, a.B, a.D);
+        entries.build(lds, a.C, a.k, a.B, a.D);
         __syncthreads();
     }
     for (; ch < last; ++ch) {
@@ -275,169 +330,174 @@ __global__ __launch_bounds__(512) void k_codes_product(const ProductArgs a) {
 // all four pairs need, come through LDS: up to ST - 1 steps ahead, copied there without passing registers, 16-byte pieces of row r in the
 // order c ^ (r mod 8).  gridDim.z workgroups share the columns; every one of them reads all tokens' activations of its columns, so that a
 // compute unit reads its share of X instead of all of it (64 tokens of 4096 columns are 512 KB).
+// Rows of X begin at multiples of 16 bytes and go on to a multiple of 128 columns, with zeros behind the layer's last.
+// What bounds it is the issue of instructions by two wavefronts a SIMD, so offsets inside a workgroup's rows and tokens are 32 bits
+// (16 rows of 4,000,000 codes of 8 bits are 2^29 bits, 64 tokens of as many float columns 2^30 bytes).
 template <typename T, int NT>
 struct TileOfTokens {
     static constexpr int ROW = 128 * (int)sizeof(T);  // bytes of a token's step
     static constexpr int STAGE = NT * 16 * ROW;
     static constexpr int FIT = 128 * 1024 / (2 * STAGE);
     static constexpr int ST = FIT < 4 ? FIT : 4;
-    static constexpr int TABLE = 8192;
+    static constexpr int TABLE = 32 * 1024;
     static constexpr int LDS = TABLE + 2 * ST * STAGE;
     static_assert(ST >= 2, "stages");
 };
 
-template <typename T, int IB, int W, int L, int NT>
+template <typename T, int IB, int W, int L, int NT, bool ALIGNED>
 __global__ __launch_bounds__(512) void k_codes_tile(const ProductArgs a) {
     typedef TileOfTokens<T, NT> Tile;
     constexpr int NB = L / W * IB;
     constexpr int PER = Elem<T>::PER16, FR = 8 / PER, SUB = L / 8, CC = 32 / L;
     constexpr int ROW = Tile::ROW, PIECES_ROW = ROW / 16, ST = Tile::ST;
     constexpr int PP = Tile::STAGE / 1024 / 4;  // copies of a wavefront for a step
-    static_assert((W << IB) * (int)sizeof(T) <= Tile::TABLE, "table");
+    static_assert(Table<T, IB, W>::BYTES <= Tile::TABLE, "table");
     extern __shared__ __align__(1024) unsigned char lds[];
-    T* table = reinterpret_cast<T*>(lds);
+    const unsigned char* table = Table<T, IB, W>::own(lds);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int li = lane & 15, q = lane >> 4, rw = wave & 3, half = wave >> 2;
     unsigned char* stage = lds + Tile::TABLE + half * ST * Tile::STAGE;
-    const int64_t n0 = (int64_t)blockIdx.x * 64 + rw * 16;
-    const int64_t row = min(n0 + li, a.rows - 1);
-    const int64_t t0 = (int64_t)blockIdx.y * (16 * NT);
-    const int each = (a.steps + gridDim.z - 1) / gridDim.z;
-    const int first = min(a.steps, (int)blockIdx.z * each), last = min(a.steps, first + each);
-    const int turns = (last - first + 1) / 2;  // steps first + 2 i + half; the last may be missing for the odd half
-    const int copied = a.x_pieces ? min(last, (int)(a.cols / 128)) : first;  // steps before this one are copied straight to LDS
-    const int64_t row_bit = row * a.row_bits + q * NB;
-    const int64_t room = a.nwords * 32 - 32 * CodeRun<NB>::SPAN - (min(n0 + 15, a.rows - 1) * a.row_bits + 3 * NB);
-    const int64_t safe = room < 0 ? 0 : room / (4 * NB) + 1;  // chunks before this one have all words that their runs may touch
-
     const Table<T, IB, W> entries(a.C, a.k, a.B, a.D);
-    const T* X = static_cast<const T*>(a.X);
-    auto fetch = [&](int i, int slot) {
-        const int step = first + 2 * i + half;
-        if (step >= last) return;
+    // 16 rows from n0 on, clamped; 16 NT tokens from t0 on
+    const int64_t n0 = min((int64_t)blockIdx.x * 64 + rw * 16, a.rows - 1), t0 = (int64_t)blockIdx.y * (16 * NT);
+    const int row = (int)min((int64_t)li, a.rows - 1 - n0);
+    const int whole = (int)(a.cols / 128);  // steps without the broken one
+    const int each = (whole + gridDim.z - 1) / gridDim.z;
+    const int first = min(whole, (int)blockIdx.z * each), last = min(whole, first + each);
+    const int turns = (last - first + 1) / 2;  // steps first + 2 i + half; the odd half may have no last one
+    const int64_t bit0 = n0 * a.row_bits;
+    const uint32_t* words = a.words + (bit0 >> 5);
+    const int limit = (int)min(a.nwords - (bit0 >> 5) - CodeRun<NB>::SPAN, (int64_t)1 << 30);
+    const unsigned row_bit = (unsigned)(bit0 & 31) + (unsigned)row * (unsigned)a.row_bits + q * NB;
+    const bool scaled = a.groups > 0;
+    const float* S = scaled ? a.S + n0 * a.groups : nullptr;
+    const unsigned S_row = (unsigned)(row * a.groups);
+    const unsigned char* X = reinterpret_cast<const unsigned char*>(static_cast<const T*>(a.X) + t0 * a.ldx);
+
+    unsigned src[PP];  // of this lane's pieces, from X on
 #pragma unroll
-        for (int p = 0; p < PP; ++p) {
-            const int at = (rw * PP + p) * 64 + lane, r = at / PIECES_ROW, c = (at % PIECES_ROW) ^ (r & 7);
-            const T* src = X + min(t0 + r, a.n - 1) * a.ldx;
-            const int64_t col = (int64_t)step * 128 + c * PER;
-            unsigned char* dst = stage + slot * Tile::STAGE + (rw * PP + p) * 1024;
-            if (step < copied) {
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + col),
-                                                 (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
-            } else {
-                struct alignas(16) Piece { T v[PER]; } y;
-                if (col + PER <= a.cols) {
-                    const u32x4 v = *reinterpret_cast<const u32x4_any*>(src + col);
-                    __builtin_memcpy(&y, &v, 16);
-                } else {
+    for (int p = 0; p < PP; ++p) {
+        const int at = (rw * PP + p) * 64 + lane, r = at / PIECES_ROW, c = (at % PIECES_ROW) ^ (r & 7);
+        src[p] = (unsigned)min((int64_t)r, a.n - 1 - t0) * (unsigned)(a.ldx * sizeof(T)) + c * 16;
+    }
+    auto fetch = [&](int step, int slot) {
+        const unsigned char* from = X + (int64_t)step * ROW;
 #pragma unroll
-                    for (int e = 0; e < PER; ++e) y.v[e] = col + e < a.cols ? src[col + e] : (T)0.f;
-                }
-                *reinterpret_cast<Piece*>(dst + lane * 16) = y;
-            }
-        }
+        for (int p = 0; p < PP; ++p)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + src[p]),
+                                             (__attribute__((address_space(3))) void*)(stage + slot * Tile::STAGE + (rw * PP + p) * 1024), 16,
+                                             0, 0);
+    };
+    auto scale_of = [&](int chunk) {
+        if (!scaled) return 1.f;
+        return S[S_row + min(__umulhi(2u * (unsigned)chunk, a.group_magic), (unsigned)(a.groups - 1))];
     };
     CodeRun<NB> run[ST][CC];
     float scale[ST][CC];
-    const bool scaled = a.groups > 0;
-    const float* S = scaled ? a.S + row * a.groups : reinterpret_cast<const float*>(a.words);
-    const int last_group = scaled ? a.groups - 1 : 0;
-    auto ask = [&](int i, int slot) {
-        const int step = first + 2 * i + half;
-        if (step >= last) return;
-        if ((int64_t)(step + 1) * CC <= safe) {
+    auto ask = [&](int step, int slot) {
 #pragma unroll
-            for (int c = 0; c < CC; ++c) run[slot][c].template load<false, false>(a.words, a.nwords, row_bit + (int64_t)(step * CC + c) * (4 * NB));
-        } else {
-#pragma unroll
-            for (int c = 0; c < CC; ++c) run[slot][c].template load<false, true>(a.words, a.nwords, row_bit + (int64_t)(step * CC + c) * (4 * NB));
+        for (int c = 0; c < CC; ++c) {
+            run[slot][c].template load_inside<ALIGNED>(words, limit, row_bit + (unsigned)(step * CC + c) * (4 * NB));
+            scale[slot][c] = scale_of(step * CC + c);
         }
-#pragma unroll
-        for (int c = 0; c < CC; ++c) scale[slot][c] = S[min((int)__umulhi(2u * (unsigned)(step * CC + c), a.group_magic), last_group)];
     };
     floatx4 acc[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    auto use = [&](int i, int slot) {
-        const int step = first + 2 * i + half;
-        if (step >= last) return;
-        const bool whole = (int64_t)(step + 1) * 128 <= a.cols;
+    auto use = [&](const CodeRun<NB>& codes, float by, int c, int slot, int64_t cut) {
         const unsigned char* x = stage + slot * Tile::STAGE + li * ROW;
+        floatx4 part[NT];
 #pragma unroll
-        for (int c = 0; c < CC; ++c) {
-            floatx4 part[NT];
+        for (int j = 0; j < NT; ++j) part[j] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < NT; ++j) part[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < SUB; ++s) {
+            u32x4 wf[FR];
+            eight_weights<T, IB, W, NB>(wf, codes, s, table);
+            const int k = c * 4 * L + q * L + s * 8;
+            if (cut >= 0) cut_weights<T>(wf, cut + k, a.cols);
 #pragma unroll
-            for (int s = 0; s < SUB; ++s) {
-                u32x4 wf[FR];
-                eight_weights<T, IB, W, NB>(wf, run[slot][c], s, table);
-                const int k = c * 4 * L + q * L + s * 8;
-                if (!whole) cut_weights<T>(wf, (int64_t)step * 128 + k, a.cols);
+            for (int f = 0; f < FR; ++f) {
+                const unsigned char* piece = x + (((k / PER + f) ^ (li & 7)) << 4);
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
-#pragma unroll
-                    for (int f = 0; f < FR; ++f) {
-                        const u32x4 xf = *reinterpret_cast<const u32x4*>(x + j * 16 * ROW + (((k / PER + f) ^ (li & 7)) << 4));
-                        mma16<T>(part[j], xf, wf[f]);
-                    }
+                for (int j = 0; j < NT; ++j) mma16<T>(part[j], *reinterpret_cast<const u32x4*>(piece + j * 16 * ROW), wf[f]);
             }
-            const float by = scaled ? scale[slot][c] : 1.f;
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) acc[j][r] = fmaf(by, part[j][r], acc[j][r]);
         }
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[j][r] = fmaf(by, part[j][r], acc[j][r]);
     };
 #pragma unroll
     for (int u = 0; u < ST - 1; ++u)
         if (u < turns) {
-            ask(u, u);
-            fetch(u, u);
+            const int step = min(first + 2 * u + half, last - 1);
+            ask(step, u);
+            fetch(step, u);
         }
-    entries.build(table, a.C, a.k, a.B, a.D);
+    entries.build(lds, a.C, a.k, a.B, a.D);
     for (int i0 = 0; i0 < turns; i0 += ST) {
 #pragma unroll
         for (int u = 0; u < ST; ++u) {
             const int i = i0 + u;
             if (i < turns) {
-                // this step's copies are there: of all loads at most those of the ST - 2 steps behind it may be missing; where
-                // some of these were not copied, none
+                // this step's copies are there: of all loads at most as many may be missing as the copies of the ST - 2 steps behind
+                // it, and near the end, where there are fewer steps behind it, none
                 asm volatile("" ::: "memory");
-                if (first + 2 * (i + ST - 2) + half < copied)
+                if (i + ST - 2 < turns)
                     __builtin_amdgcn_s_waitcnt(0x0070 | ((PP * (ST - 2)) & 15) | (((PP * (ST - 2)) >> 4) << 14));
                 else
                     __builtin_amdgcn_s_waitcnt(0x0070);
                 __builtin_amdgcn_s_barrier();
                 asm volatile("" ::: "memory");
                 if (i + ST - 1 < turns) {
-                    ask(i + ST - 1, (u + ST - 1) % ST);
-                    fetch(i + ST - 1, (u + ST - 1) % ST);
+                    const int step = min(first + 2 * (i + ST - 1) + half, last - 1);
+                    ask(step, (u + ST - 1) % ST);
+                    fetch(step, (u + ST - 1) % ST);
                 }
-                use(i, u);
+                if (first + 2 * i + half < last) {
+#pragma unroll
+                    for (int c = 0; c < CC; ++c) use(run[u][c], scale[u][c], c, u, -1);
+                }
             }
         }
     }
-    // the odd steps' sums join the even ones'
     __syncthreads();
-    float* red = reinterpret_cast<float*>(lds + Tile::TABLE) + rw * (NT * 256) + lane;
-    if (half == 1) {
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) red[(j * 4 + r) * 64] = acc[j][r];
+    if (whole * (int64_t)128 < a.cols && blockIdx.z + 1 == gridDim.z) {  // the row's broken step
+        if (half == 0) fetch(whole, 0);
+        __builtin_amdgcn_s_waitcnt(0x0070);
+        __syncthreads();
+        if (half == 0)
+            for (int c = 0; c < CC; ++c) {
+                CodeRun<NB> codes;
+                codes.template load<false, true>(a.words, a.nwords, (n0 + row) * a.row_bits + q * NB + (int64_t)(whole * CC + c) * (4 * NB));
+                use(codes, scale_of(whole * CC + c), c, 0, (int64_t)whole * 128);
+            }
+        __syncthreads();
     }
-    __syncthreads();
-    if (half == 1 || n0 + li >= a.rows) return;
+    // The odd and the even steps' sums: of every two tiles of tokens each half of the workgroup finishes one.
+    float* red = reinterpret_cast<float*>(lds + Tile::TABLE) + rw * (NT * 256) + lane * 4;
 #pragma unroll
     for (int j = 0; j < NT; ++j)
+        if ((j & 1) != half) *reinterpret_cast<floatx4*>(red + j * 256) = acc[j];
+    __syncthreads();
+    if ((int64_t)blockIdx.x * 64 + rw * 16 + li >= a.rows) return;
+    const bool shared = gridDim.z > 1;
+    const int64_t pitch = shared ? a.rows : a.ldy;
+    const int64_t out0 = ((shared ? (int64_t)blockIdx.z * a.n : 0) + t0 + q * 4) * pitch + n0 + li;
+    float* sums = a.sums + out0;
+    T* Y = static_cast<T*>(a.Y) + out0;
+    const int tokens = (int)min(a.n - t0, (int64_t)(16 * NT));
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int64_t t = t0 + j * 16 + q * 4 + r;
-            const float sum = acc[j][r] + red[(j * 4 + r) * 64];
-            if (t >= a.n) continue;
-            if (gridDim.z > 1) a.sums[((int64_t)blockIdx.z * a.n + t) * a.rows + row] = sum;
-            else static_cast<T*>(a.Y)[t * a.ldy + row] = Elem<T>::down(sum);
+    for (int j = 0; j < NT; ++j)
+        if ((j & 1) == half) {
+            const floatx4 other = *reinterpret_cast<const floatx4*>(red + j * 256);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float sum = acc[j][r] + other[r];
+                if (j * 16 + q * 4 + r >= tokens) continue;
+                if (shared) sums[(j * 16 + r) * pitch] = sum;
+                else Y[(j * 16 + r) * pitch] = Elem<T>::down(sum);
+            }
         }
 }
 

@@ -27,20 +27,24 @@ static ProductFn for_type(int W, int L, bool aligned) {
     return nullptr;
 }
 
-template <typename T, int W>
-static ProductFn tile_for_run(int L, int NT) {
+template <typename T, int W, int NT>
+static ProductFn tile_for_run(int L, bool aligned) {
     constexpr int IB = CODE_BITS;
-    if (NT == 2) return L == 8 ? &k_codes_tile<T, IB, W, 8, 2> : L == 16 ? &k_codes_tile<T, IB, W, 16, 2> : &k_codes_tile<T, IB, W, 32, 2>;
-    return L == 8 ? &k_codes_tile<T, IB, W, 8, 4> : L == 16 ? &k_codes_tile<T, IB, W, 16, 4> : &k_codes_tile<T, IB, W, 32, 4>;
+    if (L == 8) return &k_codes_tile<T, IB, W, 8, NT, false>;
+    if (L == 16) return &k_codes_tile<T, IB, W, 16, NT, false>;
+    if constexpr (32 / W * IB % 32 == 0) {
+        if (aligned) return &k_codes_tile<T, IB, W, 32, NT, true>;
+    }
+    return &k_codes_tile<T, IB, W, 32, NT, false>;
 }
 
 template <typename T>
-static ProductFn tile_for_type(int W, int L, int NT) {
+static ProductFn tile_for_type(int W, int L, int NT, bool aligned) {
     switch (W) {
-        case 1: if constexpr (CODE_BITS >= 5) return tile_for_run<T, 1>(L, NT); break;
-        case 2: if constexpr (CODE_BITS >= 5) return tile_for_run<T, 2>(L, NT); break;
-        case 4: if constexpr (CODE_BITS >= 5) return tile_for_run<T, 4>(L, NT); break;
-        case 8: return tile_for_run<T, 8>(L, NT);
+        case 1: if constexpr (CODE_BITS >= 5) return NT == 2 ? tile_for_run<T, 1, 2>(L, aligned) : tile_for_run<T, 1, 4>(L, aligned); break;
+        case 2: if constexpr (CODE_BITS >= 5) return NT == 2 ? tile_for_run<T, 2, 2>(L, aligned) : tile_for_run<T, 2, 4>(L, aligned); break;
+        case 4: if constexpr (CODE_BITS >= 5) return NT == 2 ? tile_for_run<T, 4, 2>(L, aligned) : tile_for_run<T, 4, 4>(L, aligned); break;
+        case 8: return NT == 2 ? tile_for_run<T, 8, 2>(L, aligned) : tile_for_run<T, 8, 4>(L, aligned);
     }
     return nullptr;
 }
@@ -55,10 +59,10 @@ ProductFn CODES_PRODUCT_NAME(CODE_BITS)(int dtype, int W, int L, bool aligned) {
 
 #define CODES_TILE_NAME2(b) codes_tile_kernel_##b
 #define CODES_TILE_NAME(b) CODES_TILE_NAME2(b)
-ProductFn CODES_TILE_NAME(CODE_BITS)(int dtype, int W, int L, int NT) {
-    if (dtype == 0) return tile_for_type<float>(W, L, NT);
-    if (dtype == 1) return tile_for_type<f16>(W, L, NT);
-    return tile_for_type<bf16>(W, L, NT);
+ProductFn CODES_TILE_NAME(CODE_BITS)(int dtype, int W, int L, int NT, bool aligned) {
+    if (dtype == 0) return tile_for_type<float>(W, L, NT, aligned);
+    if (dtype == 1) return tile_for_type<f16>(W, L, NT, aligned);
+    return tile_for_type<bf16>(W, L, NT, aligned);
 }
 
 }  // namespace idkm

@@ -11,7 +11,7 @@ namespace idkm {
 typedef void (*ProductFn)(const ProductArgs);
 ProductFn codes_product_kernel(int dtype, int IB, int W, int L, bool aligned);
 // 17 tokens and more, 16 NT of them at a time (NT in {2, 4}).
-ProductFn codes_tile_kernel(int dtype, int IB, int W, int L, int NT);
+ProductFn codes_tile_kernel(int dtype, int IB, int W, int L, int NT, bool aligned);
 
 struct TileShape {
     int bm, bn, threads;

@@ -24,20 +24,20 @@ ProductFn codes_product_kernel_6(int, int, int, bool);
 ProductFn codes_product_kernel_7(int, int, int, bool);
 ProductFn codes_product_kernel_8(int, int, int, bool);
 
-ProductFn codes_tile_kernel_1(int, int, int, int);
-ProductFn codes_tile_kernel_2(int, int, int, int);
-ProductFn codes_tile_kernel_3(int, int, int, int);
-ProductFn codes_tile_kernel_4(int, int, int, int);
-ProductFn codes_tile_kernel_5(int, int, int, int);
-ProductFn codes_tile_kernel_6(int, int, int, int);
-ProductFn codes_tile_kernel_7(int, int, int, int);
-ProductFn codes_tile_kernel_8(int, int, int, int);
+ProductFn codes_tile_kernel_1(int, int, int, int, bool);
+ProductFn codes_tile_kernel_2(int, int, int, int, bool);
+ProductFn codes_tile_kernel_3(int, int, int, int, bool);
+ProductFn codes_tile_kernel_4(int, int, int, int, bool);
+ProductFn codes_tile_kernel_5(int, int, int, int, bool);
+ProductFn codes_tile_kernel_6(int, int, int, int, bool);
+ProductFn codes_tile_kernel_7(int, int, int, int, bool);
+ProductFn codes_tile_kernel_8(int, int, int, int, bool);
 
-ProductFn codes_tile_kernel(int dtype, int IB, int W, int L, int NT) {
-    static ProductFn (*const by_bits[8])(int, int, int, int) = {
+ProductFn codes_tile_kernel(int dtype, int IB, int W, int L, int NT, bool aligned) {
+    static ProductFn (*const by_bits[8])(int, int, int, int, bool) = {
         codes_tile_kernel_1, codes_tile_kernel_2, codes_tile_kernel_3, codes_tile_kernel_4,
         codes_tile_kernel_5, codes_tile_kernel_6, codes_tile_kernel_7, codes_tile_kernel_8};
-    return IB >= 1 && IB <= 8 ? by_bits[IB - 1](dtype, W, L, NT) : nullptr;
+    return IB >= 1 && IB <= 8 ? by_bits[IB - 1](dtype, W, L, NT, aligned) : nullptr;
 }
 
 ProductFn codes_product_kernel(int dtype, int IB, int W, int L, bool aligned) {
@@ -132,7 +132,8 @@ int groups_of(const idkm_codes_desc& w) { return w.S ? (int)((w.cols + w.group -
 struct FewPlan {
     ProductFn fn = nullptr;
     unsigned group_magic = 0;
-    int threads, steps = 0;
+    int threads;
+    int64_t pad = 0;  // columns to which X is brought for the tiles
     int parts = 1;  // workgroups that share a row's sum
     dim3 grid;
     size_t lds;
@@ -154,23 +155,25 @@ FewPlan few_plan(const idkm_codes_desc& w, int64_t n) {
         if (chunks * of_group >= ((int64_t)1 << 31)) return p;
         p.group_magic = (unsigned)((((int64_t)1 << 31) + of_group - 1) / of_group);
     }
+    if (n > VECTOR_TOKENS && w.rows * w.cols / w.d * bits < 1024) return p;  // a run's words have to be there
+    const bool aligned = (w.cols / w.d * bits) % 32 == 0 && (32 / W * IB) % 32 == 0;
     if (n <= VECTOR_TOKENS) {
-        const bool aligned = (w.cols / w.d * bits) % 32 == 0 && (32 / W * IB) % 32 == 0;
         p.fn = codes_product_kernel(w.dtype, IB, W, L, aligned);
         const int waves = chunks < 8 ? (int)chunks : 8;
         p.threads = waves * 64;
         p.grid = dim3((unsigned)((w.rows + 15) / 16));
-        const size_t table = (size_t)(W << IB) * esize_of(w.dtype), sums = (size_t)waves * 1024;
+        const size_t table = (size_t)128 << IB, sums = (size_t)waves * 1024;
         p.lds = table > sums ? table : sums;
         return p;
     }
     const int NT = n <= 32 ? 2 : 4;
-    p.fn = codes_tile_kernel(w.dtype, IB, W, L, NT);
+    p.fn = codes_tile_kernel(w.dtype, IB, W, L, NT, aligned);
     p.threads = 512;
-    p.steps = (int)((w.cols + 127) / 128);
+    p.pad = up_to(w.cols, 128);
+    const int64_t steps = p.pad / 128;
     const int64_t blocks = (w.rows + 63) / 64, tokens = (n + 16 * NT - 1) / (16 * NT);
     int64_t parts = 256 / (blocks * tokens);
-    if (parts > p.steps / 4) parts = p.steps / 4;
+    if (parts > steps / 4) parts = steps / 4;
     if (parts > 16) parts = 16;
     p.parts = parts < 1 ? 1 : (int)parts;
     p.grid = dim3((unsigned)blocks, (unsigned)tokens, (unsigned)p.parts);
@@ -179,8 +182,10 @@ FewPlan few_plan(const idkm_codes_desc& w, int64_t n) {
     return p;
 }
 
+// Workspace: the parts' sums, and X with whole steps (which not every call needs).
+int64_t few_sums(const FewPlan& p, const idkm_codes_desc& w, int64_t n) { return p.parts > 1 ? up_to(4 * p.parts * n * w.rows, 256) : 0; }
 int64_t few_bytes(const FewPlan& p, const idkm_codes_desc& w, int64_t n) {
-    return p.parts > 1 ? up_to(4 * p.parts * n * w.rows, 256) : 0;
+    return few_sums(p, w, n) + up_to(n * p.pad * esize_of(w.dtype), 256);
 }
 
 // ---- tile products
@@ -387,12 +392,16 @@ idkm_status idkm_codes_linear(idkm_ctx* ctx, const idkm_codes_desc* w, const voi
             a.Y = Y;
             a.ldy = ldy;
             a.n = n;
-            a.steps = few.steps;
-            a.x_pieces = ldx * es % 16 == 0 && aligned_to(X, 16);
             if (const char* e = wrong_workspace(workspace, workspace_bytes, few_bytes(few, *w, n)))
                 return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
             a.sums = static_cast<float*>(workspace);
             return launched(ctx, [&] {
+                if (few.pad > 0 && (few.pad != w->cols || ldx * es % 16 != 0 || !aligned_to(X, 16) || ldx > (1 << 23))) {
+                    void* copy = static_cast<unsigned char*>(workspace) + few_sums(few, *w, n);
+                    launch_pad_rows(w->dtype, X, ldx, n, w->cols, copy, few.pad, s);
+                    a.X = copy;
+                    a.ldx = few.pad;
+                }
                 if (few.lds > 64 * 1024)
                     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(few.fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)few.lds);
                 hipLaunchKernelGGL(few.fn, few.grid, dim3((unsigned)few.threads), few.lds, s, a);
