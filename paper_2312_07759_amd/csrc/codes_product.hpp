@@ -325,28 +325,30 @@ __global__ __launch_bounds__(512) void k_codes_product(const ProductArgs a) {
     }
 }
 
-// More than 16 tokens: 16 NT of them and 64 rows of the layer to a workgroup, whose four pairs of wavefronts take 16 rows each; one
-// of a pair takes the even steps of 128 columns and one the odd ones.  The codes go the same way as above.  The activations, which
-// all four pairs need, come through LDS: up to ST - 1 steps ahead, copied there without passing registers, 16-byte pieces of row r in the
+// More than 16 tokens: 16 NT of them and 64 rows of the layer to a workgroup.  Its wavefronts are G teams of four, one for each 16 rows;
+// the teams take the steps of 128 columns in turn.  The codes go the same way as above.  The activations, which all four wavefronts of a
+// team need, come through LDS: up to ST - 1 steps ahead, copied there without passing registers, 16-byte pieces of row r in the
 // order c ^ (r mod 8).  gridDim.z workgroups share the columns; every one of them reads all tokens' activations of its columns, so that a
 // compute unit reads its share of X instead of all of it (64 tokens of 4096 columns are 512 KB).
 // Rows of X begin at multiples of 16 bytes and go on to a multiple of 128 columns, with zeros behind the layer's last.
-// What bounds it is the issue of instructions by two wavefronts a SIMD, so offsets inside a workgroup's rows and tokens are 32 bits
+// What bounds it is the issue of instructions by G wavefronts a SIMD, so offsets inside a workgroup's rows and tokens are 32 bits
 // (16 rows of 4,000,000 codes of 8 bits are 2^29 bits, 64 tokens of as many float columns 2^30 bytes).
 template <typename T, int NT>
 struct TileOfTokens {
     static constexpr int ROW = 128 * (int)sizeof(T);  // bytes of a token's step
     static constexpr int STAGE = NT * 16 * ROW;
-    static constexpr int FIT = 128 * 1024 / (2 * STAGE);
+    static constexpr int G = sizeof(T) == 4 ? 2 : 4, THREADS = 256 * G;
+    static constexpr int FIT = 128 * 1024 / (G * STAGE);
     static constexpr int ST = FIT < 4 ? FIT : 4;
     static constexpr int TABLE = 32 * 1024;
-    static constexpr int LDS = TABLE + 2 * ST * STAGE;
+    static constexpr int LDS = TABLE + G * ST * STAGE;
     static_assert(ST >= 2, "stages");
 };
 
 template <typename T, int IB, int W, int L, int NT, bool ALIGNED>
-__global__ __launch_bounds__(512) void k_codes_tile(const ProductArgs a) {
+__global__ __launch_bounds__((TileOfTokens<T, NT>::THREADS)) void k_codes_tile(const ProductArgs a) {
     typedef TileOfTokens<T, NT> Tile;
+    constexpr int G = Tile::G;
     constexpr int NB = L / W * IB;
     constexpr int PER = Elem<T>::PER16, FR = 8 / PER, SUB = L / 8, CC = 32 / L;
     constexpr int ROW = Tile::ROW, PIECES_ROW = ROW / 16, ST = Tile::ST;
@@ -355,8 +357,8 @@ __global__ __launch_bounds__(512) void k_codes_tile(const ProductArgs a) {
     extern __shared__ __align__(1024) unsigned char lds[];
     const unsigned char* table = Table<T, IB, W>::own(lds);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int li = lane & 15, q = lane >> 4, rw = wave & 3, half = wave >> 2;
-    unsigned char* stage = lds + Tile::TABLE + half * ST * Tile::STAGE;
+    const int li = lane & 15, q = lane >> 4, rw = wave & 3, team = wave >> 2;
+    unsigned char* stage = lds + Tile::TABLE + team * ST * Tile::STAGE;
     const Table<T, IB, W> entries(a.C, a.k, a.B, a.D);
     // 16 rows from n0 on, clamped; 16 NT tokens from t0 on
     const int64_t n0 = min((int64_t)blockIdx.x * 64 + rw * 16, a.rows - 1), t0 = (int64_t)blockIdx.y * (16 * NT);
@@ -364,7 +366,7 @@ __global__ __launch_bounds__(512) void k_codes_tile(const ProductArgs a) {
     const int whole = (int)(a.cols / 128);  // steps without the broken one
     const int each = (whole + gridDim.z - 1) / gridDim.z;
     const int first = min(whole, (int)blockIdx.z * each), last = min(whole, first + each);
-    const int turns = (last - first + 1) / 2;  // steps first + 2 i + half; the odd half may have no last one
+    const int turns = (last - first + G - 1) / G;  // steps first + G i + team; some teams may have no last one
     const int64_t bit0 = n0 * a.row_bits;
     const uint32_t* words = a.words + (bit0 >> 5);
     const int limit = (int)min(a.nwords - (bit0 >> 5) - CodeRun<NB>::SPAN, (int64_t)1 << 30);
@@ -430,7 +432,7 @@ __global__ __launch_bounds__(512) void k_codes_tile(const ProductArgs a) {
 #pragma unroll
     for (int u = 0; u < ST - 1; ++u)
         if (u < turns) {
-            const int step = min(first + 2 * u + half, last - 1);
+            const int step = min(first + G * u + team, last - 1);
             ask(step, u);
             fetch(step, u);
         }
@@ -450,11 +452,11 @@ __global__ __launch_bounds__(512) void k_codes_tile(const ProductArgs a) {
                 __builtin_amdgcn_s_barrier();
                 asm volatile("" ::: "memory");
                 if (i + ST - 1 < turns) {
-                    const int step = min(first + 2 * (i + ST - 1) + half, last - 1);
+                    const int step = min(first + G * (i + ST - 1) + team, last - 1);
                     ask(step, (u + ST - 1) % ST);
                     fetch(step, (u + ST - 1) % ST);
                 }
-                if (first + 2 * i + half < last) {
+                if (first + G * i + team < last) {
 #pragma unroll
                     for (int c = 0; c < CC; ++c) use(run[u][c], scale[u][c], c, u, -1);
                 }
@@ -463,10 +465,10 @@ __global__ __launch_bounds__(512) void k_codes_tile(const ProductArgs a) {
     }
     __syncthreads();
     if (whole * (int64_t)128 < a.cols && blockIdx.z + 1 == gridDim.z) {  // the row's broken step
-        if (half == 0) fetch(whole, 0);
+        if (team == 0) fetch(whole, 0);
         __builtin_amdgcn_s_waitcnt(0x0070);
         __syncthreads();
-        if (half == 0)
+        if (team == 0)
             for (int c = 0; c < CC; ++c) {
                 CodeRun<NB> codes;
                 codes.template load<false, true>(a.words, a.nwords, (n0 + row) * a.row_bits + q * NB + (int64_t)(whole * CC + c) * (4 * NB));
@@ -474,11 +476,11 @@ __global__ __launch_bounds__(512) void k_codes_tile(const ProductArgs a) {
             }
         __syncthreads();
     }
-    // The odd and the even steps' sums: of every two tiles of tokens each half of the workgroup finishes one.
+    // The teams' sums, in order: tile j of the tokens is finished by team j mod G.
     float* red = reinterpret_cast<float*>(lds + Tile::TABLE) + rw * (NT * 256) + lane * 4;
 #pragma unroll
     for (int j = 0; j < NT; ++j)
-        if ((j & 1) != half) *reinterpret_cast<floatx4*>(red + j * 256) = acc[j];
+        if (j % G != team) *reinterpret_cast<floatx4*>(red + (team * 4 * NT + j) * 256) = acc[j];
     __syncthreads();
     if ((int64_t)blockIdx.x * 64 + rw * 16 + li >= a.rows) return;
     const bool shared = gridDim.z > 1;
@@ -489,14 +491,15 @@ __global__ __launch_bounds__(512) void k_codes_tile(const ProductArgs a) {
     const int tokens = (int)min(a.n - t0, (int64_t)(16 * NT));
 #pragma unroll
     for (int j = 0; j < NT; ++j)
-        if ((j & 1) == half) {
-            const floatx4 other = *reinterpret_cast<const floatx4*>(red + j * 256);
+        if (j % G == team) {
+            floatx4 sum{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int g = 0; g < G; ++g) sum += g == team ? acc[j] : *reinterpret_cast<const floatx4*>(red + (g * 4 * NT + j) * 256);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float sum = acc[j][r] + other[r];
                 if (j * 16 + q * 4 + r >= tokens) continue;
-                if (shared) sums[(j * 16 + r) * pitch] = sum;
-                else Y[(j * 16 + r) * pitch] = Elem<T>::down(sum);
+                if (shared) sums[(j * 16 + r) * pitch] = sum[r];
+                else Y[(j * 16 + r) * pitch] = Elem<T>::down(sum[r]);
             }
         }
 }

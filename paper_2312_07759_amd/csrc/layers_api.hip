@@ -168,7 +168,7 @@ FewPlan few_plan(const idkm_codes_desc& w, int64_t n) {
     }
     const int NT = n <= 32 ? 2 : 4;
     p.fn = codes_tile_kernel(w.dtype, IB, W, L, NT, aligned);
-    p.threads = 512;
+    p.threads = w.dtype == IDKM_F32 ? TileOfTokens<float, 2>::THREADS : TileOfTokens<bf16, 2>::THREADS;
     p.pad = up_to(w.cols, 128);
     const int64_t steps = p.pad / 128;
     const int64_t blocks = (w.rows + 63) / 64, tokens = (n + 16 * NT - 1) / (16 * NT);
