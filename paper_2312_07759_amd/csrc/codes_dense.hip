@@ -3,14 +3,17 @@
 
 namespace idkm {
 
-// dC[e] = the sum of bins[w][e], one wavefront to an e.
-__global__ __launch_bounds__(64) void k_join_bins(const float* __restrict__ bins, int nwg, int kd, float* __restrict__ dC) {
-    const int e = blockIdx.x;
+// dC[e] = the sum of bins[e][w], w < n, in float64: a workgroup to an e.
+__global__ __launch_bounds__(256) void k_join_bins(const float* __restrict__ bins, int64_t n, float* __restrict__ dC) {
+    __shared__ double waves[4];
+    const float* mine = bins + blockIdx.x * n;
     double sum = 0.0;
-    for (int w = threadIdx.x; w < nwg; w += 64) sum += (double)bins[(size_t)w * kd + e];
+    for (int64_t w = threadIdx.x; w < n; w += 256) sum += (double)mine[w];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    if (threadIdx.x == 0) dC[e] = (float)sum;
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) dC[blockIdx.x] = (float)(waves[0] + waves[1] + waves[2] + waves[3]);
 }
 
 __global__ __launch_bounds__(256) void k_fill_zero(float* out, int64_t n) {
@@ -42,8 +45,21 @@ static size_t codebook_lds(DenseArgs& a, int esize) {
         }                                          \
     } while (0)
 
+// The kernels with lookups, for the codes that they take; a run's words (three at most) have to be there.
+static bool launch_fast(int dtype, const DenseArgs& a, bool columns, hipStream_t s) {
+    if (a.bits > 8 || (a.d != 1 && a.d != 2 && a.d != 4 && a.d != 8) || a.nwords < 4) return false;
+    const int at_once = codes_at_once(a.bits, a.d), IB = at_once * a.bits, W = at_once * a.d;
+    const DenseFn fn = codes_dense_kernel(dtype, IB, W, columns);
+    const size_t table = (size_t)128 << IB, tile = columns ? (dtype == 0 ? TransposeTile<float>::WORDS : TransposeTile<bf16>::WORDS) * 4 : 0;
+    int64_t grid = columns ? ((a.count + 63) / 64) * ((a.pad + 63) / 64) : (a.count * (a.pad / 8) + 255) / 256;
+    if (grid > 1024) grid = 1024;  // four workgroups to a compute unit, each with one table
+    hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(256), table + tile, s, a);
+    return true;
+}
+
 void launch_dense_rows(int dtype, const DenseArgs& args, hipStream_t s) {
     DenseArgs a = args;
+    if (launch_fast(dtype, a, false, s)) return;
     BY_TYPE(dtype, T, {
         const size_t lds = codebook_lds(a, sizeof(T));
         hipLaunchKernelGGL(k_dense_rows<T>, dim3(grid_for(a.count * (a.pad / 8))), dim3(256), lds, s, a);
@@ -52,6 +68,7 @@ void launch_dense_rows(int dtype, const DenseArgs& args, hipStream_t s) {
 
 void launch_dense_cols(int dtype, const DenseArgs& args, hipStream_t s) {
     DenseArgs a = args;
+    if (launch_fast(dtype, a, true, s)) return;
     const dim3 grid((unsigned)((a.count + 63) / 64), (unsigned)((a.pad + 63) / 64));
     BY_TYPE(dtype, T, {
         const size_t lds = codebook_lds(a, sizeof(T));
@@ -73,16 +90,53 @@ void launch_join_parts(int dtype, const float* parts, int nz, int64_t M, int64_t
     BY_TYPE(dtype, T, hipLaunchKernelGGL(k_join_parts<T>, dim3(grid_for(M * N)), dim3(256), 0, s, parts, nz, M, N, static_cast<T*>(out), ldo));
 }
 
-void launch_codes_bins(int dtype, const BinArgs& a, int grid, int waves, hipStream_t s) {
-    const size_t lds = a.bins ? (size_t)waves * a.codes * 64 * sizeof(float) : 0;
+void launch_codes_bins(int dtype, const BinArgs& args, int grid, int waves, hipStream_t s) {
+    BinArgs a = args;
+    const size_t book = (size_t)a.k * a.d * (dtype == 0 ? 4 : 2);
+    a.c_in_lds = a.dS && book <= 16 * 1024;
+    const size_t lds = (a.bins ? (size_t)waves * a.codes * 256 : 0) + (a.c_in_lds ? book : 0);
     BY_TYPE(dtype, T, {
-        (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_codes_bins<T>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        if (lds > 64 * 1024)
+            (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_codes_bins<T>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         hipLaunchKernelGGL(k_codes_bins<T>, dim3((unsigned)grid), dim3((unsigned)waves * 64), lds, s, a);
     });
 }
 
-void launch_join_bins(const float* bins, int nwg, int kd, float* dC, hipStream_t s) {
-    hipLaunchKernelGGL(k_join_bins, dim3((unsigned)kd), dim3(64), 0, s, bins, nwg, kd, dC);
+template <typename T>
+static void launch_bins_runs(const BinArgs& a, bool wide, int grid, int waves, hipStream_t s) {
+    void (*const narrow_fn)(const BinArgs) = a.d == 1 ? &k_codes_bins_runs<T, 1> : a.d == 2 ? &k_codes_bins_runs<T, 2>
+                                             : a.d == 4 ? &k_codes_bins_runs<T, 4> : &k_codes_bins_runs<T, 8>;
+    void (*const wide_fn)(const BinArgs) = a.d == 1 ? &k_codes_bins_wide<T, 1> : a.d == 2 ? &k_codes_bins_wide<T, 2>
+                                           : a.d == 4 ? &k_codes_bins_wide<T, 4> : &k_codes_bins_wide<T, 8>;
+    void (*const fn)(const BinArgs) = wide ? wide_fn : narrow_fn;
+    const size_t lds = wide ? (a.bins ? (size_t)waves * 64 * a.k * 4 : 0) : ((a.bins ? (size_t)waves * 64 : 0) + 1) * a.k * a.d * 4;
+    if (lds > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3((unsigned)waves * 64), lds, s, a);
+}
+
+void launch_codes_bins_runs(int dtype, const BinArgs& a, bool wide, int grid, int waves, hipStream_t s) {
+    BY_TYPE(dtype, T, launch_bins_runs<T>(a, wide, grid, waves, s));
+}
+
+// dS[r, g] = the sum of the row's segments of the group, in order.
+__global__ __launch_bounds__(256) void k_join_segments(const float* __restrict__ segments, int per_row, int of_group, int groups, int64_t n,
+                                                       float* __restrict__ dS) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / groups;
+        const int g = (int)(i - r * groups), last = min(per_row, (g + 1) * of_group);
+        float sum = 0.f;
+        for (int j = g * of_group; j < last; ++j) sum += segments[r * per_row + j];
+        dS[i] = sum;
+    }
+}
+
+void launch_join_segments(const float* segments, int64_t rows, int64_t cols, int group, int groups, float* dS, hipStream_t s) {
+    const int per_row = (int)((cols + 31) / 32), of_group = groups > 1 ? group / 32 : per_row;
+    hipLaunchKernelGGL(k_join_segments, dim3(grid_for(rows * groups)), dim3(256), 0, s, segments, per_row, of_group, groups, rows * groups, dS);
+}
+
+void launch_join_bins(const float* bins, int64_t n, int kd, float* dC, hipStream_t s) {
+    hipLaunchKernelGGL(k_join_bins, dim3((unsigned)kd), dim3(256), 0, s, bins, n, dC);
 }
 
 void launch_fill_zero(float* out, int64_t n, hipStream_t s) {

@@ -1,6 +1,6 @@
 // Kernels around the tile product: layers written out as matrices, operands padded and transposed, parts of a sum joined.
 #pragma once
-#include "elem.hpp"
+#include "codes_product.hpp"
 
 namespace idkm {
 
@@ -17,7 +17,141 @@ struct DenseArgs {
     int64_t first, count;  // rows (or, transposed, columns) to write
     int64_t pad;           // columns (transposed: rows) of the written matrix, zero from the layer's end on
     void* out;             // T [count, pad]
+    unsigned group_magic;  // ceil(2^31 / (group / 32)), or 0 for one group
+    int group_32;          // group / 32
 };
+
+// Group of column c: the product with the rounded-up inverse is off by one at most, and then too large.
+__device__ __forceinline__ int group_of(const DenseArgs& a, int c) {
+    const unsigned x = (unsigned)c >> 5;
+    unsigned g = __umulhi(2u * x, a.group_magic);
+    if ((uint64_t)g * (unsigned)a.group_32 > x) --g;
+    return (int)g;
+}
+
+// A 64 x 64 tile through LDS: every thread of 256 brings columns 8 c .. 8 c + 7 of rows 2 p and 2 p + 1 (p = thread / 8, c = thread
+// % 8) and the tile goes out as 64 rows of its transpose, 16 bytes at a time.
+template <typename T>
+struct TransposeTile {
+    static constexpr int PITCH = sizeof(T) == 4 ? 65 : 33;  // words between columns
+    static constexpr int WORDS = 64 * PITCH;
+    uint32_t* lds;
+    __device__ __forceinline__ void put(const T* a, const T* b) const {
+        const int p = threadIdx.x >> 3, c = (threadIdx.x & 7) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (sizeof(T) == 4) {
+                lds[(c + e) * PITCH + 2 * p] = __builtin_bit_cast(uint32_t, a[e]);
+                lds[(c + e) * PITCH + 2 * p + 1] = __builtin_bit_cast(uint32_t, b[e]);
+            } else {
+                lds[(c + e) * PITCH + p] = __builtin_bit_cast(uint16_t, a[e]) | (uint32_t)__builtin_bit_cast(uint16_t, b[e]) << 16;
+            }
+        }
+    }
+    // out: the tile's first element; columns left to write, elements between their rows, elements of a row there is room for
+    __device__ __forceinline__ void emit(T* out, int64_t columns, int64_t pitch, int64_t room) const {
+        constexpr int PIECES = 64 * (int)sizeof(T) / 16;
+#pragma unroll
+        for (int i = 0; i < 64 * PIECES / 256; ++i) {
+            const int at = i * 256 + threadIdx.x, c = at / PIECES, k = at % PIECES;
+            if (c >= columns || k * Elem<T>::PER16 >= room) continue;  // room is a multiple of a piece
+            const uint32_t* w = lds + c * PITCH + k * 4;
+            *reinterpret_cast<u32x4*>(out + c * pitch + k * Elem<T>::PER16) = u32x4{w[0], w[1], w[2], w[3]};
+        }
+    }
+};
+
+// Columns c .. c + 7 of row r, scaled and rounded to T once (an operand of the matrix instruction: the relative error, eps / 2 at
+// most, is that of a weight stored in T), zeros behind the last column.
+template <typename T, int IB, int W>
+__device__ __forceinline__ void eight_of_layer(T* out, const DenseArgs& a, int64_t r, int c, const unsigned char* table) {
+    constexpr int NB = 8 / W * IB;
+    CodeRun<NB> run;
+    const int64_t bit = (r * (a.cols / a.d) + c / a.d) * a.bits;
+    const bool whole = c + 8 <= a.cols;
+    if (whole) {
+        const int64_t base = min(bit >> 5, a.nwords - CodeRun<NB>::SPAN);
+        run.template load_inside<false>(a.words + base, 0, (unsigned)(bit - (base << 5)));
+    } else {
+        run.template load<false, true>(a.words, a.nwords, bit);
+    }
+    u32x4 raw[8 / Elem<T>::PER16];
+    eight_weights<T, IB, W, NB>(raw, run, 0, table);
+    __builtin_memcpy(out, raw, sizeof(raw));
+    if (a.S) {
+        const float s = a.S[r * a.groups + group_of(a, c)];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[e] = Elem<T>::down(Elem<T>::up(out[e]) * s);
+    }
+    if (!whole) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c + e >= a.cols) out[e] = (T)0.f;
+    }
+}
+
+// The layer's rows: a thread takes 8 columns of a row at a time.  Bound by the writes (with one code read at a time, 26 us for
+// 4096 x 4096 in 16 bits; written at the rate of a fill it is 5).
+template <typename T, int IB, int W>
+__global__ __launch_bounds__(256) void k_dense_rows_fast(const DenseArgs a) {
+    extern __shared__ __align__(128) unsigned char lds[];
+    const Table<T, IB, W> entries(a.C, a.k, a.bits, a.d);
+    entries.build(lds, a.C, a.k, a.bits, a.d);
+    const unsigned char* table = Table<T, IB, W>::own(lds);
+    __syncthreads();
+    const int per_row = (int)(a.pad / 8);
+    const int64_t step = (int64_t)gridDim.x * 256, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t rows_step = step / per_row;
+    const int cols_step = (int)(step - rows_step * per_row);
+    int64_t r = at / per_row;
+    int c = (int)(at - r * per_row);
+    while (r < a.count) {
+        struct alignas(16) Eight { T v[8]; } w;
+        if (c * 8 < a.cols) {
+            eight_of_layer<T, IB, W>(w.v, a, a.first + r, c * 8, table);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w.v[e] = (T)0.f;
+        }
+        *reinterpret_cast<Eight*>(static_cast<T*>(a.out) + r * a.pad + c * 8) = w;
+        r += rows_step;
+        c += cols_step;
+        if (c >= per_row) {
+            c -= per_row;
+            ++r;
+        }
+    }
+}
+
+// The layer's columns: out[c, r] = w[r, c], 64 x 64 weights at a time.
+template <typename T, int IB, int W>
+__global__ __launch_bounds__(256) void k_dense_cols_fast(const DenseArgs a) {
+    extern __shared__ __align__(128) unsigned char lds[];
+    const Table<T, IB, W> entries(a.C, a.k, a.bits, a.d);
+    entries.build(lds, a.C, a.k, a.bits, a.d);
+    const unsigned char* table = Table<T, IB, W>::own(lds);
+    const TransposeTile<T> tile{reinterpret_cast<uint32_t*>(lds + Table<T, IB, W>::BYTES)};
+    const int tiles_c = (int)((a.count + 63) / 64), tiles_r = (int)((a.pad + 63) / 64);
+    for (int t = blockIdx.x; t < tiles_c * tiles_r; t += gridDim.x) {
+        const int tr = t / tiles_c, tc = t - tr * tiles_c;
+        const int64_t r0 = (int64_t)tr * 64 + (threadIdx.x >> 3) * 2;
+        const int c0 = (int)a.first + tc * 64 + (threadIdx.x & 7) * 8;
+        T w[2][8];
+        __syncthreads();  // the table is there, and the last tile has gone out
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            if (r0 + b < a.rows && c0 < a.cols) {
+                eight_of_layer<T, IB, W>(w[b], a, r0 + b, c0, table);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[b][e] = (T)0.f;
+            }
+        }
+        tile.put(w[0], w[1]);
+        __syncthreads();
+        tile.emit(static_cast<T*>(a.out) + (int64_t)tc * 64 * a.pad + tr * 64, a.count - tc * 64, a.pad, a.pad - tr * 64);
+    }
+}
 
 __device__ __forceinline__ uint32_t code_at(const uint32_t* words, int64_t nwords, int64_t i, int bits) {
     const int64_t off = i * bits, w = off >> 5;
@@ -143,17 +277,27 @@ __global__ __launch_bounds__(256) void k_pad_rows(const T* __restrict__ in, int6
 // out[N, pad] = in[M, N]^T, zero behind column M.
 template <typename T>
 __global__ __launch_bounds__(256) void k_transpose(const T* __restrict__ in, int64_t ldi, int64_t M, int64_t N, T* __restrict__ out, int64_t pad) {
-    __shared__ T tile[64][64 + 16 / sizeof(T) / 2];
-    const int64_t nb = (int64_t)blockIdx.x * 64, mb = (int64_t)blockIdx.y * 64;
-    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
-        const int64_t m = mb + (e >> 6), n = nb + (e & 63);
-        tile[e & 63][e >> 6] = m < M && n < N ? in[m * ldi + n] : (T)0.f;
+    __shared__ __align__(16) uint32_t lds[TransposeTile<T>::WORDS];
+    const TransposeTile<T> tile{lds};
+    const int64_t n0 = (int64_t)blockIdx.x * 64, m0 = (int64_t)blockIdx.y * 64;
+    const int64_t m = m0 + (threadIdx.x >> 3) * 2, n = n0 + (threadIdx.x & 7) * 8;
+    T v[2][8];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        const T* row = in + (m + b) * ldi;
+        if (m + b < M && n + 8 <= N) {
+            u32x4 raw[8 / Elem<T>::PER16];
+#pragma unroll
+            for (int f = 0; f < 8 / Elem<T>::PER16; ++f) raw[f] = reinterpret_cast<const u32x4_any*>(row + n)[f];
+            __builtin_memcpy(v[b], raw, sizeof(raw));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[b][e] = m + b < M && n + e < N ? row[n + e] : (T)0.f;
+        }
     }
+    tile.put(v[0], v[1]);
     __syncthreads();
-    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
-        const int64_t n = nb + (e >> 6), m = mb + (e & 63);
-        if (n < N && m < pad) out[n * pad + m] = tile[e >> 6][e & 63];
-    }
+    tile.emit(out + n0 * pad + m0, N - n0, pad, pad - m0);
 }
 
 // out[M, N] (rows ldo apart) = the sum over z, in order, of parts[z, M, N].

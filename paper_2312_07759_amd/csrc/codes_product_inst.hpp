@@ -65,4 +65,28 @@ ProductFn CODES_TILE_NAME(CODE_BITS)(int dtype, int W, int L, int NT, bool align
     return tile_for_type<bf16>(W, L, NT, aligned);
 }
 
+template <typename T, int W>
+static DenseFn dense_for_width(bool columns) {
+    return columns ? &k_dense_cols_fast<T, CODE_BITS, W> : &k_dense_rows_fast<T, CODE_BITS, W>;
+}
+
+template <typename T>
+static DenseFn dense_for_type(int W, bool columns) {
+    switch (W) {
+        case 1: if constexpr (CODE_BITS >= 5) return dense_for_width<T, 1>(columns); break;
+        case 2: if constexpr (CODE_BITS >= 5) return dense_for_width<T, 2>(columns); break;
+        case 4: if constexpr (CODE_BITS >= 5) return dense_for_width<T, 4>(columns); break;
+        case 8: return dense_for_width<T, 8>(columns);
+    }
+    return nullptr;
+}
+
+#define CODES_DENSE_NAME2(b) codes_dense_kernel_##b
+#define CODES_DENSE_NAME(b) CODES_DENSE_NAME2(b)
+DenseFn CODES_DENSE_NAME(CODE_BITS)(int dtype, int W, bool columns) {
+    if (dtype == 0) return dense_for_type<float>(W, columns);
+    if (dtype == 1) return dense_for_type<f16>(W, columns);
+    return dense_for_type<bf16>(W, columns);
+}
+
 }  // namespace idkm

@@ -13,6 +13,10 @@ ProductFn codes_product_kernel(int dtype, int IB, int W, int L, bool aligned);
 // 17 tokens and more, 16 NT of them at a time (NT in {2, 4}).
 ProductFn codes_tile_kernel(int dtype, int IB, int W, int L, int NT, bool aligned);
 
+// A layer written out, codes looked up as above; columns: its transpose.
+typedef void (*DenseFn)(const DenseArgs);
+DenseFn codes_dense_kernel(int dtype, int IB, int W, bool columns);
+
 struct TileShape {
     int bm, bn, threads;
     size_t lds;
@@ -28,8 +32,10 @@ void launch_pad_rows(int dtype, const void* in, int64_t ldi, int64_t M, int64_t 
 void launch_transpose(int dtype, const void* in, int64_t ldi, int64_t M, int64_t N, void* out, int64_t pad, hipStream_t s);
 void launch_join_parts(int dtype, const float* parts, int nz, int64_t M, int64_t N, void* out, int64_t ldo, hipStream_t s);
 void launch_codes_bins(int dtype, const BinArgs& a, int grid, int waves, hipStream_t s);
+void launch_codes_bins_runs(int dtype, const BinArgs& a, bool wide, int grid, int waves, hipStream_t s);
+void launch_join_segments(const float* segments, int64_t rows, int64_t cols, int group, int groups, float* dS, hipStream_t s);
 void launch_fill_zero(float* out, int64_t n, hipStream_t s);
-void launch_join_bins(const float* bins, int nwg, int kd, float* dC, hipStream_t s);
+void launch_join_bins(const float* bins, int64_t n, int kd, float* dC, hipStream_t s);
 
 constexpr int SCALE_FWD = 0, UNSCALE_FWD = 1, UNSCALE_BWD = 2, SCALE_BWD = 3;
 struct ScaleArgs {

@@ -33,6 +33,22 @@ ProductFn codes_tile_kernel_6(int, int, int, int, bool);
 ProductFn codes_tile_kernel_7(int, int, int, int, bool);
 ProductFn codes_tile_kernel_8(int, int, int, int, bool);
 
+DenseFn codes_dense_kernel_1(int, int, bool);
+DenseFn codes_dense_kernel_2(int, int, bool);
+DenseFn codes_dense_kernel_3(int, int, bool);
+DenseFn codes_dense_kernel_4(int, int, bool);
+DenseFn codes_dense_kernel_5(int, int, bool);
+DenseFn codes_dense_kernel_6(int, int, bool);
+DenseFn codes_dense_kernel_7(int, int, bool);
+DenseFn codes_dense_kernel_8(int, int, bool);
+
+DenseFn codes_dense_kernel(int dtype, int IB, int W, bool columns) {
+    static DenseFn (*const by_bits[8])(int, int, bool) = {
+        codes_dense_kernel_1, codes_dense_kernel_2, codes_dense_kernel_3, codes_dense_kernel_4,
+        codes_dense_kernel_5, codes_dense_kernel_6, codes_dense_kernel_7, codes_dense_kernel_8};
+    return IB >= 1 && IB <= 8 ? by_bits[IB - 1](dtype, W, columns) : nullptr;
+}
+
 ProductFn codes_tile_kernel(int dtype, int IB, int W, int L, int NT, bool aligned) {
     static ProductFn (*const by_bits[8])(int, int, int, int, bool) = {
         codes_tile_kernel_1, codes_tile_kernel_2, codes_tile_kernel_3, codes_tile_kernel_4,
@@ -250,6 +266,8 @@ DenseArgs dense_of(const idkm_codes_desc& w) {
     a.S = w.S;
     a.group = w.S ? (w.group < w.cols ? w.group : (int)w.cols) : 1;
     a.groups = groups_of(w);
+    a.group_32 = a.group >= 32 ? a.group / 32 : 1;
+    a.group_magic = a.groups > 1 ? (unsigned)((((int64_t)1 << 31) + a.group_32 - 1) / a.group_32) : 0;
     return a;
 }
 
@@ -293,33 +311,58 @@ void operand_of(int dtype, const void* in, int64_t ldi, int64_t n, int64_t sum, 
 
 // Gradients of the layer itself.
 struct LayerGradLayout {
-    int64_t pad, panel, panels, dy, x, p, bins, bytes;
+    int64_t pad, ldp, panel, panels, dy, x, p, bins, segments, bytes;
     TilePlan plan;
-    int group, groups, lanes, waves, codes, grid;
+    bool runs, wide, segmented;  // which of the kernels for bins
+    int group, groups, lanes, run, waves, codes, grid;
 };
 
 LayerGradLayout layer_grad_layout(const idkm_codes_desc& w, int64_t n) {
-    const int es = esize_of(w.dtype);
-    LayerGradLayout l;
+    const int es = esize_of(w.dtype), bits = idkm_code_bits(w.k);
+    LayerGradLayout l{};
     l.pad = up_to(n, TP_STEP / es);
-    l.panel = panel_of(w.rows, w.cols);
+    l.ldp = up_to(w.cols, 8);
+    l.panel = panel_of(w.rows, l.ldp);
     l.panels = (w.rows + l.panel - 1) / l.panel;
     l.plan = tile_plan(l.panel, w.cols, l.pad * es / TP_STEP, w.dtype);
-    // a wavefront takes a group of a row at a time; without scales, some hundred columns
-    l.group = w.S ? (int)(w.group < w.cols ? w.group : w.cols) : (int)(w.cols < 512 ? w.cols : 512 / w.d * w.d);
-    l.groups = (int)((w.cols + l.group - 1) / l.group);
-    l.lanes = 64 / w.d * w.d;
-    l.codes = w.k < 512 ? w.k : 512;  // bins of 512 codewords fill 128 KB
-    l.waves = (128 * 1024) / (l.codes * 256);
+    l.group = w.S ? (int)(w.group < w.cols ? w.group : w.cols) : 0;
+    l.runs = bits <= 8 && (w.d == 1 || w.d == 2 || w.d == 4 || w.d == 8) && w.rows * w.cols / w.d * bits > 96;
+    l.wide = l.runs && w.k * w.d > 256;  // bins of all components for every lane: 64 KB a wavefront at most
+    int64_t tasks;  // of a wavefront, in a panel
+    int bin_bytes;  // of a wavefront
+    if (l.runs) {
+        if (!w.S) l.group = (int)up_to(w.cols, 8);
+        l.groups = w.S ? groups_of(w) : 1;
+        // lanes of a group of 8 m columns lie together in a wavefront's 512 where m is a power of two
+        l.segmented = w.S && (l.wide || l.group > 512 || l.group % 8 != 0 || (l.group & (l.group - 1)) != 0);
+        tasks = l.panel * ((w.cols + 511) / 512);
+        bin_bytes = (l.wide ? w.k : w.k * w.d) * 256;
+        l.codes = w.k;
+    } else {
+        // a wavefront takes groups of a row at a time; without scales, some hundred columns
+        if (!w.S) l.group = (int)(w.cols < 512 ? w.cols : 512 / w.d * w.d);
+        l.groups = (int)((w.cols + l.group - 1) / l.group);
+        l.lanes = 64 / w.d * w.d;
+        if (w.S && l.group % 64 == 32 && l.group < 256 && 32 % w.d == 0) l.lanes = 32;  // no step of which half is behind the group
+        const int steps = (l.group + l.lanes - 1) / l.lanes;
+        l.run = steps >= 16 ? 1 : 16 / steps;
+        if (l.run > l.groups) l.run = l.groups;
+        l.codes = w.k < 512 ? w.k : 512;  // bins of 512 codewords fill 128 KB
+        tasks = l.panel * ((l.groups + l.run - 1) / l.run);
+        bin_bytes = l.codes * 256;
+    }
+    l.waves = 128 * 1024 / bin_bytes;
     if (l.waves > 4) l.waves = 4;
-    int64_t grid = (l.panel * l.groups + l.waves - 1) / l.waves;
-    const int64_t most = l.codes * 256 * l.waves > 32 * 1024 ? 512 : 2048;
+    // as many workgroups as the compute units hold at once: every one has bins to clear and to write
+    int64_t grid = (tasks + l.waves - 1) / l.waves, most = 256 * (150 * 1024 / (bin_bytes * l.waves + 4096));
+    if (most > 2048) most = 2048;
     l.grid = (int)(grid < most ? grid : most);
     l.dy = 0;
     l.x = buffer(w.rows * l.pad, es);
     l.p = l.x + buffer(w.cols * l.pad, es);
-    l.bins = l.p + buffer(l.panel * w.cols * l.plan.parts, 4);
-    l.bytes = l.bins + buffer(l.panels * l.grid * w.k * w.d, 4);
+    l.bins = l.p + buffer(l.panel * l.ldp * l.plan.parts, 4);
+    l.segments = l.bins + buffer(l.panels * l.grid * w.k * w.d, 4);
+    l.bytes = l.segments + (l.segmented ? buffer(w.rows * ((w.cols + 31) / 32), 4) : 0);
     return l;
 }
 
@@ -497,7 +540,7 @@ idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, 
                 t.steps = (int)(l.pad * es / TP_STEP);
                 t.wide = 1;
                 t.out = ws + l.p;
-                t.ldo = w->cols;
+                t.ldo = l.ldp;
                 run_tile(w->dtype, l.plan, t, s);
                 BinArgs b{};
                 b.words = w->words;
@@ -513,20 +556,30 @@ idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, 
                 b.groups = l.groups;
                 b.P = reinterpret_cast<const float*>(ws + l.p);
                 b.parts = l.plan.parts;
-                b.ldp = w->cols;
+                b.ldp = l.ldp;
+                b.run = l.run;
+                b.pitch = l.panels * l.grid;
+                b.at = written;
                 b.first = r;
                 b.count = count;
                 b.lanes = l.lanes;
-                for (int c0 = 0; c0 < (dC ? w->k : 1); c0 += l.codes) {
+                b.bins = dC ? bins : nullptr;
+                b.segments = l.segmented && dS ? reinterpret_cast<float*>(ws + l.segments) : nullptr;
+                if (l.runs) {
+                    b.dS = dS;
+                    launch_codes_bins_runs(w->dtype, b, l.wide, l.grid, l.waves, s);
+                }
+                for (int c0 = 0; !l.runs && c0 < (dC ? w->k : 1); c0 += l.codes) {
                     b.dS = c0 == 0 ? dS : nullptr;
-                    b.bins = dC ? bins + written * w->k * w->d : nullptr;
                     b.code0 = c0;
                     b.codes = l.codes;
                     launch_codes_bins(w->dtype, b, l.grid, l.waves, s);
                 }
                 written += l.grid;
             }
-            if (dC) launch_join_bins(bins, (int)written, w->k * w->d, dC, s);
+            if (dS && l.segmented)
+                launch_join_segments(reinterpret_cast<const float*>(ws + l.segments), w->rows, w->cols, l.group, l.groups, dS, s);
+            if (dC) launch_join_bins(bins, written, w->k * w->d, dC, s);
         });
     });
 }
