@@ -49,7 +49,7 @@ static size_t codebook_lds(DenseArgs& a, int esize) {
 static bool launch_fast(int dtype, const DenseArgs& a, bool columns, hipStream_t s) {
     if (a.bits > 8 || (a.d != 1 && a.d != 2 && a.d != 4 && a.d != 8) || a.nwords < 4) return false;
     const int at_once = codes_at_once(a.bits, a.d), IB = at_once * a.bits, W = at_once * a.d;
-    const DenseFn fn = codes_dense_kernel(dtype, IB, W, columns);
+    const DenseFn fn = codes_dense_kernel(dtype, IB, W, columns, a.row_bits % 32 == 0);
     const size_t table = (size_t)128 << IB, tile = columns ? (dtype == 0 ? TransposeTile<float>::WORDS : TransposeTile<bf16>::WORDS) * 4 : 0;
     int64_t grid = columns ? ((a.count + 63) / 64) * ((a.pad + 63) / 64) : (a.count * (a.pad / 8) + 255) / 256;
     if (grid > 1024) grid = 1024;  // four workgroups to a compute unit, each with one table

@@ -19,6 +19,8 @@ struct DenseArgs {
     void* out;             // T [count, pad]
     unsigned group_magic;  // ceil(2^31 / (group / 32)), or 0 for one group
     int group_32;          // group / 32
+    int64_t row_bits;
+    int d_log;  // of d in {1, 2, 4, 8}
 };
 
 // Group of column c: the product with the rounded-up inverse is off by one at most, and then too large.
@@ -61,39 +63,44 @@ struct TransposeTile {
     }
 };
 
-// Columns c .. c + 7 of row r, scaled and rounded to T once (an operand of the matrix instruction: the relative error, eps / 2 at
-// most, is that of a weight stored in T), zeros behind the last column.
-template <typename T, int IB, int W>
-__device__ __forceinline__ void eight_of_layer(T* out, const DenseArgs& a, int64_t r, int c, const unsigned char* table) {
-    constexpr int NB = 8 / W * IB;
+// Eight columns of a row of the layer on their way: asked for, and brought to T.  A scaled weight is rounded once (it is an operand
+// of the matrix instruction: the relative error, eps / 2 at most, is that of a weight stored in T); zeros behind the last column.
+template <typename T, int IB, int W, bool ALIGNED>
+struct EightOfLayer {
+    static constexpr int NB = 8 / W * IB;
     CodeRun<NB> run;
-    const int64_t bit = (r * (a.cols / a.d) + c / a.d) * a.bits;
-    const bool whole = c + 8 <= a.cols;
-    if (whole) {
-        const int64_t base = min(bit >> 5, a.nwords - CodeRun<NB>::SPAN);
-        run.template load_inside<false>(a.words + base, 0, (unsigned)(bit - (base << 5)));
-    } else {
-        run.template load<false, true>(a.words, a.nwords, bit);
+    float s;
+    __device__ __forceinline__ void ask(const DenseArgs& a, int64_t r, int c) {
+        const int64_t bit = r * a.row_bits + (unsigned)((c >> a.d_log) * a.bits);
+        if (c + 8 <= a.cols) {
+            const int64_t base = ALIGNED ? bit >> 5 : min(bit >> 5, a.nwords - CodeRun<NB>::SPAN);
+            run.template load_inside<ALIGNED>(a.words + base, 0, (unsigned)(bit - (base << 5)));
+        } else {
+            run.template load<false, true>(a.words, a.nwords, bit);
+        }
+        if (a.S) s = a.S[r * a.groups + group_of(a, c)];
     }
-    u32x4 raw[8 / Elem<T>::PER16];
-    eight_weights<T, IB, W, NB>(raw, run, 0, table);
-    __builtin_memcpy(out, raw, sizeof(raw));
-    if (a.S) {
-        const float s = a.S[r * a.groups + group_of(a, c)];
+    __device__ __forceinline__ void bring(T* out, const DenseArgs& a, int c, const unsigned char* table) const {
+        u32x4 raw[8 / Elem<T>::PER16];
+        eight_weights<T, IB, W, NB>(raw, run, 0, table);
+        __builtin_memcpy(out, raw, sizeof(raw));
+        if (a.S) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) out[e] = Elem<T>::down(Elem<T>::up(out[e]) * s);
-    }
-    if (!whole) {
+            for (int e = 0; e < 8; ++e) out[e] = Elem<T>::down(Elem<T>::up(out[e]) * s);
+        }
+        if (c + 8 > a.cols) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (c + e >= a.cols) out[e] = (T)0.f;
+            for (int e = 0; e < 8; ++e)
+                if (c + e >= a.cols) out[e] = (T)0.f;
+        }
     }
-}
+};
 
-// The layer's rows: a thread takes 8 columns of a row at a time.  Bound by the writes (with one code read at a time, 26 us for
-// 4096 x 4096 in 16 bits; written at the rate of a fill it is 5).
-template <typename T, int IB, int W>
+// The layer's rows: a thread takes 8 columns at a time, four such pieces asked for together.  Bound by the writes: 4096 x 4096
+// in 16 bits took 26 us with one code read at a time and 15 with one piece; written at the rate of a fill it is 5.
+template <typename T, int IB, int W, bool ALIGNED>
 __global__ __launch_bounds__(256) void k_dense_rows_fast(const DenseArgs a) {
+    constexpr int U = 4;
     extern __shared__ __align__(128) unsigned char lds[];
     const Table<T, IB, W> entries(a.C, a.k, a.bits, a.d);
     entries.build(lds, a.C, a.k, a.bits, a.d);
@@ -106,25 +113,38 @@ __global__ __launch_bounds__(256) void k_dense_rows_fast(const DenseArgs a) {
     int64_t r = at / per_row;
     int c = (int)(at - r * per_row);
     while (r < a.count) {
-        struct alignas(16) Eight { T v[8]; } w;
-        if (c * 8 < a.cols) {
-            eight_of_layer<T, IB, W>(w.v, a, a.first + r, c * 8, table);
-        } else {
+        EightOfLayer<T, IB, W, ALIGNED> eight[U];
+        int64_t rows[U];
+        int cols[U];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w.v[e] = (T)0.f;
+        for (int u = 0; u < U; ++u) {
+            rows[u] = r;
+            cols[u] = c * 8;
+            if (r < a.count && c * 8 < a.cols) eight[u].ask(a, a.first + r, c * 8);
+            r += rows_step;
+            c += cols_step;
+            if (c >= per_row) {
+                c -= per_row;
+                ++r;
+            }
         }
-        *reinterpret_cast<Eight*>(static_cast<T*>(a.out) + r * a.pad + c * 8) = w;
-        r += rows_step;
-        c += cols_step;
-        if (c >= per_row) {
-            c -= per_row;
-            ++r;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (rows[u] >= a.count) continue;
+            struct alignas(16) Eight { T v[8]; } w;
+            if (cols[u] < a.cols) {
+                eight[u].bring(w.v, a, cols[u], table);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w.v[e] = (T)0.f;
+            }
+            *reinterpret_cast<Eight*>(static_cast<T*>(a.out) + rows[u] * a.pad + cols[u]) = w;
         }
     }
 }
 
-// The layer's columns: out[c, r] = w[r, c], 64 x 64 weights at a time.
-template <typename T, int IB, int W>
+// The layer's columns: out[c, r] = w[r, c], 64 x 64 weights at a time, the next tile's asked for before this one goes through LDS.
+template <typename T, int IB, int W, bool ALIGNED>
 __global__ __launch_bounds__(256) void k_dense_cols_fast(const DenseArgs a) {
     extern __shared__ __align__(128) unsigned char lds[];
     const Table<T, IB, W> entries(a.C, a.k, a.bits, a.d);
@@ -132,27 +152,38 @@ __global__ __launch_bounds__(256) void k_dense_cols_fast(const DenseArgs a) {
     const unsigned char* table = Table<T, IB, W>::own(lds);
     const TransposeTile<T> tile{reinterpret_cast<uint32_t*>(lds + Table<T, IB, W>::BYTES)};
     const int tiles_c = (int)((a.count + 63) / 64), tiles_r = (int)((a.pad + 63) / 64);
-    for (int t = blockIdx.x; t < tiles_c * tiles_r; t += gridDim.x) {
+    const int lr = (threadIdx.x >> 3) * 2, lc = (threadIdx.x & 7) * 8;
+    EightOfLayer<T, IB, W, ALIGNED> eight[2];
+    auto ask = [&](int t) {
+        const int tr = t / tiles_c, c0 = (int)a.first + (t - tr * tiles_c) * 64 + lc;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+            if (tr * 64 + lr + b < a.rows && c0 < a.cols) eight[b].ask(a, tr * 64 + lr + b, c0);
+    };
+    int t = blockIdx.x;
+    if (t < tiles_c * tiles_r) ask(t);
+    for (; t < tiles_c * tiles_r; t += gridDim.x) {
         const int tr = t / tiles_c, tc = t - tr * tiles_c;
-        const int64_t r0 = (int64_t)tr * 64 + (threadIdx.x >> 3) * 2;
-        const int c0 = (int)a.first + tc * 64 + (threadIdx.x & 7) * 8;
+        const int c0 = (int)a.first + tc * 64 + lc;
         T w[2][8];
         __syncthreads();  // the table is there, and the last tile has gone out
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            if (r0 + b < a.rows && c0 < a.cols) {
-                eight_of_layer<T, IB, W>(w[b], a, r0 + b, c0, table);
+            if (tr * 64 + lr + b < a.rows && c0 < a.cols) {
+                eight[b].bring(w[b], a, c0, table);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) w[b][e] = (T)0.f;
             }
         }
+        if (t + (int)gridDim.x < tiles_c * tiles_r) ask(t + gridDim.x);
         tile.put(w[0], w[1]);
         __syncthreads();
         tile.emit(static_cast<T*>(a.out) + (int64_t)tc * 64 * a.pad + tr * 64, a.count - tc * 64, a.pad, a.pad - tr * 64);
     }
 }
 
+// Codes of more bits and codewords of other lengths, one code at a time.
 __device__ __forceinline__ uint32_t code_at(const uint32_t* words, int64_t nwords, int64_t i, int bits) {
     const int64_t off = i * bits, w = off >> 5;
     const int sh = (int)(off & 31);

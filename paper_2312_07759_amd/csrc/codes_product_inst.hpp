@@ -66,27 +66,30 @@ ProductFn CODES_TILE_NAME(CODE_BITS)(int dtype, int W, int L, int NT, bool align
 }
 
 template <typename T, int W>
-static DenseFn dense_for_width(bool columns) {
-    return columns ? &k_dense_cols_fast<T, CODE_BITS, W> : &k_dense_rows_fast<T, CODE_BITS, W>;
+static DenseFn dense_for_width(bool columns, bool aligned) {
+    if constexpr (8 / W * CODE_BITS % 32 == 0) {
+        if (aligned) return columns ? &k_dense_cols_fast<T, CODE_BITS, W, true> : &k_dense_rows_fast<T, CODE_BITS, W, true>;
+    }
+    return columns ? &k_dense_cols_fast<T, CODE_BITS, W, false> : &k_dense_rows_fast<T, CODE_BITS, W, false>;
 }
 
 template <typename T>
-static DenseFn dense_for_type(int W, bool columns) {
+static DenseFn dense_for_type(int W, bool columns, bool aligned) {
     switch (W) {
-        case 1: if constexpr (CODE_BITS >= 5) return dense_for_width<T, 1>(columns); break;
-        case 2: if constexpr (CODE_BITS >= 5) return dense_for_width<T, 2>(columns); break;
-        case 4: if constexpr (CODE_BITS >= 5) return dense_for_width<T, 4>(columns); break;
-        case 8: return dense_for_width<T, 8>(columns);
+        case 1: if constexpr (CODE_BITS >= 5) return dense_for_width<T, 1>(columns, aligned); break;
+        case 2: if constexpr (CODE_BITS >= 5) return dense_for_width<T, 2>(columns, aligned); break;
+        case 4: if constexpr (CODE_BITS >= 5) return dense_for_width<T, 4>(columns, aligned); break;
+        case 8: return dense_for_width<T, 8>(columns, aligned);
     }
     return nullptr;
 }
 
 #define CODES_DENSE_NAME2(b) codes_dense_kernel_##b
 #define CODES_DENSE_NAME(b) CODES_DENSE_NAME2(b)
-DenseFn CODES_DENSE_NAME(CODE_BITS)(int dtype, int W, bool columns) {
-    if (dtype == 0) return dense_for_type<float>(W, columns);
-    if (dtype == 1) return dense_for_type<f16>(W, columns);
-    return dense_for_type<bf16>(W, columns);
+DenseFn CODES_DENSE_NAME(CODE_BITS)(int dtype, int W, bool columns, bool aligned) {
+    if (dtype == 0) return dense_for_type<float>(W, columns, aligned);
+    if (dtype == 1) return dense_for_type<f16>(W, columns, aligned);
+    return dense_for_type<bf16>(W, columns, aligned);
 }
 
 }  // namespace idkm

@@ -13,9 +13,9 @@ ProductFn codes_product_kernel(int dtype, int IB, int W, int L, bool aligned);
 // 17 tokens and more, 16 NT of them at a time (NT in {2, 4}).
 ProductFn codes_tile_kernel(int dtype, int IB, int W, int L, int NT, bool aligned);
 
-// A layer written out, codes looked up as above; columns: its transpose.
+// A layer written out, codes looked up as above; columns: its transpose; aligned: eight columns' codes begin with a word.
 typedef void (*DenseFn)(const DenseArgs);
-DenseFn codes_dense_kernel(int dtype, int IB, int W, bool columns);
+DenseFn codes_dense_kernel(int dtype, int IB, int W, bool columns, bool aligned);
 
 struct TileShape {
     int bm, bn, threads;

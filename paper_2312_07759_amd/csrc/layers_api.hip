@@ -33,20 +33,20 @@ ProductFn codes_tile_kernel_6(int, int, int, int, bool);
 ProductFn codes_tile_kernel_7(int, int, int, int, bool);
 ProductFn codes_tile_kernel_8(int, int, int, int, bool);
 
-DenseFn codes_dense_kernel_1(int, int, bool);
-DenseFn codes_dense_kernel_2(int, int, bool);
-DenseFn codes_dense_kernel_3(int, int, bool);
-DenseFn codes_dense_kernel_4(int, int, bool);
-DenseFn codes_dense_kernel_5(int, int, bool);
-DenseFn codes_dense_kernel_6(int, int, bool);
-DenseFn codes_dense_kernel_7(int, int, bool);
-DenseFn codes_dense_kernel_8(int, int, bool);
+DenseFn codes_dense_kernel_1(int, int, bool, bool);
+DenseFn codes_dense_kernel_2(int, int, bool, bool);
+DenseFn codes_dense_kernel_3(int, int, bool, bool);
+DenseFn codes_dense_kernel_4(int, int, bool, bool);
+DenseFn codes_dense_kernel_5(int, int, bool, bool);
+DenseFn codes_dense_kernel_6(int, int, bool, bool);
+DenseFn codes_dense_kernel_7(int, int, bool, bool);
+DenseFn codes_dense_kernel_8(int, int, bool, bool);
 
-DenseFn codes_dense_kernel(int dtype, int IB, int W, bool columns) {
-    static DenseFn (*const by_bits[8])(int, int, bool) = {
+DenseFn codes_dense_kernel(int dtype, int IB, int W, bool columns, bool aligned) {
+    static DenseFn (*const by_bits[8])(int, int, bool, bool) = {
         codes_dense_kernel_1, codes_dense_kernel_2, codes_dense_kernel_3, codes_dense_kernel_4,
         codes_dense_kernel_5, codes_dense_kernel_6, codes_dense_kernel_7, codes_dense_kernel_8};
-    return IB >= 1 && IB <= 8 ? by_bits[IB - 1](dtype, W, columns) : nullptr;
+    return IB >= 1 && IB <= 8 ? by_bits[IB - 1](dtype, W, columns, aligned) : nullptr;
 }
 
 ProductFn codes_tile_kernel(int dtype, int IB, int W, int L, int NT, bool aligned) {
@@ -266,6 +266,8 @@ DenseArgs dense_of(const idkm_codes_desc& w) {
     a.S = w.S;
     a.group = w.S ? (w.group < w.cols ? w.group : (int)w.cols) : 1;
     a.groups = groups_of(w);
+    a.row_bits = w.cols / w.d * a.bits;
+    a.d_log = w.d == 8 ? 3 : w.d == 4 ? 2 : w.d == 2 ? 1 : 0;
     a.group_32 = a.group >= 32 ? a.group / 32 : 1;
     a.group_magic = a.groups > 1 ? (unsigned)((((int64_t)1 << 31) + a.group_32 - 1) / a.group_32) : 0;
     return a;
