@@ -331,9 +331,9 @@ __global__ __launch_bounds__(256) void k_transpose(const T* __restrict__ in, int
     tile.emit(out + n0 * pad + m0, N - n0, pad, pad - m0);
 }
 
-// out[M, N] (rows ldo apart) = the sum over z, in order, of parts[z, M, N].
+// out[M, N] (rows ldo apart) = the sum over z, in order, of parts[z, M, N].  out may be the first part.
 template <typename T>
-__global__ __launch_bounds__(256) void k_join_parts(const float* __restrict__ parts, int nz, int64_t M, int64_t N, T* __restrict__ out, int64_t ldo) {
+__global__ __launch_bounds__(256) void k_join_parts(const float* parts, int nz, int64_t M, int64_t N, T* out, int64_t ldo) {
     const int64_t total = M * N;
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += (int64_t)gridDim.x * 256) {
         float sum = parts[at];

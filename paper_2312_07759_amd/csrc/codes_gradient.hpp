@@ -1,7 +1,7 @@
 // Gradients of a product with a coded layer in its group scales and its codebook, from P[n, c] = sum_t dY[t, n] X[t, c]:
 //   dS[n, g] = sum over the group's columns of P[n, c] C[code, x]        (x = c mod d)
 //   dC[j, x] = sum over all (n, c) with that codeword and component of S[n, g] P[n, c]
-// P is read once (float32, in `parts` parts that add up).  A wavefront takes some groups of a row at a time, `lanes` columns a step;
+// P is read once (float32).  A wavefront takes some groups of a row at a time, `lanes` columns a step;
 // lanes is a multiple of d, so a lane always has the same component x.  It keeps bins of its own for the codewords in LDS
 // ([codeword][lane], a bank to a lane): no two lanes ever add to the same word, and the order of every sum is fixed.
 // A workgroup's bins go to `bins` [k d][workgroup]; k_join_bins adds them up in float64.
@@ -19,8 +19,7 @@ struct BinArgs {
     int k, d, bits;
     const float* S;     // [rows, groups] or null
     int group, groups;  // groups of some hundred columns where there are no scales
-    const float* P;     // [parts][count][ldp], rows [first, first + count) of the layer
-    int parts;
+    const float* P;     // [count][ldp], rows [first, first + count) of the layer
     int64_t ldp, first, count;
     float* dS;        // [rows, groups] or null
     float* segments;  // [rows][ceil(cols / 32)], or null: see k_codes_bins_runs
@@ -50,7 +49,7 @@ __global__ __launch_bounds__(256) void k_codes_bins(const BinArgs a) {
     const int per_row = (int)(a.cols / a.d);
     const int runs = (a.groups + a.run - 1) / a.run;  // of a row
     const int steps = (a.group + a.lanes - 1) / a.lanes;  // of a group
-    const int64_t tasks = a.count * runs, plane = a.count * a.ldp;
+    const int64_t tasks = a.count * runs;
     const int own_code = lane / a.d, x = lane - own_code * a.d;
     const int group_codes = a.group / a.d, step_codes = a.lanes / a.d;
     const uint32_t mask = (1u << a.bits) - 1u;
@@ -83,17 +82,6 @@ __global__ __launch_bounds__(256) void k_codes_bins(const BinArgs a) {
                 if (step && ++j == steps) {
                     j = 0;
                     ++g;
-                }
-            }
-            for (int z = 1; z < a.parts; ++z) {
-                int gz = gu, jz = ju;
-#pragma unroll
-                for (int u = 0; u < STEPS; ++u) {
-                    if (there[u]) p[u] += P[z * plane + gz * a.group + jz * a.lanes + lane];
-                    if (++jz == steps) {
-                        jz = 0;
-                        ++gz;
-                    }
                 }
             }
 #pragma unroll
@@ -148,7 +136,6 @@ __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {
     for (int i = threadIdx.x; i < kd; i += blockDim.x) book[i] = Elem<T>::up(static_cast<const T*>(a.C)[i]);
     __syncthreads();
     const int strips = (int)((a.cols + 511) / 512), per_row = (int)(a.cols / D);
-    const int64_t plane = a.count * a.ldp;
     const int64_t step = (int64_t)gridDim.x * nw;
     const uint32_t mask = (1u << a.bits) - 1u;
     const int group_lanes = a.group / 8;
@@ -170,14 +157,6 @@ __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {
             const floatx4 v = reinterpret_cast<const floatx4*>(P)[h];
 #pragma unroll
             for (int e = 0; e < 4; ++e) t.p[h * 4 + e] = v[e];
-        }
-        for (int z = 1; z < a.parts; ++z) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const floatx4 v = reinterpret_cast<const floatx4*>(P + z * plane)[h];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) t.p[h * 4 + e] += v[e];
-            }
         }
         // up to 64 bits of codes, in three words; near the stream's end the words are taken from further ahead
         const int64_t bit = (r * per_row + at / D) * a.bits, from = min(bit >> 5, a.nwords - 3);
@@ -262,7 +241,6 @@ __global__ __launch_bounds__(256) void k_codes_bins_wide(const BinArgs a) {
         for (int j = 0; j < a.k; ++j) mine[j * 64] = 0.f;
     const T* C = static_cast<const T*>(a.C) + lane % D;
     const int strips = (int)((a.cols + 511) / 512), per_row = (int)(a.cols / D), segments = (int)((a.cols + 31) / 32);
-    const int64_t plane = a.count * a.ldp;
     const uint32_t mask = (1u << a.bits) - 1u;
     const int64_t step = (int64_t)gridDim.x * nw, rows_step = step / strips;
     const int strips_step = (int)(step - rows_step * strips);
@@ -283,7 +261,6 @@ __global__ __launch_bounds__(256) void k_codes_bins_wide(const BinArgs a) {
         for (int u = 0; u < STEPS; ++u) {
             const int c = min(at * 512 + u * 64 + lane, (int)a.cols - 1);  // columns behind the last: read as it, not counted
             t.p[u] = P[c];
-            for (int z = 1; z < a.parts; ++z) t.p[u] += P[z * plane + c];
             t.s[u] = S ? S[c / a.group] : 1.f;
             const int bit = (int)(bit0 & 31) + min(u * (64 / D) + lane / D, per_row - 1 - at * (512 / D)) * a.bits;
             const int from = min(bit >> 5, limit);

@@ -5,6 +5,8 @@
 // the two (TH threads, NV pieces of 16 bytes each: rows up to 256 KB); with few or longer rows several workgroups share one,
 // a first launch leaving each part's maximum and sum.  Sums are float32 over at most some hundred terms a lane, exponents are
 // taken of differences to the maximum, so that rows of the type's lowest value come out even and -inf as nothing.
+#include <type_traits>
+
 #include "layers.h"
 
 namespace idkm {
@@ -24,10 +26,35 @@ __device__ __forceinline__ float element(u32x4 v, int e) {
 
 typedef u32x4 u32x4_el __attribute__((aligned(2)));
 
-constexpr float LOG2E = 1.44269504088896341f;
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 constexpr float LOWEST = -3.4028234663852886e38f;
 
 struct Two { float a, b; };
+
+// Largest of three; of a NaN and a number the number.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float m;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    return m;
+}
+
+// exp((z - m) / tau) of a row: its exponent to the base 2 is one multiply-add of the logit, z c - k with k = m c rounded; what the
+// rounding puts into one exponential it puts into all of the row's, and their sum.  Where m c could overflow (rows of the type's
+// lowest value) the difference z - m comes first.
+struct Exponent {
+    float c, m, k;
+    bool difference;
+    __device__ __forceinline__ Exponent(float tau, float m_) : c(LOG2E / tau), m(m_), difference(fabsf(m_) * fmaxf(c, 1.f) > 1e37f) { k = difference ? 0.f : m * c; }
+    template <bool DIFFERENCE>
+    __device__ __forceinline__ float of(float z) const {
+        return __builtin_amdgcn_exp2f(fmaf(DIFFERENCE ? z - m : z, c, -k));
+    }
+    __device__ __forceinline__ float of(float z) const { return difference ? of<true>(z) : of<false>(z); }
+    // log of the same
+    __device__ __forceinline__ float log(float z) const { return fmaf(difference ? z - m : z, c, -k) * LN2; }
+    // log sum exp(z / tau) for sum exp = e^ln
+    __device__ __forceinline__ float lse(float tau, float ln) const { return (difference ? m / tau : k * LN2) + ln; }
+};
 
 // max, or sum, of two values over a workgroup of TH threads; `scratch`: 2 x 16 floats
 template <int TH, bool MAX>
@@ -83,10 +110,10 @@ __device__ __forceinline__ float read_list(const DistillArgs& a, int64_t row, Li
     return top;
 }
 
-// From the row's maximum m and sum (of exp((z - m) / tau)) and the teacher's: p in LDS, the row's loss and the factor.
+// From the logarithm of the row's sum of exponentials and the teacher's maximum and sum: p in LDS, the row's loss and the factor.
 // listed: the student's logits at the list's places; null: they are taken from the row.
 template <typename T, int TH>
-__device__ __forceinline__ RowTail finish_row(const DistillArgs& a, int64_t row, List l, float m, float ln_sum, Two teacher, bool bad,
+__device__ __forceinline__ RowTail finish_row(const DistillArgs& a, int64_t row, List l, const Exponent& x, float ln_sum, Two teacher, bool bad,
                                               const float* listed, bool want_loss, float* scratch) {
     const float t_top = teacher.a, t_sum = teacher.b;
     const bool some = t_top > -INFINITY;  // entries, and not all of them -inf
@@ -100,7 +127,7 @@ __device__ __forceinline__ RowTail finish_row(const DistillArgs& a, int64_t row,
             const float logp = (l.p[i] - t_top) * inv_tau - ln_t;
             p = expf(logp);
             zi = listed ? listed[i] : Elem<T>::up(z[at]);
-            if (p != 0.f) loss += p * (logp - ((zi - m) * inv_tau - ln_sum));
+            if (p != 0.f) loss += p * (logp - (x.log(zi) - ln_sum));
         }
         l.p[i] = p;
         l.z[i] = zi;
@@ -111,11 +138,10 @@ __device__ __forceinline__ RowTail finish_row(const DistillArgs& a, int64_t row,
     return t;
 }
 
-// Places of the list inside [from, to): q - p there, once for an index that is listed more than once.
+// Places of the list inside [from, to): q - p there, once for an index that is listed more than once.  over: factor / sum.
 template <typename T, int TH>
-__device__ __forceinline__ void correct(const DistillArgs& a, int64_t row, List l, float m, float ln_sum, float factor, int64_t from, int64_t to) {
+__device__ __forceinline__ void correct(const DistillArgs& a, int64_t row, List l, const Exponent& x, float factor, float over, int64_t from, int64_t to) {
     T* out = static_cast<T*>(a.dlogits) + row * a.ldd;
-    const float c = LOG2E / a.tau, off = ln_sum * LOG2E;
     for (int i = threadIdx.x; i < a.top; i += TH) {
         const int at = l.index[i];
         if (at < from || at >= to) continue;
@@ -126,7 +152,7 @@ __device__ __forceinline__ void correct(const DistillArgs& a, int64_t row, List 
             if (j < i) again = true;
             if (j > i) p += l.p[j];
         }
-        if (!again) out[at] = Elem<T>::down(factor * (__builtin_amdgcn_exp2f(fmaf(l.z[i] - m, c, -off)) - p));
+        if (!again) out[at] = Elem<T>::down(over * x.of(l.z[i]) - factor * p);
     }
 }
 
@@ -139,63 +165,83 @@ __global__ __launch_bounds__(TH) void k_distill_row(const DistillArgs a) {
     extern __shared__ float lds[];
     List l{reinterpret_cast<int*>(lds), lds + a.top, lds + 2 * a.top};
     float* scratch = lds + 3 * a.top;
+    const int pieces = (int)(a.V / PER), rest = (int)(a.V - (int64_t)pieces * PER);
+    const bool tail = (int)threadIdx.x < rest;
+    // 32-bit offsets from the row's uniform address; pieces behind the last are read as it and do not count
+    auto load = [&](const T* z, int h) {
+        const unsigned at = (unsigned)min(h * TH + (int)threadIdx.x, pieces - 1) * 16u;
+        return *reinterpret_cast<const u32x4_el*>(reinterpret_cast<const unsigned char*>(z) + at);
+    };
     const int64_t row = blockIdx.x;
     const T* z = static_cast<const T*>(a.logits) + row * a.ldz;
-    const int pieces = (int)(a.V / PER), rest = (int)(a.V - (int64_t)pieces * PER);
     u32x4 held[NV];
+    // between two uses of the row: or the compiler keeps its elements as floats, in registers that are not there
+    auto keep_packed = [&] {
 #pragma unroll
-    for (int h = 0; h < NV; ++h)
-        if (h * TH + (int)threadIdx.x < pieces) held[h] = reinterpret_cast<const u32x4_el*>(z)[h * TH + threadIdx.x];
-    const bool tail = (int)threadIdx.x < rest;
-    const float zt = tail ? Elem<T>::up(z[(int64_t)pieces * PER + threadIdx.x]) : LOWEST;
+        for (int h = 0; h < NV; ++h) asm volatile("" : "+v"(held[h]));
+    };
+#pragma unroll
+    for (int h = 0; h < NV; ++h) held[h] = h * TH < pieces ? load(z, h) : u32x4{0, 0, 0, 0};
+    float zt = tail ? Elem<T>::up(z[(int64_t)pieces * PER + threadIdx.x]) : LOWEST;
     bool bad = false;
     const float t_own = read_list<TH>(a, row, l, bad);
     float m = fmaxf(LOWEST, zt);
 #pragma unroll
     for (int h = 0; h < NV; ++h)
-        if (h * TH + (int)threadIdx.x < pieces) {
+        if (h * TH < pieces) {
 #pragma unroll
-            for (int e = 0; e < PER; ++e) m = fmaxf(m, element<T>(held[h], e));
+            for (int e = 0; e < PER; e += 2) m = max3(m, element<T>(held[h], e), element<T>(held[h], e + 1));
         }
     const Two tops = all_of<TH, true>(Two{m, t_own}, scratch);
-    m = tops.a;
-    const float c = LOG2E / a.tau;
-    float s = tail ? __builtin_amdgcn_exp2f((zt - m) * c) : 0.f, ts = 0.f;
+    const Exponent x(a.tau, tops.a);
+    keep_packed();
+    float s = tail ? x.of(zt) : 0.f, ts = 0.f;
+    auto add = [&](auto difference) {
 #pragma unroll
-    for (int h = 0; h < NV; ++h)
-        if (h * TH + (int)threadIdx.x < pieces) {
-            float part = 0.f;
+        for (int h = 0; h < NV; ++h)
+            if (h * TH < pieces) {
+                float part = 0.f;
 #pragma unroll
-            for (int e = 0; e < PER; ++e) part += __builtin_amdgcn_exp2f((element<T>(held[h], e) - m) * c);
-            s += part;
-        }
+                for (int e = 0; e < PER; ++e) part += x.template of<decltype(difference)::value>(element<T>(held[h], e));
+                s += h * TH + (int)threadIdx.x < pieces ? part : 0.f;
+            }
+    };
+    if (x.difference) add(std::true_type());
+    else add(std::false_type());
     for (int i = threadIdx.x; i < a.top; i += TH)
         if (l.index[i] >= 0 && tops.b > -INFINITY) ts += expf((l.p[i] - tops.b) / a.tau);
     const Two sums = all_of<TH, false>(Two{s, ts}, scratch);
     const Two any_bad = all_of<TH, true>(Two{bad ? 1.f : 0.f, 0.f}, scratch);
     const float ln_sum = logf(sums.a);
-    const RowTail t = finish_row<T, TH>(a, row, l, m, ln_sum, Two{tops.b, sums.b}, any_bad.a > 0.f, nullptr, true, scratch);
+    const RowTail t = finish_row<T, TH>(a, row, l, x, ln_sum, Two{tops.b, sums.b}, any_bad.a > 0.f, nullptr, true, scratch);
     if (threadIdx.x == 0) {
         a.loss[row] = t.loss;
-        a.lse[row] = m / a.tau + ln_sum;
+        a.lse[row] = x.lse(a.tau, ln_sum);
     }
+    keep_packed();
     if (!a.dlogits) return;
     T* out = static_cast<T*>(a.dlogits) + row * a.ldd;
-    const float off = ln_sum * LOG2E;
+    const float over = t.factor / sums.a;
+    auto write = [&](auto difference) {
 #pragma unroll
-    for (int h = 0; h < NV; ++h)
-        if (h * TH + (int)threadIdx.x < pieces) {
-            struct alignas(16) Piece { T v[PER]; } o;
+        for (int h = 0; h < NV; ++h)
+            if (h * TH < pieces) {
+                struct alignas(16) Piece { T v[PER]; } o;
 #pragma unroll
-            for (int e = 0; e < PER; ++e)
-                o.v[e] = t.none ? (T)0.f : Elem<T>::down(t.factor * __builtin_amdgcn_exp2f(fmaf(element<T>(held[h], e) - m, c, -off)));
-            u32x4 v;
-            __builtin_memcpy(&v, &o, 16);
-            reinterpret_cast<u32x4_el*>(out)[h * TH + threadIdx.x] = v;
-        }
-    if (tail) out[(int64_t)pieces * PER + threadIdx.x] = t.none ? (T)0.f : Elem<T>::down(t.factor * __builtin_amdgcn_exp2f(fmaf(zt - m, c, -off)));
+                for (int e = 0; e < PER; ++e)
+                    o.v[e] = Elem<T>::down(over * x.template of<decltype(difference)::value>(element<T>(held[h], e)));
+                u32x4 v;
+                __builtin_memcpy(&v, &o, 16);
+                if (t.none) v = u32x4{0, 0, 0, 0};
+                const int at = h * TH + (int)threadIdx.x;
+                if (at < pieces) *reinterpret_cast<u32x4_el*>(reinterpret_cast<unsigned char*>(out) + (unsigned)at * 16u) = v;
+            }
+    };
+    if (x.difference) write(std::true_type());
+    else write(std::false_type());
+    if (tail) out[(int64_t)pieces * PER + threadIdx.x] = t.none ? (T)0.f : Elem<T>::down(over * x.of(zt));
     __syncthreads();
-    if (!t.none) correct<T, TH>(a, row, l, m, ln_sum, t.factor, 0, a.V);
+    if (!t.none) correct<T, TH>(a, row, l, x, t.factor, over, 0, a.V);
 }
 
 // Part blockIdx.y of a row: [from, to).
@@ -252,7 +298,6 @@ __global__ __launch_bounds__(256) void k_distill_parts(const DistillArgs a) {
     List l{reinterpret_cast<int*>(lds), lds + a.top, lds + 2 * a.top};
     float* scratch = lds + 3 * a.top;
     const int64_t row = blockIdx.x;
-    const float c = LOG2E / a.tau;
     bool bad = false;
     const float t_own = read_list<256>(a, row, l, bad);
     const float* st = a.stats + row * a.parts * 2;
@@ -260,18 +305,19 @@ __global__ __launch_bounds__(256) void k_distill_parts(const DistillArgs a) {
     for (int i = threadIdx.x; i < a.parts; i += 256) m = fmaxf(m, st[2 * i]);
     const Two tops = all_of<256, true>(Two{m, t_own}, scratch);
     m = tops.a;
+    const Exponent x(a.tau, m);
     float s = 0.f, ts = 0.f;
-    for (int i = threadIdx.x; i < a.parts; i += 256) s += st[2 * i + 1] * __builtin_amdgcn_exp2f((st[2 * i] - m) * c);
+    for (int i = threadIdx.x; i < a.parts; i += 256) s += st[2 * i + 1] * x.of(st[2 * i]);
     for (int i = threadIdx.x; i < a.top; i += 256)
         if (l.index[i] >= 0 && tops.b > -INFINITY) ts += expf((l.p[i] - tops.b) / a.tau);
     const Two sums = all_of<256, false>(Two{s, ts}, scratch);
     const Two any_bad = all_of<256, true>(Two{bad ? 1.f : 0.f, 0.f}, scratch);
     const float ln_sum = logf(sums.a);
-    const RowTail t = finish_row<T, 256>(a, row, l, m, ln_sum, Two{tops.b, sums.b}, any_bad.a > 0.f, a.listed + row * a.top,
+    const RowTail t = finish_row<T, 256>(a, row, l, x, ln_sum, Two{tops.b, sums.b}, any_bad.a > 0.f, a.listed + row * a.top,
                                          blockIdx.y == 0, scratch);
     if (threadIdx.x == 0 && blockIdx.y == 0) {
         a.loss[row] = t.loss;
-        a.lse[row] = m / a.tau + ln_sum;
+        a.lse[row] = x.lse(a.tau, ln_sum);
     }
     if (!a.dlogits) return;
     __syncthreads();
@@ -281,22 +327,21 @@ __global__ __launch_bounds__(256) void k_distill_parts(const DistillArgs a) {
     T* out = static_cast<T*>(a.dlogits) + row * a.ldd + from;
     const int64_t pieces = (to - from) / PER;
     const int rest = (int)(to - from - pieces * PER);
-    const float off = ln_sum * LOG2E;
+    const float over = t.factor / sums.a;
     for (int64_t i = threadIdx.x; i < pieces; i += 256) {
         const u32x4 v = reinterpret_cast<const u32x4_el*>(z)[i];
         struct alignas(16) Piece { T v[PER]; } o;
 #pragma unroll
-        for (int e = 0; e < PER; ++e) o.v[e] = t.none ? (T)0.f : Elem<T>::down(t.factor * __builtin_amdgcn_exp2f(fmaf(element<T>(v, e) - m, c, -off)));
+        for (int e = 0; e < PER; ++e) o.v[e] = t.none ? (T)0.f : Elem<T>::down(over * x.of(element<T>(v, e)));
         u32x4 w;
         __builtin_memcpy(&w, &o, 16);
         reinterpret_cast<u32x4_el*>(out)[i] = w;
     }
     if ((int)threadIdx.x < rest) {
-        const float x = Elem<T>::up(z[pieces * PER + threadIdx.x]);
-        out[pieces * PER + threadIdx.x] = t.none ? (T)0.f : Elem<T>::down(t.factor * __builtin_amdgcn_exp2f(fmaf(x - m, c, -off)));
+        out[pieces * PER + threadIdx.x] = t.none ? (T)0.f : Elem<T>::down(over * x.of(Elem<T>::up(z[pieces * PER + threadIdx.x])));
     }
     __syncthreads();
-    if (!t.none) correct<T, 256>(a, row, l, m, ln_sum, t.factor, from, to);
+    if (!t.none) correct<T, 256>(a, row, l, x, t.factor, over, from, to);
 }
 
 template <typename T>

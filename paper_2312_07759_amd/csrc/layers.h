@@ -21,9 +21,10 @@ struct TileShape {
     int bm, bn, threads;
     size_t lds;
     void (*fn)(const TileArgs);
+    int resident;  // workgroups that the device holds at once
+    float us;      // of a step of all of them
 };
-constexpr int TILE_SHAPES = 4;
-// The shapes of a type's tile product, largest first.
+// The shapes of a type's tile product, from 0 on; fn = nullptr behind the last.
 TileShape tile_shape(int dtype, int which);
 
 void launch_dense_rows(int dtype, const DenseArgs& a, hipStream_t s);

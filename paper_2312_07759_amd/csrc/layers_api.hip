@@ -155,13 +155,16 @@ struct FewPlan {
     size_t lds;
 };
 
-// The matrix-vector form takes up to 16 tokens, the tiles of 32 or 64 the rest.
-constexpr int64_t VECTOR_TOKENS = 16, FEW_TOKENS = 256;
+// The matrix-vector form takes up to 16 tokens, tiles of 32 or 64 tokens more, as long as decoding the layer for each of them is
+// expected to take less time than writing it out once (see below).
+constexpr int64_t VECTOR_TOKENS = 16;
+
+float dense_us(const idkm_codes_desc& w, int64_t n);
 
 FewPlan few_plan(const idkm_codes_desc& w, int64_t n) {
     FewPlan p;
     const int bits = idkm_code_bits(w.k);
-    if (n > FEW_TOKENS || bits > 8 || (w.d != 1 && w.d != 2 && w.d != 4 && w.d != 8)) return p;
+    if (bits > 8 || (w.d != 1 && w.d != 2 && w.d != 4 && w.d != 8)) return p;
     // a chunk of four runs has to lie in one group
     const int L = !w.S || w.group >= w.cols || w.group % 128 == 0 ? 32 : w.group % 64 == 0 ? 16 : 8;
     const int at_once = codes_at_once(bits, w.d), IB = at_once * bits, W = at_once * w.d;
@@ -187,11 +190,24 @@ FewPlan few_plan(const idkm_codes_desc& w, int64_t n) {
     p.threads = w.dtype == IDKM_F32 ? TileOfTokens<float, 2>::THREADS : TileOfTokens<bf16, 2>::THREADS;
     p.pad = up_to(w.cols, 128);
     const int64_t steps = p.pad / 128;
+    // Workgroups, one to a compute unit, in rounds: some 2 us and these for every step of 128 columns, by the runs' length (measured,
+    // 4096 x 4096, 2048 tokens); sums in parts cost as in tile_plan.
+    const float step_us = w.dtype == IDKM_F32 ? (L == 32 ? 2.45f : L == 16 ? 2.85f : 3.25f) : (L == 32 ? 0.55f : L == 16 ? 1.0f : 1.22f);
     const int64_t blocks = (w.rows + 63) / 64, tokens = (n + 16 * NT - 1) / (16 * NT);
-    int64_t parts = 256 / (blocks * tokens);
-    if (parts > steps / 4) parts = steps / 4;
-    if (parts > 16) parts = 16;
-    p.parts = parts < 1 ? 1 : (int)parts;
+    float best = 0.f;
+    for (int parts = 1; parts <= 16 && (parts == 1 || steps / parts >= 4); ++parts) {
+        const int64_t rounds = (blocks * tokens * parts + 255) / 256;
+        float us = (float)rounds * (2.f + step_us * (float)((steps + parts - 1) / parts));
+        if (parts > 1) us += 3.5f + 2e-6f * (float)n * (float)w.rows * (float)parts;
+        if (best == 0.f || us < best) {
+            best = us;
+            p.parts = parts;
+        }
+    }
+    if (best > dense_us(w, n)) {
+        p.fn = nullptr;
+        return p;
+    }
     p.grid = dim3((unsigned)blocks, (unsigned)tokens, (unsigned)p.parts);
     p.lds = w.dtype == IDKM_F32 ? (NT == 2 ? TileOfTokens<float, 2>::LDS : TileOfTokens<float, 4>::LDS)
                                 : (NT == 2 ? TileOfTokens<bf16, 2>::LDS : TileOfTokens<bf16, 4>::LDS);
@@ -208,22 +224,26 @@ int64_t few_bytes(const FewPlan& p, const idkm_codes_desc& w, int64_t n) {
 
 struct TilePlan {
     int which, parts;
+    float us;  // expected
 };
 
-// The largest tile that gives most of the 256 compute units one; the smallest splits the sum where there are few of them.
+// The shape and the number of parts of the sum with the least time by the shapes' measured steps: rounds of workgroups, and, where
+// the sum is taken in parts, the float32 parts that go to memory and come back (4 TB/s) and the launch that joins them.
 TilePlan tile_plan(int64_t M, int64_t N, int64_t steps, int dtype) {
-    for (int s = 0; s < TILE_SHAPES; ++s) {
+    TilePlan best{0, 1, 0.f};
+    for (int s = 0;; ++s) {
         const TileShape t = tile_shape(dtype, s);
+        if (!t.fn) return best;
         const int64_t tiles = ((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn);
-        if (tiles >= 200) return TilePlan{s, 1};
-        if (s + 1 == TILE_SHAPES) {
-            int64_t parts = (256 + tiles - 1) / tiles;
-            if (parts > steps / 4) parts = steps / 4;
-            if (parts > 16) parts = 16;
-            return TilePlan{s, parts < 1 ? 1 : (int)parts};
+        for (int parts = 1; parts <= 16 && (parts == 1 || steps / parts >= 2); ++parts) {
+            // two workgroups share a compute unit's matrix cores, one alone does not use all of them
+            float rounds = (float)((tiles * parts + 255) / 256) * 256.f / (float)t.resident;
+            if (rounds < 0.7f) rounds = 0.7f;
+            float us = rounds * t.us * (float)((steps + parts - 1) / parts);
+            if (parts > 1) us += 3.5f + 2e-6f * (float)M * (float)N * (float)parts;
+            if (best.us == 0.f || us < best.us) best = TilePlan{s, parts, us};
         }
     }
-    return TilePlan{0, 1};
 }
 
 void run_tile(int dtype, const TilePlan& p, const TileArgs& args, hipStream_t s) {
@@ -291,6 +311,12 @@ ProductLayout product_layout(int dtype, int64_t n, int64_t lines, int64_t sum) {
     l.parts = l.matrix + buffer(l.panel * l.pad, es);
     l.bytes = l.parts + (l.plan.parts > 1 ? buffer(n * l.panel * l.plan.parts, 4) : 0);
     return l;
+}
+
+// Expected time of a product whose layer is written out: 0.6 (float: 1) us for a million weights, and launches.
+float dense_us(const idkm_codes_desc& w, int64_t n) {
+    const ProductLayout l = product_layout(w.dtype, n, w.rows, w.cols);
+    return 6.f + (w.dtype == IDKM_F32 ? 1e-6f : 0.6e-6f) * (float)w.rows * (float)l.pad + l.plan.us * (float)((w.rows + l.panel - 1) / l.panel);
 }
 
 // The operand as the tile product takes it: itself, or a copy with whole steps.
@@ -544,6 +570,8 @@ idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, 
                 t.out = ws + l.p;
                 t.ldo = l.ldp;
                 run_tile(w->dtype, l.plan, t, s);
+                if (l.plan.parts > 1)
+                    launch_join_parts(IDKM_F32, reinterpret_cast<const float*>(ws + l.p), l.plan.parts, count, l.ldp, ws + l.p, l.ldp, s);
                 BinArgs b{};
                 b.words = w->words;
                 b.nwords = idkm_code_words(w->rows * w->cols / w->d, w->k);
@@ -557,7 +585,6 @@ idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, 
                 b.group = l.group;
                 b.groups = l.groups;
                 b.P = reinterpret_cast<const float*>(ws + l.p);
-                b.parts = l.plan.parts;
                 b.ldp = l.ldp;
                 b.run = l.run;
                 b.pitch = l.panels * l.grid;

@@ -90,21 +90,26 @@ __global__ __launch_bounds__(64 * WM* WN) void k_tile_product(const TileArgs a) 
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             const int next = slot == 0 ? ST - 1 : slot - 1;
-            fetch(step + ST - 1, next);
             const unsigned char* base = lds + slot * STAGE;
+            // All of the step's fragments are read first, then the copies are issued: the other way round the reads wait
+            // behind the copies' issue (256 x 128 x 4096: 66 us instead of 62 for 2048 x 4096).
+            u32x4 fa[2][TM], fb[2][TN];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                u32x4 fa[TM], fb[TN];
                 const int c = (((h << 2) | q) ^ (li & 7)) << 4;
 #pragma unroll
-                for (int i = 0; i < TM; ++i) fa[i] = *reinterpret_cast<const u32x4*>(base + (row_a + i * 16) * TP_STEP + c);
+                for (int j = 0; j < TN; ++j) fb[h][j] = *reinterpret_cast<const u32x4*>(base + (row_b + j * 16) * TP_STEP + c);
 #pragma unroll
-                for (int j = 0; j < TN; ++j) fb[j] = *reinterpret_cast<const u32x4*>(base + (row_b + j * 16) * TP_STEP + c);
+                for (int i = 0; i < TM; ++i) fa[h][i] = *reinterpret_cast<const u32x4*>(base + (row_a + i * 16) * TP_STEP + c);
+            }
+            fetch(step + ST - 1, next);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) mma16<T>(acc[i][j], fb[j], fa[i]);
-            }
+                    for (int j = 0; j < TN; ++j) mma16<T>(acc[i][j], fb[h][j], fa[h][i]);
             slot = slot + 1 == ST ? 0 : slot + 1;
         }
         __builtin_amdgcn_s_waitcnt(0x0f70);  // nothing may still be written into this LDS when it is given to others
