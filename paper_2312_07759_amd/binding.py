@@ -308,6 +308,7 @@ class Context:
         self._h = h
         self.device = int(device)
         self._keep = None
+        self._distill_bytes = {}  # workspace sizes by shape
 
     def close(self):
         if getattr(self, "_h", None):
@@ -501,7 +502,7 @@ class Context:
     def group_scale(self, W, group):
         """idkm_group_scale: W [rows, cols] float32 -> (S [rows, ceil(cols / group)], Z = W / S)."""
         w, rows, cols, scales = self._grouped(W, group, "W")
-        S, Z = W.new_empty(scales), W.new_empty((rows, cols))
+        S, Z = W.new_empty(scales), _t().empty_like(W)
         st = self._lib.idkm_group_scale(self._h, w, rows, cols, group, S.data_ptr(), Z.data_ptr(), self._raw_stream())
         if st:
             self._check(st)
@@ -511,7 +512,7 @@ class Context:
         """idkm_group_unscale: S Zq."""
         z, rows, cols, scales = self._grouped(Zq, group, "Zq")
         s = _flat(S, Zq.dtype, scales, self.device, "S")
-        Wq = Zq.new_empty((rows, cols))
+        Wq = _t().empty_like(Zq)
         st = self._lib.idkm_group_unscale(self._h, z, s, rows, cols, group, Wq.data_ptr(), self._raw_stream())
         if st:
             self._check(st)
@@ -522,7 +523,7 @@ class Context:
         z, rows, cols, scales = self._grouped(Zq, group, "Zq")
         g = _flat(dWq, Zq.dtype, Zq.shape, self.device, "dWq")
         s = _flat(S, Zq.dtype, scales, self.device, "S")
-        dZq, dS = Zq.new_empty((rows, cols)), Zq.new_empty(scales)
+        dZq, dS = _t().empty_like(Zq), _t().empty_like(S)
         st = self._lib.idkm_group_unscale_backward(self._h, g, z, s, rows, cols, group, dZq.data_ptr(), dS.data_ptr(),
                                                    self._raw_stream())
         if st:
@@ -535,7 +536,7 @@ class Context:
         g = _flat(dZ, Z.dtype, Z.shape, self.device, "dZ")
         s = _flat(S, Z.dtype, scales, self.device, "S")
         ds = _flat(dS, Z.dtype, scales, self.device, "dS") if dS is not None else None
-        dW = Z.new_empty((rows, cols))
+        dW = _t().empty_like(Z)
         st = self._lib.idkm_group_scale_backward(self._h, z, s, g, ds, rows, cols, group, dW.data_ptr(), self._raw_stream())
         if st:
             self._check(st)
@@ -566,7 +567,12 @@ class Context:
             ldd = _rows(out, logits.dtype, V, dev, "out")
             if out.shape[0] != n:
                 raise TypeError(f"out must have {n} rows")
-        need = self._lib.idkm_distill_workspace(n, V, top, code)
+        key = (n, V, top, code)
+        need = self._distill_bytes.get(key)
+        if need is None:
+            if len(self._distill_bytes) > 4096:
+                self._distill_bytes.clear()
+            need = self._distill_bytes[key] = self._lib.idkm_distill_workspace(n, V, top, code)
         ws = logits.new_empty((need,), dtype=torch.uint8) if need > 0 else None
         st = self._lib.idkm_distill(self._h, logits.data_ptr(), n, V, ldz, code, i, t, top, tau, w, loss.data_ptr(), lse.data_ptr(),
                                     out.data_ptr() if out is not None else None, ldd, ws.data_ptr() if need > 0 else None, need,

@@ -1,10 +1,25 @@
 // Launches of the kernels around the tile product.
+#include <atomic>
+
 #include "layers.h"
 
 namespace idkm {
 
-// dC[e] = the sum of bins[e][w], w < n, in float64: a workgroup to an e.
-__global__ __launch_bounds__(256) void k_join_bins(const float* __restrict__ bins, int64_t n, float* __restrict__ dC) {
+// dC[e] = the sum of bins[e][w], w < n, in float64: a workgroup to an e.  The workgroups behind them add up segments:
+// dS[r, g] = the sum of the row's segments of the group, in order.
+__global__ __launch_bounds__(256) void k_join_gradients(const float* __restrict__ bins, int64_t n, int kd, float* __restrict__ dC,
+                                                        const float* __restrict__ segments, int per_row, int of_group, int groups, int64_t scales,
+                                                        float* __restrict__ dS) {
+    if ((int)blockIdx.x >= kd) {
+        for (int64_t i = (int64_t)(blockIdx.x - kd) * 256 + threadIdx.x; i < scales; i += (int64_t)(gridDim.x - kd) * 256) {
+            const int64_t r = i / groups;
+            const int g = (int)(i - r * groups), last = min(per_row, (g + 1) * of_group);
+            float sum = 0.f;
+            for (int j = g * of_group; j < last; ++j) sum += segments[r * per_row + j];
+            dS[i] = sum;
+        }
+        return;
+    }
     __shared__ double waves[4];
     const float* mine = bins + blockIdx.x * n;
     double sum = 0.0;
@@ -29,6 +44,19 @@ static size_t codebook_lds(DenseArgs& a, int esize) {
     const size_t bytes = (size_t)a.k * a.d * esize;
     a.c_in_lds = bytes <= 32 * 1024;
     return a.c_in_lds ? bytes : 0;
+}
+
+// Kernels with more than 64 KB of dynamic LDS have to be told once on every device; what has been told is kept, without a lock
+// (two threads may tell it twice).
+void allow_lds(const void* fn, size_t bytes) {
+    if (bytes <= 64 * 1024) return;
+    static std::atomic<uintptr_t> told[1024];
+    int device = 0;
+    (void)hipGetDevice(&device);
+    const uintptr_t key = reinterpret_cast<uintptr_t>(fn) ^ (uintptr_t)(device + 1) << 56;
+    std::atomic<uintptr_t>& slot = told[(key >> 4 ^ key >> 14 ^ key >> 56) & 1023];
+    if (slot.load(std::memory_order_relaxed) == key) return;
+    if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess) slot.store(key, std::memory_order_relaxed);
 }
 
 #define BY_TYPE(dtype, T, ...)                     \
@@ -76,14 +104,17 @@ void launch_dense_cols(int dtype, const DenseArgs& args, hipStream_t s) {
     });
 }
 
-void launch_pad_rows(int dtype, const void* in, int64_t ldi, int64_t M, int64_t N, void* out, int64_t pad, hipStream_t s) {
-    BY_TYPE(dtype, T, hipLaunchKernelGGL(k_pad_rows<T>, dim3(grid_for(M * pad)), dim3(256), 0, s, static_cast<const T*>(in), ldi, M, N,
-                                         static_cast<T*>(out), pad));
+void add_operand(OperandArgs* a, const void* in, int64_t ldi, int64_t M, int64_t N, void* out, int64_t pad, bool transposed) {
+    Operand& o = a->job[a->jobs++];
+    o = Operand{in, ldi, M, N, out, pad, transposed, 0, 0};
+    o.tiles_n = ((transposed ? N : pad) + 63) / 64;
+    o.tiles = o.tiles_n * (((transposed ? pad : M) + 63) / 64);
 }
 
-void launch_transpose(int dtype, const void* in, int64_t ldi, int64_t M, int64_t N, void* out, int64_t pad, hipStream_t s) {
-    const dim3 grid((unsigned)((N + 63) / 64), (unsigned)((pad + 63) / 64));
-    BY_TYPE(dtype, T, hipLaunchKernelGGL(k_transpose<T>, grid, dim3(256), 0, s, static_cast<const T*>(in), ldi, M, N, static_cast<T*>(out), pad));
+void launch_operands(int dtype, const OperandArgs& a, hipStream_t s) {
+    int64_t tiles = 0;
+    for (int j = 0; j < a.jobs; ++j) tiles += a.job[j].tiles;
+    if (tiles > 0) BY_TYPE(dtype, T, hipLaunchKernelGGL(k_operands<T>, dim3((unsigned)tiles), dim3(256), 0, s, a));
 }
 
 void launch_join_parts(int dtype, const float* parts, int nz, int64_t M, int64_t N, void* out, int64_t ldo, hipStream_t s) {
@@ -96,8 +127,7 @@ void launch_codes_bins(int dtype, const BinArgs& args, int grid, int waves, hipS
     a.c_in_lds = a.dS && book <= 16 * 1024;
     const size_t lds = (a.bins ? (size_t)waves * a.codes * 256 : 0) + (a.c_in_lds ? book : 0);
     BY_TYPE(dtype, T, {
-        if (lds > 64 * 1024)
-            (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_codes_bins<T>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        allow_lds(reinterpret_cast<const void*>(&k_codes_bins<T>), lds);
         hipLaunchKernelGGL(k_codes_bins<T>, dim3((unsigned)grid), dim3((unsigned)waves * 64), lds, s, a);
     });
 }
@@ -110,7 +140,7 @@ static void launch_bins_runs(const BinArgs& a, bool wide, int grid, int waves, h
                                            : a.d == 4 ? &k_codes_bins_wide<T, 4> : &k_codes_bins_wide<T, 8>;
     void (*const fn)(const BinArgs) = wide ? wide_fn : narrow_fn;
     const size_t lds = wide ? (a.bins ? (size_t)waves * 64 * a.k * 4 : 0) : ((a.bins ? (size_t)waves * 64 : 0) + 1) * a.k * a.d * 4;
-    if (lds > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    allow_lds(reinterpret_cast<const void*>(fn), lds);
     hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3((unsigned)waves * 64), lds, s, a);
 }
 
@@ -118,25 +148,13 @@ void launch_codes_bins_runs(int dtype, const BinArgs& a, bool wide, int grid, in
     BY_TYPE(dtype, T, launch_bins_runs<T>(a, wide, grid, waves, s));
 }
 
-// dS[r, g] = the sum of the row's segments of the group, in order.
-__global__ __launch_bounds__(256) void k_join_segments(const float* __restrict__ segments, int per_row, int of_group, int groups, int64_t n,
-                                                       float* __restrict__ dS) {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / groups;
-        const int g = (int)(i - r * groups), last = min(per_row, (g + 1) * of_group);
-        float sum = 0.f;
-        for (int j = g * of_group; j < last; ++j) sum += segments[r * per_row + j];
-        dS[i] = sum;
-    }
-}
-
-void launch_join_segments(const float* segments, int64_t rows, int64_t cols, int group, int groups, float* dS, hipStream_t s) {
+void launch_join_gradients(const float* bins, int64_t n, int kd, float* dC, const float* segments, int64_t rows, int64_t cols, int group,
+                           int groups, float* dS, hipStream_t s) {
     const int per_row = (int)((cols + 31) / 32), of_group = groups > 1 ? group / 32 : per_row;
-    hipLaunchKernelGGL(k_join_segments, dim3(grid_for(rows * groups)), dim3(256), 0, s, segments, per_row, of_group, groups, rows * groups, dS);
-}
-
-void launch_join_bins(const float* bins, int64_t n, int kd, float* dC, hipStream_t s) {
-    hipLaunchKernelGGL(k_join_bins, dim3((unsigned)kd), dim3(256), 0, s, bins, n, dC);
+    if (!dC) kd = 0;
+    const unsigned grid = (unsigned)kd + (segments ? grid_for(rows * groups) : 0u);
+    if (grid > 0)
+        hipLaunchKernelGGL(k_join_gradients, dim3(grid), dim3(256), 0, s, bins, n, kd, dC, segments, per_row, of_group, groups, rows * groups, dS);
 }
 
 void launch_fill_zero(float* out, int64_t n, hipStream_t s) {

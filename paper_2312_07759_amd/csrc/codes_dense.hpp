@@ -295,40 +295,55 @@ __global__ __launch_bounds__(256) void k_dense_cols(const DenseArgs a) {
     }
 }
 
-// out[M, pad] = in[M, N] with rows ldi apart, zero behind column N.
-template <typename T>
-__global__ __launch_bounds__(256) void k_pad_rows(const T* __restrict__ in, int64_t ldi, int64_t M, int64_t N, T* __restrict__ out, int64_t pad) {
-    const int64_t total = M * pad;
-    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += (int64_t)gridDim.x * 256) {
-        const int64_t m = at / pad, n = at - m * pad;
-        out[at] = n < N ? in[m * ldi + n] : (T)0.f;
-    }
-}
+// Operands brought to the form in which the tile product takes them, several in one launch.
+//   rows        out[M, pad] = in[M, N], zero behind column N
+//   transposed  out[N, pad] = in[M, N]^T, zero behind column M
+struct Operand {
+    const void* in;
+    int64_t ldi, M, N;
+    void* out;
+    int64_t pad;
+    int transposed;
+    int64_t tiles, tiles_n;  // of 64 x 64, and along N (rows: along pad)
+};
+struct OperandArgs {
+    Operand job[3];
+    int jobs;
+};
 
-// out[N, pad] = in[M, N]^T, zero behind column M.
 template <typename T>
-__global__ __launch_bounds__(256) void k_transpose(const T* __restrict__ in, int64_t ldi, int64_t M, int64_t N, T* __restrict__ out, int64_t pad) {
+__global__ __launch_bounds__(256) void k_operands(const OperandArgs a) {
     __shared__ __align__(16) uint32_t lds[TransposeTile<T>::WORDS];
-    const TransposeTile<T> tile{lds};
-    const int64_t n0 = (int64_t)blockIdx.x * 64, m0 = (int64_t)blockIdx.y * 64;
+    int64_t t = blockIdx.x;
+    int j = 0;
+    while (j + 1 < a.jobs && t >= a.job[j].tiles) t -= a.job[j++].tiles;
+    const Operand& o = a.job[j];
+    const int64_t tm = t / o.tiles_n, m0 = tm * 64, n0 = (t - tm * o.tiles_n) * 64;
     const int64_t m = m0 + (threadIdx.x >> 3) * 2, n = n0 + (threadIdx.x & 7) * 8;
-    T v[2][8];
+    struct alignas(16) Eight { T v[8]; } v[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-        const T* row = in + (m + b) * ldi;
-        if (m + b < M && n + 8 <= N) {
+        const T* row = static_cast<const T*>(o.in) + (m + b) * o.ldi;
+        if (m + b < o.M && n + 8 <= o.N) {
             u32x4 raw[8 / Elem<T>::PER16];
 #pragma unroll
             for (int f = 0; f < 8 / Elem<T>::PER16; ++f) raw[f] = reinterpret_cast<const u32x4_any*>(row + n)[f];
-            __builtin_memcpy(v[b], raw, sizeof(raw));
+            __builtin_memcpy(v[b].v, raw, sizeof(raw));
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[b][e] = m + b < M && n + e < N ? row[n + e] : (T)0.f;
+            for (int e = 0; e < 8; ++e) v[b].v[e] = m + b < o.M && n + e < o.N ? row[n + e] : (T)0.f;
         }
     }
-    tile.put(v[0], v[1]);
-    __syncthreads();
-    tile.emit(out + n0 * pad + m0, N - n0, pad, pad - m0);
+    if (o.transposed) {  // the same for the whole workgroup
+        const TransposeTile<T> tile{lds};
+        tile.put(v[0].v, v[1].v);
+        __syncthreads();
+        tile.emit(static_cast<T*>(o.out) + n0 * o.pad + m0, o.N - n0, o.pad, o.pad - m0);
+    } else {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+            if (m + b < o.M && n < o.pad) *reinterpret_cast<Eight*>(static_cast<T*>(o.out) + (m + b) * o.pad + n) = v[b];
+    }
 }
 
 // out[M, N] (rows ldo apart) = the sum over z, in order, of parts[z, M, N].  out may be the first part.

@@ -29,14 +29,17 @@ TileShape tile_shape(int dtype, int which);
 
 void launch_dense_rows(int dtype, const DenseArgs& a, hipStream_t s);
 void launch_dense_cols(int dtype, const DenseArgs& a, hipStream_t s);
-void launch_pad_rows(int dtype, const void* in, int64_t ldi, int64_t M, int64_t N, void* out, int64_t pad, hipStream_t s);
-void launch_transpose(int dtype, const void* in, int64_t ldi, int64_t M, int64_t N, void* out, int64_t pad, hipStream_t s);
+void allow_lds(const void* fn, size_t bytes);  // before a launch of fn with so much dynamic LDS
+// Up to three operands to a launch.
+void add_operand(OperandArgs* a, const void* in, int64_t ldi, int64_t M, int64_t N, void* out, int64_t pad, bool transposed);
+void launch_operands(int dtype, const OperandArgs& a, hipStream_t s);
 void launch_join_parts(int dtype, const float* parts, int nz, int64_t M, int64_t N, void* out, int64_t ldo, hipStream_t s);
 void launch_codes_bins(int dtype, const BinArgs& a, int grid, int waves, hipStream_t s);
 void launch_codes_bins_runs(int dtype, const BinArgs& a, bool wide, int grid, int waves, hipStream_t s);
-void launch_join_segments(const float* segments, int64_t rows, int64_t cols, int group, int groups, float* dS, hipStream_t s);
 void launch_fill_zero(float* out, int64_t n, hipStream_t s);
-void launch_join_bins(const float* bins, int64_t n, int kd, float* dC, hipStream_t s);
+// dC from bins [kd][n] (null: not), dS from segments (null: not).
+void launch_join_gradients(const float* bins, int64_t n, int kd, float* dC, const float* segments, int64_t rows, int64_t cols, int group,
+                           int groups, float* dS, hipStream_t s);
 
 constexpr int SCALE_FWD = 0, UNSCALE_FWD = 1, UNSCALE_BWD = 2, SCALE_BWD = 3;
 struct ScaleArgs {

@@ -251,7 +251,7 @@ void run_tile(int dtype, const TilePlan& p, const TileArgs& args, hipStream_t s)
     TileArgs a = args;
     a.tiles_m = (int)((a.M + t.bm - 1) / t.bm);
     a.tiles_n = (int)((a.N + t.bn - 1) / t.bn);
-    if (t.lds > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(t.fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)t.lds);
+    allow_lds(reinterpret_cast<const void*>(t.fn), t.lds);
     hipLaunchKernelGGL(t.fn, dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)p.parts), dim3((unsigned)t.threads), t.lds, s, a);
 }
 
@@ -319,15 +319,15 @@ float dense_us(const idkm_codes_desc& w, int64_t n) {
     return 6.f + (w.dtype == IDKM_F32 ? 1e-6f : 0.6e-6f) * (float)w.rows * (float)l.pad + l.plan.us * (float)((w.rows + l.panel - 1) / l.panel);
 }
 
-// The operand as the tile product takes it: itself, or a copy with whole steps.
+// The operand as the tile product takes it: itself, or a copy with whole steps, which `copies` is to make.
 void operand_of(int dtype, const void* in, int64_t ldi, int64_t n, int64_t sum, const ProductLayout& l, unsigned char* ws, TileArgs* a,
-                hipStream_t s) {
+                OperandArgs* copies) {
     const int es = esize_of(dtype);
     if (sum == l.pad && ldi * es % 16 == 0 && aligned_to(in, 16)) {
         a->A = in;
         a->lda = ldi;
     } else {
-        launch_pad_rows(dtype, in, ldi, n, sum, ws + l.operand, l.pad, s);
+        add_operand(copies, in, ldi, n, sum, ws + l.operand, l.pad, false);
         a->A = ws + l.operand;
         a->lda = l.pad;
     }
@@ -469,12 +469,13 @@ idkm_status idkm_codes_linear(idkm_ctx* ctx, const idkm_codes_desc* w, const voi
             return launched(ctx, [&] {
                 if (few.pad > 0 && (few.pad != w->cols || ldx * es % 16 != 0 || !aligned_to(X, 16) || ldx > (1 << 23))) {
                     void* copy = static_cast<unsigned char*>(workspace) + few_sums(few, *w, n);
-                    launch_pad_rows(w->dtype, X, ldx, n, w->cols, copy, few.pad, s);
+                    OperandArgs o{};
+                    add_operand(&o, X, ldx, n, w->cols, copy, few.pad, false);
+                    launch_operands(w->dtype, o, s);
                     a.X = copy;
                     a.ldx = few.pad;
                 }
-                if (few.lds > 64 * 1024)
-                    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(few.fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)few.lds);
+                allow_lds(reinterpret_cast<const void*>(few.fn), few.lds);
                 hipLaunchKernelGGL(few.fn, few.grid, dim3((unsigned)few.threads), few.lds, s, a);
                 if (few.parts > 1) launch_join_parts(w->dtype, a.sums, few.parts, n, w->rows, Y, ldy, s);
             });
@@ -484,7 +485,9 @@ idkm_status idkm_codes_linear(idkm_ctx* ctx, const idkm_codes_desc* w, const voi
         unsigned char* ws = static_cast<unsigned char*>(workspace);
         return launched(ctx, [&] {
             TileArgs t{};
-            operand_of(w->dtype, X, ldx, n, w->cols, l, ws, &t, s);
+            OperandArgs copies{};
+            operand_of(w->dtype, X, ldx, n, w->cols, l, ws, &t, &copies);
+            launch_operands(w->dtype, copies, s);
             for (int64_t r = 0; r < w->rows; r += l.panel) {
                 DenseArgs a = dense_of(*w);
                 a.first = r;
@@ -503,8 +506,7 @@ int64_t idkm_codes_linear_backward_workspace(const idkm_codes_desc* w, int64_t n
     idkm_status st;
     if (wrong_layer(w, &st) || n < 0 || n > MAX_SIDE) return -1;
     if (n == 0) return 0;
-    const int64_t a = product_layout(w->dtype, n, w->cols, w->rows).bytes, b = layer_grad_layout(*w, n).bytes;
-    return a > b ? a : b;
+    return product_layout(w->dtype, n, w->cols, w->rows).bytes + layer_grad_layout(*w, n).bytes;
 }
 
 idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, const void* X, int64_t ldx, const void* dY, int64_t lddy,
@@ -535,25 +537,31 @@ idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, 
         if (const char* e = wrong_workspace(workspace, workspace_bytes, need)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
         unsigned char* ws = static_cast<unsigned char*>(workspace);
         return launched(ctx, [&] {
+            const ProductLayout d = product_layout(w->dtype, n, w->cols, w->rows);
+            const LayerGradLayout l = layer_grad_layout(*w, n);
+            TileArgs td{};
+            OperandArgs copies{};
+            if (dX) operand_of(w->dtype, dY, lddy, n, w->rows, d, ws, &td, &copies);
+            unsigned char* of_x = ws;
+            ws += d.bytes;
+            if (layer) {
+                add_operand(&copies, dY, lddy, n, w->rows, ws + l.dy, l.pad, true);
+                add_operand(&copies, X, ldx, n, w->cols, ws + l.x, l.pad, true);
+            }
+            launch_operands(w->dtype, copies, s);
             if (dX) {
-                const ProductLayout l = product_layout(w->dtype, n, w->cols, w->rows);
-                TileArgs t{};
-                operand_of(w->dtype, dY, lddy, n, w->rows, l, ws, &t, s);
-                for (int64_t c = 0; c < w->cols; c += l.panel) {
+                for (int64_t c = 0; c < w->cols; c += d.panel) {
                     DenseArgs a = dense_of(*w);
                     a.first = c;
-                    a.count = w->cols - c < l.panel ? w->cols - c : l.panel;
-                    a.pad = l.pad;
-                    a.out = ws + l.matrix;
+                    a.count = w->cols - c < d.panel ? w->cols - c : d.panel;
+                    a.pad = d.pad;
+                    a.out = of_x + d.matrix;
                     launch_dense_cols(w->dtype, a, s);
-                    t.N = a.count;
-                    run_product(w->dtype, l.plan, t, static_cast<unsigned char*>(dX) + c * es, lddx, reinterpret_cast<float*>(ws + l.parts), s);
+                    td.N = a.count;
+                    run_product(w->dtype, d.plan, td, static_cast<unsigned char*>(dX) + c * es, lddx, reinterpret_cast<float*>(of_x + d.parts), s);
                 }
             }
             if (!layer) return;
-            const LayerGradLayout l = layer_grad_layout(*w, n);
-            launch_transpose(w->dtype, dY, lddy, n, w->rows, ws + l.dy, l.pad, s);
-            launch_transpose(w->dtype, X, ldx, n, w->cols, ws + l.x, l.pad, s);
             float* bins = reinterpret_cast<float*>(ws + l.bins);
             int64_t written = 0;
             for (int64_t r = 0; r < w->rows; r += l.panel) {
@@ -606,9 +614,8 @@ idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, 
                 }
                 written += l.grid;
             }
-            if (dS && l.segmented)
-                launch_join_segments(reinterpret_cast<const float*>(ws + l.segments), w->rows, w->cols, l.group, l.groups, dS, s);
-            if (dC) launch_join_bins(bins, written, w->k * w->d, dC, s);
+            launch_join_gradients(bins, written, w->k * w->d, dC, l.segmented && dS ? reinterpret_cast<const float*>(ws + l.segments) : nullptr, w->rows,
+                                  w->cols, l.group, l.groups, dS, s);
         });
     });
 }
