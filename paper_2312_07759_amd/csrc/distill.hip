@@ -2,8 +2,8 @@
 //   p = softmax(teacher / tau) over the row's entries,  q = softmax(z / tau) over all V,
 //   loss = sum p (log p - log q),  lse = log sum exp(z / tau),  dz = weight / tau (q - p)   (zeros where a row has no entry)
 // Bound by memory: the row is read once and its gradient written once.  A row stays in the registers of its workgroup between
-// the two (TH threads, NV pieces of 16 bytes each: rows up to 256 KB); with few or longer rows several workgroups share one,
-// a first launch leaving each part's maximum and sum.  Sums are float32 over at most some hundred terms a lane, exponents are
+// the two (TH threads, NV pieces of 16 bytes each: rows up to 128 KB); with few rows several workgroups share one, a first launch
+// leaving each part's maximum and sum.  Sums are float32 over at most some hundred terms a lane, exponents are
 // taken of differences to the maximum, so that rows of the type's lowest value come out even and -inf as nothing.
 #include <type_traits>
 
@@ -158,9 +158,12 @@ __device__ __forceinline__ void correct(const DistillArgs& a, int64_t row, List 
 
 }  // namespace
 
-// One workgroup to a row (TH > 64) or one wavefront, the row in registers.
-template <typename T, int TH, int NV>
-__global__ __launch_bounds__(TH) void k_distill_row(const DistillArgs a) {
+// One workgroup to a row (TH > 64) or one wavefront, the row in registers.  Longer rows (up to any length) keep their first NV TH pieces
+// there; the rest is read a second time for the gradient, from the last-level cache.  So two workgroups fit a compute unit, and one's
+// memory traffic covers the other's exponentials: 2048 rows of 128000 bfloat16 logits, all of a row in the registers of the one workgroup
+// that then fits, took 278 us.
+template <typename T, int TH, int NV, bool LONG>
+__global__ __launch_bounds__(TH, TH == 512 ? 4 : 1) void k_distill_row(const DistillArgs a) {
     constexpr int PER = Elem<T>::PER16;
     extern __shared__ float lds[];
     List l{reinterpret_cast<int*>(lds), lds + a.top, lds + 2 * a.top};
@@ -192,10 +195,35 @@ __global__ __launch_bounds__(TH) void k_distill_row(const DistillArgs a) {
 #pragma unroll
             for (int e = 0; e < PER; e += 2) m = max3(m, element<T>(held[h], e), element<T>(held[h], e + 1));
         }
+    // the rest: a running maximum and sum
+    float m_rest = LOWEST, s_rest = 0.f;
+    if constexpr (LONG) {
+        const float c = LOG2E / a.tau;
+        for (int i = NV * TH + (int)threadIdx.x; i < pieces; i += 4 * TH) {
+            u32x4 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                v[u] = *reinterpret_cast<const u32x4_el*>(reinterpret_cast<const unsigned char*>(z) + (unsigned)min(i + u * TH, pieces - 1) * 16u);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                float top = m_rest, part = 0.f;
+#pragma unroll
+                for (int e = 0; e < PER; e += 2) top = max3(top, element<T>(v[u], e), element<T>(v[u], e + 1));
+#pragma unroll
+                for (int e = 0; e < PER; ++e) part += __builtin_amdgcn_exp2f((element<T>(v[u], e) - top) * c);
+                if (i + u * TH < pieces) {
+                    s_rest = fmaf(s_rest, __builtin_amdgcn_exp2f((m_rest - top) * c), part);
+                    m_rest = top;
+                }
+            }
+        }
+        m = fmaxf(m, m_rest);
+    }
     const Two tops = all_of<TH, true>(Two{m, t_own}, scratch);
     const Exponent x(a.tau, tops.a);
     keep_packed();
     float s = tail ? x.of(zt) : 0.f, ts = 0.f;
+    if constexpr (LONG) s += s_rest != 0.f ? s_rest * x.of(m_rest) : 0.f;
     auto add = [&](auto difference) {
 #pragma unroll
         for (int h = 0; h < NV; ++h)
@@ -236,6 +264,24 @@ __global__ __launch_bounds__(TH) void k_distill_row(const DistillArgs a) {
                 const int at = h * TH + (int)threadIdx.x;
                 if (at < pieces) *reinterpret_cast<u32x4_el*>(reinterpret_cast<unsigned char*>(out) + (unsigned)at * 16u) = v;
             }
+        if constexpr (LONG) {
+            for (int i = NV * TH + (int)threadIdx.x; i < pieces; i += 4 * TH) {
+                u32x4 r[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    r[u] = *reinterpret_cast<const u32x4_el*>(reinterpret_cast<const unsigned char*>(z) + (unsigned)min(i + u * TH, pieces - 1) * 16u);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    struct alignas(16) Piece { T v[PER]; } o;
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) o.v[e] = Elem<T>::down(over * x.template of<decltype(difference)::value>(element<T>(r[u], e)));
+                    u32x4 v;
+                    __builtin_memcpy(&v, &o, 16);
+                    if (t.none) v = u32x4{0, 0, 0, 0};
+                    if (i + u * TH < pieces) *reinterpret_cast<u32x4_el*>(reinterpret_cast<unsigned char*>(out) + (unsigned)(i + u * TH) * 16u) = v;
+                }
+            }
+        }
     };
     if (x.difference) write(std::true_type());
     else write(std::false_type());
@@ -356,19 +402,19 @@ static void launch_for(const DistillArgs& a, hipStream_t s) {
     }
     const int64_t pieces = a.V / Elem<T>::PER16;
     const dim3 grid((unsigned)a.n);
-    if (pieces <= 4 * 64) hipLaunchKernelGGL((k_distill_row<T, 64, 4>), grid, dim3(64), lds, s, a);
-    else if (pieces <= 4 * 256) hipLaunchKernelGGL((k_distill_row<T, 256, 4>), grid, dim3(256), lds, s, a);
-    else if (pieces <= 16 * 256) hipLaunchKernelGGL((k_distill_row<T, 256, 16>), grid, dim3(256), lds, s, a);
-    else hipLaunchKernelGGL((k_distill_row<T, 1024, 16>), grid, dim3(1024), lds, s, a);
+    if (pieces <= 4 * 64) hipLaunchKernelGGL((k_distill_row<T, 64, 4, false>), grid, dim3(64), lds, s, a);
+    else if (pieces <= 4 * 256) hipLaunchKernelGGL((k_distill_row<T, 256, 4, false>), grid, dim3(256), lds, s, a);
+    else if (pieces <= 16 * 256) hipLaunchKernelGGL((k_distill_row<T, 256, 16, false>), grid, dim3(256), lds, s, a);
+    else if (pieces <= 16 * 512) hipLaunchKernelGGL((k_distill_row<T, 512, 16, false>), grid, dim3(512), lds, s, a);
+    else hipLaunchKernelGGL((k_distill_row<T, 512, 16, true>), grid, dim3(512), lds, s, a);
 }
 
 void distill_plan(int64_t n, int64_t V, int esize, int64_t* part, int* parts) {
     const int64_t per = 16 / esize, row_bytes = V * esize;
     *part = 0;
     *parts = 0;
-    const bool held = V / per <= 16 * 1024;
     const int64_t want = (1024 + n - 1) / n;  // four workgroups to a compute unit
-    if (held && (n >= 256 || row_bytes <= 16 * 1024)) return;
+    if (n >= 256 || row_bytes <= 16 * 1024) return;
     int64_t p = want;
     const int64_t most = (row_bytes + 16 * 1024 - 1) / (16 * 1024);
     if (p > most) p = most;
