@@ -318,7 +318,7 @@ idkm_status idkm_group_scale_backward(idkm_ctx* ctx, const float* Z, const float
  * NaN in a row's list makes its loss and gradient NaN.  Logits of -inf have q = 0.
  *   weight, dlogits_out  device [n] float32 and [n,V] (rows ldd apart), both or neither NULL (neither: loss and lse only).
  *                        dlogits_out may be logits itself, with ldd = ldz.
- *   index, teacher       device [n,top] int32 and float32, 1 <= top <= 1024.
+ *   index, teacher       device [n,top] int32 and float32, 1 <= top <= 1024; n < 2^31, V <= 2^29.
  *   workspace            as for idkm_codes_linear, of idkm_distill_workspace bytes.
  * Enqueues on hip_stream, does not wait; n = 0 is a no-op.  Logits and gradient are aligned to their element type.
  */

@@ -70,6 +70,7 @@ using namespace idkm;
 namespace {
 
 constexpr int64_t MAX_SIDE = 4000000;      // rows, columns, tokens: 64 of them to a workgroup fit one grid dimension
+constexpr int64_t MAX_VOCABULARY = (int64_t)1 << 29;  // offsets in a row are 32 bits of bytes
 constexpr int64_t PANEL = (int64_t)1 << 26;  // weights of a layer that are written out at a time
 
 idkm_status refuse(idkm_ctx* ctx, idkm_status s, const char* msg) {
@@ -682,7 +683,7 @@ idkm_status idkm_group_scale_backward(idkm_ctx* ctx, const float* Z, const float
 }
 
 int64_t idkm_distill_workspace(int64_t n, int64_t V, int32_t top, int32_t dtype) {
-    if (n < 0 || V < 1 || top < 1 || top > 1024 || dtype < 0 || dtype > 2 || n > INT_MAX || V > INT_MAX) return -1;
+    if (n < 0 || V < 1 || top < 1 || top > 1024 || dtype < 0 || dtype > 2 || n > INT_MAX || V > MAX_VOCABULARY) return -1;
     if (n == 0) return 0;
     int64_t part;
     int parts;
@@ -695,7 +696,8 @@ idkm_status idkm_distill(idkm_ctx* ctx, const void* logits, int64_t n, int64_t V
                          void* dlogits_out, int64_t ldd, void* workspace, int64_t workspace_bytes, void* hip_stream) {
     return entry(ctx, [&]() -> idkm_status {
         if (dtype != IDKM_F32 && dtype != IDKM_F16 && dtype != IDKM_BF16) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dtype must be an idkm_dtype");
-        if (n < 0 || V < 1 || n > INT_MAX || V > INT_MAX) return refuse(ctx, IDKM_ERR_INVALID_ARG, "need n >= 0 and V >= 1, below 2^31");
+        if (n < 0 || V < 1) return refuse(ctx, IDKM_ERR_INVALID_ARG, "need n >= 0 and V >= 1");
+        if (n > INT_MAX || V > MAX_VOCABULARY) return refuse(ctx, IDKM_ERR_UNSUPPORTED, "need n < 2^31 and V <= 2^29");
         if (top < 1 || top > 1024) return refuse(ctx, IDKM_ERR_INVALID_ARG, "need 1 <= top <= 1024");
         if (!(tau > 0.f) || !std::isfinite(tau)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "tau must be finite and > 0");
         if ((weight != nullptr) != (dlogits_out != nullptr))
