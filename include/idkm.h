@@ -251,8 +251,10 @@ idkm_status idkm_unpack_quantize(idkm_ctx* ctx, const uint32_t* words, int64_t m
  *   w[r,c] = S[r, c div group] C[code of sub-vector (r cols + c) div d, c mod d]
  * with S left out where it is NULL.  A code >= k makes its weights NaN, as in idkm_unpack_quantize.
  * Activations, outputs and the codebook are of one type, dtype; scales, dC and dS are float32.  All sums are float32; results
- * are rounded once.  Two things are rounded to 16 bits on the way, with 16-bit types and scales only: the product S C where the
- * layer is written out as a matrix for the matrix cores (many tokens, and dX), to the type, as a stored 16-bit weight is.
+ * are rounded once.  One thing is rounded on the way, with 16-bit types and scales only: the product S C, to the type, as a stored
+ * 16-bit weight is, where the layer is written out as a matrix for the matrix cores (dX, and many tokens; idkm_codes_linear does it
+ * where that is expected to be faster, and otherwise multiplies sums by S).  Codewords are meant to be finite: an infinite one makes
+ * infinities or NaN of the outputs of the rows that use it.
  *
  *   idkm_codes_linear           Y[t,r] = sum_c X[t,c] w[r,c] for n tokens (n = 0 is a no-op)
  *   idkm_codes_linear_backward  from dY [n, rows]:  dX[t,c] = sum_r dY[t,r] w[r,c];  with P[r,c] = sum_t dY[t,r] X[t,c],
@@ -265,7 +267,7 @@ idkm_status idkm_unpack_quantize(idkm_ctx* ctx, const uint32_t* words, int64_t m
  *       run at the same time need one each, and so does every captured graph that may be replayed beside other work.
  *   Both enqueue on hip_stream, do not wait, allocate nothing and can be captured into a graph.
  * Limits: 1 <= k <= 1024, 1 <= d <= 64; a group shorter than a row is a multiple of 32 and of d (any group >= cols: one scale
- * a row); rows, cols, n <= 4,000,000, rows cols <= 2^36.  Fast for up to 64 tokens: k <= 256 with d in {1, 2, 4, 8}.
+ * a row); rows, cols, n <= 4,000,000, rows cols <= 2^36.  k <= 256 with d in {1, 2, 4, 8} have the fast kernels.
  */
 typedef enum { IDKM_F32 = 0, IDKM_F16 = 1, IDKM_BF16 = 2 } idkm_dtype;
 typedef struct {
@@ -317,7 +319,7 @@ idkm_status idkm_group_scale_backward(idkm_ctx* ctx, const float* Z, const float
  * A row without entries, or whose entries are all -inf, has loss 0 and gradient 0, whatever its logits are; an index >= V or a
  * NaN in a row's list makes its loss and gradient NaN.  Logits of -inf have q = 0.
  *   weight, dlogits_out  device [n] float32 and [n,V] (rows ldd apart), both or neither NULL (neither: loss and lse only).
- *                        dlogits_out may be logits itself, with ldd = ldz.
+ *                        dlogits_out may be logits itself, with ldd = ldz; otherwise they do not overlap.
  *   index, teacher       device [n,top] int32 and float32, 1 <= top <= 1024; n < 2^31, V <= 2^29.
  *   workspace            as for idkm_codes_linear, of idkm_distill_workspace bytes.
  * Enqueues on hip_stream, does not wait; n = 0 is a no-op.  Logits and gradient are aligned to their element type.

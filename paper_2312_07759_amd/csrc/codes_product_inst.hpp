@@ -4,25 +4,27 @@
 
 namespace idkm {
 
-template <typename T, int W>
+template <typename T, int W, bool APART>
 static ProductFn for_run(int L, bool aligned) {
     constexpr int IB = CODE_BITS;
-    if (L == 8) return &k_codes_product<T, IB, W, 8, false>;
-    if (L == 16) return &k_codes_product<T, IB, W, 16, false>;
-    if constexpr (32 / W * IB % 32 == 0) {
-        if (aligned) return &k_codes_product<T, IB, W, 32, true>;
+    if constexpr (!APART) {
+        if (L == 8) return &k_codes_product<T, IB, W, 8, false, false>;
+        if (L == 16) return &k_codes_product<T, IB, W, 16, false, false>;
     }
-    return &k_codes_product<T, IB, W, 32, false>;
+    if constexpr (32 / W * IB % 32 == 0) {
+        if (aligned) return &k_codes_product<T, IB, W, 32, true, APART>;
+    }
+    return &k_codes_product<T, IB, W, 32, false, APART>;
 }
 
 template <typename T>
-static ProductFn for_type(int W, int L, bool aligned) {
+static ProductFn for_type(int W, int L, bool aligned, bool apart) {
     // codes of one to four bits are looked up together until they are eight weights or five bits and more
     switch (W) {
-        case 1: if constexpr (CODE_BITS >= 5) return for_run<T, 1>(L, aligned); break;
-        case 2: if constexpr (CODE_BITS >= 5) return for_run<T, 2>(L, aligned); break;
-        case 4: if constexpr (CODE_BITS >= 5) return for_run<T, 4>(L, aligned); break;
-        case 8: return for_run<T, 8>(L, aligned);
+        case 1: if constexpr (CODE_BITS >= 5) return apart ? for_run<T, 1, true>(L, aligned) : for_run<T, 1, false>(L, aligned); break;
+        case 2: if constexpr (CODE_BITS >= 5) return apart ? for_run<T, 2, true>(L, aligned) : for_run<T, 2, false>(L, aligned); break;
+        case 4: if constexpr (CODE_BITS >= 5) return apart ? for_run<T, 4, true>(L, aligned) : for_run<T, 4, false>(L, aligned); break;
+        case 8: return apart ? for_run<T, 8, true>(L, aligned) : for_run<T, 8, false>(L, aligned);
     }
     return nullptr;
 }
@@ -51,10 +53,10 @@ static ProductFn tile_for_type(int W, int L, int NT, bool aligned) {
 
 #define CODES_PRODUCT_NAME2(b) codes_product_kernel_##b
 #define CODES_PRODUCT_NAME(b) CODES_PRODUCT_NAME2(b)
-ProductFn CODES_PRODUCT_NAME(CODE_BITS)(int dtype, int W, int L, bool aligned) {
-    if (dtype == 0) return for_type<float>(W, L, aligned);
-    if (dtype == 1) return for_type<f16>(W, L, aligned);
-    return for_type<bf16>(W, L, aligned);
+ProductFn CODES_PRODUCT_NAME(CODE_BITS)(int dtype, int W, int L, bool aligned, bool apart) {
+    if (dtype == 0) return for_type<float>(W, L, aligned, apart);
+    if (dtype == 1) return for_type<f16>(W, L, aligned, apart);
+    return for_type<bf16>(W, L, aligned, apart);
 }
 
 #define CODES_TILE_NAME2(b) codes_tile_kernel_##b

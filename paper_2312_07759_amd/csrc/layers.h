@@ -7,9 +7,10 @@
 namespace idkm {
 
 // Up to 16 tokens, straight from the codes.  IB bits looked up at once give W weights (see codes_at_once), L weights of a row to a
-// lane at a time (8, 16, 32); aligned: every run of codes begins with a word.  nullptr if not instantiated.
+// lane at a time (8, 16, 32); aligned: every run of codes begins with a word; apart: up to 4 tokens, L = 32, a scale for every run.
+// nullptr if not instantiated.
 typedef void (*ProductFn)(const ProductArgs);
-ProductFn codes_product_kernel(int dtype, int IB, int W, int L, bool aligned);
+ProductFn codes_product_kernel(int dtype, int IB, int W, int L, bool aligned, bool apart);
 // 17 tokens and more, 16 NT of them at a time (NT in {2, 4}).
 ProductFn codes_tile_kernel(int dtype, int IB, int W, int L, int NT, bool aligned);
 

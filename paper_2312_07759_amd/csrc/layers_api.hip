@@ -15,14 +15,14 @@ namespace idkm {
 int context_device(const idkm_ctx* ctx);
 void context_error(idkm_ctx* ctx, const char* msg);
 
-ProductFn codes_product_kernel_1(int, int, int, bool);
-ProductFn codes_product_kernel_2(int, int, int, bool);
-ProductFn codes_product_kernel_3(int, int, int, bool);
-ProductFn codes_product_kernel_4(int, int, int, bool);
-ProductFn codes_product_kernel_5(int, int, int, bool);
-ProductFn codes_product_kernel_6(int, int, int, bool);
-ProductFn codes_product_kernel_7(int, int, int, bool);
-ProductFn codes_product_kernel_8(int, int, int, bool);
+ProductFn codes_product_kernel_1(int, int, int, bool, bool);
+ProductFn codes_product_kernel_2(int, int, int, bool, bool);
+ProductFn codes_product_kernel_3(int, int, int, bool, bool);
+ProductFn codes_product_kernel_4(int, int, int, bool, bool);
+ProductFn codes_product_kernel_5(int, int, int, bool, bool);
+ProductFn codes_product_kernel_6(int, int, int, bool, bool);
+ProductFn codes_product_kernel_7(int, int, int, bool, bool);
+ProductFn codes_product_kernel_8(int, int, int, bool, bool);
 
 ProductFn codes_tile_kernel_1(int, int, int, int, bool);
 ProductFn codes_tile_kernel_2(int, int, int, int, bool);
@@ -56,11 +56,11 @@ ProductFn codes_tile_kernel(int dtype, int IB, int W, int L, int NT, bool aligne
     return IB >= 1 && IB <= 8 ? by_bits[IB - 1](dtype, W, L, NT, aligned) : nullptr;
 }
 
-ProductFn codes_product_kernel(int dtype, int IB, int W, int L, bool aligned) {
-    static ProductFn (*const by_bits[8])(int, int, int, bool) = {
+ProductFn codes_product_kernel(int dtype, int IB, int W, int L, bool aligned, bool apart) {
+    static ProductFn (*const by_bits[8])(int, int, int, bool, bool) = {
         codes_product_kernel_1, codes_product_kernel_2, codes_product_kernel_3, codes_product_kernel_4,
         codes_product_kernel_5, codes_product_kernel_6, codes_product_kernel_7, codes_product_kernel_8};
-    return IB >= 1 && IB <= 8 ? by_bits[IB - 1](dtype, W, L, aligned) : nullptr;
+    return IB >= 1 && IB <= 8 ? by_bits[IB - 1](dtype, W, L, aligned, apart) : nullptr;
 }
 
 }  // namespace idkm
@@ -166,19 +166,20 @@ FewPlan few_plan(const idkm_codes_desc& w, int64_t n) {
     FewPlan p;
     const int bits = idkm_code_bits(w.k);
     if (bits > 8 || (w.d != 1 && w.d != 2 && w.d != 4 && w.d != 8)) return p;
-    // a chunk of four runs has to lie in one group
-    const int L = !w.S || w.group >= w.cols || w.group % 128 == 0 ? 32 : w.group % 64 == 0 ? 16 : 8;
+    // a chunk of four runs has to lie in one group, where their sums are not kept apart
+    const bool together = !w.S || w.group >= w.cols || w.group % 128 == 0, apart = !together && n <= 4;
+    const int L = together || apart ? 32 : w.group % 64 == 0 ? 16 : 8;
     const int at_once = codes_at_once(bits, w.d), IB = at_once * bits, W = at_once * w.d;
     const int64_t chunks = (w.cols + 4 * L - 1) / (4 * L);
-    if (w.S && w.group < w.cols) {  // exact while chunks (chunks of a group) < 2^31
-        const int64_t of_group = w.group / (4 * L);
-        if (chunks * of_group >= ((int64_t)1 << 31)) return p;
+    if (w.S && w.group < w.cols) {  // in chunks, or runs; exact while all (those of a group) < 2^31
+        const int64_t of_group = w.group / (apart ? 32 : 4 * L);
+        if ((apart ? 4 : 1) * chunks * of_group >= ((int64_t)1 << 31)) return p;
         p.group_magic = (unsigned)((((int64_t)1 << 31) + of_group - 1) / of_group);
     }
     if (n > VECTOR_TOKENS && w.rows * w.cols / w.d * bits < 1024) return p;  // a run's words have to be there
     const bool aligned = (w.cols / w.d * bits) % 32 == 0 && (32 / W * IB) % 32 == 0;
     if (n <= VECTOR_TOKENS) {
-        p.fn = codes_product_kernel(w.dtype, IB, W, L, aligned);
+        p.fn = codes_product_kernel(w.dtype, IB, W, L, aligned, apart);
         const int waves = chunks < 8 ? (int)chunks : 8;
         p.threads = waves * 64;
         p.grid = dim3((unsigned)((w.rows + 15) / 16));
