@@ -132,14 +132,23 @@ void launch_codes_bins(int dtype, const BinArgs& args, int grid, int waves, hipS
     });
 }
 
+// Lanes that have the same bins in k_codes_bins_wide: 16 KB a wavefront.
+int bins_shared_by(int k) { return k <= 64 ? 1 : k <= 128 ? 2 : 4; }
+
+template <typename T, int SHARE>
+static void (*wide_for(int d))(const BinArgs) {
+    return d == 1 ? &k_codes_bins_wide<T, 1, SHARE> : d == 2 ? &k_codes_bins_wide<T, 2, SHARE>
+           : d == 4 ? &k_codes_bins_wide<T, 4, SHARE> : &k_codes_bins_wide<T, 8, SHARE>;
+}
+
 template <typename T>
 static void launch_bins_runs(const BinArgs& a, bool wide, int grid, int waves, hipStream_t s) {
     void (*const narrow_fn)(const BinArgs) = a.d == 1 ? &k_codes_bins_runs<T, 1> : a.d == 2 ? &k_codes_bins_runs<T, 2>
                                              : a.d == 4 ? &k_codes_bins_runs<T, 4> : &k_codes_bins_runs<T, 8>;
-    void (*const wide_fn)(const BinArgs) = a.d == 1 ? &k_codes_bins_wide<T, 1> : a.d == 2 ? &k_codes_bins_wide<T, 2>
-                                           : a.d == 4 ? &k_codes_bins_wide<T, 4> : &k_codes_bins_wide<T, 8>;
+    const int share = wide ? bins_shared_by(a.k) : 1;
+    void (*const wide_fn)(const BinArgs) = share == 1 ? wide_for<T, 1>(a.d) : share == 2 ? wide_for<T, 2>(a.d) : wide_for<T, 4>(a.d);
     void (*const fn)(const BinArgs) = wide ? wide_fn : narrow_fn;
-    const size_t lds = wide ? (a.bins ? (size_t)waves * 64 * a.k * 4 : 0) : ((a.bins ? (size_t)waves * 64 : 0) + 1) * a.k * a.d * 4;
+    const size_t lds = wide ? (a.bins ? (size_t)waves * (64 / share) * a.k * 4 : 0) : ((a.bins ? (size_t)waves * 64 : 0) + 1) * a.k * a.d * 4;
     allow_lds(reinterpret_cast<const void*>(fn), lds);
     hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3((unsigned)waves * 64), lds, s, a);
 }

@@ -231,14 +231,17 @@ __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {
 
 // The same codes with larger codebooks: a lane has one component, as in the first kernel, and a wavefront takes 512 columns of a row
 // in eight steps of 64; the next 512 are asked for before these are used.  dS goes through `segments` always.
-template <typename T, int D>
+// SHARE lanes have the same bins and add to them one after another: with bins for every lane, 256 codewords leave room for two wavefronts
+// on a compute unit, which wait for every one of their loads (512 x 4608, k = 256, d = 4: 30 us).
+template <typename T, int D, int SHARE>
 __global__ __launch_bounds__(256) void k_codes_bins_wide(const BinArgs a) {
-    constexpr int STEPS = 8;
-    extern __shared__ __align__(16) float bin_lds[];  // [wave][k][64]
+    constexpr int STEPS = 8, WIDTH = 64 / SHARE;
+    extern __shared__ __align__(16) float bin_lds[];  // [wave][k][WIDTH]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
-    float* mine = bin_lds + wave * a.k * 64 + lane;
+    float* mine = bin_lds + wave * a.k * WIDTH + lane % WIDTH;
+    const int turn = lane / WIDTH;
     if (a.bins)
-        for (int j = 0; j < a.k; ++j) mine[j * 64] = 0.f;
+        for (int j = lane; j < a.k * WIDTH; j += 64) bin_lds[wave * a.k * WIDTH + j] = 0.f;
     const T* C = static_cast<const T*>(a.C) + lane % D;
     const int strips = (int)((a.cols + 511) / 512), per_row = (int)(a.cols / D), segments = (int)((a.cols + 31) / 32);
     const uint32_t mask = (1u << a.bits) - 1u;
@@ -284,7 +287,14 @@ __global__ __launch_bounds__(256) void k_codes_bins_wide(const BinArgs a) {
             const int c = strip * 512 + u * 64 + lane;
             const uint32_t code = (uint32_t)(((uint64_t)now.hi[u] << 32 | now.lo[u]) >> now.sh[u]) & mask;
             const bool none = code >= (uint32_t)a.k, counts = c < a.cols;
-            if (a.bins) mine[(none ? 0 : code) * 64] += counts && !none ? now.s[u] * now.p[u] : 0.f;
+            const float v = counts && !none ? now.s[u] * now.p[u] : 0.f;
+            if (a.bins) {
+#pragma unroll
+                for (int t = 0; t < SHARE; ++t) {
+                    if (turn == t) mine[(none ? 0 : code) * WIDTH] += v;
+                    asm volatile("" ::: "memory");  // one turn after another
+                }
+            }
             if (a.segments) {
                 float sum = counts ? now.p[u] * (none ? __builtin_nanf("") : Elem<T>::up(C[none ? 0 : code * D])) : 0.f;
 #pragma unroll
@@ -302,7 +312,7 @@ __global__ __launch_bounds__(256) void k_codes_bins_wide(const BinArgs a) {
         const int j = e / D, i = e % D;
         double sum = 0.0;
         for (int w = 0; w < nw; ++w)
-            for (int l = i; l < 64; l += D) sum += (double)bin_lds[(w * a.k + j) * 64 + ((l + j * D) & 63)];
+            for (int l = i; l < WIDTH; l += D) sum += (double)bin_lds[(w * a.k + j) * WIDTH + (l + j * D) % WIDTH];
         a.bins[e * a.pitch + a.at + blockIdx.x] = (float)sum;
     }
 }

@@ -36,6 +36,7 @@ void add_operand(OperandArgs* a, const void* in, int64_t ldi, int64_t M, int64_t
 void launch_operands(int dtype, const OperandArgs& a, hipStream_t s);
 void launch_join_parts(int dtype, const float* parts, int nz, int64_t M, int64_t N, void* out, int64_t ldo, hipStream_t s);
 void launch_codes_bins(int dtype, const BinArgs& a, int grid, int waves, hipStream_t s);
+int bins_shared_by(int k);
 void launch_codes_bins_runs(int dtype, const BinArgs& a, bool wide, int grid, int waves, hipStream_t s);
 void launch_fill_zero(float* out, int64_t n, hipStream_t s);
 // dC from bins [kd][n] (null: not), dS from segments (null: not).

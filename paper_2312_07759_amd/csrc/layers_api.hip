@@ -366,7 +366,7 @@ LayerGradLayout layer_grad_layout(const idkm_codes_desc& w, int64_t n) {
         // lanes of a group of 8 m columns lie together in a wavefront's 512 where m is a power of two
         l.segmented = w.S && (l.wide || l.group > 512 || l.group % 8 != 0 || (l.group & (l.group - 1)) != 0);
         tasks = l.panel * ((w.cols + 511) / 512);
-        bin_bytes = (l.wide ? w.k : w.k * w.d) * 256;
+        bin_bytes = l.wide ? w.k * 256 / bins_shared_by(w.k) : w.k * w.d * 256;
         l.codes = w.k;
     } else {
         // a wavefront takes groups of a row at a time; without scales, some hundred columns
