@@ -80,7 +80,9 @@ static bool launch_fast(int dtype, const DenseArgs& a, bool columns, hipStream_t
     const DenseFn fn = codes_dense_kernel(dtype, IB, W, columns, a.row_bits % 32 == 0);
     const size_t table = (size_t)128 << IB, tile = columns ? (dtype == 0 ? TransposeTile<float>::WORDS : TransposeTile<bf16>::WORDS) * 4 : 0;
     int64_t grid = columns ? ((a.count + 63) / 64) * ((a.pad + 63) / 64) : (a.count * (a.pad / 8) + 255) / 256;
-    if (grid > 1024) grid = 1024;  // four workgroups to a compute unit, each with one table
+    // as many workgroups as the compute units hold at once, each with one table
+    const int64_t most = columns ? 768 : 1024;
+    if (grid > most) grid = most;
     hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(256), table + tile, s, a);
     return true;
 }
