@@ -144,7 +144,7 @@ struct CodeRun {
         for (int i = 0; i < NWORDS; ++i) w[i] = ALIGNED ? raw[i] : __builtin_amdgcn_alignbit(raw[i + 1], raw[i], sh);
     }
     // The same without a branch, for a run that lies in the stream as a whole (which has at least SPAN words): near its end the
-    // words are taken from one further ahead.  `bit` counts from `words` on; no window begins behind word `limit`.
+    // words are taken from one further ahead.  `bit` counts from `words` on; no window begins behind word `limit`, which is >= 0.
     template <bool ALIGNED>
     __device__ __forceinline__ void load_inside(const uint32_t* words, int limit, unsigned bit) {
         constexpr int RAW = ALIGNED ? NWORDS : SPAN;
@@ -384,9 +384,11 @@ __global__ __launch_bounds__((TileOfTokens<T, NT>::THREADS)) void k_codes_tile(c
     const int first = min(whole, (int)blockIdx.z * each), last = min(whole, first + each);
     const int turns = (last - first + G - 1) / G;  // steps first + G i + team; some teams may have no last one
     const int64_t bit0 = n0 * a.row_bits;
-    const uint32_t* words = a.words + (bit0 >> 5);
-    const int limit = (int)min(a.nwords - (bit0 >> 5) - CodeRun<NB>::SPAN, (int64_t)1 << 30);
-    const unsigned row_bit = (unsigned)(bit0 & 31) + (unsigned)row * (unsigned)a.row_bits + q * NB;
+    // offsets count from a word from which on there are at least SPAN of them (the stream has 32)
+    const int64_t word0 = min(bit0 >> 5, a.nwords - CodeRun<NB>::SPAN);
+    const uint32_t* words = a.words + word0;
+    const int limit = (int)min(a.nwords - word0 - CodeRun<NB>::SPAN, (int64_t)1 << 30);
+    const unsigned row_bit = (unsigned)(bit0 - (word0 << 5)) + (unsigned)row * (unsigned)a.row_bits + q * NB;
     const bool scaled = a.groups > 0;
     const float* S = scaled ? a.S + n0 * a.groups : nullptr;
     const unsigned S_row = (unsigned)(row * a.groups);

@@ -180,3 +180,15 @@ def test_oracle_words_equal_packed_codes(ctx):
     layer = Layer(20, 64, 6, 2, 0, torch.float32, seed=4)
     words = ctx.pack_codes(torch.from_numpy(layer.codes.astype(np.int32)).cuda(), 6)
     assert torch.equal(words.cpu(), layer.words) and np.array_equal(orc.unpack_codes(layer.words.numpy().view(np.uint32), 640, 6), layer.codes)
+
+
+@pytest.mark.parametrize("rows,cols,k,d", [(65, 128, 2, 8), (81, 128, 2, 8), (97, 136, 2, 8), (113, 128, 2, 8), (65, 192, 2, 8), (129, 128, 3, 8), (129, 128, 2, 4)])
+def test_last_rows_of_few_bits(ctx, rows, cols, k, d):
+    """The last 16 rows of the layer are one row whose codes lie in the stream's last word, which a window of two words begins before."""
+    for dtype in (torch.float32, torch.float16):
+        layer = Layer(rows, cols, k, d, 0, dtype, seed=6)
+        w = layer.weights()
+        for n in (17, 40, 130):
+            X = draw((n, cols), dtype, n)
+            ref = X.double() @ w.t()
+            check(ctx.codes_linear(layer.on_gpu(binding), X.cuda()), ref, HALF_STEP[dtype] * ref.abs() + sum_error(X.double().abs() @ w.abs().t(), cols))
