@@ -117,18 +117,18 @@ def _no_capture(*tensors):
 class _CodesProduct(torch.autograd.Function):
     @staticmethod
     def forward(fn, X, C, S, module):
-        fn.module = module
-        fn.save_for_backward(X, C, S)
-        return _context(X.get_device()).codes_linear(module.layer(X.dtype), X)
+        fn.layer = module.layer(X.dtype)
+        fn.save_for_backward(X, C, S, module.words)
+        return _context(X.get_device()).codes_linear(fn.layer, X)
 
     @staticmethod
     @once_differentiable
     def backward(fn, dY):
-        X, C, S = fn.saved_tensors
+        X, C, S, _ = fn.saved_tensors
         need_X, need_C, need_S = fn.needs_input_grad[:3]
-        r = _context(X.get_device()).codes_linear_backward(fn.module.layer(X.dtype), X, dY.contiguous(), want_dX=need_X, want_dC=need_C,
+        r = _context(X.get_device()).codes_linear_backward(fn.layer, X, dY.contiguous(), want_dX=need_X, want_dC=need_C,
                                                            want_dS=need_S)
-        return r.get("dX"), r["dC"].to(C.dtype) if need_C else None, r.get("dS"), None
+        return r.get("dX"), r["dC"].to(C.dtype) if need_C else None, r["dS"].to(S.dtype) if need_S else None, None
 
 
 class CodesLinear(torch.nn.Module):
@@ -140,19 +140,13 @@ class CodesLinear(torch.nn.Module):
         super().__init__()
         self.rows, self.cols, self.group = layer.rows, layer.cols, layer.group
         self.register_buffer("words", layer.words)
-        self.C = torch.nn.Parameter(layer.C.detach().float())
+        self.C = torch.nn.Parameter(layer.C.detach().to(torch.float32, copy=True))
         self.S = torch.nn.Parameter(layer.S.detach().clone()) if layer.S is not None else None
-        self._layers = {}
 
     def layer(self, dtype):
-        """The stored layer with its codebook in `dtype`, made again when a parameter has changed."""
-        state = (self.C._version, self.C.data_ptr(), self.words.data_ptr(), None if self.S is None else self.S.data_ptr())
-        held = self._layers.get(dtype)
-        if held is None or held[0] != state:
-            S = None if self.S is None else self.S.detach()
-            held = self._layers[dtype] = (state, binding.CodesLayer(self.words, self.rows, self.cols, self.C.detach().to(dtype).contiguous(), S,
-                                                                    self.group))
-        return held[1]
+        """The stored layer as it is now, with its codebook in `dtype`."""
+        S = None if self.S is None else self.S.detach().float()
+        return binding.CodesLayer(self.words, self.rows, self.cols, self.C.detach().to(dtype).contiguous(), S, self.group)
 
     def forward(self, X):
         if X.shape[-1] != self.cols:
