@@ -22,7 +22,8 @@ class _Quantize(torch.autograd.Function):
         Z, d = W.detach(), C0.shape[1]
         if layer.group:
             S, Z = layer.ctx.group_scale(Z, layer.group)
-            layer.S = S
+            layer.S, layer.turn = S, layer.turn + 1
+            fn.turn = layer.turn
         out = layer.ctx.forward(Z.view(-1, d), C0, layer.tau, layer.tol, layer.max_iter, layer.dist, want_Wq=True)
         layer.last_forward = out["info"]
         layer.C = out["C"]
@@ -38,6 +39,8 @@ class _Quantize(torch.autograd.Function):
         layer = fn.layer
         dWq = dWq.contiguous()
         if layer.group:
+            if fn.turn != layer.turn:  # the library's state, W's borrowed address in it, is of that other call
+                raise RuntimeError("the layer has been quantised again since: its backward pass has to come first")
             Z, S, Zq = fn.scaled
             dWq, dS = layer.ctx.group_unscale_backward(dWq, Zq, S, layer.group)
         res = layer.ctx.backward(dWq.view(-1, layer.C.shape[1]), layer.bwd_mode, tol=layer.bwd_tol, max_iter=layer.bwd_max_iter,
@@ -65,7 +68,7 @@ class SoftKMeansQuantize:
         self.tau, self.dist, self.tol, self.max_iter = float(tau), int(dist), float(tol), int(max_iter)
         self.bwd_mode, self.bwd_tol, self.bwd_max_iter, self.alpha = int(bwd_mode), float(bwd_tol), int(bwd_max_iter), float(alpha)
         self.last_forward = self.last_backward = self.C = self.S = None
-        self.group = int(group)
+        self.group, self.turn = int(group), 0
         if self.group < 0:
             raise ValueError("group must be >= 0")
 
@@ -80,18 +83,23 @@ class SoftKMeansQuantize:
     @torch.no_grad()
     def stored(self, W, C0, dtype=torch.float32):
         """The [rows, cols] layer W solved from C0 and brought to its stored form, every sub-vector replaced by its closest codeword:
-        a binding.CodesLayer with a codebook of `dtype` (that of the activations it will be multiplied with)."""
+        a binding.CodesLayer with a codebook of `dtype` (that of the activations it will be multiplied with).  Solved in a context of its
+        own: a backward pass that is still to come finds its state."""
         if W.dim() != 2 or C0.dim() != 2 or W.shape[1] % C0.shape[1]:
             raise ValueError("W must be [rows, cols] with cols a multiple of d, and C0 [k, d]")
         (rows, cols), (k, d) = W.shape, C0.shape
         if self.group and self.group < cols and (self.group % 32 or self.group % d):
             raise ValueError("a stored group shorter than a row must be a multiple of 32 and of d")
         Z, S = W.detach().contiguous(), None
-        if self.group:
-            S, Z = self.ctx.group_scale(Z, self.group)
-        out = self.ctx.forward(Z.view(-1, d), C0.contiguous(), self.tau, self.tol, self.max_iter, self.dist, want_Wq=False, want_assign=True)
-        self.C, self.S, self.last_forward = out["C"], S, out["info"]
-        return binding.CodesLayer(self.ctx.pack_codes(out["assign"], k), rows, cols, out["C"].to(dtype), S, self.group)
+        ctx = binding.Context(self.ctx.device)
+        try:
+            if self.group:
+                S, Z = ctx.group_scale(Z, self.group)
+            out = ctx.forward(Z.view(-1, d), C0.contiguous(), self.tau, self.tol, self.max_iter, self.dist, want_Wq=False, want_assign=True)
+            words = ctx.pack_codes(out["assign"], k)
+        finally:
+            ctx.close()
+        return binding.CodesLayer(words, rows, cols, out["C"].to(dtype), S, self.group)
 
     def close(self):
         self.ctx.close()
@@ -114,6 +122,11 @@ def _no_capture(*tensors):
         raise RuntimeError("a differentiable call cannot be captured: capture Context.codes_linear, codes_linear_backward and distill")
 
 
+def _no_captured_backward():
+    if torch.cuda.is_current_stream_capturing():
+        raise RuntimeError("a backward pass cannot be captured: capture Context.codes_linear_backward and distill")
+
+
 class _CodesProduct(torch.autograd.Function):
     @staticmethod
     def forward(fn, X, C, S, module):
@@ -124,6 +137,7 @@ class _CodesProduct(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(fn, dY):
+        _no_captured_backward()
         X, C, S, _ = fn.saved_tensors
         need_X, need_C, need_S = fn.needs_input_grad[:3]
         r = _context(X.get_device()).codes_linear_backward(fn.layer, X, dY.contiguous(), want_dX=need_X, want_dC=need_C,
@@ -165,6 +179,7 @@ class _Distill(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(fn, dloss):
+        _no_captured_backward()
         logits, index, teacher = fn.saved_tensors
         return _context(logits.get_device()).distill(logits, index, teacher, fn.tau, dloss.float().contiguous())[2], None, None, None
 

@@ -50,3 +50,32 @@ def test_parameters_in_16_bits():
     ref = autograd.CodesLinear(m.layer(torch.bfloat16))
     ref(X).sum().backward()
     assert torch.equal(ref.C.grad.bfloat16(), m.C.grad) and torch.equal(ref.S.grad.bfloat16(), m.S.grad)
+
+
+@pytest.mark.parametrize("group", [0, 64])
+def test_stored_between_forward_and_backward(group):
+    """Storing a layer (this one's other weights, here) leaves the state that its backward pass needs."""
+    W, G, C0 = draw((24, 128), torch.float32, 1).cuda(), draw((24, 128), torch.float32, 2).cuda(), torch.linspace(-2, 2, 4, device="cuda").view(4, 1)
+    shape = (24, 128) if group else (24 * 128, 1)
+    grads = []
+    for between in (False, True):
+        q = autograd.SoftKMeansQuantize(0.3, binding.DIST_SQL2, tol=1e-7, group=group)
+        w = W.view(shape).clone().requires_grad_()
+        Wq, _ = q(w, C0)
+        if between:
+            q.stored(draw((24, 128), torch.float32, 3).cuda(), C0 * 0.5)
+        Wq.backward(G.view(shape))
+        grads.append(w.grad)
+        q.close()
+    assert torch.equal(*grads)
+
+
+def test_backward_of_an_earlier_grouped_call_is_refused():
+    q = autograd.SoftKMeansQuantize(0.3, binding.DIST_SQL2, group=64)
+    W, C0 = draw((24, 128), torch.float32, 1).cuda().requires_grad_(), torch.linspace(-2, 2, 4, device="cuda").view(4, 1)
+    first, second = q(W, C0)[0], q(W * 1.5, C0)[0]
+    with pytest.raises(RuntimeError, match="quantised again"):
+        first.sum().backward()
+    second.sum().backward()
+    assert W.grad.isfinite().all()
+    q.close()

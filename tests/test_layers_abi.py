@@ -50,3 +50,12 @@ def test_other_refused_sizes():
     assert lib.idkm_codes_linear_backward(None, ctypes.byref(d), None, 256, None, 64, 1, None, 256, None, None, None, 0, None) == 1
     assert lib.idkm_group_scale(None, None, 1, 1, 1, None, None, None) == 1
     assert lib.idkm_distill(None, None, 1, 1, 1, 0, None, None, 1, 1.0, None, None, None, None, 1, None, 0, None) == 1
+
+
+def test_captured_backward_passes_are_refused(monkeypatch):
+    torch = pytest.importorskip("torch")
+    from paper_2312_07759_amd import autograd
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    for function in (autograd._CodesProduct, autograd._Distill):
+        with pytest.raises(RuntimeError, match="captured"):
+            function.backward(None, torch.zeros(1))
