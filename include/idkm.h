@@ -253,7 +253,8 @@ idkm_status idkm_unpack_quantize(idkm_ctx* ctx, const uint32_t* words, int64_t m
  * Activations, outputs and the codebook are of one type, dtype; scales, dC and dS are float32.  All sums are float32; results
  * are rounded once.  One thing is rounded on the way, with 16-bit types and scales only: the product S C, to the type, as a stored
  * 16-bit weight is, where the layer is written out as a matrix for the matrix cores (dX, and many tokens; idkm_codes_linear does it
- * where that is expected to be faster, and otherwise multiplies sums by S).  Codewords are meant to be finite: an infinite one makes
+ * where that is expected to be faster, and otherwise multiplies sums by S); a float16 product beyond 65504 becomes infinite there, and
+ * one below 2^-14 keeps fewer bits.  Codewords are meant to be finite: an infinite one makes
  * infinities or NaN of the outputs of the rows that use it.
  *
  *   idkm_codes_linear           Y[t,r] = sum_c X[t,c] w[r,c] for n tokens (n = 0 is a no-op)
@@ -320,7 +321,7 @@ idkm_status idkm_group_scale_backward(idkm_ctx* ctx, const float* Z, const float
  * NaN in a row's list makes its loss and gradient NaN.  Logits of -inf have q = 0.
  *   weight, dlogits_out  device [n] float32 and [n,V] (rows ldd apart), both or neither NULL (neither: loss and lse only).
  *                        dlogits_out may be logits itself, with ldd = ldz; otherwise they do not overlap.
- *   index, teacher       device [n,top] int32 and float32, 1 <= top <= 1024; n < 2^31, V <= 2^29.
+ *   index, teacher       device [n,top] int32 and float32, 1 <= top <= 1024; n < 2^31, V <= 2^29; tau >= 2^-126, finite.
  *   workspace            as for idkm_codes_linear, of idkm_distill_workspace bytes.
  * Enqueues on hip_stream, does not wait; n = 0 is a no-op.  Logits and gradient are aligned to their element type.
  */

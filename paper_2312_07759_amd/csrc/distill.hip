@@ -401,12 +401,25 @@ static void launch_for(const DistillArgs& a, hipStream_t s) {
         return;
     }
     const int64_t pieces = a.V / Elem<T>::PER16;
-    const dim3 grid((unsigned)a.n);
-    if (pieces <= 4 * 64) hipLaunchKernelGGL((k_distill_row<T, 64, 4, false>), grid, dim3(64), lds, s, a);
-    else if (pieces <= 4 * 256) hipLaunchKernelGGL((k_distill_row<T, 256, 4, false>), grid, dim3(256), lds, s, a);
-    else if (pieces <= 16 * 256) hipLaunchKernelGGL((k_distill_row<T, 256, 16, false>), grid, dim3(256), lds, s, a);
-    else if (pieces <= 16 * 512) hipLaunchKernelGGL((k_distill_row<T, 512, 16, false>), grid, dim3(512), lds, s, a);
-    else hipLaunchKernelGGL((k_distill_row<T, 512, 16, true>), grid, dim3(512), lds, s, a);
+    // a launch has less than 2^32 threads
+    constexpr int64_t ROWS = (int64_t)1 << 22;
+    for (int64_t r = 0; r < a.n; r += ROWS) {
+        DistillArgs b = a;
+        b.n = a.n - r < ROWS ? a.n - r : ROWS;
+        b.logits = static_cast<const T*>(a.logits) + r * a.ldz;
+        b.index = a.index + r * a.top;
+        b.teacher = a.teacher + r * a.top;
+        if (a.weight) b.weight = a.weight + r;
+        b.loss = a.loss + r;
+        b.lse = a.lse + r;
+        if (a.dlogits) b.dlogits = static_cast<T*>(a.dlogits) + r * a.ldd;
+        const dim3 grid((unsigned)b.n);
+        if (pieces <= 4 * 64) hipLaunchKernelGGL((k_distill_row<T, 64, 4, false>), grid, dim3(64), lds, s, b);
+        else if (pieces <= 4 * 256) hipLaunchKernelGGL((k_distill_row<T, 256, 4, false>), grid, dim3(256), lds, s, b);
+        else if (pieces <= 16 * 256) hipLaunchKernelGGL((k_distill_row<T, 256, 16, false>), grid, dim3(256), lds, s, b);
+        else if (pieces <= 16 * 512) hipLaunchKernelGGL((k_distill_row<T, 512, 16, false>), grid, dim3(512), lds, s, b);
+        else hipLaunchKernelGGL((k_distill_row<T, 512, 16, true>), grid, dim3(512), lds, s, b);
+    }
 }
 
 void distill_plan(int64_t n, int64_t V, int esize, int64_t* part, int* parts) {

@@ -1,5 +1,6 @@
 // C entry points of the operators on coded layers (products and their gradients), group scales and the loss against a
 // teacher: checks of arguments, choice of kernels, layout of the caller's workspace.
+#include <cfloat>
 #include <climits>
 #include <cmath>
 #include <cstdint>
@@ -700,7 +701,8 @@ idkm_status idkm_distill(idkm_ctx* ctx, const void* logits, int64_t n, int64_t V
         if (n < 0 || V < 1) return refuse(ctx, IDKM_ERR_INVALID_ARG, "need n >= 0 and V >= 1");
         if (n > INT_MAX || V > MAX_VOCABULARY) return refuse(ctx, IDKM_ERR_UNSUPPORTED, "need n < 2^31 and V <= 2^29");
         if (top < 1 || top > 1024) return refuse(ctx, IDKM_ERR_INVALID_ARG, "need 1 <= top <= 1024");
-        if (!(tau > 0.f) || !std::isfinite(tau)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "tau must be finite and > 0");
+        if (!(tau >= FLT_MIN) || !std::isfinite(tau))  // of a smaller one the inverse is infinite
+            return refuse(ctx, IDKM_ERR_INVALID_ARG, "tau must be finite and > 0, and not subnormal");
         if ((weight != nullptr) != (dlogits_out != nullptr))
             return refuse(ctx, IDKM_ERR_INVALID_ARG, "weight and dlogits_out go together");
         if (n == 0) return IDKM_OK;

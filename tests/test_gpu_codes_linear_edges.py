@@ -192,3 +192,30 @@ def test_last_rows_of_few_bits(ctx, rows, cols, k, d):
             X = draw((n, cols), dtype, n)
             ref = X.double() @ w.t()
             check(ctx.codes_linear(layer.on_gpu(binding), X.cuda()), ref, HALF_STEP[dtype] * ref.abs() + sum_error(X.double().abs() @ w.abs().t(), cols))
+
+
+def test_more_rows_of_logits_than_a_launch_takes(ctx):
+    """2^26 + 5 rows of one wavefront each are more than 2^32 threads; single logits, and pairs."""
+    n = 2 ** 26 + 5
+    z = torch.arange(n * 2, device="cuda", dtype=torch.int32).remainder_(1009).to(torch.float16).mul_(2.0 ** -8).view(n, 2)
+    index = torch.zeros(n, 1, dtype=torch.int32, device="cuda")
+    teacher, weight = torch.zeros(n, 1, device="cuda"), torch.ones(n, device="cuda")
+    loss, lse, dz = ctx.distill(z, index, teacher, 1.0, weight)
+    for s in (slice(0, 1000), slice(2 ** 22 - 500, 2 ** 22 + 500), slice(n - 1000, n)):
+        q = torch.log_softmax(z[s].double(), 1)
+        check(loss[s], -q[:, 0].cpu(), torch.full((1000,), 1e-5, dtype=torch.float64))
+        check(dz[s], (q.exp() - torch.tensor([1.0, 0.0], device="cuda", dtype=torch.float64)).cpu(), torch.full((1000, 2), 1e-3, dtype=torch.float64))
+    assert bool(lse.isfinite().all()) and bool((dz.abs().sum(1) > 0).all())
+
+
+def test_smallest_and_largest_temperatures(ctx):
+    z, index, teacher = draw((3, 50), torch.float32, 1).cuda(), torch.zeros(3, 1, dtype=torch.int32, device="cuda"), torch.zeros(3, 1, device="cuda")
+    for tau in (0.0, -1.0, 2.0 ** -127, float("inf"), float("nan")):
+        with pytest.raises(binding.IdkmError):
+            ctx.distill(z, index, teacher, tau)
+    loss, _ = ctx.distill(z, index, teacher, 3e38)
+    check(loss, torch.full((3,), 50.0, dtype=torch.float64).log(), torch.full((3,), 2e-6, dtype=torch.float64))
+    z = torch.zeros(3, 50, device="cuda")
+    loss, lse, dz = ctx.distill(z, index, teacher, 2.0 ** -126, torch.full((3,), 2.0 ** -126, device="cuda"))
+    check(loss, torch.full((3,), 50.0, dtype=torch.float64).log(), torch.full((3,), 2e-6, dtype=torch.float64))
+    check(dz[:, 1:], torch.full((3, 49), 0.02, dtype=torch.float64), torch.full((3, 49), 1e-8, dtype=torch.float64))
