@@ -97,7 +97,7 @@ struct EightOfLayer {
 };
 
 // The layer's rows: a thread takes 8 columns at a time, four such pieces asked for together.  Bound by the writes: 4096 x 4096
-// in 16 bits took 26 us with one code read at a time and 15 with one piece; written at the rate of a fill it is 5.
+// in 16 bits takes 12.5 us (it took 26 with one code read at a time and 15 with one piece); written at the rate of a fill it is 5.
 template <typename T, int IB, int W, bool ALIGNED>
 __global__ __launch_bounds__(256) void k_dense_rows_fast(const DenseArgs a) {
     constexpr int U = 4;
@@ -144,6 +144,7 @@ __global__ __launch_bounds__(256) void k_dense_rows_fast(const DenseArgs a) {
 }
 
 // The layer's columns: out[c, r] = w[r, c], 64 x 64 weights at a time, the next tile's asked for before this one goes through LDS.
+// 4096 x 4096 in 16 bits: 17 us (24 with nothing asked for ahead); bound by the lookups and the LDS traffic of the transposition.
 template <typename T, int IB, int W, bool ALIGNED>
 __global__ __launch_bounds__(256) void k_dense_cols_fast(const DenseArgs a) {
     extern __shared__ __align__(128) unsigned char lds[];

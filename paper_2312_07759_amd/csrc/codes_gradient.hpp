@@ -4,7 +4,7 @@
 // P is read once (float32).  A wavefront takes some groups of a row at a time, `lanes` columns a step;
 // lanes is a multiple of d, so a lane always has the same component x.  It keeps bins of its own for the codewords in LDS
 // ([codeword][lane], a bank to a lane): no two lanes ever add to the same word, and the order of every sum is fixed.
-// A workgroup's bins go to `bins` [k d][workgroup]; k_join_bins adds them up in float64.
+// A workgroup's bins go to `bins` [k d][workgroup]; k_join_gradients adds them up in float64.
 // Bound by reading P: STEPS of them are asked for before the first is used.
 #pragma once
 #include "codes_dense.hpp"
@@ -121,8 +121,8 @@ __global__ __launch_bounds__(256) void k_codes_bins(const BinArgs a) {
 
 // The same for codes of up to 8 bits, D in {1, 2, 4, 8} and small codebooks: a lane takes 8 consecutive columns at a time and
 // keeps bins for all k D components.  Ten instructions a column instead of some 75, which bound the kernel above (4096 x 4096, k = 16:
-// 127 us).  dS: lanes of a group are added up where they are a power of two of at most 64, otherwise sums of 32 columns go to
-// `segments`, which k_join_segments adds up.
+// 127 us; this one 25 to 28, of which P at the rate of a copy is 13).  dS: lanes of a group are added up where they are a power of two of at most 64, otherwise sums of 32 columns go to
+// `segments`, which k_join_gradients adds up.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {
     constexpr int NC = 8 / D;
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {
 // The same codes with larger codebooks: a lane has one component, as in the first kernel, and a wavefront takes 512 columns of a row
 // in eight steps of 64; the next 512 are asked for before these are used.  dS goes through `segments` always.
 // SHARE lanes have the same bins and add to them one after another: with bins for every lane, 256 codewords leave room for two wavefronts
-// on a compute unit, which wait for every one of their loads (512 x 4608, k = 256, d = 4: 30 us).
+// on a compute unit, which wait for every one of their loads (512 x 4608, k = 256, d = 4: 30 us; 18 with eight wavefronts).
 template <typename T, int D, int SHARE>
 __global__ __launch_bounds__(256) void k_codes_bins_wide(const BinArgs a) {
     constexpr int STEPS = 8, WIDTH = 64 / SHARE;

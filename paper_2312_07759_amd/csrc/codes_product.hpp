@@ -7,6 +7,8 @@
 // The table holds the codewords in X's type, as they are given; a group's scale multiplies the float32 sum over its part
 // of the row, so nothing is rounded but the result.
 // The wavefronts of a workgroup share 16 rows of the layer and split the sum; their partial sums meet in LDS, in order.
+// Bound by the latency of one batch of loads and the issue of few wavefronts, not yet by memory: one token, 4096 x 4096, 4 bits, bfloat16
+// 6.2 us (8.9 MB; a large copy moves them in 1.7), 1000 x 512, k = 256, d = 4, float32 4.4 us.
 #pragma once
 #include <type_traits>
 
@@ -347,7 +349,8 @@ __global__ __launch_bounds__(512) void k_codes_product(const ProductArgs a) {
 // order c ^ (r mod 8).  gridDim.z workgroups share the columns; every one of them reads all tokens' activations of its columns, so that a
 // compute unit reads its share of X instead of all of it (64 tokens of 4096 columns are 512 KB).
 // Rows of X begin at multiples of 16 bytes and go on to a multiple of 128 columns, with zeros behind the layer's last.
-// What bounds it is the issue of instructions by G wavefronts a SIMD, so offsets inside a workgroup's rows and tokens are 32 bits
+// 61 tokens, 4096 x 4096, 3 bits, groups of 64, bfloat16: 14.6 us and 3.9 for the joining of four parts; 4 bits in groups of 128, 64 tokens: 13 in
+// all.  A workgroup has eight steps here: it is bound by the issue of instructions by G wavefronts a SIMD, so offsets inside a workgroup's rows and tokens are 32 bits
 // (16 rows of 4,000,000 codes of 8 bits are 2^29 bits, 64 tokens of as many float columns 2^30 bytes).
 template <typename T, int NT>
 struct TileOfTokens {

@@ -3,7 +3,7 @@
 //   loss = sum p (log p - log q),  lse = log sum exp(z / tau),  dz = weight / tau (q - p)   (zeros where a row has no entry)
 // Bound by memory: the row is read once and its gradient written once.  A row stays in the registers of its workgroup between
 // the two (TH threads, NV pieces of 16 bytes each: rows up to 128 KB); with few rows several workgroups share one, a first launch
-// leaving each part's maximum and sum.  Sums are float32 over at most some hundred terms a lane, exponents are
+// leaving each part's maximum and sum (5 rows of 50001 float32 logits: 3.8 and 7.2 us).  Sums are float32 over at most some hundred terms a lane, exponents are
 // taken of differences to the maximum, so that rows of the type's lowest value come out even and -inf as nothing.
 #include <type_traits>
 
@@ -161,7 +161,7 @@ __device__ __forceinline__ void correct(const DistillArgs& a, int64_t row, List 
 // One workgroup to a row (TH > 64) or one wavefront, the row in registers.  Longer rows (up to any length) keep their first NV TH pieces
 // there; the rest is read a second time for the gradient, from the last-level cache.  So two workgroups fit a compute unit, and one's
 // memory traffic covers the other's exponentials: 2048 rows of 128000 bfloat16 logits, all of a row in the registers of the one workgroup
-// that then fits, took 278 us.
+// that then fits, took 278 us; it is 250 now, where the logits read once and the gradient written once take 201 at the rate of a copy.
 template <typename T, int TH, int NV, bool LONG>
 __global__ __launch_bounds__(TH, TH == 512 ? 4 : 1) void k_distill_row(const DistillArgs a) {
     constexpr int PER = Elem<T>::PER16;
