@@ -21,7 +21,7 @@ DenseFn codes_dense_kernel(int dtype, int IB, int W, bool columns, bool aligned)
 struct TileShape {
     int bm, bn, threads;
     size_t lds;
-    void (*fn)(const TileArgs);
+    void (*fn)(const TileJobs);
     int resident;  // workgroups that the device holds at once
     float us;      // of a step of all of them
 };

@@ -230,43 +230,70 @@ struct TilePlan {
     float us;  // expected
 };
 
-// The shape and the number of parts of the sum with the least time by the shapes' measured steps: rounds of workgroups, and, where
-// the sum is taken in parts, the float32 parts that go to memory and come back (4 TB/s) and the launch that joins them.
+int64_t tiles_of(const TileShape& t, int64_t M, int64_t N) { return ((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn); }
+
+// Float32 parts that go to memory and come back (4 TB/s), and the launch that joins them.
+float join_us(int64_t M, int64_t N, int parts) { return parts > 1 ? 3.5f + 2e-6f * (float)M * (float)N * (float)parts : 0.f; }
+
+// A shape with the number of parts of the sum with the least time by its measured step: rounds of workgroups, and the joining of the parts.
+TilePlan shape_plan(int which, const TileShape& t, int64_t M, int64_t N, int64_t steps) {
+    TilePlan best{which, 1, 0.f};
+    const int64_t tiles = tiles_of(t, M, N);
+    for (int parts = 1; parts <= 16 && (parts == 1 || steps / parts >= 2); ++parts) {
+        // two workgroups share a compute unit's matrix cores, one alone does not use all of them
+        float rounds = (float)((tiles * parts + 255) / 256) * 256.f / (float)t.resident;
+        if (rounds < 0.7f) rounds = 0.7f;
+        const float us = rounds * t.us * (float)((steps + parts - 1) / parts) + join_us(M, N, parts);
+        if (best.us == 0.f || us < best.us) best = TilePlan{which, parts, us};
+    }
+    return best;
+}
+
+// .. and the shape with the least time.
 TilePlan tile_plan(int64_t M, int64_t N, int64_t steps, int dtype) {
     TilePlan best{0, 1, 0.f};
     for (int s = 0;; ++s) {
         const TileShape t = tile_shape(dtype, s);
         if (!t.fn) return best;
-        const int64_t tiles = ((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn);
-        for (int parts = 1; parts <= 16 && (parts == 1 || steps / parts >= 2); ++parts) {
-            // two workgroups share a compute unit's matrix cores, one alone does not use all of them
-            float rounds = (float)((tiles * parts + 255) / 256) * 256.f / (float)t.resident;
-            if (rounds < 0.7f) rounds = 0.7f;
-            float us = rounds * t.us * (float)((steps + parts - 1) / parts);
-            if (parts > 1) us += 3.5f + 2e-6f * (float)M * (float)N * (float)parts;
-            if (best.us == 0.f || us < best.us) best = TilePlan{s, parts, us};
-        }
+        const TilePlan p = shape_plan(s, t, M, N, steps);
+        if (best.us == 0.f || p.us < best.us) best = p;
     }
 }
 
-void run_tile(int dtype, const TilePlan& p, const TileArgs& args, hipStream_t s) {
+unsigned set_tiles(const TileShape& t, int parts, TileArgs* a) {
+    a->tiles_m = (int)((a->M + t.bm - 1) / t.bm);
+    a->tiles_n = (int)((a->N + t.bn - 1) / t.bn);
+    a->parts = parts;
+    return (unsigned)(a->tiles_m * a->tiles_n) * (unsigned)parts;
+}
+
+// One product, or (second != nullptr, of the same shape) two in one launch.
+void run_tiles(int dtype, const TilePlan& p, const TileArgs& args, hipStream_t s, const TilePlan* p2 = nullptr, const TileArgs* second = nullptr) {
     const TileShape t = tile_shape(dtype, p.which);
-    TileArgs a = args;
-    a.tiles_m = (int)((a.M + t.bm - 1) / t.bm);
-    a.tiles_n = (int)((a.N + t.bn - 1) / t.bn);
+    TileJobs jobs{};
+    jobs.job[0] = args;
+    jobs.first = set_tiles(t, p.parts, &jobs.job[0]);
+    unsigned grid = jobs.first;
+    if (second) {
+        jobs.job[1] = *second;
+        grid += set_tiles(t, p2->parts, &jobs.job[1]);
+    }
     allow_lds(reinterpret_cast<const void*>(t.fn), t.lds);
-    hipLaunchKernelGGL(t.fn, dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)p.parts), dim3((unsigned)t.threads), t.lds, s, a);
+    hipLaunchKernelGGL(t.fn, dim3(grid), dim3((unsigned)t.threads), t.lds, s, jobs);
 }
 
 // Bytes of a buffer in the workspace.
 int64_t buffer(int64_t elements, int esize) { return up_to(elements * esize, 256); }
 
 // out[M, N] in T (rows ldo apart): in one part, or in several that are joined.
+void set_out(const TilePlan& p, TileArgs* a, void* out, int64_t ldo, float* parts) {
+    a->wide = p.parts > 1;
+    a->out = a->wide ? (void*)parts : out;
+    a->ldo = a->wide ? a->N : ldo;
+}
 void run_product(int dtype, const TilePlan& p, TileArgs a, void* out, int64_t ldo, float* parts, hipStream_t s) {
-    a.wide = p.parts > 1;
-    a.out = a.wide ? (void*)parts : out;
-    a.ldo = a.wide ? a.N : ldo;
-    run_tile(dtype, p, a, s);
+    set_out(p, &a, out, ldo, parts);
+    run_tiles(dtype, p, a, s);
     if (p.parts > 1) launch_join_parts(dtype, parts, p.parts, a.M, a.N, out, ldo, s);
 }
 
@@ -302,13 +329,13 @@ struct ProductLayout {
     TilePlan plan;
 };
 
-// lines: the layer's rows (product) or columns (dX); sum: the other side.
-ProductLayout product_layout(int dtype, int64_t n, int64_t lines, int64_t sum) {
+// lines: the layer's rows (product) or columns (dX); sum: the other side.  plan: null for the best one.
+ProductLayout product_layout(int dtype, int64_t n, int64_t lines, int64_t sum, const TilePlan* plan = nullptr) {
     const int es = esize_of(dtype);
     ProductLayout l;
     l.pad = up_to(sum, TP_STEP / es);
     l.panel = panel_of(lines, l.pad);
-    l.plan = tile_plan(n, l.panel, l.pad * es / TP_STEP, dtype);
+    l.plan = plan ? *plan : tile_plan(n, l.panel, l.pad * es / TP_STEP, dtype);
     l.operand = 0;
     l.matrix = buffer(n * l.pad, es);
     l.parts = l.matrix + buffer(l.panel * l.pad, es);
@@ -348,14 +375,14 @@ struct LayerGradLayout {
     int group, groups, lanes, run, waves, codes, grid;
 };
 
-LayerGradLayout layer_grad_layout(const idkm_codes_desc& w, int64_t n) {
+LayerGradLayout layer_grad_layout(const idkm_codes_desc& w, int64_t n, const TilePlan* plan = nullptr) {
     const int es = esize_of(w.dtype), bits = idkm_code_bits(w.k);
     LayerGradLayout l{};
     l.pad = up_to(n, TP_STEP / es);
     l.ldp = up_to(w.cols, 8);
     l.panel = panel_of(w.rows, l.ldp);
     l.panels = (w.rows + l.panel - 1) / l.panel;
-    l.plan = tile_plan(l.panel, w.cols, l.pad * es / TP_STEP, w.dtype);
+    l.plan = plan ? *plan : tile_plan(l.panel, w.cols, l.pad * es / TP_STEP, w.dtype);
     l.group = w.S ? (int)(w.group < w.cols ? w.group : w.cols) : 0;
     l.runs = bits <= 8 && (w.d == 1 || w.d == 2 || w.d == 4 || w.d == 8) && w.rows * w.cols / w.d * bits > 96;
     l.wide = l.runs && w.k * w.d > 256;  // bins of all components for every lane: 64 KB a wavefront at most
@@ -395,6 +422,56 @@ LayerGradLayout layer_grad_layout(const idkm_codes_desc& w, int64_t n) {
     l.segments = l.bins + buffer(l.panels * l.grid * w.k * w.d, 4);
     l.bytes = l.segments + (l.segmented ? buffer(w.rows * ((w.cols + 31) / 32), 4) : 0);
     return l;
+}
+
+// Both products of a backward pass: each in launches of its own, or in one launch, where the layer is one panel of either.
+struct GradLayout {
+    ProductLayout d;
+    LayerGradLayout l;
+    bool together;
+    int64_t bytes;
+};
+
+// The same for any of the gradients: their bits do not depend on which others are wanted.
+GradLayout grad_layout(const idkm_codes_desc& w, int64_t n) {
+    GradLayout g;
+    g.d = product_layout(w.dtype, n, w.cols, w.rows);
+    g.l = layer_grad_layout(w, n);
+    g.together = false;
+    g.bytes = g.d.bytes + g.l.bytes;
+    if (g.d.panel < w.cols || g.l.panels > 1) return g;
+    // In one launch there is one rest of workgroups that do not fill the device instead of two, and one launch less.  Longer sums go
+    // first, so that on average half a workgroup of the shorter ones is what the last compute unit is behind.  Float32, 1001 tokens, 512 x
+    // 4608: 114 us apart; see below.
+    const int64_t steps_d = g.d.pad * esize_of(w.dtype) / TP_STEP, steps_l = g.l.pad * esize_of(w.dtype) / TP_STEP;
+    float least = g.d.plan.us + g.l.plan.us + 3.f;
+    TilePlan best_d{}, best_l{};
+    for (int s = 0;; ++s) {
+        const TileShape t = tile_shape(w.dtype, s);
+        if (!t.fn) break;
+        const TilePlan d = shape_plan(s, t, n, w.cols, steps_d), l = shape_plan(s, t, w.rows, w.cols, steps_l);
+        const float count_d = (float)(tiles_of(t, n, w.cols) * d.parts), count_l = (float)(tiles_of(t, w.rows, w.cols) * l.parts);
+        const float each_d = (float)((steps_d + d.parts - 1) / d.parts), each_l = (float)((steps_l + l.parts - 1) / l.parts);
+        const float longer = each_d > each_l ? each_d : each_l, shorter = each_d > each_l ? each_l : each_d;
+        const float alone = count_d + count_l <= 256.f && t.resident > 256 ? 0.7f : 1.f;
+        // a workgroup begins and ends in some 0.8 us, which tells where a large P has few steps
+        const float ends = 0.8f / t.us;
+        float us = (count_d * (each_d + ends) + count_l * (each_l + ends)) / (float)t.resident + 0.5f * shorter;
+        if (us < alone * longer) us = alone * longer;
+        us = us * t.us + join_us(n, w.cols, d.parts) + join_us(w.rows, w.cols, l.parts);
+        if (us < least) {
+            least = us;
+            best_d = d;
+            best_l = l;
+            g.together = true;
+        }
+    }
+    if (g.together) {
+        g.d = product_layout(w.dtype, n, w.cols, w.rows, &best_d);
+        g.l = layer_grad_layout(w, n, &best_l);
+        g.bytes = g.d.bytes + g.l.bytes;
+    }
+    return g;
 }
 
 const char* wrong_workspace(const void* ws, int64_t have, int64_t need) {
@@ -509,7 +586,7 @@ int64_t idkm_codes_linear_backward_workspace(const idkm_codes_desc* w, int64_t n
     idkm_status st;
     if (wrong_layer(w, &st) || n < 0 || n > MAX_SIDE) return -1;
     if (n == 0) return 0;
-    return product_layout(w->dtype, n, w->cols, w->rows).bytes + layer_grad_layout(*w, n).bytes;
+    return grad_layout(*w, n).bytes;
 }
 
 idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, const void* X, int64_t ldx, const void* dY, int64_t lddy,
@@ -536,12 +613,13 @@ idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, 
         if (dX && lddx < w->cols) return refuse(ctx, IDKM_ERR_INVALID_ARG, "lddx must be >= cols");
         if (!aligned_to(dY, es) || !aligned_to(X, es) || !aligned_to(dX, es))
             return refuse(ctx, IDKM_ERR_INVALID_ARG, "X, dY and dX must be aligned to their type");
-        const int64_t need = idkm_codes_linear_backward_workspace(w, n);
-        if (const char* e = wrong_workspace(workspace, workspace_bytes, need)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
+        const GradLayout g = grad_layout(*w, n);
+        const bool together = g.together && dX && layer;
+        if (const char* e = wrong_workspace(workspace, workspace_bytes, g.bytes)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
         unsigned char* ws = static_cast<unsigned char*>(workspace);
         return launched(ctx, [&] {
-            const ProductLayout d = product_layout(w->dtype, n, w->cols, w->rows);
-            const LayerGradLayout l = layer_grad_layout(*w, n);
+            const ProductLayout& d = g.d;
+            const LayerGradLayout& l = g.l;
             TileArgs td{};
             OperandArgs copies{};
             if (dX) operand_of(w->dtype, dY, lddy, n, w->rows, d, ws, &td, &copies);
@@ -561,7 +639,9 @@ idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, 
                     a.out = of_x + d.matrix;
                     launch_dense_cols(w->dtype, a, s);
                     td.N = a.count;
-                    run_product(w->dtype, d.plan, td, static_cast<unsigned char*>(dX) + c * es, lddx, reinterpret_cast<float*>(of_x + d.parts), s);
+                    float* parts = reinterpret_cast<float*>(of_x + d.parts);
+                    if (together) set_out(d.plan, &td, dX, lddx, parts);
+                    else run_product(w->dtype, d.plan, td, static_cast<unsigned char*>(dX) + c * es, lddx, parts, s);
                 }
             }
             if (!layer) return;
@@ -580,7 +660,16 @@ idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, 
                 t.wide = 1;
                 t.out = ws + l.p;
                 t.ldo = l.ldp;
-                run_tile(w->dtype, l.plan, t, s);
+                if (!together) {
+                    run_tiles(w->dtype, l.plan, t, s);
+                } else {
+                    if ((td.steps + d.plan.parts - 1) / d.plan.parts > (t.steps + l.plan.parts - 1) / l.plan.parts)
+                        run_tiles(w->dtype, d.plan, td, s, &l.plan, &t);
+                    else
+                        run_tiles(w->dtype, l.plan, t, s, &d.plan, &td);
+                    if (d.plan.parts > 1)
+                        launch_join_parts(w->dtype, reinterpret_cast<const float*>(of_x + d.parts), d.plan.parts, n, w->cols, dX, lddx, s);
+                }
                 if (l.plan.parts > 1)
                     launch_join_parts(IDKM_F32, reinterpret_cast<const float*>(ws + l.p), l.plan.parts, count, l.ldp, ws + l.p, l.ldp, s);
                 BinArgs b{};

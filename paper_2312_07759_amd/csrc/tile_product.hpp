@@ -21,14 +21,20 @@ struct TileArgs {
     int steps;         // steps of 128 bytes along the sum
     void* out;         // T [M, ldo], or float when `wide`
     int64_t ldo;
-    int wide;          // 1: float32 sums; the z-th of gridDim.y parts of the sum goes to out + z M ldo
-    int tiles_m, tiles_n;
+    int wide;          // 1: float32 sums; the z-th of `parts` parts of the sum goes to out + z M ldo
+    int tiles_m, tiles_n, parts;
+};
+
+// One product, or two that do not depend on each other in one launch: the workgroups of the first come first.
+struct TileJobs {
+    TileArgs job[2];
+    unsigned first;  // workgroups of job[0]
 };
 
 constexpr int TP_STEP = 128;  // bytes
 
 template <typename T, int BM, int BN, int WM, int WN, int ST>
-__global__ __launch_bounds__(64 * WM* WN) void k_tile_product(const TileArgs a) {
+__global__ __launch_bounds__(64 * WM* WN) void k_tile_product(const TileJobs jobs) {
     constexpr int NW = WM * WN;
     constexpr int PIECES = (BM + BN) / 8;      // 8 rows of 128 bytes: what a wavefront copies at once
     constexpr int PPW = PIECES / NW;
@@ -39,18 +45,21 @@ __global__ __launch_bounds__(64 * WM* WN) void k_tile_product(const TileArgs a) 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Workgroups go to the eight dies in turn: a die gets a run of neighbouring tiles, which share rows of A and B in its
     // cache.  Inside a run tiles go down strips of eight rows of tiles.
+    const int of = blockIdx.x < jobs.first ? 0 : 1;
+    const TileArgs& a = jobs.job[of];
     const int total = a.tiles_m * a.tiles_n;
-    int t = blockIdx.x;
+    int t = blockIdx.x - (of ? jobs.first : 0u);
+    const int parts = a.parts, z = __builtin_amdgcn_readfirstlane(t / total);
+    t -= z * total;
     {
         const int die = t & 7, at = t >> 3, whole = total >> 3, rest = total & 7;
         t = die * whole + (die < rest ? die : rest) + at;
     }
-    const int strip = 8 * a.tiles_n, s0 = t / strip, in = t - s0 * strip;
+    const int strip = 8 * a.tiles_n, s0 = __builtin_amdgcn_readfirstlane(t / strip), in = t - s0 * strip;
     const int high = min(8, a.tiles_m - s0 * 8);
-    const int tm = s0 * 8 + in % high, tn = in / high;
+    const int tn = __builtin_amdgcn_readfirstlane(in / high), tm = s0 * 8 + in - tn * high;
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     // this workgroup's part of the sum
-    const int parts = gridDim.y, z = blockIdx.y;
     const int each = (a.steps + parts - 1) / parts;
     const int first = min(a.steps, z * each), last = min(a.steps, first + each);
 
