@@ -220,12 +220,26 @@ __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {
     }
     if (!a.bins) return;
     __syncthreads();
-    for (int e = wave; e < kd; e += nw) {
+    // A component's 64 bins of every wavefront go to `split` lanes, as many as there are for each: with a wavefront to one component, seven
+    // exchanges for each, 200 components took some 30 us.  Lanes begin at different banks.
+    int split = 64;
+    while (split > 1 && split * kd > (int)blockDim.x) split >>= 1;
+    const int part = threadIdx.x & (split - 1), n = 64 / split;
+    for (int e0 = 0; e0 < kd; e0 += blockDim.x / split) {
+        const int e = e0 + threadIdx.x / split;
         double sum = 0.0;
-        for (int w = 0; w < nw; ++w) sum += (double)bin_lds[(w * kd + e) * 64 + lane];
+        for (int w = 0; w < nw && e < kd; ++w) {
+            const float* of = bin_lds + (w * kd + e) * 64;
+            for (int i = 0; i < n; i += 8) {
+                float v[8];
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-        if (lane == 0) a.bins[e * a.pitch + a.at + blockIdx.x] = (float)sum;
+                for (int u = 0; u < 8; ++u) v[u] = of[((i + u) * split + part + e * split) & 63];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) sum += i + u < n ? (double)v[u] : 0.0;
+            }
+        }
+        for (int o = split / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+        if (e < kd && part == 0) a.bins[e * a.pitch + a.at + blockIdx.x] = (float)sum;
     }
 }
 
