@@ -296,25 +296,46 @@ __global__ __launch_bounds__(256) void k_codes_bins_wide(const BinArgs a) {
             ++rn;
         }
         if (rn < a.count) ask(next, rn, sn);
+        uint32_t code[STEPS];
+        float w[STEPS];
 #pragma unroll
         for (int u = 0; u < STEPS; ++u) {
-            const int c = strip * 512 + u * 64 + lane;
-            const uint32_t code = (uint32_t)(((uint64_t)now.hi[u] << 32 | now.lo[u]) >> now.sh[u]) & mask;
-            const bool none = code >= (uint32_t)a.k, counts = c < a.cols;
-            const float v = counts && !none ? now.s[u] * now.p[u] : 0.f;
-            if (a.bins) {
+            code[u] = (uint32_t)(((uint64_t)now.hi[u] << 32 | now.lo[u]) >> now.sh[u]) & mask;
+            if (a.segments) w[u] = Elem<T>::up(C[code[u] < (uint32_t)a.k ? code[u] * D : 0]);
+        }
+        if (a.bins) {
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                const bool none = code[u] >= (uint32_t)a.k, counts = strip * 512 + u * 64 + lane < a.cols;
+                const float v = counts && !none ? now.s[u] * now.p[u] : 0.f;
 #pragma unroll
                 for (int t = 0; t < SHARE; ++t) {
-                    if (turn == t) mine[(none ? 0 : code) * WIDTH] += v;
+                    if (turn == t) mine[(none ? 0 : code[u]) * WIDTH] += v;
                     asm volatile("" ::: "memory");  // one turn after another
                 }
             }
-            if (a.segments) {
-                float sum = counts ? now.p[u] * (none ? __builtin_nanf("") : Elem<T>::up(C[none ? 0 : code * D])) : 0.f;
+        }
+        if (a.segments) {
+            // Sums over 32 lanes of eight steps: lanes exchange the half of their values that the other one goes on with, so that a lane
+            // ends with one step's sum after nine exchanges instead of forty.
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-                if ((lane & 31) == 0 && counts) a.segments[(a.first + rr) * segments + (c >> 5)] = sum;
+            for (int u = 0; u < STEPS; ++u) {
+                const bool counts = strip * 512 + u * 64 + lane < a.cols;
+                w[u] = counts ? now.p[u] * (code[u] < (uint32_t)a.k ? w[u] : __builtin_nanf("")) : 0.f;
             }
+#pragma unroll
+            for (int o = 16, half = 4; half > 0; o >>= 1, half >>= 1) {
+                const bool upper = lane & o;
+#pragma unroll
+                for (int i = 0; i < half; ++i) {
+                    const float send = upper ? w[i] : w[i + half], keep = upper ? w[i + half] : w[i];
+                    w[i] = keep + __shfl_xor(send, o);
+                }
+            }
+            w[0] += __shfl_xor(w[0], 2);
+            w[0] += __shfl_xor(w[0], 1);
+            const int u = (lane >> 4 & 1) * 4 + (lane >> 3 & 1) * 2 + (lane >> 2 & 1), c = strip * 512 + u * 64 + (lane & 32);
+            if ((lane & 3) == 0 && c < a.cols) a.segments[(a.first + rr) * segments + (c >> 5)] = w[0];
         }
         now = next;
         rr = rn;
