@@ -446,14 +446,14 @@ class Context:
         ldx = _rows(X, layer.dtype, layer.cols, dev, "X")
         n = X.shape[0]
         if out is None:
-            out = X.new_empty((n, layer.rows))
+            out = X.new_empty(n, layer.rows)
             ldy = layer.rows
         else:
             ldy = _rows(out, layer.dtype, layer.rows, dev, "out")
             if out.shape[0] != n:
                 raise TypeError(f"out must have {n} rows")
         need = layer.workspace_bytes(n)
-        ws = X.new_empty((need,), dtype=_t().uint8) if need > 0 else None
+        ws = X.new_empty(need, dtype=_t().uint8) if need > 0 else None
         st = self._lib.idkm_codes_linear(self._h, layer._at, X.data_ptr(), n, ldx, out.data_ptr(), ldy,
                                          ws.data_ptr() if need > 0 else None, need, self._raw_stream())
         if st:
@@ -478,13 +478,13 @@ class Context:
             raise TypeError("X is needed for dC and dS")
         res = {}
         if want_dX:
-            res["dX"] = dY.new_empty((n, layer.cols))
+            res["dX"] = dY.new_empty(n, layer.cols)
         if want_dC:
-            res["dC"] = dY.new_empty((layer.k, layer.d), dtype=torch.float32)
+            res["dC"] = dY.new_empty(layer.k, layer.d, dtype=torch.float32)
         if want_dS:
-            res["dS"] = dY.new_empty((layer.rows, layer.groups), dtype=torch.float32)
+            res["dS"] = dY.new_empty(layer.rows, layer.groups, dtype=torch.float32)
         need = layer.workspace_bytes(n, True)
-        ws = dY.new_empty((need,), dtype=torch.uint8) if need > 0 else None
+        ws = dY.new_empty(need, dtype=torch.uint8) if need > 0 else None
         at = {key: t.data_ptr() for key, t in res.items()}
         self._check(self._lib.idkm_codes_linear_backward(
             self._h, layer._at, X.data_ptr() if X is not None else None, ldx, dY.data_ptr(), ldy, n, at.get("dX"), layer.cols,
@@ -502,7 +502,7 @@ class Context:
     def group_scale(self, W, group):
         """idkm_group_scale: W [rows, cols] float32 -> (S [rows, ceil(cols / group)], Z = W / S)."""
         w, rows, cols, scales = self._grouped(W, group, "W")
-        S, Z = W.new_empty(scales), _t().empty_like(W)
+        S, Z = W.new_empty(*scales), _t().empty_like(W)
         st = self._lib.idkm_group_scale(self._h, w, rows, cols, group, S.data_ptr(), Z.data_ptr(), self._raw_stream())
         if st:
             self._check(st)
@@ -556,13 +556,13 @@ class Context:
         t = _flat(teacher, torch.float32, (n, top), dev, "teacher")
         i = _flat(index, torch.int32, (n, top), dev, "index")
         w = _flat(weight, torch.float32, (n,), dev, "weight") if weight is not None else None
-        loss, lse = teacher.new_empty((n,)), teacher.new_empty((n,))
+        loss, lse = teacher.new_empty(n), teacher.new_empty(n)
         ldd = V
         if weight is None:
             if out is not None:
                 raise TypeError("the gradient needs weights")
         elif out is None:
-            out = logits.new_empty((n, V))
+            out = torch.empty_like(logits) if ldz == V else logits.new_empty(n, V)
         else:
             ldd = _rows(out, logits.dtype, V, dev, "out")
             if out.shape[0] != n:
@@ -573,7 +573,7 @@ class Context:
             if len(self._distill_bytes) > 4096:
                 self._distill_bytes.clear()
             need = self._distill_bytes[key] = self._lib.idkm_distill_workspace(n, V, top, code)
-        ws = logits.new_empty((need,), dtype=torch.uint8) if need > 0 else None
+        ws = logits.new_empty(need, dtype=torch.uint8) if need > 0 else None
         st = self._lib.idkm_distill(self._h, logits.data_ptr(), n, V, ldz, code, i, t, top, tau, w, loss.data_ptr(), lse.data_ptr(),
                                     out.data_ptr() if out is not None else None, ldd, ws.data_ptr() if need > 0 else None, need,
                                     self._raw_stream())
