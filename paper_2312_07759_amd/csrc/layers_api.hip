@@ -441,8 +441,9 @@ GradLayout grad_layout(const idkm_codes_desc& w, int64_t n) {
     g.bytes = g.d.bytes + g.l.bytes;
     if (g.d.panel < w.cols || g.l.panels > 1) return g;
     // In one launch there is one rest of workgroups that do not fill the device instead of two, and one launch less.  Longer sums go
-    // first, so that on average half a workgroup of the shorter ones is what the last compute unit is behind.  Float32, 1001 tokens, 512 x
-    // 4608: 114 us apart; see below.
+    // first, so that on average half a workgroup of the shorter ones is what the last compute unit is behind.  Whole calls, apart and together:
+    // 512 x 4608 float32, 1001 tokens 144 and 122 us; 1024 x 1024, 1001 tokens 73 and 66, in bfloat16 36 and 32; 64 x 576 bfloat16 21 and
+    // 17; 4096 x 4096 bfloat16, 64 tokens 73 and 80, which is left apart.
     const int64_t steps_d = g.d.pad * esize_of(w.dtype) / TP_STEP, steps_l = g.l.pad * esize_of(w.dtype) / TP_STEP;
     float least = g.d.plan.us + g.l.plan.us + 3.f;
     TilePlan best_d{}, best_l{};
@@ -454,9 +455,11 @@ GradLayout grad_layout(const idkm_codes_desc& w, int64_t n) {
         const float each_d = (float)((steps_d + d.parts - 1) / d.parts), each_l = (float)((steps_l + l.parts - 1) / l.parts);
         const float longer = each_d > each_l ? each_d : each_l, shorter = each_d > each_l ? each_l : each_d;
         const float alone = count_d + count_l <= 256.f && t.resident > 256 ? 0.7f : 1.f;
-        // a workgroup begins and ends in some 0.8 us, which tells where a large P has few steps
-        const float ends = 0.8f / t.us;
-        float us = (count_d * (each_d + ends) + count_l * (each_l + ends)) / (float)t.resident + 0.5f * shorter;
+        // A workgroup begins and ends in some 2.4 us, of which two on a compute unit hide a part from each other: that tells where there are few
+        // steps.  Nothing is left over where all are resident at once.
+        const float ends = (t.resident > 256 ? 0.8f : 2.4f) / t.us;
+        float us = (count_d * (each_d + ends) + count_l * (each_l + ends)) / (float)t.resident;
+        if (count_d + count_l > (float)t.resident) us += 0.5f * shorter;
         if (us < alone * longer) us = alone * longer;
         us = us * t.us + join_us(n, w.cols, d.parts) + join_us(w.rows, w.cols, l.parts);
         if (us < least) {
