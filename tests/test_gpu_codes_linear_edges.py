@@ -219,3 +219,15 @@ def test_smallest_and_largest_temperatures(ctx):
     loss, lse, dz = ctx.distill(z, index, teacher, 2.0 ** -126, torch.full((3,), 2.0 ** -126, device="cuda"))
     check(loss, torch.full((3,), 50.0, dtype=torch.float64).log(), torch.full((3,), 2e-6, dtype=torch.float64))
     check(dz[:, 1:], torch.full((3, 49), 0.02, dtype=torch.float64), torch.full((3, 49), 1e-8, dtype=torch.float64))
+
+
+@pytest.mark.parametrize("rows,cols,group,n", [(2000, 96, 32, 5), (1500, 200, 64, 70), (96, 1000, 0, 6000), (700, 1100, 1100, 300), (108, 734, 64, 7)])
+@pytest.mark.parametrize("k,d", [(16, 1), (100, 2)])
+def test_gradients_whose_sums_are_long(ctx, rows, cols, group, n, k, d):
+    """dX sums over many rows, the layer's own gradients over many tokens: parts of either, in one launch or in two."""
+    from test_gpu_codes_linear import run_gradient
+    for dtype in (torch.float32, torch.bfloat16):
+        layer = Layer(rows, cols, k, d, group, dtype, seed=8)
+        got = run_gradient(ctx, layer, n)
+        again = ctx.codes_linear_backward(layer.on_gpu(binding), draw((n, cols), dtype, 1).cuda(), draw((n, rows), dtype, 2).cuda(), want_dC=False, want_dS=False)
+        assert list(again) == ["dX"] and torch.equal(again["dX"], got["dX"])
