@@ -246,7 +246,7 @@ __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {
 // The same codes with larger codebooks: a lane has one component, as in the first kernel, and a wavefront takes 512 columns of a row
 // in eight steps of 64; the next 512 are asked for before these are used.  dS goes through `segments` always.
 // SHARE lanes have the same bins and add to them one after another: with bins for every lane, 256 codewords leave room for two wavefronts
-// on a compute unit, which wait for every one of their loads (512 x 4608, k = 256, d = 4: 30 us; 18 with eight wavefronts).
+// on a compute unit, which wait for every one of their loads (512 x 4608, k = 256, d = 4: 30 us; 18 with eight wavefronts, whose turns are then what takes longest).
 template <typename T, int D, int SHARE>
 __global__ __launch_bounds__(256) void k_codes_bins_wide(const BinArgs a) {
     constexpr int STEPS = 8, WIDTH = 64 / SHARE;
