@@ -27,7 +27,7 @@ struct DenseArgs {
 __device__ __forceinline__ int group_of(const DenseArgs& a, int c) {
     const unsigned x = (unsigned)c >> 5;
     unsigned g = __umulhi(2u * x, a.group_magic);
-    if ((uint64_t)g * (unsigned)a.group_32 > x) --g;
+    if (__umul24(g, (unsigned)a.group_32) > x) --g;  // both below 2^17
     return (int)g;
 }
 
@@ -70,15 +70,16 @@ struct EightOfLayer {
     static constexpr int NB = 8 / W * IB;
     CodeRun<NB> run;
     float s;
-    __device__ __forceinline__ void ask(const DenseArgs& a, int64_t r, int c) {
-        const int64_t bit = r * a.row_bits + (unsigned)((c >> a.d_log) * a.bits);
+    // row_bit, row_scale: where row r's codes and scales begin, r row_bits and r groups
+    __device__ __forceinline__ void ask(const DenseArgs& a, int64_t row_bit, int64_t row_scale, int c) {
+        const int64_t bit = row_bit + (unsigned)((c >> a.d_log) * a.bits);
         if (c + 8 <= a.cols) {
             const int64_t base = ALIGNED ? bit >> 5 : min(bit >> 5, a.nwords - CodeRun<NB>::SPAN);
             run.template load_inside<ALIGNED>(a.words + base, 0, (unsigned)(bit - (base << 5)));
         } else {
             run.template load<false, true>(a.words, a.nwords, bit);
         }
-        if (a.S) s = a.S[r * a.groups + group_of(a, c)];
+        if (a.S) s = a.S[row_scale + group_of(a, c)];
     }
     __device__ __forceinline__ void bring(T* out, const DenseArgs& a, int c, const unsigned char* table) const {
         u32x4 raw[8 / Elem<T>::PER16];
@@ -96,50 +97,65 @@ struct EightOfLayer {
     }
 };
 
-// The layer's rows: a thread takes 8 columns at a time, four such pieces asked for together.  Bound by the writes: 4096 x 4096
-// in 16 bits takes 12.5 us (it took 26 with one code read at a time and 15 with one piece); written at the rate of a fill it is 5.
+// The layer's rows: a thread takes 8 columns at a time, four such pieces asked for together, the first before the table is built and the
+// next before these are brought.  4096 x 4096 in 16 bits takes 11.2 us (26 with one code read at a time, 15 with one piece, 12.5 with the pieces asked
+// for when they are needed); bound by issue: some 80 instructions for 8 scaled weights are 5 us, and written at the rate of a fill it is 5.
 template <typename T, int IB, int W, bool ALIGNED>
 __global__ __launch_bounds__(256) void k_dense_rows_fast(const DenseArgs a) {
     constexpr int U = 4;
     extern __shared__ __align__(128) unsigned char lds[];
     const Table<T, IB, W> entries(a.C, a.k, a.bits, a.d);
-    entries.build(lds, a.C, a.k, a.bits, a.d);
     const unsigned char* table = Table<T, IB, W>::own(lds);
-    __syncthreads();
     const int per_row = (int)(a.pad / 8);
+    // a thread's next piece is `step` pieces on: its row, column, codes and scales follow by additions
     const int64_t step = (int64_t)gridDim.x * 256, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t rows_step = step / per_row;
-    const int cols_step = (int)(step - rows_step * per_row);
-    int64_t r = at / per_row;
-    int c = (int)(at - r * per_row);
-    while (r < a.count) {
+    const int rows_step = (int)(step / per_row), cols_step = (int)(step - (int64_t)rows_step * per_row), count = (int)a.count;
+    const int64_t bits_step = rows_step * a.row_bits, scales_step = (int64_t)rows_step * a.groups;
+    int r = (int)min(at / per_row, (int64_t)count);
+    int c = (int)(at - at / per_row * per_row);
+    int64_t row_bit = (a.first + r) * a.row_bits, row_scale = (a.first + r) * a.groups;
+    struct Batch {
         EightOfLayer<T, IB, W, ALIGNED> eight[U];
-        int64_t rows[U];
-        int cols[U];
+        int rows[U], cols[U];
+    };
+    auto ask = [&](Batch& b) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            rows[u] = r;
-            cols[u] = c * 8;
-            if (r < a.count && c * 8 < a.cols) eight[u].ask(a, a.first + r, c * 8);
+            b.rows[u] = r;
+            b.cols[u] = c * 8;
+            if (r < count && c * 8 < a.cols) b.eight[u].ask(a, row_bit, row_scale, c * 8);
             r += rows_step;
+            row_bit += bits_step;
+            row_scale += scales_step;
             c += cols_step;
             if (c >= per_row) {
                 c -= per_row;
                 ++r;
+                row_bit += a.row_bits;
+                row_scale += a.groups;
             }
         }
+    };
+    T* out = static_cast<T*>(a.out) + at * 8;
+    Batch now, next;
+    ask(now);
+    entries.build(lds, a.C, a.k, a.bits, a.d);
+    __syncthreads();
+    for (; now.rows[0] < count; out += U * step * 8) {
+        ask(next);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (rows[u] >= a.count) continue;
+            if (now.rows[u] >= count) continue;
             struct alignas(16) Eight { T v[8]; } w;
-            if (cols[u] < a.cols) {
-                eight[u].bring(w.v, a, cols[u], table);
+            if (now.cols[u] < a.cols) {
+                now.eight[u].bring(w.v, a, now.cols[u], table);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) w.v[e] = (T)0.f;
             }
-            *reinterpret_cast<Eight*>(static_cast<T*>(a.out) + rows[u] * a.pad + cols[u]) = w;
+            *reinterpret_cast<Eight*>(out + u * step * 8) = w;
         }
+        now = next;
     }
 }
 
@@ -149,7 +165,6 @@ template <typename T, int IB, int W, bool ALIGNED>
 __global__ __launch_bounds__(256) void k_dense_cols_fast(const DenseArgs a) {
     extern __shared__ __align__(128) unsigned char lds[];
     const Table<T, IB, W> entries(a.C, a.k, a.bits, a.d);
-    entries.build(lds, a.C, a.k, a.bits, a.d);
     const unsigned char* table = Table<T, IB, W>::own(lds);
     const TransposeTile<T> tile{reinterpret_cast<uint32_t*>(lds + Table<T, IB, W>::BYTES)};
     const int tiles_c = (int)((a.count + 63) / 64), tiles_r = (int)((a.pad + 63) / 64);
@@ -159,10 +174,11 @@ __global__ __launch_bounds__(256) void k_dense_cols_fast(const DenseArgs a) {
         const int tr = t / tiles_c, c0 = (int)a.first + (t - tr * tiles_c) * 64 + lc;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
-            if (tr * 64 + lr + b < a.rows && c0 < a.cols) eight[b].ask(a, tr * 64 + lr + b, c0);
+            if (tr * 64 + lr + b < a.rows && c0 < a.cols) eight[b].ask(a, (tr * 64 + lr + b) * a.row_bits, (int64_t)(tr * 64 + lr + b) * a.groups, c0);
     };
     int t = blockIdx.x;
     if (t < tiles_c * tiles_r) ask(t);
+    entries.build(lds, a.C, a.k, a.bits, a.d);
     for (; t < tiles_c * tiles_r; t += gridDim.x) {
         const int tr = t / tiles_c, tc = t - tr * tiles_c;
         const int c0 = (int)a.first + tc * 64 + lc;
