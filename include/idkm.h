@@ -318,7 +318,8 @@ idkm_status idkm_group_scale_backward(idkm_ctx* ctx, const float* Z, const float
  *   loss_out[t] = sum p (log p - log q),   lse_out[t] = log sum exp(z / tau)
  *   dlogits_out[t,v] = weight[t] / tau (q_v - p_v): the gradient of sum_t weight[t] loss[t]
  * A row without entries, or whose entries are all -inf, has loss 0 and gradient 0, whatever its logits are; an index >= V or a
- * NaN in a row's list makes its loss and gradient NaN.  Logits of -inf have q = 0.
+ * NaN in a row's list makes its loss and gradient NaN.  Logits of -inf have q = 0; a logit of +inf or NaN makes the row's lse NaN, and
+ * its loss and gradient where it has entries.
  *   weight, dlogits_out  device [n] float32 and [n,V] (rows ldd apart), both or neither NULL (neither: loss and lse only).
  *                        dlogits_out may be logits itself, with ldd = ldz; otherwise they do not overlap.
  *   index, teacher       device [n,top] int32 and float32, 1 <= top <= 1024; n < 2^31, V <= 2^29; tau >= 2^-126, finite.

@@ -38,13 +38,14 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return m;
 }
 
-// exp((z - m) / tau) of a row: its exponent to the base 2 is one multiply-add of the logit, z c - k with k = m c rounded; what the
-// rounding puts into one exponential it puts into all of the row's, and their sum.  Where m c could overflow (rows of the type's
-// lowest value) the difference z - m comes first.
+// exp((z - m) / tau) of a row: its exponent to the base 2 is one multiply-add of the logit, z c - k with k = m c rounded.  The
+// rounding, up to |k| 2^-24, is an exponent that all of the row's exponentials and their sum get: a common factor of at most sqrt(2) while
+// |k| <= 2^23, but infinities or nothing from 2^31 on (a row of -1e10, or small temperatures).  Beyond 2^23 the difference z - m
+// comes first, which costs one instruction more for a logit.
 struct Exponent {
     float c, m, k;
     bool difference;
-    __device__ __forceinline__ Exponent(float tau, float m_) : c(LOG2E / tau), m(m_), difference(fabsf(m_) * fmaxf(c, 1.f) > 1e37f) { k = difference ? 0.f : m * c; }
+    __device__ __forceinline__ Exponent(float tau, float m_) : c(LOG2E / tau), m(m_), difference(!(fabsf(m_) * c <= 8388608.f)) { k = difference ? 0.f : m * c; }
     template <bool DIFFERENCE>
     __device__ __forceinline__ float of(float z) const {
         return __builtin_amdgcn_exp2f(fmaf(DIFFERENCE ? z - m : z, c, -k));
