@@ -20,10 +20,11 @@ class _Quantize(torch.autograd.Function):
     def forward(fn, W, C0, layer):
         fn.layer = layer
         Z, d = W.detach(), C0.shape[1]
+        layer.turn += 1
+        fn.turn = layer.turn
         if layer.group:
             S, Z = layer.ctx.group_scale(Z, layer.group)
-            layer.S, layer.turn = S, layer.turn + 1
-            fn.turn = layer.turn
+            layer.S = S
         out = layer.ctx.forward(Z.view(-1, d), C0, layer.tau, layer.tol, layer.max_iter, layer.dist, want_Wq=True)
         layer.last_forward = out["info"]
         layer.C = out["C"]
@@ -37,10 +38,10 @@ class _Quantize(torch.autograd.Function):
     @staticmethod
     def backward(fn, dWq, _dC):
         layer = fn.layer
+        if fn.turn != layer.turn:  # the library's state, W's borrowed address in it, is of that other call
+            raise RuntimeError("the layer has been quantised again since: its backward pass has to come first")
         dWq = dWq.contiguous()
         if layer.group:
-            if fn.turn != layer.turn:  # the library's state, W's borrowed address in it, is of that other call
-                raise RuntimeError("the layer has been quantised again since: its backward pass has to come first")
             Z, S, Zq = fn.scaled
             dWq, dS = layer.ctx.group_unscale_backward(dWq, Zq, S, layer.group)
         res = layer.ctx.backward(dWq.view(-1, layer.C.shape[1]), layer.bwd_mode, tol=layer.bwd_tol, max_iter=layer.bwd_max_iter,
@@ -55,7 +56,8 @@ class _Quantize(torch.autograd.Function):
 class SoftKMeansQuantize:
     """One layer's quantiser.  `layer(W, C0)` returns (Wq, C*) with Wq differentiable with respect to W by implicit
     differentiation of the soft k-means fixed point (bwd_mode: binding.BWD_IMPLICIT, BWD_JFB, BWD_DENSE, BWD_GMRES).
-    C* is returned detached, to warm-start the next step's C0.
+    C* is returned detached, to warm-start the next step's C0.  The state that a backward pass needs is the last call's: the backward pass
+    of a call comes before the next call, or raises.
 
     group > 0: W is [rows, cols] with cols a multiple of d, and every group of `group` consecutive weights of a row is divided by its
     root mean square before the clustering and multiplied by it after it; the gradient goes through the scales too.  The codebook
