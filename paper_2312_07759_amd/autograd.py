@@ -147,10 +147,18 @@ class _CodesProduct(torch.autograd.Function):
         return r.get("dX"), r["dC"].to(C.dtype) if need_C else None, r["dS"].to(S.dtype) if need_S else None, None
 
 
+def _as_rows(t):
+    """A matrix as the kernels take it, its rows contiguous and apart: itself, or a copy (of a transposed or repeated one, say)."""
+    n, width = t.shape
+    if (width > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < width):
+        return t.contiguous()
+    return t
+
+
 class CodesLinear(torch.nn.Module):
-    """Product with a [rows, cols] layer in its stored form (binding.CodesLayer): X [..., cols] -> X w^T [..., rows], in X's type (float32,
-    float16 or bfloat16).  The codes stay; the codebook C (float32) and the scales S are parameters, so that both, and what lies
-    below, can be trained."""
+    """Product with a [rows, cols] layer in its stored form (binding.CodesLayer): X [..., cols] of any strides -> X w^T [..., rows], in X's
+    type (float32, float16 or bfloat16).  The codes stay; the codebook C (float32) and the scales S are parameters, so that both, and
+    what lies below, can be trained."""
 
     def __init__(self, layer):
         super().__init__()
@@ -168,7 +176,7 @@ class CodesLinear(torch.nn.Module):
         if X.shape[-1] != self.cols:
             raise ValueError(f"X must be [..., {self.cols}], got {tuple(X.shape)}")
         _no_capture(X, self.C, self.S)
-        return _CodesProduct.apply(X.reshape(-1, self.cols), self.C, self.S, self).view(*X.shape[:-1], self.rows)
+        return _CodesProduct.apply(_as_rows(X.reshape(-1, self.cols)), self.C, self.S, self).view(*X.shape[:-1], self.rows)
 
 
 class _Distill(torch.autograd.Function):
@@ -187,7 +195,9 @@ class _Distill(torch.autograd.Function):
 
 
 def distill(logits, index, teacher, tau=1.0):
-    """Losses [n] of logits [n, V] against the teacher's largest logits (index int32, teacher float32, both [n, top]; a negative index is no
+    """Losses [n] of logits [n, V] (any strides) against the teacher's largest logits (index int32, teacher float32, both [n, top]; a negative index is no
     entry; see binding.Context.distill), differentiable in the logits."""
     _no_capture(logits)
+    if logits.dim() == 2:
+        logits = _as_rows(logits)
     return _Distill.apply(logits, index, teacher, float(tau))
