@@ -131,10 +131,10 @@ def _no_captured_backward():
 
 class _CodesProduct(torch.autograd.Function):
     @staticmethod
-    def forward(fn, X, C, S, module):
-        fn.layer = module.layer(X.dtype)
-        fn.save_for_backward(X, C, S, module.words)
-        return _context(X.get_device()).codes_linear(fn.layer, X)
+    def forward(fn, X, C, S, layer):
+        fn.layer = layer
+        fn.save_for_backward(X, C, S, layer.words)
+        return _context(X.get_device()).codes_linear(layer, X)
 
     @staticmethod
     @once_differentiable
@@ -167,16 +167,20 @@ class CodesLinear(torch.nn.Module):
         self.C = torch.nn.Parameter(layer.C.detach().to(torch.float32, copy=True))
         self.S = torch.nn.Parameter(layer.S.detach().clone()) if layer.S is not None else None
 
-    def layer(self, dtype):
-        """The stored layer as it is now, with its codebook in `dtype`."""
-        S = None if self.S is None else self.S.detach().float()
-        return binding.CodesLayer(self.words, self.rows, self.cols, self.C.detach().to(dtype).contiguous(), S, self.group)
+    def layer(self, dtype, copy=False):
+        """The stored layer as it is now, with its codebook in `dtype`.  copy: codebook and scales stay as they are now, also where the
+        parameters are written to behind autograd's back (through .data)."""
+        S = None if self.S is None else self.S.detach().to(torch.float32, copy=copy).contiguous()
+        C = self.C.detach().to(dtype, copy=copy).contiguous()
+        return binding.CodesLayer(self.words, self.rows, self.cols, C, S, self.group)
 
     def forward(self, X):
         if X.shape[-1] != self.cols:
             raise ValueError(f"X must be [..., {self.cols}], got {tuple(X.shape)}")
         _no_capture(X, self.C, self.S)
-        return _CodesProduct.apply(_as_rows(X.reshape(-1, self.cols)), self.C, self.S, self).view(*X.shape[:-1], self.rows)
+        tracked = torch.is_grad_enabled() and (X.requires_grad or self.C.requires_grad or (self.S is not None and self.S.requires_grad))
+        layer = self.layer(X.dtype, copy=tracked)
+        return _CodesProduct.apply(_as_rows(X.reshape(-1, self.cols)), self.C, self.S, layer).view(*X.shape[:-1], self.rows)
 
 
 class _Distill(torch.autograd.Function):
