@@ -114,6 +114,8 @@ def _context(device):
     """This thread's context on a device (a context serves one thread at a time, and the backward pass runs on another)."""
     held = _local.__dict__.setdefault("contexts", {})
     if device not in held:
+        if torch.cuda.is_current_stream_capturing():  # a context allocates, which would end the capture
+            raise RuntimeError("a thread's first call on a device cannot be captured: make one before, or a CodesLinear")
         held[device] = binding.Context(device)
     return held[device]
 
@@ -162,6 +164,7 @@ class CodesLinear(torch.nn.Module):
 
     def __init__(self, layer):
         super().__init__()
+        _context(layer.device)
         self.rows, self.cols, self.group = layer.rows, layer.cols, layer.group
         self.register_buffer("words", layer.words)
         self.C = torch.nn.Parameter(layer.C.detach().to(torch.float32, copy=True))
