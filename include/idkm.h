@@ -314,9 +314,11 @@ idkm_status idkm_group_scale_backward(idkm_ctx* ctx, const float* Z, const float
  * Loss of a quantised network against the network it was made from: Kullback-Leibler divergence of the student's softmax from
  * the softmax of the teacher's largest logits, and its gradient.  For each of n rows of logits z (V of them, rows ldz
  * elements apart, type dtype) the teacher's list holds up to `top` pairs (index, value); an entry with a negative index is none.
- *   p = softmax(teacher / tau) over the row's entries (entries of one index add up),  q = softmax(z / tau) over all V
- *   loss_out[t] = sum p (log p - log q),   lse_out[t] = log sum exp(z / tau)
- *   dlogits_out[t,v] = weight[t] / tau (q_v - p_v): the gradient of sum_t weight[t] loss[t]
+ *   p_e = softmax(teacher / tau) over the row's entries e,  q = softmax(z / tau) over all V
+ *   loss_out[t] = sum over e of p_e (log p_e - log q at the entry's index),   lse_out[t] = log sum exp(z / tau)
+ *   dlogits_out[t,v] = weight[t] / tau (q_v - the sum of p_e over the entries of index v): the gradient of sum_t weight[t] loss[t]
+ * An index that a row lists more than once keeps its entries apart in the loss, which is then below the divergence of their sum by a
+ * term that does not depend on the logits (and may be negative); the gradient is that of either.
  * A row without entries, or whose entries are all -inf, has loss 0 and gradient 0, whatever its logits are; an index >= V or a
  * NaN in a row's list makes its loss and gradient NaN.  Logits of -inf have q = 0; a logit of +inf or NaN makes the row's lse NaN, and
  * its loss and gradient where it has entries.

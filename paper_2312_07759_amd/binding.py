@@ -544,8 +544,8 @@ class Context:
 
     def distill(self, logits, index, teacher, tau, weight=None, out=None):
         """idkm_distill: (loss [n], lse [n]) of logits [n, V] against the teacher's list (index int32, teacher float32, both
-        [n, top]; a negative index is no entry), and with weight [n] also the gradient of (weight * loss).sum() in the
-        logits; `out` (which may be the logits themselves) receives it."""
+        [n, top]; a negative index is no entry, entries of one index stay apart in the loss), and with weight [n] also the
+        gradient of (weight * loss).sum() in the logits; `out` (which may be the logits themselves) receives it."""
         torch, dev = _t(), self.device
         code = _dtype(logits, "logits")
         if logits.dim() != 2 or index.dim() != 2:

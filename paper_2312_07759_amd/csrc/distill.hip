@@ -1,6 +1,7 @@
 // Kullback-Leibler loss of a student's logits z [n, V] against the teacher's largest logits (index, value; -1: no entry):
 //   p = softmax(teacher / tau) over the row's entries,  q = softmax(z / tau) over all V,
 //   loss = sum p (log p - log q),  lse = log sum exp(z / tau),  dz = weight / tau (q - p)   (zeros where a row has no entry)
+// Entries of one index stay apart in the loss and add up in the gradient, which does not know how p is divided among them.
 // Bound by memory: the row is read once and its gradient written once.  A row stays in the registers of its workgroup between
 // the two (TH threads, NV pieces of 16 bytes each: rows up to 128 KB); with few rows several workgroups share one, a first launch
 // leaving each part's maximum and sum (5 rows of 50001 float32 logits: 3.8 and 7.2 us).  Sums are float32 over at most some hundred terms a lane, exponents are

@@ -82,3 +82,27 @@ def test_logits_that_are_no_numbers(ctx):  # noqa: F811
         assert bool(lse[:3].isnan().all()) and bool(loss[:2].isnan().all()) and bool(dz[:2].isnan().all())
         assert loss[2] == 0 and not dz[2].any()
         assert bool(lse[3:].isfinite().all()) and bool(loss[3:].isfinite().all()) and bool(dz[3:].isfinite().all())
+
+
+@pytest.mark.parametrize("V", [300, 40_000])
+def test_an_index_listed_twice(ctx, V):  # noqa: F811
+    """Its entries stay apart in the loss: two equal ones at a logit that is all of the softmax give -log 2.  The gradient is that of one
+    entry with their sum, and so is the loss but for the entries' own term, whatever the logits are."""
+    z = torch.full((2, V), -200.0)
+    z[:, 7] = 100.0
+    index = torch.tensor([[7, 7], [7, -1]], dtype=torch.int32)
+    loss, lse, dz = (x.cpu() for x in ctx.distill(z.cuda(), index.cuda(), torch.zeros(2, 2, device="cuda"), 1.0, torch.ones(2, device="cuda")))
+    assert abs(float(loss[0]) + math.log(2)) < 1e-6 and abs(float(loss[1])) < 1e-6
+    assert float((dz[0] - dz[1]).abs().max()) <= 2.0 ** -22          # 1/2 + 1/2 and 1, of an exponential off by two steps at most
+    z, index, teacher, weight = make(4, V, 6, torch.float32, 14, holes=False)
+    twice, merged, both = index.clone(), index.clone(), teacher.clone()
+    twice[:, 1] = index[:, 0]
+    merged[:, 1] = -1
+    both[:, 0] = torch.logsumexp(teacher[:, :2].double(), 1).float()
+    a, b = (ctx.distill(z.cuda(), i.cuda(), t.cuda(), 1.0, weight.cuda()) for i, t in ((twice, teacher), (merged, both)))
+    lp = torch.log_softmax(teacher.double(), 1)
+    own = (lp[:, :2].exp() * lp[:, :2]).sum(1) - torch.logsumexp(lp[:, :2], 1).exp() * torch.logsumexp(lp[:, :2], 1)
+    # logarithms up to 40 in float32, exponents and the merged teacher's rounding of 2^-24 of up to 40
+    rel = 2.0 ** -24 * (32 + 4 * 40)
+    check(a[0], b[0].double().cpu() + own, torch.full((4,), 40 * rel, dtype=torch.float64), "loss")
+    check(a[2], b[2].double().cpu(), 2 * rel * weight.double()[:, None] * torch.ones(V), "dlogits")
