@@ -299,7 +299,7 @@ idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, 
  *   idkm_group_scale_backward    dW = dZ / S + Z / count (dS - sum over the group of dZ Z / S)   (0 in a group of zeros);
  *                                dS NULL: zero
  * The [rows, cols] output may be the call's first [rows, cols] input (dZ in the last one).  Enqueue on hip_stream, do not wait;
- * rows = 0 is a no-op.  rows cols <= 2^36.
+ * rows = 0 is a no-op.  rows cols <= 2^36, cols <= 2^31 - 64.
  */
 idkm_status idkm_group_scale(idkm_ctx* ctx, const float* W, int64_t rows, int64_t cols, int64_t group, float* S_out,
                              float* Z_out, void* hip_stream);

@@ -72,6 +72,7 @@ namespace {
 
 constexpr int64_t MAX_SIDE = 4000000;      // rows, columns, tokens: 64 of them to a workgroup fit one grid dimension
 constexpr int64_t MAX_VOCABULARY = (int64_t)1 << 29;  // offsets in a row are 32 bits of bytes
+constexpr int64_t MAX_SCALED_COLS = INT_MAX - 63;  // a lane's 32-bit place in a row goes up to 64 weights beyond its end
 constexpr int64_t PANEL = (int64_t)1 << 26;  // weights of a layer that are written out at a time
 
 idkm_status refuse(idkm_ctx* ctx, idkm_status s, const char* msg) {
@@ -487,7 +488,7 @@ const char* wrong_workspace(const void* ws, int64_t have, int64_t need) {
 const char* wrong_scale_shape(int64_t rows, int64_t cols, int64_t group) {
     if (rows < 0 || cols < 1) return "need rows >= 0 and cols >= 1";
     if (group < 1) return "group must be >= 1";
-    if (rows > ((int64_t)1 << 36) || cols > INT_MAX || (rows > 0 && cols > ((int64_t)1 << 36) / rows)) return "the matrix is too large";
+    if (rows > ((int64_t)1 << 36) || cols > MAX_SCALED_COLS || (rows > 0 && cols > ((int64_t)1 << 36) / rows)) return "the matrix is too large";
     return nullptr;
 }
 
