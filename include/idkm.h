@@ -251,9 +251,9 @@ idkm_status idkm_unpack_quantize(idkm_ctx* ctx, const uint32_t* words, int64_t m
  *   w[r,c] = S[r, c div group] C[code of sub-vector (r cols + c) div d, c mod d]
  * with S left out where it is NULL.  A code >= k makes its weights NaN, as in idkm_unpack_quantize.
  * Activations, outputs and the codebook are of one type, dtype; scales, dC and dS are float32.  All sums are float32; results
- * are rounded once.  One thing is rounded on the way, with 16-bit types and scales only: the product S C, to the type, as a stored
- * 16-bit weight is, where the layer is written out as a matrix for the matrix cores (dX, and many tokens; idkm_codes_linear does it
- * where that is expected to be faster, and otherwise multiplies sums by S); a float16 product beyond 65504 becomes infinite there, and
+ * are rounded once; a group's scale multiplies the float32 sum over its part of the row.  One thing is rounded on the way, in dX with
+ * 16-bit types and scales: the product S C, to the type, as a stored 16-bit weight is (along dX's sum every weight has another scale,
+ * so none can multiply a sum); a float16 product beyond 65504 becomes infinite there, and
  * one below 2^-14 keeps fewer bits.  Codewords are meant to be finite: an infinite one makes
  * infinities or NaN of the outputs of the rows that use it.
  *

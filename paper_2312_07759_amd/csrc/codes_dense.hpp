@@ -21,6 +21,9 @@ struct DenseArgs {
     int group_32;          // group / 32
     int64_t row_bits;
     int d_log;  // of d in {1, 2, 4, 8}
+    // rows only: the codewords go out as they are, and S transposed to scales_out [groups, scale_pitch], row `first` its first
+    float* scales_out;  // or null
+    int64_t scale_pitch;
 };
 
 // Group of column c: the product with the rounded-up inverse is off by one at most, and then too large.
@@ -63,8 +66,9 @@ struct TransposeTile {
     }
 };
 
-// Eight columns of a row of the layer on their way: asked for, and brought to T.  A scaled weight is rounded once (it is an operand
-// of the matrix instruction: the relative error, eps / 2 at most, is that of a weight stored in T); zeros behind the last column.
+// Eight columns of a row of the layer on their way: asked for, and brought to T.  Where the weights are scaled here (columns, for dX, along
+// whose sum every weight has another scale; and float32) each is rounded once: it is an operand of the matrix instruction, and the
+// relative error, eps / 2 at most, is that of a weight stored in T.  Zeros behind the last column.
 template <typename T, int IB, int W, bool ALIGNED>
 struct EightOfLayer {
     static constexpr int NB = 8 / W * IB;
@@ -81,11 +85,16 @@ struct EightOfLayer {
         }
         if (a.S) s = a.S[row_scale + group_of(a, c)];
     }
+    // in the place of scaling the weights: the thread of a group's first columns writes its scale, of row r
+    __device__ __forceinline__ void put_scale(const DenseArgs& a, int r, int c) const {
+        const int g = group_of(a, c);
+        if (g * a.group == c) a.scales_out[g * a.scale_pitch + r] = s;
+    }
     __device__ __forceinline__ void bring(T* out, const DenseArgs& a, int c, const unsigned char* table) const {
         u32x4 raw[8 / Elem<T>::PER16];
         eight_weights<T, IB, W, NB>(raw, run, 0, table);
         __builtin_memcpy(out, raw, sizeof(raw));
-        if (a.S) {
+        if (a.S && !a.scales_out) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) out[e] = Elem<T>::down(Elem<T>::up(out[e]) * s);
         }
@@ -149,6 +158,7 @@ __global__ __launch_bounds__(256) void k_dense_rows_fast(const DenseArgs a) {
             struct alignas(16) Eight { T v[8]; } w;
             if (now.cols[u] < a.cols) {
                 now.eight[u].bring(w.v, a, now.cols[u], table);
+                if (a.scales_out) now.eight[u].put_scale(a, now.rows[u], now.cols[u]);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) w.v[e] = (T)0.f;
@@ -241,6 +251,7 @@ __global__ __launch_bounds__(256) void k_dense_rows(const DenseArgs a) {
         if (c0 < a.cols) {
             code = code_at(a.words, a.nwords, i0 + j, a.bits);
             if (a.S) s = a.S[r * a.groups + c0 / a.group];  // groups are multiples of 32: eight columns lie in one
+            if (a.scales_out && c0 % a.group == 0) a.scales_out[c0 / a.group * a.scale_pitch + rr] = s;
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -248,7 +259,7 @@ __global__ __launch_bounds__(256) void k_dense_rows(const DenseArgs a) {
                 w.v[e] = (T)0.f;
                 continue;
             }
-            w.v[e] = weight_of<T>(code, x, C, a.k, a.d, s, a.S != nullptr);
+            w.v[e] = weight_of<T>(code, x, C, a.k, a.d, s, a.S != nullptr && !a.scales_out);
             if (++x == a.d) {
                 x = 0;
                 ++j;

@@ -25,8 +25,8 @@ struct TileShape {
     int resident;  // workgroups that the device holds at once
     float us;      // of a step of all of them
 };
-// The shapes of a type's tile product, from 0 on; fn = nullptr behind the last.
-TileShape tile_shape(int dtype, int which);
+// The shapes of a type's tile product, from 0 on; fn = nullptr behind the last.  scaled: SC of k_tile_product, 16-bit types only.
+TileShape tile_shape(int dtype, int which, int scaled);
 
 void launch_dense_rows(int dtype, const DenseArgs& a, hipStream_t s);
 void launch_dense_cols(int dtype, const DenseArgs& a, hipStream_t s);

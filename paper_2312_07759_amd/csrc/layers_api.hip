@@ -229,6 +229,7 @@ int64_t few_bytes(const FewPlan& p, const idkm_codes_desc& w, int64_t n) {
 struct TilePlan {
     int which, parts;
     float us;  // expected
+    int scaled;  // see tile_shape
 };
 
 int64_t tiles_of(const TileShape& t, int64_t M, int64_t N) { return ((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn); }
@@ -237,26 +238,26 @@ int64_t tiles_of(const TileShape& t, int64_t M, int64_t N) { return ((M + t.bm -
 float join_us(int64_t M, int64_t N, int parts) { return parts > 1 ? 3.5f + 2e-6f * (float)M * (float)N * (float)parts : 0.f; }
 
 // A shape with the number of parts of the sum with the least time by its measured step: rounds of workgroups, and the joining of the parts.
-TilePlan shape_plan(int which, const TileShape& t, int64_t M, int64_t N, int64_t steps) {
-    TilePlan best{which, 1, 0.f};
+TilePlan shape_plan(int which, const TileShape& t, int64_t M, int64_t N, int64_t steps, int scaled) {
+    TilePlan best{which, 1, 0.f, scaled};
     const int64_t tiles = tiles_of(t, M, N);
     for (int parts = 1; parts <= 16 && (parts == 1 || steps / parts >= 2); ++parts) {
         // two workgroups share a compute unit's matrix cores, one alone does not use all of them
         float rounds = (float)((tiles * parts + 255) / 256) * 256.f / (float)t.resident;
         if (rounds < 0.7f) rounds = 0.7f;
         const float us = rounds * t.us * (float)((steps + parts - 1) / parts) + join_us(M, N, parts);
-        if (best.us == 0.f || us < best.us) best = TilePlan{which, parts, us};
+        if (best.us == 0.f || us < best.us) best = TilePlan{which, parts, us, scaled};
     }
     return best;
 }
 
 // .. and the shape with the least time.
-TilePlan tile_plan(int64_t M, int64_t N, int64_t steps, int dtype) {
-    TilePlan best{0, 1, 0.f};
+TilePlan tile_plan(int64_t M, int64_t N, int64_t steps, int dtype, int scaled) {
+    TilePlan best{0, 1, 0.f, scaled};
     for (int s = 0;; ++s) {
-        const TileShape t = tile_shape(dtype, s);
+        const TileShape t = tile_shape(dtype, s, scaled);
         if (!t.fn) return best;
-        const TilePlan p = shape_plan(s, t, M, N, steps);
+        const TilePlan p = shape_plan(s, t, M, N, steps, scaled);
         if (best.us == 0.f || p.us < best.us) best = p;
     }
 }
@@ -270,7 +271,7 @@ unsigned set_tiles(const TileShape& t, int parts, TileArgs* a) {
 
 // One product, or (second != nullptr, of the same shape) two in one launch.
 void run_tiles(int dtype, const TilePlan& p, const TileArgs& args, hipStream_t s, const TilePlan* p2 = nullptr, const TileArgs* second = nullptr) {
-    const TileShape t = tile_shape(dtype, p.which);
+    const TileShape t = tile_shape(dtype, p.which, p.scaled);
     TileJobs jobs{};
     jobs.job[0] = args;
     jobs.first = set_tiles(t, p.parts, &jobs.job[0]);
@@ -326,27 +327,41 @@ DenseArgs dense_of(const idkm_codes_desc& w) {
 
 // Layout of the workspace of a product: operand rows brought to whole steps, the layer's panel, parts.
 struct ProductLayout {
-    int64_t pad, panel, operand, matrix, parts, bytes;
+    int64_t pad, panel, operand, matrix, parts, scales, scale_pitch, bytes;
     TilePlan plan;
 };
 
 // lines: the layer's rows (product) or columns (dX); sum: the other side.  plan: null for the best one.
-ProductLayout product_layout(int dtype, int64_t n, int64_t lines, int64_t sum, const TilePlan* plan = nullptr) {
+// scaled: see scaled_of; the scales of a panel's groups are laid out anew.
+ProductLayout product_layout(int dtype, int64_t n, int64_t lines, int64_t sum, const TilePlan* plan = nullptr, int scaled = 0, int groups = 0) {
     const int es = esize_of(dtype);
     ProductLayout l;
     l.pad = up_to(sum, TP_STEP / es);
     l.panel = panel_of(lines, l.pad);
-    l.plan = plan ? *plan : tile_plan(n, l.panel, l.pad * es / TP_STEP, dtype);
+    l.plan = plan ? *plan : tile_plan(n, l.panel, l.pad * es / TP_STEP, dtype, scaled);
     l.operand = 0;
     l.matrix = buffer(n * l.pad, es);
     l.parts = l.matrix + buffer(l.panel * l.pad, es);
-    l.bytes = l.parts + (l.plan.parts > 1 ? buffer(n * l.panel * l.plan.parts, 4) : 0);
+    l.scales = l.parts + (l.plan.parts > 1 ? buffer(n * l.panel * l.plan.parts, 4) : 0);
+    l.scale_pitch = up_to(l.panel, 128);
+    l.bytes = l.scales + (scaled ? buffer(groups * l.scale_pitch, 4) : 0);
     return l;
+}
+
+// Which tile product multiplies by the scales of a layer that is written out for Y: with 16-bit types it is one that takes them beside the
+// codewords, so that S C is not rounded; groups of odd multiples of 32 take the one that looks for a scale every half step.
+int scaled_of(const idkm_codes_desc& w) {
+    if (!w.S || w.dtype == IDKM_F32) return 0;
+    return w.group >= w.cols || w.group % 64 == 0 ? 1 : 2;
+}
+
+ProductLayout written_out(const idkm_codes_desc& w, int64_t n) {
+    return product_layout(w.dtype, n, w.rows, w.cols, nullptr, scaled_of(w), groups_of(w));
 }
 
 // Expected time of a product whose layer is written out: 0.6 (float: 1) us for a million weights, and launches.
 float dense_us(const idkm_codes_desc& w, int64_t n) {
-    const ProductLayout l = product_layout(w.dtype, n, w.rows, w.cols);
+    const ProductLayout l = written_out(w, n);
     return 6.f + (w.dtype == IDKM_F32 ? 1e-6f : 0.6e-6f) * (float)w.rows * (float)l.pad + l.plan.us * (float)((w.rows + l.panel - 1) / l.panel);
 }
 
@@ -383,7 +398,7 @@ LayerGradLayout layer_grad_layout(const idkm_codes_desc& w, int64_t n, const Til
     l.ldp = up_to(w.cols, 8);
     l.panel = panel_of(w.rows, l.ldp);
     l.panels = (w.rows + l.panel - 1) / l.panel;
-    l.plan = plan ? *plan : tile_plan(l.panel, w.cols, l.pad * es / TP_STEP, w.dtype);
+    l.plan = plan ? *plan : tile_plan(l.panel, w.cols, l.pad * es / TP_STEP, w.dtype, 0);
     l.group = w.S ? (int)(w.group < w.cols ? w.group : w.cols) : 0;
     l.runs = bits <= 8 && (w.d == 1 || w.d == 2 || w.d == 4 || w.d == 8) && w.rows * w.cols / w.d * bits > 96;
     l.wide = l.runs && w.k * w.d > 256;  // bins of all components for every lane: 64 KB a wavefront at most
@@ -449,9 +464,9 @@ GradLayout grad_layout(const idkm_codes_desc& w, int64_t n) {
     float least = g.d.plan.us + g.l.plan.us + 3.f;
     TilePlan best_d{}, best_l{};
     for (int s = 0;; ++s) {
-        const TileShape t = tile_shape(w.dtype, s);
+        const TileShape t = tile_shape(w.dtype, s, 0);
         if (!t.fn) break;
-        const TilePlan d = shape_plan(s, t, n, w.cols, steps_d), l = shape_plan(s, t, w.rows, w.cols, steps_l);
+        const TilePlan d = shape_plan(s, t, n, w.cols, steps_d, 0), l = shape_plan(s, t, w.rows, w.cols, steps_l, 0);
         const float count_d = (float)(tiles_of(t, n, w.cols) * d.parts), count_l = (float)(tiles_of(t, w.rows, w.cols) * l.parts);
         const float each_d = (float)((steps_d + d.parts - 1) / d.parts), each_l = (float)((steps_l + l.parts - 1) / l.parts);
         const float longer = each_d > each_l ? each_d : each_l, shorter = each_d > each_l ? each_l : each_d;
@@ -511,7 +526,7 @@ int64_t idkm_codes_linear_workspace(const idkm_codes_desc* w, int64_t n) {
     if (n == 0) return 0;
     const FewPlan few = few_plan(*w, n);
     if (few.fn) return few_bytes(few, *w, n);
-    return product_layout(w->dtype, n, w->rows, w->cols).bytes;
+    return written_out(*w, n).bytes;
 }
 
 idkm_status idkm_codes_linear(idkm_ctx* ctx, const idkm_codes_desc* w, const void* X, int64_t n, int64_t ldx, void* Y, int64_t ldy,
@@ -564,7 +579,7 @@ idkm_status idkm_codes_linear(idkm_ctx* ctx, const idkm_codes_desc* w, const voi
                 if (few.parts > 1) launch_join_parts(w->dtype, a.sums, few.parts, n, w->rows, Y, ldy, s);
             });
         }
-        const ProductLayout l = product_layout(w->dtype, n, w->rows, w->cols);
+        const ProductLayout l = written_out(*w, n);
         if (const char* e = wrong_workspace(workspace, workspace_bytes, l.bytes)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
         unsigned char* ws = static_cast<unsigned char*>(workspace);
         return launched(ctx, [&] {
@@ -572,8 +587,16 @@ idkm_status idkm_codes_linear(idkm_ctx* ctx, const idkm_codes_desc* w, const voi
             OperandArgs copies{};
             operand_of(w->dtype, X, ldx, n, w->cols, l, ws, &t, &copies);
             launch_operands(w->dtype, copies, s);
+            const int unit = l.plan.scaled == 1 ? 64 : 32;
+            t.groups = groups_of(*w);
+            t.group = w->group < w->cols ? w->group / unit : INT_MAX;
+            t.scale_pitch = l.scale_pitch;
+            float* scales = l.plan.scaled ? reinterpret_cast<float*>(ws + l.scales) : nullptr;
+            t.scales = scales;
             for (int64_t r = 0; r < w->rows; r += l.panel) {
                 DenseArgs a = dense_of(*w);
+                a.scales_out = scales;
+                a.scale_pitch = l.scale_pitch;
                 a.first = r;
                 a.count = w->rows - r < l.panel ? w->rows - r : l.panel;
                 a.pad = l.pad;
