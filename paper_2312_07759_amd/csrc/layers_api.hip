@@ -194,9 +194,13 @@ FewPlan few_plan(const idkm_codes_desc& w, int64_t n) {
     p.threads = w.dtype == IDKM_F32 ? TileOfTokens<float, 2>::THREADS : TileOfTokens<bf16, 2>::THREADS;
     p.pad = up_to(w.cols, 128);
     const int64_t steps = p.pad / 128;
-    // Workgroups, one to a compute unit, in rounds: some 2 us and these for every step of 128 columns, by the runs' length (measured,
-    // 4096 x 4096, 2048 tokens); sums in parts cost as in tile_plan.
-    const float step_us = w.dtype == IDKM_F32 ? (L == 32 ? 2.45f : L == 16 ? 2.85f : 3.25f) : (L == 32 ? 0.55f : L == 16 ? 1.0f : 1.22f);
+    // Workgroups, one to a compute unit, in rounds: some 2 us and these for every step of 128 columns, by the runs' length (32, 16, 8) and by the
+    // weights that a lookup gives (1, 2, 4 and more): measured, 4096 x 4096, 512 and 1024 tokens, codebooks of 2 to 256 codewords; sums in
+    // parts cost as in tile_plan.  Both forms, measured, 256 tokens in bfloat16, scales for 32 weights: 43 us from the codes and 38 written out with 16 codewords,
+    // 58 and 38 with 256; for 128 weights 24 and 39, 24 and 35; 512 tokens 43 and 47, 44 and 45.
+    static const float measured[2][3][3] = {{{0.65f, 1.05f, 1.7f}, {0.6f, 1.02f, 1.23f}, {0.55f, 0.85f, 1.23f}},
+                                            {{2.5f, 2.85f, 3.75f}, {2.45f, 2.85f, 3.25f}, {2.4f, 2.65f, 3.25f}}};
+    const float step_us = measured[w.dtype == IDKM_F32][W == 1 ? 0 : W == 2 ? 1 : 2][L == 32 ? 0 : L == 16 ? 1 : 2];
     const int64_t blocks = (w.rows + 63) / 64, tokens = (n + 16 * NT - 1) / (16 * NT);
     float best = 0.f;
     for (int parts = 1; parts <= 16 && (parts == 1 || steps / parts >= 4); ++parts) {
@@ -362,7 +366,7 @@ ProductLayout written_out(const idkm_codes_desc& w, int64_t n) {
 // Expected time of a product whose layer is written out: 0.6 (float: 1) us for a million weights, and launches.
 float dense_us(const idkm_codes_desc& w, int64_t n) {
     const ProductLayout l = written_out(w, n);
-    return 6.f + (w.dtype == IDKM_F32 ? 1e-6f : 0.6e-6f) * (float)w.rows * (float)l.pad + l.plan.us * (float)((w.rows + l.panel - 1) / l.panel);
+    return 8.f + (w.dtype == IDKM_F32 ? 1e-6f : 0.6e-6f) * (float)w.rows * (float)l.pad + l.plan.us * (float)((w.rows + l.panel - 1) / l.panel);
 }
 
 // The operand as the tile product takes it: itself, or a copy with whole steps, which `copies` is to make.
