@@ -108,7 +108,8 @@ struct EightOfLayer {
 
 // The layer's rows: a thread takes 8 columns at a time, four such pieces asked for together, the first before the table is built and the
 // next before these are brought.  4096 x 4096 in 16 bits takes 11.2 us (26 with one code read at a time, 15 with one piece, 12.5 with the pieces asked
-// for when they are needed); bound by issue: some 80 instructions for 8 scaled weights are 5 us, and written at the rate of a fill it is 5.
+// for when they are needed), 12 to 14 with the scales written beside the codewords; bound by issue: some 80 instructions for 8 scaled weights are 5 us, and written at the
+// rate of a fill it is 5.
 template <typename T, int IB, int W, bool ALIGNED>
 __global__ __launch_bounds__(256) void k_dense_rows_fast(const DenseArgs a) {
     constexpr int U = 4;

@@ -121,7 +121,7 @@ __global__ __launch_bounds__(256) void k_codes_bins(const BinArgs a) {
 
 // The same for codes of up to 8 bits, D in {1, 2, 4, 8} and small codebooks: a lane takes 8 consecutive columns at a time and
 // keeps bins for all k D components.  Ten instructions a column instead of some 75, which bound the kernel above (4096 x 4096, k = 16:
-// 127 us; this one 25 to 28, of which P at the rate of a copy is 13).  dS: lanes of a group are added up where they are a power of two of at most 64, otherwise sums of 32 columns go to
+// 127 us; this one 25 to 30, of which P at the rate of a copy is 13).  dS: lanes of a group are added up where they are a power of two of at most 64, otherwise sums of 32 columns go to
 // `segments`, which k_join_gradients adds up.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {

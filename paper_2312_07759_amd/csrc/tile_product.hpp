@@ -7,7 +7,8 @@
 // multiples of 16 bytes.  Rows behind the last one are read from the last one and not stored.
 // 2048 x 4096 x 4096 in bfloat16: 62 us, 1100 TFLOP/s (the library's 61.9); 4096 x 4096 x 2048 with float32 results: 63 (the library's 52.8, with
 // results of 16 bits); 512 x 4608 x 1024 in float32: 57 (the library's 64).  Bound by the matrix cores and, between two steps, by the
-// barrier: a workgroup fills a compute unit, so nothing covers it.
+// barrier: nothing covers it where a workgroup fills a compute unit (16 bits: 256 x 128, 256 x 256 and 128 x 128 with four stages; float: 128 x 128);
+// of the other shapes two fit.
 #pragma once
 #include "elem.hpp"
 
@@ -40,8 +41,8 @@ constexpr int TP_STEP = 128;  // bytes
 
 // SC: 0 no scales; 1 one scale of a row of B for every step (64 elements of 16 bits), 2 one for every half step, which is what one matrix
 // instruction sums.  The instructions of a step, or half step, begin at zero and their float32 sum times the scale is added to the tile's, so
-// that a scaled weight is never rounded to T.  Scales come into LDS with the step that they belong to.  2048 x 4096 x 4096 in bfloat16: 74 to 81 us
-// with SC = 1, 90 with SC = 2, where SC = 0 takes 62 to 66: an addition for every element of the tile and step, beside two matrix instructions for 64.
+// that a scaled weight is never rounded to T.  Scales come into LDS with the step that they belong to.  2048 x 4096 x 4096 in bfloat16: 74 to 87 us
+// with SC = 1, 90 with SC = 2, where SC = 0 takes 62 to 70: an addition for every element of the tile and step, beside two matrix instructions for 64.
 template <typename T, int BM, int BN, int WM, int WN, int ST, int SC>
 __global__ __launch_bounds__(64 * WM * WN, SC > 0 ? 2 : 1) void k_tile_product(const TileJobs jobs) {
     constexpr int NW = WM * WN;
