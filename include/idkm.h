@@ -289,6 +289,34 @@ idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, 
                                        void* workspace, int64_t workspace_bytes, void* hip_stream);
 
 /*
+ * Lookups: rows of an embedding table by token, times a scale alpha (finite), and their gradients.  ids: device, int32 or int64 (id_bytes 4
+ * or 8) [n].  A negative id is no token (padding): its row of Y is zero and it has no part in the gradients.  An id >= rows makes its row of Y
+ * NaN and has no part in the gradients.
+ *   idkm_embedding                 Y[t] = alpha W[id_t] of a float32 table W [rows, cols], contiguous (the quantiser's Wq, say); Y [n, cols] of type
+ *                                  dtype, rows ldy apart
+ *   idkm_embedding_backward        dW[v] = alpha sum of dY[t] over the tokens t with id_t = v, float32 [rows, cols], contiguous; all of it is written
+ *   idkm_codes_embedding           the same of a table in its stored form: Y[t,c] = alpha w[id_t,c] with w as for idkm_codes_linear; nothing is
+ *                                  rounded but Y
+ *   idkm_codes_embedding_backward  with P[v,c] = alpha sum of dY[t,c] over the tokens of v: dS[v,g] = sum over the group's columns of P[v,c]
+ *                                  C[code, c mod d] (all rows are written) and dC[j,i] = the sum of S P over the components i of all sub-vectors
+ *                                  with code j.  dC, dS may each be NULL (not wanted).
+ * Tokens are sorted by row, and a row's sum is taken in the order of the tokens (in parts, in order, where there are many): results repeat.
+ * n = 0 writes zeros to the gradients.  Types, strides, alignment, workspace, limits and enqueueing as for idkm_codes_linear; n <= 4,000,000.
+ */
+idkm_status idkm_embedding(idkm_ctx* ctx, const float* W, int64_t rows, int64_t cols, const void* ids, int32_t id_bytes, int64_t n,
+                           float alpha, void* Y, int64_t ldy, idkm_dtype dtype, void* hip_stream);
+int64_t idkm_embedding_backward_workspace(int64_t rows, int64_t cols, int64_t n);
+idkm_status idkm_embedding_backward(idkm_ctx* ctx, int64_t rows, int64_t cols, const void* ids, int32_t id_bytes, int64_t n, float alpha,
+                                    const void* dY, int64_t lddy, idkm_dtype dtype, float* dW, void* workspace, int64_t workspace_bytes,
+                                    void* hip_stream);
+idkm_status idkm_codes_embedding(idkm_ctx* ctx, const idkm_codes_desc* w, const void* ids, int32_t id_bytes, int64_t n, float alpha, void* Y,
+                                 int64_t ldy, void* hip_stream);
+int64_t idkm_codes_embedding_backward_workspace(const idkm_codes_desc* w, int64_t n);
+idkm_status idkm_codes_embedding_backward(idkm_ctx* ctx, const idkm_codes_desc* w, const void* ids, int32_t id_bytes, int64_t n, float alpha,
+                                          const void* dY, int64_t lddy, float* dC, float* dS, void* workspace, int64_t workspace_bytes,
+                                          void* hip_stream);
+
+/*
  * Scales of groups: a layer whose rows or parts of rows differ in size is divided by the root mean square of each group of
  * `group` consecutive weights of a row (the last one of a row may be shorter) before it is clustered, so that one codebook and one
  * temperature serve all of it, and multiplied by it afterwards.  All tensors float32, contiguous: W, Z, Zq [rows, cols],

@@ -25,7 +25,8 @@ EXPORTS = ["idkm_version", "idkm_limits", "idkm_status_string", "idkm_create", "
            "idkm_set_path", "idkm_set_matrix_cores", "idkm_set_tile_limit", "idkm_set_spin_limit", "idkm_set_kernel_timing", "idkm_last_kernel_ms", "idkm_set_gmres_basis", "idkm_advance_sequence", "idkm_forward", "idkm_backward", "idkm_step_F", "idkm_step_JCT", "idkm_get_cotangents", "idkm_forward_noalloc", "idkm_noalloc_last_error",
            "idkm_calibrate", "idkm_code_bits", "idkm_code_words", "idkm_pack_codes", "idkm_unpack_quantize",
            "idkm_codes_linear_workspace", "idkm_codes_linear", "idkm_codes_linear_backward_workspace",
-           "idkm_codes_linear_backward", "idkm_group_scale", "idkm_group_unscale", "idkm_group_unscale_backward",
+           "idkm_codes_linear_backward", "idkm_embedding", "idkm_embedding_backward_workspace", "idkm_embedding_backward",
+           "idkm_codes_embedding", "idkm_codes_embedding_backward_workspace", "idkm_codes_embedding_backward", "idkm_group_scale", "idkm_group_unscale", "idkm_group_unscale_backward",
            "idkm_group_scale_backward", "idkm_distill_workspace", "idkm_distill",
            "idkm_batch_create", "idkm_batch_destroy", "idkm_batch_last_error", "idkm_batch_launches",
            "idkm_batch_context", "idkm_batch_forward", "idkm_batch_backward"]
@@ -138,6 +139,19 @@ def load_library():
     lib.idkm_codes_linear_backward_workspace.restype = i64
     lib.idkm_codes_linear_backward.argtypes = [vp, desc, vp, i64, vp, i64, i64, vp, i64, vp, vp, vp, i64, vp]
     lib.idkm_codes_linear_backward.restype = C.c_int
+    f32 = C.c_float
+    lib.idkm_embedding.argtypes = [vp, vp, i64, i64, vp, i32, i64, f32, vp, i64, C.c_int, vp]
+    lib.idkm_embedding.restype = C.c_int
+    lib.idkm_embedding_backward_workspace.argtypes = [i64, i64, i64]
+    lib.idkm_embedding_backward_workspace.restype = i64
+    lib.idkm_embedding_backward.argtypes = [vp, i64, i64, vp, i32, i64, f32, vp, i64, C.c_int, vp, vp, i64, vp]
+    lib.idkm_embedding_backward.restype = C.c_int
+    lib.idkm_codes_embedding.argtypes = [vp, desc, vp, i32, i64, f32, vp, i64, vp]
+    lib.idkm_codes_embedding.restype = C.c_int
+    lib.idkm_codes_embedding_backward_workspace.argtypes = [desc, i64]
+    lib.idkm_codes_embedding_backward_workspace.restype = i64
+    lib.idkm_codes_embedding_backward.argtypes = [vp, desc, vp, i32, i64, f32, vp, i64, vp, vp, vp, i64, vp]
+    lib.idkm_codes_embedding_backward.restype = C.c_int
     lib.idkm_group_scale.argtypes = [vp, vp, i64, i64, i64, vp, vp, vp]
     lib.idkm_group_scale.restype = C.c_int
     lib.idkm_group_unscale.argtypes = [vp, vp, vp, i64, i64, i64, vp, vp]
@@ -283,13 +297,14 @@ class CodesLayer:
         self._at = C.byref(self._desc)
         self._bytes = {}  # workspace sizes by (call, tokens)
 
-    def workspace_bytes(self, n, backward=False):
-        """Bytes that codes_linear (or codes_linear_backward) of n tokens works in; raises for a layer it refuses."""
-        key = (n, backward)
+    def workspace_bytes(self, n, backward=False, lookup=False):
+        """Bytes that codes_linear (or codes_linear_backward, or codes_embedding_backward) of n tokens works in; raises for a layer it refuses."""
+        key = (n, backward, lookup)
         b = self._bytes.get(key)
         if b is None:
             lib = load_library()
-            b = (lib.idkm_codes_linear_backward_workspace if backward else lib.idkm_codes_linear_workspace)(self._at, n)
+            b = (lib.idkm_codes_embedding_backward_workspace if lookup else
+                 lib.idkm_codes_linear_backward_workspace if backward else lib.idkm_codes_linear_workspace)(self._at, n)
             if len(self._bytes) > 4096:
                 self._bytes.clear()
             self._bytes[key] = b
@@ -489,6 +504,91 @@ class Context:
         self._check(self._lib.idkm_codes_linear_backward(
             self._h, layer._at, X.data_ptr() if X is not None else None, ldx, dY.data_ptr(), ldy, n, at.get("dX"), layer.cols,
             at.get("dC"), at.get("dS"), ws.data_ptr() if need > 0 else None, need, self._raw_stream()))
+        return res
+
+    def _tokens(self, ids):
+        """Address, bytes of an id and number of tokens' ids, int32 or int64 and contiguous in one dimension."""
+        torch = _t()
+        if not isinstance(ids, torch.Tensor) or ids.get_device() != self.device:
+            raise TypeError(f"ids must be in the memory of device {self.device}")
+        wide = ids.dtype is torch.int64
+        if not (wide or ids.dtype is torch.int32) or ids.dim() != 1 or not ids.is_contiguous():
+            raise TypeError(f"ids must be contiguous int32 or int64 of one dimension, got {ids.dtype} {tuple(ids.shape)}")
+        return ids.data_ptr(), 8 if wide else 4, ids.shape[0]
+
+    def _looked_up(self, out, n, cols, dtype, ids):
+        if out is None:
+            return ids.new_empty(n, cols, dtype=dtype), cols
+        ldy = _rows(out, dtype, cols, self.device, "out")
+        if out.shape[0] != n:
+            raise TypeError(f"out must have {n} rows")
+        return out, ldy
+
+    def embedding(self, W, ids, alpha=1.0, dtype=None, out=None):
+        """idkm_embedding: rows ids [n] (int32 or int64; a negative one is padding, a row of zeros) of the float32 table W [rows, cols], times
+        alpha, in `dtype` (float32 unless given, or `out`'s)."""
+        torch = _t()
+        if W.dim() != 2:
+            raise TypeError(f"W must be a matrix, got {tuple(W.shape)}")
+        w = _flat(W, torch.float32, W.shape, self.device, "W")
+        at, width, n = self._tokens(ids)
+        rows, cols = W.shape
+        dtype = out.dtype if dtype is None and out is not None else dtype or torch.float32
+        out, ldy = self._looked_up(out, n, cols, dtype, ids)
+        st = self._lib.idkm_embedding(self._h, w, rows, cols, at, width, n, alpha, out.data_ptr(), ldy, _dtype(out, "out"), self._raw_stream())
+        if st:
+            self._check(st)
+        return out
+
+    def embedding_backward(self, dY, ids, rows, alpha=1.0):
+        """idkm_embedding_backward: dW [rows, cols] float32 from dY [n, cols], zero in the rows of which there is no token."""
+        torch = _t()
+        at, width, n = self._tokens(ids)
+        if dY.dim() != 2 or dY.shape[0] != n:
+            raise TypeError(f"dY must have {n} rows")
+        code, cols = _dtype(dY, "dY"), dY.shape[1]
+        ldy = _rows(dY, dY.dtype, cols, self.device, "dY")
+        dW = dY.new_empty(rows, cols, dtype=torch.float32)
+        need = self._lib.idkm_embedding_backward_workspace(rows, cols, n)
+        ws = dY.new_empty(need, dtype=torch.uint8) if need > 0 else None
+        st = self._lib.idkm_embedding_backward(self._h, rows, cols, at, width, n, alpha, dY.data_ptr(), ldy, code, dW.data_ptr(),
+                                               ws.data_ptr() if need > 0 else None, need, self._raw_stream())
+        if st:
+            self._check(st)
+        return dW
+
+    def codes_embedding(self, layer, ids, alpha=1.0, out=None):
+        """idkm_codes_embedding: rows ids [n] of a table in its stored form (a CodesLayer), times alpha, [n, cols] in the layer's type."""
+        if layer.device != self.device:
+            raise TypeError(f"the layer must be in the memory of device {self.device}")
+        at, width, n = self._tokens(ids)
+        out, ldy = self._looked_up(out, n, layer.cols, layer.dtype, ids)
+        st = self._lib.idkm_codes_embedding(self._h, layer._at, at, width, n, alpha, out.data_ptr(), ldy, self._raw_stream())
+        if st:
+            self._check(st)
+        return out
+
+    def codes_embedding_backward(self, layer, ids, dY, alpha=1.0, want_dC=True, want_dS=True):
+        """idkm_codes_embedding_backward: dict of float32 dC [k, d] and, for a layer with scales, dS [rows, groups]."""
+        torch, dev = _t(), self.device
+        if layer.device != dev:
+            raise TypeError(f"the layer must be in the memory of device {dev}")
+        at, width, n = self._tokens(ids)
+        ldy = _rows(dY, layer.dtype, layer.cols, dev, "dY")
+        if dY.shape[0] != n:
+            raise TypeError(f"dY must have {n} rows")
+        res = {}
+        if want_dC:
+            res["dC"] = dY.new_empty(layer.k, layer.d, dtype=torch.float32)
+        if want_dS and layer.S is not None:
+            res["dS"] = dY.new_empty(layer.rows, layer.groups, dtype=torch.float32)
+        need = layer.workspace_bytes(n, lookup=True)
+        ws = dY.new_empty(need, dtype=torch.uint8) if need > 0 else None
+        to = {key: t.data_ptr() for key, t in res.items()}
+        st = self._lib.idkm_codes_embedding_backward(self._h, layer._at, at, width, n, alpha, dY.data_ptr(), ldy, to.get("dC"), to.get("dS"),
+                                                     ws.data_ptr() if need > 0 else None, need, self._raw_stream())
+        if st:
+            self._check(st)
         return res
 
     def _grouped(self, t, group, name):

@@ -6,17 +6,19 @@
 namespace idkm {
 
 // dC[e] = the sum of bins[e][w], w < n, in float64: a workgroup to an e.  The workgroups behind them add up segments:
-// dS[r, g] = the sum of the row's segments of the group, in order.
+// dS[r, g] = the sum of the row's segments of the group, in order; listed: the segments' row i belongs to row listed[i], for *listed_count rows.
 __global__ __launch_bounds__(256) void k_join_gradients(const float* __restrict__ bins, int64_t n, int kd, float* __restrict__ dC,
                                                         const float* __restrict__ segments, int per_row, int of_group, int groups, int64_t scales,
-                                                        float* __restrict__ dS) {
+                                                        float* __restrict__ dS, const int32_t* __restrict__ listed,
+                                                        const int32_t* __restrict__ listed_count) {
     if ((int)blockIdx.x >= kd) {
+        if (listed) scales = (int64_t)*listed_count * groups;
         for (int64_t i = (int64_t)(blockIdx.x - kd) * 256 + threadIdx.x; i < scales; i += (int64_t)(gridDim.x - kd) * 256) {
             const int64_t r = i / groups;
             const int g = (int)(i - r * groups), last = min(per_row, (g + 1) * of_group);
             float sum = 0.f;
             for (int j = g * of_group; j < last; ++j) sum += segments[r * per_row + j];
-            dS[i] = sum;
+            dS[listed ? (int64_t)listed[r] * groups + g : i] = sum;
         }
         return;
     }
@@ -58,20 +60,6 @@ void allow_lds(const void* fn, size_t bytes) {
     if (slot.load(std::memory_order_relaxed) == key) return;
     if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess) slot.store(key, std::memory_order_relaxed);
 }
-
-#define BY_TYPE(dtype, T, ...)                     \
-    do {                                           \
-        if ((dtype) == 0) {                        \
-            using T = float;                       \
-            __VA_ARGS__;                           \
-        } else if ((dtype) == 1) {                 \
-            using T = f16;                         \
-            __VA_ARGS__;                           \
-        } else {                                   \
-            using T = bf16;                        \
-            __VA_ARGS__;                           \
-        }                                          \
-    } while (0)
 
 // The kernels with lookups, for the codes that they take; a run's words (three at most) have to be there.
 static bool launch_fast(int dtype, const DenseArgs& a, bool columns, hipStream_t s) {
@@ -129,26 +117,27 @@ void launch_codes_bins(int dtype, const BinArgs& args, int grid, int waves, hipS
     a.c_in_lds = a.dS && book <= 16 * 1024;
     const size_t lds = (a.bins ? (size_t)waves * a.codes * 256 : 0) + (a.c_in_lds ? book : 0);
     BY_TYPE(dtype, T, {
-        allow_lds(reinterpret_cast<const void*>(&k_codes_bins<T>), lds);
-        hipLaunchKernelGGL(k_codes_bins<T>, dim3((unsigned)grid), dim3((unsigned)waves * 64), lds, s, a);
+        void (*const fn)(const BinArgs) = a.listed ? &k_codes_bins<T, true> : &k_codes_bins<T, false>;
+        allow_lds(reinterpret_cast<const void*>(fn), lds);
+        hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3((unsigned)waves * 64), lds, s, a);
     });
 }
 
 // Lanes that have the same bins in k_codes_bins_wide: 16 KB a wavefront.
 int bins_shared_by(int k) { return k <= 64 ? 1 : k <= 128 ? 2 : 4; }
 
-template <typename T, int SHARE>
+template <typename T, int SHARE, bool LISTED>
 static void (*wide_for(int d))(const BinArgs) {
-    return d == 1 ? &k_codes_bins_wide<T, 1, SHARE> : d == 2 ? &k_codes_bins_wide<T, 2, SHARE>
-           : d == 4 ? &k_codes_bins_wide<T, 4, SHARE> : &k_codes_bins_wide<T, 8, SHARE>;
+    return d == 1 ? &k_codes_bins_wide<T, 1, SHARE, LISTED> : d == 2 ? &k_codes_bins_wide<T, 2, SHARE, LISTED>
+           : d == 4 ? &k_codes_bins_wide<T, 4, SHARE, LISTED> : &k_codes_bins_wide<T, 8, SHARE, LISTED>;
 }
 
-template <typename T>
+template <typename T, bool LISTED>
 static void launch_bins_runs(const BinArgs& a, bool wide, int grid, int waves, hipStream_t s) {
-    void (*const narrow_fn)(const BinArgs) = a.d == 1 ? &k_codes_bins_runs<T, 1> : a.d == 2 ? &k_codes_bins_runs<T, 2>
-                                             : a.d == 4 ? &k_codes_bins_runs<T, 4> : &k_codes_bins_runs<T, 8>;
+    void (*const narrow_fn)(const BinArgs) = a.d == 1 ? &k_codes_bins_runs<T, 1, LISTED> : a.d == 2 ? &k_codes_bins_runs<T, 2, LISTED>
+                                             : a.d == 4 ? &k_codes_bins_runs<T, 4, LISTED> : &k_codes_bins_runs<T, 8, LISTED>;
     const int share = wide ? bins_shared_by(a.k) : 1;
-    void (*const wide_fn)(const BinArgs) = share == 1 ? wide_for<T, 1>(a.d) : share == 2 ? wide_for<T, 2>(a.d) : wide_for<T, 4>(a.d);
+    void (*const wide_fn)(const BinArgs) = share == 1 ? wide_for<T, 1, LISTED>(a.d) : share == 2 ? wide_for<T, 2, LISTED>(a.d) : wide_for<T, 4, LISTED>(a.d);
     void (*const fn)(const BinArgs) = wide ? wide_fn : narrow_fn;
     const size_t lds = wide ? (a.bins ? (size_t)waves * (64 / share) * a.k * 4 : 0) : ((a.bins ? (size_t)waves * 64 : 0) + 1) * a.k * a.d * 4;
     allow_lds(reinterpret_cast<const void*>(fn), lds);
@@ -156,16 +145,18 @@ static void launch_bins_runs(const BinArgs& a, bool wide, int grid, int waves, h
 }
 
 void launch_codes_bins_runs(int dtype, const BinArgs& a, bool wide, int grid, int waves, hipStream_t s) {
-    BY_TYPE(dtype, T, launch_bins_runs<T>(a, wide, grid, waves, s));
+    if (a.listed) BY_TYPE(dtype, T, launch_bins_runs<T, true>(a, wide, grid, waves, s));
+    else BY_TYPE(dtype, T, launch_bins_runs<T, false>(a, wide, grid, waves, s));
 }
 
 void launch_join_gradients(const float* bins, int64_t n, int kd, float* dC, const float* segments, int64_t rows, int64_t cols, int group,
-                           int groups, float* dS, hipStream_t s) {
+                           int groups, float* dS, hipStream_t s, const int32_t* listed, const int32_t* listed_count) {
     const int per_row = (int)((cols + 31) / 32), of_group = groups > 1 ? group / 32 : per_row;
     if (!dC) kd = 0;
     const unsigned grid = (unsigned)kd + (segments ? grid_for(rows * groups) : 0u);
     if (grid > 0)
-        hipLaunchKernelGGL(k_join_gradients, dim3(grid), dim3(256), 0, s, bins, n, kd, dC, segments, per_row, of_group, groups, rows * groups, dS);
+        hipLaunchKernelGGL(k_join_gradients, dim3(grid), dim3(256), 0, s, bins, n, kd, dC, segments, per_row, of_group, groups, rows * groups, dS, listed,
+                           listed_count);
 }
 
 void launch_fill_zero(float* out, int64_t n, hipStream_t s) {

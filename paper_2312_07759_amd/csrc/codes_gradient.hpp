@@ -29,9 +29,14 @@ struct BinArgs {
     int lanes;         // of a wavefront that take part: a multiple of d
     int run;           // groups of a row that a wavefront takes at a time
     int c_in_lds;
+    // LISTED: P's row i belongs to the layer's row listed[i], for *listed_count rows; `segments` has a row for each of them
+    const int32_t* listed;
+    const int32_t* listed_count;
+    __device__ __forceinline__ int64_t row_of(int64_t rr, bool of_list) const { return of_list ? (int64_t)listed[rr] : first + rr; }
+    __device__ __forceinline__ int64_t rows_here(bool of_list) const { return of_list ? (int64_t)*listed_count : count; }
 };
 
-template <typename T>
+template <typename T, bool LISTED>
 __global__ __launch_bounds__(256) void k_codes_bins(const BinArgs a) {
     constexpr int STEPS = 8;
     extern __shared__ __align__(16) float bin_lds[];  // [wave][codes][64], then the codebook
@@ -49,13 +54,13 @@ __global__ __launch_bounds__(256) void k_codes_bins(const BinArgs a) {
     const int per_row = (int)(a.cols / a.d);
     const int runs = (a.groups + a.run - 1) / a.run;  // of a row
     const int steps = (a.group + a.lanes - 1) / a.lanes;  // of a group
-    const int64_t tasks = a.count * runs;
+    const int64_t tasks = a.rows_here(LISTED) * runs;
     const int own_code = lane / a.d, x = lane - own_code * a.d;
     const int group_codes = a.group / a.d, step_codes = a.lanes / a.d;
     const uint32_t mask = (1u << a.bits) - 1u;
     const int two = a.nwords > 1 ? 1 : 0;
     for (int64_t task = (int64_t)blockIdx.x * nw + wave; task < tasks; task += (int64_t)gridDim.x * nw) {
-        const int64_t rr = task / runs, r = a.first + rr;
+        const int64_t rr = task / runs, r = a.row_of(rr, LISTED);
         const int g0 = (int)(task - rr * runs) * a.run, g1 = min(a.groups, g0 + a.run);
         const float* P = a.P + rr * a.ldp;
         const float* S = a.S ? a.S + r * a.groups : nullptr;
@@ -123,7 +128,7 @@ __global__ __launch_bounds__(256) void k_codes_bins(const BinArgs a) {
 // keeps bins for all k D components.  Ten instructions a column instead of some 75, which bound the kernel above (4096 x 4096, k = 16:
 // 127 us; this one 25 to 30, of which P at the rate of a copy is 13).  dS: lanes of a group are added up where they are a power of two of at most 64, otherwise sums of 32 columns go to
 // `segments`, which k_join_gradients adds up.
-template <typename T, int D>
+template <typename T, int D, bool LISTED>
 __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {
     constexpr int NC = 8 / D;
     extern __shared__ __align__(16) float bin_lds[];  // [wave][k D][64], then the codebook
@@ -148,8 +153,9 @@ __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {
         uint32_t w[3];
         int sh;
     };
+    const int64_t count = a.rows_here(LISTED);
     auto ask = [&](Item& t, int64_t row, int of) {
-        const int64_t r = a.first + row;
+        const int64_t r = a.row_of(row, LISTED);
         const int at = min(of * 512 + lane * 8, (int)(a.cols - 1) & ~7);  // lanes behind the last column read it and do not count
         const float* P = a.P + row * a.ldp + at;  // ldp is a multiple of 8
 #pragma unroll
@@ -166,16 +172,16 @@ __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {
         t.s = a.S ? a.S[r * a.groups + at / a.group] : 1.f;
     };
     Item now, next;
-    if (rr < a.count) ask(now, rr, strip);
-    while (rr < a.count) {
+    if (rr < count) ask(now, rr, strip);
+    while (rr < count) {
         int64_t rn = rr + rows_step;
         int sn = strip + strips_step;
         if (sn >= strips) {
             sn -= strips;
             ++rn;
         }
-        if (rn < a.count) ask(next, rn, sn);
-        const int64_t r = a.first + rr;
+        if (rn < count) ask(next, rn, sn);
+        const int64_t r = a.row_of(rr, LISTED);
         const int c = strip * 512 + lane * 8;
         const bool there = c < a.cols;
         const int have = there ? min(8, (int)a.cols - c) : 0;
@@ -209,7 +215,7 @@ __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {
         if (a.segments) {
             sum += __shfl_xor(sum, 1);
             sum += __shfl_xor(sum, 2);
-            if (there && (lane & 3) == 0) a.segments[r * ((a.cols + 31) / 32) + (c >> 5)] = sum;
+            if (there && (lane & 3) == 0) a.segments[(LISTED ? rr : r) * ((a.cols + 31) / 32) + (c >> 5)] = sum;
         } else if (a.dS) {
             for (int o = 1; o < group_lanes; o <<= 1) sum += __shfl_xor(sum, o);
             if (there && (lane & (group_lanes - 1)) == 0) a.dS[r * a.groups + c / a.group] = sum;
@@ -247,7 +253,7 @@ __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {
 // in eight steps of 64; the next 512 are asked for before these are used.  dS goes through `segments` always.
 // SHARE lanes have the same bins and add to them one after another: with bins for every lane, 256 codewords leave room for two wavefronts
 // on a compute unit, which wait for every one of their loads (512 x 4608, k = 256, d = 4: 30 us; 18 with eight wavefronts, whose turns are then what takes longest).
-template <typename T, int D, int SHARE>
+template <typename T, int D, int SHARE, bool LISTED>
 __global__ __launch_bounds__(256) void k_codes_bins_wide(const BinArgs a) {
     constexpr int STEPS = 8, WIDTH = 64 / SHARE;
     extern __shared__ __align__(16) float bin_lds[];  // [wave][k][WIDTH]
@@ -268,8 +274,9 @@ __global__ __launch_bounds__(256) void k_codes_bins_wide(const BinArgs a) {
         uint32_t lo[STEPS], hi[STEPS];
         int sh[STEPS];
     };
+    const int64_t count = a.rows_here(LISTED);
     auto ask = [&](Batch& t, int64_t row, int at) {
-        const int64_t r = a.first + row, bit0 = (r * per_row + at * (512 / D)) * a.bits;
+        const int64_t r = a.row_of(row, LISTED), bit0 = (r * per_row + at * (512 / D)) * a.bits;
         const uint32_t* words = a.words + (bit0 >> 5);
         const int limit = (int)min(a.nwords - 2 - (bit0 >> 5), (int64_t)1 << 30);  // at least -1: a word is there
         const float* P = a.P + row * a.ldp;
@@ -287,15 +294,15 @@ __global__ __launch_bounds__(256) void k_codes_bins_wide(const BinArgs a) {
         }
     };
     Batch now, next;
-    if (rr < a.count) ask(now, rr, strip);
-    while (rr < a.count) {
+    if (rr < count) ask(now, rr, strip);
+    while (rr < count) {
         int64_t rn = rr + rows_step;
         int sn = strip + strips_step;
         if (sn >= strips) {
             sn -= strips;
             ++rn;
         }
-        if (rn < a.count) ask(next, rn, sn);
+        if (rn < count) ask(next, rn, sn);
         uint32_t code[STEPS];
         float w[STEPS];
 #pragma unroll
@@ -335,7 +342,7 @@ __global__ __launch_bounds__(256) void k_codes_bins_wide(const BinArgs a) {
             w[0] += __shfl_xor(w[0], 2);
             w[0] += __shfl_xor(w[0], 1);
             const int u = (lane >> 4 & 1) * 4 + (lane >> 3 & 1) * 2 + (lane >> 2 & 1), c = strip * 512 + u * 64 + (lane & 32);
-            if ((lane & 3) == 0 && c < a.cols) a.segments[(a.first + rr) * segments + (c >> 5)] = w[0];
+            if ((lane & 3) == 0 && c < a.cols) a.segments[(LISTED ? rr : a.first + rr) * segments + (c >> 5)] = w[0];
         }
         now = next;
         rr = rn;

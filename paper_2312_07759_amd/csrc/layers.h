@@ -4,7 +4,24 @@
 #include "codes_product.hpp"
 #include "tile_product.hpp"
 
+// T is the type that dtype names.
+#define BY_TYPE(dtype, T, ...)                     \
+    do {                                           \
+        if ((dtype) == 0) {                        \
+            using T = float;                       \
+            __VA_ARGS__;                           \
+        } else if ((dtype) == 1) {                 \
+            using T = f16;                         \
+            __VA_ARGS__;                           \
+        } else {                                   \
+            using T = bf16;                        \
+            __VA_ARGS__;                           \
+        }                                          \
+    } while (0)
+
 namespace idkm {
+
+inline int64_t up_to(int64_t x, int64_t unit) { return (x + unit - 1) / unit * unit; }
 
 // Up to 16 tokens, straight from the codes.  IB bits looked up at once give W weights (see codes_at_once), L weights of a row to a
 // lane at a time (8, 16, 32); aligned: every run of codes begins with a word; apart: up to 4 tokens, L = 32, a scale for every run.
@@ -39,9 +56,9 @@ void launch_codes_bins(int dtype, const BinArgs& a, int grid, int waves, hipStre
 int bins_shared_by(int k);
 void launch_codes_bins_runs(int dtype, const BinArgs& a, bool wide, int grid, int waves, hipStream_t s);
 void launch_fill_zero(float* out, int64_t n, hipStream_t s);
-// dC from bins [kd][n] (null: not), dS from segments (null: not).
+// dC from bins [kd][n] (null: not), dS from segments (null: not); listed, listed_count: see BinArgs, `rows` at most then.
 void launch_join_gradients(const float* bins, int64_t n, int kd, float* dC, const float* segments, int64_t rows, int64_t cols, int group,
-                           int groups, float* dS, hipStream_t s);
+                           int groups, float* dS, hipStream_t s, const int32_t* listed = nullptr, const int32_t* listed_count = nullptr);
 
 constexpr int SCALE_FWD = 0, UNSCALE_FWD = 1, UNSCALE_BWD = 2, SCALE_BWD = 3;
 struct ScaleArgs {

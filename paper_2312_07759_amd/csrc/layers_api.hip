@@ -3,18 +3,10 @@
 #include <cfloat>
 #include <climits>
 #include <cmath>
-#include <cstdint>
-#include <cstdio>
-#include <exception>
-#include <new>
 
-#include "../../include/idkm.h"
-#include "layers.h"
+#include "entry.hpp"
 
 namespace idkm {
-
-int context_device(const idkm_ctx* ctx);
-void context_error(idkm_ctx* ctx, const char* msg);
 
 ProductFn codes_product_kernel_1(int, int, int, bool, bool);
 ProductFn codes_product_kernel_2(int, int, int, bool, bool);
@@ -64,87 +56,85 @@ ProductFn codes_product_kernel(int dtype, int IB, int W, int L, bool aligned, bo
     return IB >= 1 && IB <= 8 ? by_bits[IB - 1](dtype, W, L, aligned, apart) : nullptr;
 }
 
+BinPlan bin_plan(const idkm_codes_desc& w, int64_t lines) {
+    const int bits = idkm_code_bits(w.k);
+    BinPlan l{};
+    l.group = w.S ? (int)(w.group < w.cols ? w.group : w.cols) : 0;
+    l.runs = bits <= 8 && (w.d == 1 || w.d == 2 || w.d == 4 || w.d == 8) && w.rows * w.cols / w.d * bits > 96;
+    l.wide = l.runs && w.k * w.d > 256;  // bins of all components for every lane: 64 KB a wavefront at most
+    int64_t tasks;  // of a wavefront, in a panel
+    int bin_bytes;  // of a wavefront
+    if (l.runs) {
+        if (!w.S) l.group = (int)up_to(w.cols, 8);
+        l.groups = w.S ? groups_of(w) : 1;
+        // lanes of a group of 8 m columns lie together in a wavefront's 512 where m is a power of two
+        l.segmented = w.S && (l.wide || l.group > 512 || l.group % 8 != 0 || (l.group & (l.group - 1)) != 0);
+        tasks = lines * ((w.cols + 511) / 512);
+        bin_bytes = l.wide ? w.k * 256 / bins_shared_by(w.k) : w.k * w.d * 256;
+        l.codes = w.k;
+    } else {
+        // a wavefront takes groups of a row at a time; without scales, some hundred columns
+        if (!w.S) l.group = (int)(w.cols < 512 ? w.cols : 512 / w.d * w.d);
+        l.groups = (int)((w.cols + l.group - 1) / l.group);
+        l.lanes = 64 / w.d * w.d;
+        if (w.S && l.group % 64 == 32 && l.group < 256 && 32 % w.d == 0) l.lanes = 32;  // no step of which half is behind the group
+        const int steps = (l.group + l.lanes - 1) / l.lanes;
+        l.run = steps >= 16 ? 1 : 16 / steps;
+        if (l.run > l.groups) l.run = l.groups;
+        l.codes = w.k < 512 ? w.k : 512;  // bins of 512 codewords fill 128 KB
+        tasks = lines * ((l.groups + l.run - 1) / l.run);
+        bin_bytes = l.codes * 256;
+    }
+    l.waves = 128 * 1024 / bin_bytes;
+    if (l.waves > 4) l.waves = 4;
+    // as many workgroups as the compute units hold at once: every one has bins to clear and to write
+    int64_t grid = (tasks + l.waves - 1) / l.waves, most = 256 * (150 * 1024 / (bin_bytes * l.waves + 4096));
+    if (most > 2048) most = 2048;
+    l.grid = (int)(grid < most ? grid : most);
+    return l;
+}
+
+BinArgs bins_of(const idkm_codes_desc& w, const BinPlan& l) {
+    BinArgs b{};
+    b.words = w.words;
+    b.nwords = idkm_code_words(w.rows * w.cols / w.d, w.k);
+    b.rows = w.rows;
+    b.cols = w.cols;
+    b.C = w.C;
+    b.k = w.k;
+    b.d = w.d;
+    b.bits = idkm_code_bits(w.k);
+    b.S = w.S;
+    b.group = l.group;
+    b.groups = l.groups;
+    b.run = l.run;
+    b.lanes = l.lanes;
+    return b;
+}
+
+void run_bins(int dtype, const BinPlan& l, BinArgs b, float* dS, hipStream_t s) {
+    if (l.runs) {
+        b.dS = dS;
+        launch_codes_bins_runs(dtype, b, l.wide, l.grid, l.waves, s);
+        return;
+    }
+    for (int c0 = 0; c0 < (b.bins ? b.k : 1); c0 += l.codes) {
+        b.dS = c0 == 0 ? dS : nullptr;
+        b.code0 = c0;
+        b.codes = l.codes;
+        launch_codes_bins(dtype, b, l.grid, l.waves, s);
+    }
+}
+
 }  // namespace idkm
 
 using namespace idkm;
 
 namespace {
 
-constexpr int64_t MAX_SIDE = 4000000;      // rows, columns, tokens: 64 of them to a workgroup fit one grid dimension
 constexpr int64_t MAX_VOCABULARY = (int64_t)1 << 29;  // offsets in a row are 32 bits of bytes
 constexpr int64_t MAX_SCALED_COLS = INT_MAX - 63;  // a lane's 32-bit place in a row goes up to 64 weights beyond its end
 constexpr int64_t PANEL = (int64_t)1 << 26;  // weights of a layer that are written out at a time
-
-idkm_status refuse(idkm_ctx* ctx, idkm_status s, const char* msg) {
-    if (ctx) context_error(ctx, msg);
-    return s;
-}
-
-// The context's device is the current one inside; the caller's is again after it.
-struct OnDevice {
-    int before = -1;
-    bool ok = false;
-    explicit OnDevice(int device) {
-        if (hipGetDevice(&before) != hipSuccess) return;
-        ok = before == device || hipSetDevice(device) == hipSuccess;
-        if (before == device) before = -1;
-    }
-    ~OnDevice() {
-        if (ok && before >= 0) (void)hipSetDevice(before);
-    }
-};
-
-// Runs body() on the context's device; no exception leaves a C entry point.
-template <class Body>
-idkm_status entry(idkm_ctx* ctx, Body body) noexcept {
-    if (!ctx) return IDKM_ERR_INVALID_ARG;
-    try {
-        context_error(ctx, "");
-        return body();
-    } catch (const std::bad_alloc&) {
-        return IDKM_ERR_ALLOC;
-    } catch (...) {
-        return IDKM_ERR_DEVICE;
-    }
-}
-
-template <class Launches>
-idkm_status launched(idkm_ctx* ctx, Launches launches) {
-    OnDevice on(context_device(ctx));
-    if (!on.ok) {
-        (void)hipGetLastError();
-        return refuse(ctx, IDKM_ERR_DEVICE, "the context's device cannot be made current");
-    }
-    launches();
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? IDKM_OK : refuse(ctx, IDKM_ERR_DEVICE, hipGetErrorString(e));
-}
-
-int64_t up_to(int64_t x, int64_t unit) { return (x + unit - 1) / unit * unit; }
-int esize_of(int dtype) { return dtype == IDKM_F32 ? 4 : 2; }
-bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
-
-const char* wrong_layer(const idkm_codes_desc* w, idkm_status* st) {
-    *st = IDKM_ERR_INVALID_ARG;
-    if (!w) return "the layer must be non-NULL";
-    if (!w->words || !w->C) return "words and C must be non-NULL";
-    if (w->dtype != IDKM_F32 && w->dtype != IDKM_F16 && w->dtype != IDKM_BF16) return "dtype must be an idkm_dtype";
-    if (w->rows < 1 || w->cols < 1) return "rows and cols must be >= 1";
-    if (w->k < 1 || w->k > 1024 || w->d < 1 || w->d > 64) return "need 1 <= k <= 1024 and 1 <= d <= 64";
-    if (w->cols % w->d != 0) return "cols must be a multiple of d";
-    if (w->S) {
-        if (w->group < 1) return "group must be >= 1 where there are scales";
-        if (w->group < w->cols && (w->group % 32 != 0 || w->group % w->d != 0))
-            return "a group shorter than a row must be a multiple of 32 and of d";
-        if (!aligned_to(w->S, 4)) return "S must be aligned to its type";
-    }
-    if (!aligned_to(w->words, 4) || !aligned_to(w->C, esize_of(w->dtype))) return "words and C must be aligned to their types";
-    *st = IDKM_ERR_UNSUPPORTED;
-    if (w->rows > MAX_SIDE || w->cols > MAX_SIDE || w->rows * w->cols > ((int64_t)1 << 36)) return "the layer is too large";
-    return nullptr;
-}
-
-int groups_of(const idkm_codes_desc& w) { return w.S ? (int)((w.cols + w.group - 1) / w.group) : 0; }
 
 // ---- straight from the codes
 
@@ -288,9 +278,6 @@ void run_tiles(int dtype, const TilePlan& p, const TileArgs& args, hipStream_t s
     hipLaunchKernelGGL(t.fn, dim3(grid), dim3((unsigned)t.threads), t.lds, s, jobs);
 }
 
-// Bytes of a buffer in the workspace.
-int64_t buffer(int64_t elements, int esize) { return up_to(elements * esize, 256); }
-
 // out[M, N] in T (rows ldo apart): in one part, or in several that are joined.
 void set_out(const TilePlan& p, TileArgs* a, void* out, int64_t ldo, float* parts) {
     a->wide = p.parts > 1;
@@ -388,53 +375,20 @@ void operand_of(int dtype, const void* in, int64_t ldi, int64_t n, int64_t sum, 
 }
 
 // Gradients of the layer itself.
-struct LayerGradLayout {
+struct LayerGradLayout : BinPlan {
     int64_t pad, ldp, panel, panels, dy, x, p, bins, segments, bytes;
     TilePlan plan;
-    bool runs, wide, segmented;  // which of the kernels for bins
-    int group, groups, lanes, run, waves, codes, grid;
 };
 
 LayerGradLayout layer_grad_layout(const idkm_codes_desc& w, int64_t n, const TilePlan* plan = nullptr) {
-    const int es = esize_of(w.dtype), bits = idkm_code_bits(w.k);
+    const int es = esize_of(w.dtype);
     LayerGradLayout l{};
     l.pad = up_to(n, TP_STEP / es);
     l.ldp = up_to(w.cols, 8);
     l.panel = panel_of(w.rows, l.ldp);
     l.panels = (w.rows + l.panel - 1) / l.panel;
     l.plan = plan ? *plan : tile_plan(l.panel, w.cols, l.pad * es / TP_STEP, w.dtype, 0);
-    l.group = w.S ? (int)(w.group < w.cols ? w.group : w.cols) : 0;
-    l.runs = bits <= 8 && (w.d == 1 || w.d == 2 || w.d == 4 || w.d == 8) && w.rows * w.cols / w.d * bits > 96;
-    l.wide = l.runs && w.k * w.d > 256;  // bins of all components for every lane: 64 KB a wavefront at most
-    int64_t tasks;  // of a wavefront, in a panel
-    int bin_bytes;  // of a wavefront
-    if (l.runs) {
-        if (!w.S) l.group = (int)up_to(w.cols, 8);
-        l.groups = w.S ? groups_of(w) : 1;
-        // lanes of a group of 8 m columns lie together in a wavefront's 512 where m is a power of two
-        l.segmented = w.S && (l.wide || l.group > 512 || l.group % 8 != 0 || (l.group & (l.group - 1)) != 0);
-        tasks = l.panel * ((w.cols + 511) / 512);
-        bin_bytes = l.wide ? w.k * 256 / bins_shared_by(w.k) : w.k * w.d * 256;
-        l.codes = w.k;
-    } else {
-        // a wavefront takes groups of a row at a time; without scales, some hundred columns
-        if (!w.S) l.group = (int)(w.cols < 512 ? w.cols : 512 / w.d * w.d);
-        l.groups = (int)((w.cols + l.group - 1) / l.group);
-        l.lanes = 64 / w.d * w.d;
-        if (w.S && l.group % 64 == 32 && l.group < 256 && 32 % w.d == 0) l.lanes = 32;  // no step of which half is behind the group
-        const int steps = (l.group + l.lanes - 1) / l.lanes;
-        l.run = steps >= 16 ? 1 : 16 / steps;
-        if (l.run > l.groups) l.run = l.groups;
-        l.codes = w.k < 512 ? w.k : 512;  // bins of 512 codewords fill 128 KB
-        tasks = l.panel * ((l.groups + l.run - 1) / l.run);
-        bin_bytes = l.codes * 256;
-    }
-    l.waves = 128 * 1024 / bin_bytes;
-    if (l.waves > 4) l.waves = 4;
-    // as many workgroups as the compute units hold at once: every one has bins to clear and to write
-    int64_t grid = (tasks + l.waves - 1) / l.waves, most = 256 * (150 * 1024 / (bin_bytes * l.waves + 4096));
-    if (most > 2048) most = 2048;
-    l.grid = (int)(grid < most ? grid : most);
+    static_cast<BinPlan&>(l) = bin_plan(w, l.panel);
     l.dy = 0;
     l.x = buffer(w.rows * l.pad, es);
     l.p = l.x + buffer(w.cols * l.pad, es);
@@ -495,13 +449,6 @@ GradLayout grad_layout(const idkm_codes_desc& w, int64_t n) {
         g.bytes = g.d.bytes + g.l.bytes;
     }
     return g;
-}
-
-const char* wrong_workspace(const void* ws, int64_t have, int64_t need) {
-    if (need == 0) return nullptr;
-    if (!ws || have < need) return "the workspace is smaller than the size asked for";
-    if (!aligned_to(ws, 16)) return "the workspace must be 16-byte aligned";
-    return nullptr;
 }
 
 const char* wrong_scale_shape(int64_t rows, int64_t cols, int64_t group) {
@@ -703,38 +650,16 @@ idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, 
                 }
                 if (l.plan.parts > 1)
                     launch_join_parts(IDKM_F32, reinterpret_cast<const float*>(ws + l.p), l.plan.parts, count, l.ldp, ws + l.p, l.ldp, s);
-                BinArgs b{};
-                b.words = w->words;
-                b.nwords = idkm_code_words(w->rows * w->cols / w->d, w->k);
-                b.rows = w->rows;
-                b.cols = w->cols;
-                b.C = w->C;
-                b.k = w->k;
-                b.d = w->d;
-                b.bits = idkm_code_bits(w->k);
-                b.S = w->S;
-                b.group = l.group;
-                b.groups = l.groups;
+                BinArgs b = bins_of(*w, l);
                 b.P = reinterpret_cast<const float*>(ws + l.p);
                 b.ldp = l.ldp;
-                b.run = l.run;
                 b.pitch = l.panels * l.grid;
                 b.at = written;
                 b.first = r;
                 b.count = count;
-                b.lanes = l.lanes;
                 b.bins = dC ? bins : nullptr;
                 b.segments = l.segmented && dS ? reinterpret_cast<float*>(ws + l.segments) : nullptr;
-                if (l.runs) {
-                    b.dS = dS;
-                    launch_codes_bins_runs(w->dtype, b, l.wide, l.grid, l.waves, s);
-                }
-                for (int c0 = 0; !l.runs && c0 < (dC ? w->k : 1); c0 += l.codes) {
-                    b.dS = c0 == 0 ? dS : nullptr;
-                    b.code0 = c0;
-                    b.codes = l.codes;
-                    launch_codes_bins(w->dtype, b, l.grid, l.waves, s);
-                }
+                run_bins(w->dtype, l, b, dS, s);
                 written += l.grid;
             }
             launch_join_gradients(bins, written, w->k * w->d, dC, l.segmented && dS ? reinterpret_cast<const float*>(ws + l.segments) : nullptr, w->rows,
