@@ -289,6 +289,25 @@ idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, 
                                        void* workspace, int64_t workspace_bytes, void* hip_stream);
 
 /*
+ * Activations kept in 8 bits between a forward and a backward pass.  Every 32 columns of a row (the last ones of a row may be fewer) share a
+ * power of two 2^e: x is kept as q 2^e with whole q in [-127, 127], which is a number of x's own type.  e is the smallest with which the 32 largest
+ * size, rounded to the nearest (ties to even), is at most 127, so that no error is larger than 2^e / 2 (1/128 of that size); e >= -132, and in the
+ * last binade of the type, where a larger power could round to infinity, larger quotients are cut to 127 (an error of 2^e at most).
+ * q = -128 stands for an infinity or NaN of x, which has no part in e and comes back as NaN.
+ *   idkm_keep8      X [n, cols] (rows ldx apart) -> Q int8 [n, 32 b] (zero behind column cols), 8-byte aligned, and E [n, b], e + 133, b = ceil(cols / 32)
+ *   idkm_restore8   X_out = q 2^e, exactly
+ *   idkm_codes_linear_backward_kept   idkm_codes_linear_backward of the X that idkm_restore8 gives, with the same bits, from Q and E themselves
+ * Enqueue on hip_stream, do not wait; n = 0 is a no-op (zeros in dC and dS).  n, cols <= 4,000,000.
+ */
+idkm_status idkm_keep8(idkm_ctx* ctx, const void* X, int64_t n, int64_t cols, int64_t ldx, idkm_dtype dtype, int8_t* Q, uint8_t* E,
+                       void* hip_stream);
+idkm_status idkm_restore8(idkm_ctx* ctx, const int8_t* Q, const uint8_t* E, int64_t n, int64_t cols, idkm_dtype dtype, void* X_out, int64_t ldx,
+                          void* hip_stream);
+idkm_status idkm_codes_linear_backward_kept(idkm_ctx* ctx, const idkm_codes_desc* w, const int8_t* Q, const uint8_t* E, const void* dY,
+                                            int64_t lddy, int64_t n, void* dX, int64_t lddx, float* dC, float* dS, void* workspace,
+                                            int64_t workspace_bytes, void* hip_stream);
+
+/*
  * Lookups: rows of an embedding table by token, times a scale alpha (finite), and their gradients.  ids: device, int32 or int64 (id_bytes 4
  * or 8) [n].  A negative id is no token (padding): its row of Y is zero and it has no part in the gradients.  An id >= rows makes its row of Y
  * NaN and has no part in the gradients.
@@ -315,6 +334,33 @@ int64_t idkm_codes_embedding_backward_workspace(const idkm_codes_desc* w, int64_
 idkm_status idkm_codes_embedding_backward(idkm_ctx* ctx, const idkm_codes_desc* w, const void* ids, int32_t id_bytes, int64_t n, float alpha,
                                           const void* dY, int64_t lddy, float* dC, float* dS, void* workspace, int64_t workspace_bytes,
                                           void* hip_stream);
+
+/*
+ * Products in 8-bit integers, for prompts: twice the rate of 16 bits on the matrix cores, and half the bytes.
+ *   idkm_int8_rows             X [n, cols] of type dtype (rows ldx apart) -> scale[t] = max(max_c |X[t,c]| / 127, 2^-126), rounded to float32, and Q [n, ldq]
+ *                              = X / scale to the nearest integer, ties to even (exactly), zero behind column cols; ldq a multiple of 16, Q 16-byte aligned.  A row that
+ *                              holds an infinity or NaN has scale NaN and integers 0.  (The layer's rows are made by it, too, from float32 weights.)
+ *   idkm_int8_linear           Y[t,r] = s[t] scale[r] sum_c q[t,c] W8[r,c], with q and s what idkm_int8_rows gives for X.  The sum is exact; it is rounded to
+ *                              float32, multiplied by s[t], by scale[r], and rounded to the type.
+ *   idkm_int8_linear_backward  dX[t,c] = sum_r dY[t,r] scale[r] W8[r,c]: as if the tokens' integers were the tokens.  scale W8 is rounded to the type (the layer's
+ *                              integers and scales stay as they are); sums are float32, results are rounded once.
+ * W8 [rows, ldw]: rows a multiple of 128 elements apart, 16-byte aligned; what lies from column cols on counts for nothing.
+ * Limits: rows, n <= 4,000,000, cols <= 131072 (sums of more would not fit 32 bits).  Types, strides, alignment, workspace and enqueueing as for idkm_codes_linear.
+ */
+typedef struct {
+    const int8_t* W8; /* device [rows, ldw] */
+    int64_t rows, cols, ldw;
+    const float* scale; /* device [rows] */
+    int32_t dtype;      /* idkm_dtype of X, Y, dX, dY */
+} idkm_int8_desc;
+idkm_status idkm_int8_rows(idkm_ctx* ctx, const void* X, int64_t n, int64_t cols, int64_t ldx, idkm_dtype dtype, int8_t* Q, int64_t ldq,
+                           float* scale, void* hip_stream);
+int64_t idkm_int8_linear_workspace(const idkm_int8_desc* w, int64_t n);
+idkm_status idkm_int8_linear(idkm_ctx* ctx, const idkm_int8_desc* w, const void* X, int64_t n, int64_t ldx, void* Y, int64_t ldy,
+                             void* workspace, int64_t workspace_bytes, void* hip_stream);
+int64_t idkm_int8_linear_backward_workspace(const idkm_int8_desc* w, int64_t n);
+idkm_status idkm_int8_linear_backward(idkm_ctx* ctx, const idkm_int8_desc* w, const void* dY, int64_t lddy, int64_t n, void* dX, int64_t lddx,
+                                      void* workspace, int64_t workspace_bytes, void* hip_stream);
 
 /*
  * Scales of groups: a layer whose rows or parts of rows differ in size is divided by the root mean square of each group of

@@ -25,7 +25,8 @@ EXPORTS = ["idkm_version", "idkm_limits", "idkm_status_string", "idkm_create", "
            "idkm_set_path", "idkm_set_matrix_cores", "idkm_set_tile_limit", "idkm_set_spin_limit", "idkm_set_kernel_timing", "idkm_last_kernel_ms", "idkm_set_gmres_basis", "idkm_advance_sequence", "idkm_forward", "idkm_backward", "idkm_step_F", "idkm_step_JCT", "idkm_get_cotangents", "idkm_forward_noalloc", "idkm_noalloc_last_error",
            "idkm_calibrate", "idkm_code_bits", "idkm_code_words", "idkm_pack_codes", "idkm_unpack_quantize",
            "idkm_codes_linear_workspace", "idkm_codes_linear", "idkm_codes_linear_backward_workspace",
-           "idkm_codes_linear_backward", "idkm_embedding", "idkm_embedding_backward_workspace", "idkm_embedding_backward",
+           "idkm_codes_linear_backward", "idkm_codes_linear_backward_kept", "idkm_keep8", "idkm_restore8",
+           "idkm_int8_rows", "idkm_int8_linear_workspace", "idkm_int8_linear", "idkm_int8_linear_backward_workspace", "idkm_int8_linear_backward", "idkm_embedding", "idkm_embedding_backward_workspace", "idkm_embedding_backward",
            "idkm_codes_embedding", "idkm_codes_embedding_backward_workspace", "idkm_codes_embedding_backward", "idkm_group_scale", "idkm_group_unscale", "idkm_group_unscale_backward",
            "idkm_group_scale_backward", "idkm_distill_workspace", "idkm_distill",
            "idkm_batch_create", "idkm_batch_destroy", "idkm_batch_last_error", "idkm_batch_launches",
@@ -51,6 +52,10 @@ class IdkmBwdDesc(C.Structure):
 class IdkmCodesDesc(C.Structure):
     _fields_ = [("words", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("C", C.c_void_p), ("k", C.c_int32),
                 ("d", C.c_int32), ("S", C.c_void_p), ("group", C.c_int32), ("dtype", C.c_int32)]
+
+
+class IdkmInt8Desc(C.Structure):
+    _fields_ = [("W8", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("ldw", C.c_int64), ("scale", C.c_void_p), ("dtype", C.c_int32)]
 
 
 class IdkmLimits(C.Structure):
@@ -139,7 +144,22 @@ def load_library():
     lib.idkm_codes_linear_backward_workspace.restype = i64
     lib.idkm_codes_linear_backward.argtypes = [vp, desc, vp, i64, vp, i64, i64, vp, i64, vp, vp, vp, i64, vp]
     lib.idkm_codes_linear_backward.restype = C.c_int
-    f32 = C.c_float
+    f32, int8 = C.c_float, C.POINTER(IdkmInt8Desc)
+    lib.idkm_int8_rows.argtypes = [vp, vp, i64, i64, i64, C.c_int, vp, i64, vp, vp]
+    lib.idkm_int8_rows.restype = C.c_int
+    for name in ("idkm_int8_linear_workspace", "idkm_int8_linear_backward_workspace"):
+        getattr(lib, name).argtypes = [int8, i64]
+        getattr(lib, name).restype = i64
+    lib.idkm_int8_linear.argtypes = [vp, int8, vp, i64, i64, vp, i64, vp, i64, vp]
+    lib.idkm_int8_linear.restype = C.c_int
+    lib.idkm_int8_linear_backward.argtypes = [vp, int8, vp, i64, i64, vp, i64, vp, i64, vp]
+    lib.idkm_int8_linear_backward.restype = C.c_int
+    lib.idkm_codes_linear_backward_kept.argtypes = [vp, desc, vp, vp, vp, i64, i64, vp, i64, vp, vp, vp, i64, vp]
+    lib.idkm_codes_linear_backward_kept.restype = C.c_int
+    lib.idkm_keep8.argtypes = [vp, vp, i64, i64, i64, C.c_int, vp, vp, vp]
+    lib.idkm_keep8.restype = C.c_int
+    lib.idkm_restore8.argtypes = [vp, vp, vp, i64, i64, C.c_int, vp, i64, vp]
+    lib.idkm_restore8.restype = C.c_int
     lib.idkm_embedding.argtypes = [vp, vp, i64, i64, vp, i32, i64, f32, vp, i64, C.c_int, vp]
     lib.idkm_embedding.restype = C.c_int
     lib.idkm_embedding_backward_workspace.argtypes = [i64, i64, i64]
@@ -305,6 +325,64 @@ class CodesLayer:
             lib = load_library()
             b = (lib.idkm_codes_embedding_backward_workspace if lookup else
                  lib.idkm_codes_linear_backward_workspace if backward else lib.idkm_codes_linear_workspace)(self._at, n)
+            if len(self._bytes) > 4096:
+                self._bytes.clear()
+            self._bytes[key] = b
+        return b
+
+
+class Kept8:
+    """Activations [n, cols] of `dtype` in 8 bits, as Context.keep8 gives them: Q int8 [n, 32 b] and the powers of two E uint8 [n, b] of
+    blocks of 32 columns, b = ceil(cols / 32)."""
+
+    def __init__(self, Q, E, cols, dtype):
+        torch, blocks = _t(), -(-cols // 32)
+        if Q.dim() != 2 or Q.dtype is not torch.int8 or Q.shape[1] != 32 * blocks or not Q.is_contiguous() or not Q.is_cuda:
+            raise TypeError(f"Q must be contiguous int8 of shape (n, {32 * blocks}) in device memory")
+        if E.dtype is not torch.uint8 or E.shape != (Q.shape[0], blocks) or not E.is_contiguous() or E.device != Q.device:
+            raise TypeError(f"E must be contiguous uint8 of shape {(Q.shape[0], blocks)} beside Q")
+        self.Q, self.E, self.cols, self.dtype = Q, E, cols, dtype
+        self.code = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}.get(dtype)
+        if self.code is None:
+            raise TypeError(f"dtype must be float32, float16 or bfloat16, got {dtype}")
+        self.device, self.shape = Q.get_device(), (Q.shape[0], cols)
+
+
+class Int8Layer:
+    """A [rows, cols] layer in 8-bit integers W8 (int8) with a float32 scale [rows] for each row, for activations of `dtype`.  Context.int8_layer
+    makes one of weights or of a stored layer.  The integers are laid out here, once, in whole steps of 128 columns; W8 itself is used where it has those
+    and is aligned (and may then be changed in place, as may the scales).  cols: of W8's columns the first `cols` are the layer's."""
+
+    def __init__(self, W8, scale, dtype, cols=None):
+        torch = _t()
+        if not isinstance(W8, torch.Tensor) or not W8.is_cuda or W8.dtype is not torch.int8 or W8.dim() != 2 or not W8.is_contiguous():
+            raise TypeError("W8 must be a contiguous int8 matrix in device memory")
+        rows, width = W8.shape
+        cols = width if cols is None else int(cols)
+        if rows < 1 or not 1 <= cols <= width:
+            raise ValueError(f"rows and cols must be at least 1, got {rows} x {cols} of {width}")
+        self.code = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}.get(dtype)
+        if self.code is None:
+            raise TypeError(f"dtype must be float32, float16 or bfloat16, got {dtype}")
+        self.device, self.dtype, self.rows, self.cols = W8.get_device(), dtype, rows, cols
+        s = _flat(scale, torch.float32, (rows,), self.device, "scale")
+        if width % 128 or W8.data_ptr() % 16:
+            laid = W8.new_zeros(rows, -(-cols // 128) * 128)
+            laid[:, :cols] = W8[:, :cols]
+            W8 = laid
+        self.W8, self.scale = W8, scale
+        self._desc = IdkmInt8Desc(W8.data_ptr(), rows, cols, W8.shape[1], s, self.code)
+        self._at = C.byref(self._desc)
+        self._bytes = {}  # workspace sizes by (tokens, backward)
+        if load_library().idkm_int8_linear_workspace(self._at, 0) < 0:
+            raise ValueError(f"a layer of {rows} x {cols} is not supported")
+
+    def workspace_bytes(self, n, backward=False):
+        key = (n, backward)
+        b = self._bytes.get(key)
+        if b is None:
+            lib = load_library()
+            b = (lib.idkm_int8_linear_backward_workspace if backward else lib.idkm_int8_linear_workspace)(self._at, n)
             if len(self._bytes) > 4096:
                 self._bytes.clear()
             self._bytes[key] = b
@@ -477,16 +555,19 @@ class Context:
 
     def codes_linear_backward(self, layer, X, dY, want_dX=True, want_dC=True, want_dS=True):
         """idkm_codes_linear_backward: dict of dX [n, cols] in the layer's type and float32 dC [k, d] and, for a layer with
-        scales, dS [rows, groups].  X may be None if only dX is wanted."""
+        scales, dS [rows, groups].  X may be None if only dX is wanted, and may be a Kept8."""
         torch, dev = _t(), self.device
         if layer.device != dev:
             raise TypeError(f"the layer must be in the memory of device {dev}")
         ldy = _rows(dY, layer.dtype, layer.rows, dev, "dY")
         n = dY.shape[0]
         want_dS = want_dS and layer.S is not None
-        ldx = 0
+        ldx, kept = 0, isinstance(X, Kept8)
         if X is not None:
-            ldx = _rows(X, layer.dtype, layer.cols, dev, "X")
+            if not kept:
+                ldx = _rows(X, layer.dtype, layer.cols, dev, "X")
+            elif X.dtype is not layer.dtype or X.cols != layer.cols or X.device != dev:
+                raise TypeError(f"X must be {layer.dtype} of shape (n, {layer.cols}), kept in the memory of device {dev}")
             if X.shape[0] != n:
                 raise TypeError(f"X must have {n} rows")
         elif want_dC or want_dS:
@@ -501,10 +582,114 @@ class Context:
         need = layer.workspace_bytes(n, True)
         ws = dY.new_empty(need, dtype=torch.uint8) if need > 0 else None
         at = {key: t.data_ptr() for key, t in res.items()}
-        self._check(self._lib.idkm_codes_linear_backward(
-            self._h, layer._at, X.data_ptr() if X is not None else None, ldx, dY.data_ptr(), ldy, n, at.get("dX"), layer.cols,
-            at.get("dC"), at.get("dS"), ws.data_ptr() if need > 0 else None, need, self._raw_stream()))
+        rest = (dY.data_ptr(), ldy, n, at.get("dX"), layer.cols, at.get("dC"), at.get("dS"), ws.data_ptr() if need > 0 else None, need,
+                self._raw_stream())
+        if kept:
+            st = self._lib.idkm_codes_linear_backward_kept(self._h, layer._at, X.Q.data_ptr(), X.E.data_ptr(), *rest)
+        else:
+            st = self._lib.idkm_codes_linear_backward(self._h, layer._at, X.data_ptr() if X is not None else None, ldx, *rest)
+        self._check(st)
         return res
+
+    def keep8(self, X):
+        """idkm_keep8: X [n, cols] in 8 bits, a Kept8 that restore8 and codes_linear_backward take."""
+        torch = _t()
+        if not isinstance(X, torch.Tensor) or X.dim() != 2:
+            raise TypeError("X must be a matrix")
+        code, (n, cols) = _dtype(X, "X"), X.shape
+        ldx = _rows(X, X.dtype, cols, self.device, "X")
+        blocks = -(-cols // 32)
+        Q, E = X.new_empty(n, 32 * blocks, dtype=torch.int8), X.new_empty(n, blocks, dtype=torch.uint8)
+        st = self._lib.idkm_keep8(self._h, X.data_ptr(), n, cols, ldx, code, Q.data_ptr(), E.data_ptr(), self._raw_stream())
+        if st:
+            self._check(st)
+        return Kept8(Q, E, cols, X.dtype)
+
+    def restore8(self, kept, out=None):
+        """idkm_restore8: the activations [n, cols] that `kept` stands for, in their type."""
+        if kept.device != self.device:
+            raise TypeError(f"the activations must be in the memory of device {self.device}")
+        n, cols = kept.shape
+        if out is None:
+            out, ldx = kept.Q.new_empty(n, cols, dtype=kept.dtype), cols
+        else:
+            ldx = _rows(out, kept.dtype, cols, self.device, "out")
+            if out.shape[0] != n:
+                raise TypeError(f"out must have {n} rows")
+        st = self._lib.idkm_restore8(self._h, kept.Q.data_ptr(), kept.E.data_ptr(), n, cols, kept.code, out.data_ptr(), ldx, self._raw_stream())
+        if st:
+            self._check(st)
+        return out
+
+    def _int8_rows(self, X):
+        """The same in whole steps of 128 columns."""
+        torch = _t()
+        if not isinstance(X, torch.Tensor) or X.dim() != 2:
+            raise TypeError("X must be a matrix")
+        code, (n, cols) = _dtype(X, "X"), X.shape
+        ldx = _rows(X, X.dtype, cols, self.device, "X")
+        Q, scale = X.new_empty(n, -(-cols // 128) * 128, dtype=torch.int8), X.new_empty(n, dtype=torch.float32)
+        st = self._lib.idkm_int8_rows(self._h, X.data_ptr(), n, cols, ldx, code, Q.data_ptr(), Q.shape[1], scale.data_ptr(), self._raw_stream())
+        if st:
+            self._check(st)
+        return Q, scale
+
+    def int8_rows(self, X):
+        """idkm_int8_rows: (Q int8 [n, cols], scale float32 [n]) of X [n, cols], rows of any of the three types."""
+        Q, scale = self._int8_rows(X)
+        return Q[:, :X.shape[1]], scale
+
+    def int8_layer(self, weights, dtype=None):
+        """An Int8Layer of a matrix [rows, cols] of weights, or of a CodesLayer, whose weights are written out for it (in float32, 2^26 at a time); for
+        activations of `dtype` (the weights' own unless given)."""
+        torch, dtype = _t(), dtype or weights.dtype
+        if not isinstance(weights, CodesLayer):
+            return Int8Layer(*self._int8_rows(weights), dtype, weights.shape[1])
+        rows, cols = weights.rows, weights.cols
+        wide = CodesLayer(weights.words, rows, cols, weights.C.float(), weights.S, weights.group)
+        panel, parts = max(1, 2 ** 26 // cols), []
+        for r in range(0, rows, panel):
+            ids = torch.arange(r, min(r + panel, rows), device=weights.words.device)
+            parts.append(self._int8_rows(self.codes_embedding(wide, ids)))
+        Q, scale = (part[0] if len(parts) == 1 else torch.cat(part) for part in zip(*parts))
+        return Int8Layer(Q, scale, dtype, cols)
+
+    def int8_linear(self, layer, X, out=None):
+        """idkm_int8_linear: X [n, cols] in the layer's type -> Y [n, rows], the product of X's rows and an Int8Layer's in 8-bit integers."""
+        dev = self.device
+        if layer.device != dev:
+            raise TypeError(f"the layer must be in the memory of device {dev}")
+        ldx = _rows(X, layer.dtype, layer.cols, dev, "X")
+        n = X.shape[0]
+        if out is None:
+            out, ldy = X.new_empty(n, layer.rows), layer.rows
+        else:
+            ldy = _rows(out, layer.dtype, layer.rows, dev, "out")
+            if out.shape[0] != n:
+                raise TypeError(f"out must have {n} rows")
+        need = layer.workspace_bytes(n)
+        ws = X.new_empty(need, dtype=_t().uint8) if need > 0 else None
+        st = self._lib.idkm_int8_linear(self._h, layer._at, X.data_ptr(), n, ldx, out.data_ptr(), ldy, ws.data_ptr() if need > 0 else None, need,
+                                        self._raw_stream())
+        if st:
+            self._check(st)
+        return out
+
+    def int8_linear_backward(self, layer, dY):
+        """idkm_int8_linear_backward: dX [n, cols] from dY [n, rows], both in the layer's type."""
+        dev = self.device
+        if layer.device != dev:
+            raise TypeError(f"the layer must be in the memory of device {dev}")
+        ldy = _rows(dY, layer.dtype, layer.rows, dev, "dY")
+        n = dY.shape[0]
+        dX = dY.new_empty(n, layer.cols)
+        need = layer.workspace_bytes(n, True)
+        ws = dY.new_empty(need, dtype=_t().uint8) if need > 0 else None
+        st = self._lib.idkm_int8_linear_backward(self._h, layer._at, dY.data_ptr(), ldy, n, dX.data_ptr(), layer.cols,
+                                                 ws.data_ptr() if need > 0 else None, need, self._raw_stream())
+        if st:
+            self._check(st)
+        return dX
 
     def _tokens(self, ids):
         """Address, bytes of an id and number of tokens' ids, int32 or int64 and contiguous in one dimension."""

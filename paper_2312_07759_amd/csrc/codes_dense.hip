@@ -94,9 +94,10 @@ void launch_dense_cols(int dtype, const DenseArgs& args, hipStream_t s) {
     });
 }
 
-void add_operand(OperandArgs* a, const void* in, int64_t ldi, int64_t M, int64_t N, void* out, int64_t pad, bool transposed) {
+void add_operand(OperandArgs* a, const void* in, int64_t ldi, int64_t M, int64_t N, void* out, int64_t pad, bool transposed, const uint8_t* E,
+                 const float* scale) {
     Operand& o = a->job[a->jobs++];
-    o = Operand{in, ldi, M, N, out, pad, transposed, 0, 0};
+    o = Operand{in, ldi, M, N, out, pad, transposed, 0, 0, E, scale};
     o.tiles_n = ((transposed ? N : pad) + 63) / 64;
     o.tiles = o.tiles_n * (((transposed ? pad : M) + 63) / 64);
 }

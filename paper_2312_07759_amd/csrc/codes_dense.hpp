@@ -1,6 +1,7 @@
 // Kernels around the tile product: layers written out as matrices, operands padded and transposed, parts of a sum joined.
 #pragma once
 #include "codes_product.hpp"
+#include "keep8.hpp"
 
 namespace idkm {
 
@@ -327,6 +328,9 @@ __global__ __launch_bounds__(256) void k_dense_cols(const DenseArgs a) {
 // Operands brought to the form in which the tile product takes them, several in one launch.
 //   rows        out[M, pad] = in[M, N], zero behind column N
 //   transposed  out[N, pad] = in[M, N]^T, zero behind column M
+// E: `in` is kept in 8 bits, rows ldi apart (see keep8.hpp), and brought back on the way.
+// scale: `in` holds 8-bit integers (rows ldi apart, a multiple of 16, zero behind column N), and comes out times its row's scale, rounded to T: an operand of the
+// matrix instruction, with the relative error, eps / 2 at most, of a weight stored in T.
 struct Operand {
     const void* in;
     int64_t ldi, M, N;
@@ -334,6 +338,8 @@ struct Operand {
     int64_t pad;
     int transposed;
     int64_t tiles, tiles_n;  // of 64 x 64, and along N (rows: along pad)
+    const uint8_t* E;        // [M, ldi / 32] or null
+    const float* scale;      // [M] or null
 };
 struct OperandArgs {
     Operand job[3];
@@ -353,7 +359,22 @@ __global__ __launch_bounds__(256) void k_operands(const OperandArgs a) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
         const T* row = static_cast<const T*>(o.in) + (m + b) * o.ldi;
-        if (m + b < o.M && n + 8 <= o.N) {
+        if (o.scale) {
+            const bool there = m + b < o.M && n < o.N;
+            const u32x2 q = *reinterpret_cast<const u32x2*>(static_cast<const int8_t*>(o.in) + (there ? (m + b) * o.ldi + n : 0));
+            const float by = o.scale[there ? m + b : 0];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[b].v[e] = there ? Elem<T>::down((float)(int8_t)(q[e >> 2] >> (e & 3) * 8) * by) : (T)0.f;
+        } else if (o.E) {
+            const bool there = m + b < o.M && n < o.N;
+            const int64_t at = there ? (m + b) * o.ldi + n : 0;
+            const u32x2 q = *reinterpret_cast<const u32x2*>(static_cast<const int8_t*>(o.in) + at);
+            const int field = o.E[at / KEEP_BLOCK];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[b].v[e] = there ? Keep8<T>::value((int8_t)(q[e >> 2] >> (e & 3) * 8), field) : (T)0.f;
+        } else if (m + b < o.M && n + 8 <= o.N) {
             u32x4 raw[8 / Elem<T>::PER16];
 #pragma unroll
             for (int f = 0; f < 8 / Elem<T>::PER16; ++f) raw[f] = reinterpret_cast<const u32x4_any*>(row + n)[f];

@@ -9,6 +9,7 @@ namespace idkm {
 typedef _Float16 f16;
 typedef __bf16 bf16;
 typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef int intx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x2 u32x2_word __attribute__((aligned(4)));
@@ -41,16 +42,33 @@ struct Elem<bf16> {
     static __device__ bf16 nan() { return (bf16)__builtin_nanf(""); }
 };
 
+template <>
+struct Elem<int8_t> {
+    static constexpr int PER16 = 16;
+};
+
+// What the matrix core sums in: float32, and 32-bit integers for 8-bit ones.
+template <typename T>
+struct Sum {
+    typedef floatx4 four;
+};
+template <>
+struct Sum<int8_t> {
+    typedef intx4 four;
+};
+
 // acc[r] += sum over the fragments' elements of a[4 q + r] b[i]: the 16 x 16 block a b^T with the rows of a along acc's
 // registers (lane l: i = l % 16 is its row of a and of b on input and its row of b on output, q = l / 16).  A lane holds 16
 // bytes of its row: for 16-bit types elements 8 q .. 8 q + 7 of 32 in one instruction, for float elements 4 q .. 4 q + 3
-// of 16, of which instruction e takes element e of every lane.  Sums are float32 in the matrix core.
+// of 16, of which instruction e takes element e of every lane, for 8-bit integers elements 16 q .. 16 q + 15 of 64.
 template <typename T>
-__device__ __forceinline__ void mma16(floatx4& acc, u32x4 a, u32x4 b) {
+__device__ __forceinline__ void mma16(typename Sum<T>::four& acc, u32x4 a, u32x4 b) {
     if constexpr (sizeof(T) == 4) {
         const floatx4 fa = __builtin_bit_cast(floatx4, a), fb = __builtin_bit_cast(floatx4, b);
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[e], fb[e], acc, 0, 0, 0);
+    } else if constexpr (sizeof(T) == 1) {
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(intx4, a), __builtin_bit_cast(intx4, b), acc, 0, 0, 0);
     } else if constexpr (__is_same(T, f16)) {
         acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
     } else {

@@ -59,7 +59,7 @@ idkm_status launched(idkm_ctx* ctx, Launches launches) {
     return e == hipSuccess ? IDKM_OK : refuse(ctx, IDKM_ERR_DEVICE, hipGetErrorString(e));
 }
 
-inline int esize_of(int dtype) { return dtype == IDKM_F32 ? 4 : 2; }
+inline int esize_of(int dtype) { return dtype == IDKM_F32 ? 4 : dtype == TP_INT8 ? 1 : 2; }
 inline bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 inline const char* wrong_layer(const idkm_codes_desc* w, idkm_status* st) {

@@ -18,6 +18,14 @@ static TileShape shape_of(int which, int scaled) {
             case 0: return shape<T, 128, 128, 2, 4, 3>(256, 2.03f);
             case 1: return shape<T, 64, 64, 2, 2, 4>(512, 1.1f);
         }
+    } else if constexpr (sizeof(T) == 1) {
+        switch (which) {
+            case 0: return shape<T, 256, 256, 2, 4, 2>(256, 2.0f);
+            case 1: return shape<T, 256, 128, 4, 4, 3>(256, 1.0f);
+            case 2: return shape<T, 128, 128, 2, 4, 2>(512, 1.02f);
+            case 3: return shape<T, 128, 128, 2, 4, 4>(256, 0.56f);
+            case 4: return shape<T, 64, 64, 2, 2, 4>(512, 0.41f);
+        }
     } else if (scaled == 0) {
         switch (which) {
             case 0: return shape<T, 256, 256, 2, 4, 2>(256, 2.0f);
@@ -47,6 +55,7 @@ static TileShape shape_of(int which, int scaled) {
 TileShape tile_shape(int dtype, int which, int scaled) {
     if (dtype == 0) return shape_of<float>(which, scaled);
     if (dtype == 1) return shape_of<f16>(which, scaled);
+    if (dtype == TP_INT8) return shape_of<int8_t>(which, 0);
     return shape_of<bf16>(which, scaled);
 }
 

@@ -1,0 +1,81 @@
+// Activations to 8 bits and back.
+#include "keep8.hpp"
+#include "layers.h"
+
+namespace idkm {
+
+// Four threads to a block of 32 columns, eight columns each.
+template <typename T>
+__global__ __launch_bounds__(256) void k_keep8(const KeepArgs a) {
+    const int64_t pieces = a.n * a.blocks * 4;
+    for (int64_t base = (int64_t)blockIdx.x * 256; base < pieces; base += (int64_t)gridDim.x * 256) {
+        const int64_t at = min(base + threadIdx.x, pieces - 1);  // the last threads repeat the last piece: all take part in the exchange
+        const int64_t b = at >> 2, t = b / a.blocks, c = (b - t * a.blocks) * KEEP_BLOCK + (at & 3) * 8;
+        const T* x = static_cast<const T*>(a.X) + t * a.ldx + c;
+        struct alignas(16) Eight { T v[8]; } y;
+        if (c + 8 <= a.cols) {
+            u32x4 raw[8 / Elem<T>::PER16];
+#pragma unroll
+            for (int f = 0; f < 8 / Elem<T>::PER16; ++f) raw[f] = reinterpret_cast<const u32x4_any*>(x)[f];
+            __builtin_memcpy(&y, raw, sizeof(y));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y.v[e] = c + e < a.cols ? x[e] : (T)0.f;
+        }
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t size = __builtin_bit_cast(uint32_t, Elem<T>::up(y.v[e])) & 0x7fffffff;
+            top = size < 0x7f800000 ? max(top, size) : top;
+        }
+        top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+        const int field = Keep8<T>::field(top);
+        uint32_t q[2] = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[e >> 2] |= ((uint32_t)Keep8<T>::quotient(Elem<T>::up(y.v[e]), field) & 255u) << (e & 3) * 8;
+        if (base + threadIdx.x < pieces) {
+            *reinterpret_cast<u32x2*>(a.Q + at * 8) = u32x2{q[0], q[1]};
+            if ((at & 3) == 0) a.E[b] = (uint8_t)field;
+        }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_restore8(const KeepArgs a) {
+    const int64_t pieces = a.n * a.blocks * 4;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < pieces; at += (int64_t)gridDim.x * 256) {
+        const int64_t b = at >> 2, t = b / a.blocks, c = (b - t * a.blocks) * KEEP_BLOCK + (at & 3) * 8;
+        const u32x2 q = *reinterpret_cast<const u32x2*>(a.Q + at * 8);
+        const int field = a.E[b];
+        T* x = static_cast<T*>(a.X) + t * a.ldx + c;
+        struct alignas(16) Eight { T v[8]; } y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y.v[e] = Keep8<T>::value((int8_t)(q[e >> 2] >> (e & 3) * 8), field);
+        if (c + 8 <= a.cols) {
+            u32x4 raw[8 / Elem<T>::PER16];
+            __builtin_memcpy(raw, &y, sizeof(y));
+#pragma unroll
+            for (int f = 0; f < 8 / Elem<T>::PER16; ++f) reinterpret_cast<u32x4_any*>(x)[f] = raw[f];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e < a.cols) x[e] = y.v[e];
+        }
+    }
+}
+
+static unsigned grid_of(int64_t threads) {
+    const int64_t g = (threads + 255) / 256;
+    return (unsigned)(g < 1 ? 1 : g > 8192 ? 8192 : g);
+}
+
+void launch_keep8(int dtype, const KeepArgs& a, hipStream_t s) {
+    BY_TYPE(dtype, T, hipLaunchKernelGGL(k_keep8<T>, dim3(grid_of(a.n * a.blocks * 4)), dim3(256), 0, s, a));
+}
+
+void launch_restore8(int dtype, const KeepArgs& a, hipStream_t s) {
+    BY_TYPE(dtype, T, hipLaunchKernelGGL(k_restore8<T>, dim3(grid_of(a.n * a.blocks * 4)), dim3(256), 0, s, a));
+}
+
+}  // namespace idkm

@@ -42,6 +42,7 @@ struct TileShape {
     int resident;  // workgroups that the device holds at once
     float us;      // of a step of all of them
 };
+constexpr int TP_INT8 = 3;  // beside idkm_dtype's
 // The shapes of a type's tile product, from 0 on; fn = nullptr behind the last.  scaled: SC of k_tile_product, 16-bit types only.
 TileShape tile_shape(int dtype, int which, int scaled);
 
@@ -49,7 +50,8 @@ void launch_dense_rows(int dtype, const DenseArgs& a, hipStream_t s);
 void launch_dense_cols(int dtype, const DenseArgs& a, hipStream_t s);
 void allow_lds(const void* fn, size_t bytes);  // before a launch of fn with so much dynamic LDS
 // Up to three operands to a launch.
-void add_operand(OperandArgs* a, const void* in, int64_t ldi, int64_t M, int64_t N, void* out, int64_t pad, bool transposed);
+void add_operand(OperandArgs* a, const void* in, int64_t ldi, int64_t M, int64_t N, void* out, int64_t pad, bool transposed,
+                 const uint8_t* E = nullptr, const float* scale = nullptr);
 void launch_operands(int dtype, const OperandArgs& a, hipStream_t s);
 void launch_join_parts(int dtype, const float* parts, int nz, int64_t M, int64_t N, void* out, int64_t ldo, hipStream_t s);
 void launch_codes_bins(int dtype, const BinArgs& a, int grid, int waves, hipStream_t s);
@@ -59,6 +61,37 @@ void launch_fill_zero(float* out, int64_t n, hipStream_t s);
 // dC from bins [kd][n] (null: not), dS from segments (null: not); listed, listed_count: see BinArgs, `rows` at most then.
 void launch_join_gradients(const float* bins, int64_t n, int kd, float* dC, const float* segments, int64_t rows, int64_t cols, int group,
                            int groups, float* dS, hipStream_t s, const int32_t* listed = nullptr, const int32_t* listed_count = nullptr);
+
+void launch_keep8(int dtype, const KeepArgs& a, hipStream_t s);
+void launch_restore8(int dtype, const KeepArgs& a, hipStream_t s);
+
+// Rows in 8-bit integers: Q [n, ldq], zero behind column cols, and their scales.
+struct Int8RowsArgs {
+    const void* X;  // T [n, ldx]
+    int64_t n, cols, ldx;
+    int8_t* Q;
+    int64_t ldq;  // a multiple of 16
+    float* scale;
+};
+void launch_int8_rows(int dtype, const Int8RowsArgs& a, hipStream_t s);
+
+// Up to a few dozen tokens times a layer of 8-bit integers.
+struct Int8FewArgs {
+    const int8_t* W8;  // [rows, ldw]
+    int64_t rows, ldw;
+    const float* scale;  // [rows]
+    const int8_t* Q;     // [n, pad], or null: X itself is brought to integers by every workgroup
+    const float* q_scale;
+    const void* X;  // T [n, ldx]
+    int64_t cols, pad, ldx, n;  // pad: cols in whole steps of 128, Q's rows
+    void* Y;  // T [n, ldy]
+    int64_t ldy;
+};
+constexpr int64_t INT8_FUSED = 4 * 8192;  // elements of X that a workgroup brings to integers itself, at most
+void launch_int8_few(int dtype, const Int8FewArgs& a, hipStream_t s);
+// out[M, N] in the type of dtype = by_m by_n times the sum of the parts [nz][M, N].
+void launch_join_int8(int dtype, const int32_t* parts, int nz, int64_t M, int64_t N, const float* by_m, const float* by_n, void* out, int64_t ldo,
+                      hipStream_t s);
 
 constexpr int SCALE_FWD = 0, UNSCALE_FWD = 1, UNSCALE_BWD = 2, SCALE_BWD = 3;
 struct ScaleArgs {

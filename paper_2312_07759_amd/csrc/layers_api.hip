@@ -451,6 +451,165 @@ GradLayout grad_layout(const idkm_codes_desc& w, int64_t n) {
     return g;
 }
 
+// The input of a product, as it is (rows ld apart) or kept in 8 bits with the bytes E (rows of whole blocks).
+struct Input {
+    const void* X;
+    int64_t ld;
+    const uint8_t* E;
+    bool kept;
+};
+
+idkm_status gradients(idkm_ctx* ctx, const idkm_codes_desc* w, const Input& x, const void* dY, int64_t lddy, int64_t n, void* dX, int64_t lddx,
+                      float* dC, float* dS, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+    return entry(ctx, [&]() -> idkm_status {
+        idkm_status st;
+        if (const char* e = wrong_layer(w, &st)) return refuse(ctx, st, e);
+        if (n < 0) return refuse(ctx, IDKM_ERR_INVALID_ARG, "n must be >= 0");
+        if (n > MAX_SIDE) return refuse(ctx, IDKM_ERR_UNSUPPORTED, "too many tokens");
+        if (dS && !w->S) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dS of a layer without scales");
+        if (!aligned_to(dC, 4) || !aligned_to(dS, 4)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dC and dS must be aligned to their type");
+        hipStream_t s = (hipStream_t)hip_stream;
+        const int es = esize_of(w->dtype), groups = groups_of(*w);
+        if (n == 0)
+            return launched(ctx, [&] {
+                if (dC) launch_fill_zero(dC, (int64_t)w->k * w->d, s);
+                if (dS) launch_fill_zero(dS, w->rows * groups, s);
+            });
+        const bool layer = dC || dS;
+        if (!dX && !layer) return IDKM_OK;
+        if (!dY || lddy < w->rows) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dY must be non-NULL and lddy >= rows");
+        if (layer && x.kept && (!x.X || !x.E)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "Q and E must be non-NULL");
+        if (layer && (!x.X || x.ld < w->cols)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "X must be non-NULL and ldx >= cols");
+        if (dX && lddx < w->cols) return refuse(ctx, IDKM_ERR_INVALID_ARG, "lddx must be >= cols");
+        if (!aligned_to(dY, es) || !aligned_to(x.X, x.kept ? 8 : es) || !aligned_to(dX, es))
+            return refuse(ctx, IDKM_ERR_INVALID_ARG, "X, dY and dX must be aligned to their type");
+        const GradLayout g = grad_layout(*w, n);
+        const bool together = g.together && dX && layer;
+        if (const char* e = wrong_workspace(workspace, workspace_bytes, g.bytes)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
+        unsigned char* ws = static_cast<unsigned char*>(workspace);
+        return launched(ctx, [&] {
+            const ProductLayout& d = g.d;
+            const LayerGradLayout& l = g.l;
+            TileArgs td{};
+            OperandArgs copies{};
+            if (dX) operand_of(w->dtype, dY, lddy, n, w->rows, d, ws, &td, &copies);
+            unsigned char* of_x = ws;
+            ws += d.bytes;
+            if (layer) {
+                add_operand(&copies, dY, lddy, n, w->rows, ws + l.dy, l.pad, true);
+                add_operand(&copies, x.X, x.ld, n, w->cols, ws + l.x, l.pad, true, x.kept ? x.E : nullptr);
+            }
+            launch_operands(w->dtype, copies, s);
+            if (dX) {
+                for (int64_t c = 0; c < w->cols; c += d.panel) {
+                    DenseArgs a = dense_of(*w);
+                    a.first = c;
+                    a.count = w->cols - c < d.panel ? w->cols - c : d.panel;
+                    a.pad = d.pad;
+                    a.out = of_x + d.matrix;
+                    launch_dense_cols(w->dtype, a, s);
+                    td.N = a.count;
+                    float* parts = reinterpret_cast<float*>(of_x + d.parts);
+                    if (together) set_out(d.plan, &td, dX, lddx, parts);
+                    else run_product(w->dtype, d.plan, td, static_cast<unsigned char*>(dX) + c * es, lddx, parts, s);
+                }
+            }
+            if (!layer) return;
+            float* bins = reinterpret_cast<float*>(ws + l.bins);
+            int64_t written = 0;
+            for (int64_t r = 0; r < w->rows; r += l.panel) {
+                const int64_t count = w->rows - r < l.panel ? w->rows - r : l.panel;
+                TileArgs t{};
+                t.A = ws + l.dy + r * l.pad * es;
+                t.lda = l.pad;
+                t.M = count;
+                t.B = ws + l.x;
+                t.ldb = l.pad;
+                t.N = w->cols;
+                t.steps = (int)(l.pad * es / TP_STEP);
+                t.wide = 1;
+                t.out = ws + l.p;
+                t.ldo = l.ldp;
+                if (!together) {
+                    run_tiles(w->dtype, l.plan, t, s);
+                } else {
+                    if ((td.steps + d.plan.parts - 1) / d.plan.parts > (t.steps + l.plan.parts - 1) / l.plan.parts)
+                        run_tiles(w->dtype, d.plan, td, s, &l.plan, &t);
+                    else
+                        run_tiles(w->dtype, l.plan, t, s, &d.plan, &td);
+                    if (d.plan.parts > 1)
+                        launch_join_parts(w->dtype, reinterpret_cast<const float*>(of_x + d.parts), d.plan.parts, n, w->cols, dX, lddx, s);
+                }
+                if (l.plan.parts > 1)
+                    launch_join_parts(IDKM_F32, reinterpret_cast<const float*>(ws + l.p), l.plan.parts, count, l.ldp, ws + l.p, l.ldp, s);
+                BinArgs b = bins_of(*w, l);
+                b.P = reinterpret_cast<const float*>(ws + l.p);
+                b.ldp = l.ldp;
+                b.pitch = l.panels * l.grid;
+                b.at = written;
+                b.first = r;
+                b.count = count;
+                b.bins = dC ? bins : nullptr;
+                b.segments = l.segmented && dS ? reinterpret_cast<float*>(ws + l.segments) : nullptr;
+                run_bins(w->dtype, l, b, dS, s);
+                written += l.grid;
+            }
+            launch_join_gradients(bins, written, w->k * w->d, dC, l.segmented && dS ? reinterpret_cast<const float*>(ws + l.segments) : nullptr, w->rows,
+                                  w->cols, l.group, l.groups, dS, s);
+        });
+    });
+}
+
+idkm_status wrong_kept(idkm_ctx* ctx, int64_t n, int64_t cols, int dtype, const void* X, int64_t ldx, const void* Q, const void* E) {
+    if (dtype != IDKM_F32 && dtype != IDKM_F16 && dtype != IDKM_BF16) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dtype must be an idkm_dtype");
+    if (n < 0 || cols < 1) return refuse(ctx, IDKM_ERR_INVALID_ARG, "need n >= 0 and cols >= 1");
+    if (n > MAX_SIDE || cols > MAX_SIDE) return refuse(ctx, IDKM_ERR_UNSUPPORTED, "too many rows or columns");
+    if (n == 0) return IDKM_OK;
+    if (!X || !Q || !E || ldx < cols) return refuse(ctx, IDKM_ERR_INVALID_ARG, "X, Q and E must be non-NULL and ldx >= cols");
+    if (!aligned_to(X, esize_of(dtype)) || !aligned_to(Q, 8)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "X must be aligned to its type and Q to 8 bytes");
+    return IDKM_OK;
+}
+
+// ---- 8-bit integers
+
+constexpr int64_t MAX_INT8_COLS = 131072;  // 127^2 times as many fit 32 bits
+
+idkm_status wrong_int8(idkm_ctx* ctx, const idkm_int8_desc* w, int64_t n) {
+    if (!w) return refuse(ctx, IDKM_ERR_INVALID_ARG, "the layer must be non-NULL");
+    if (!w->W8 || !w->scale) return refuse(ctx, IDKM_ERR_INVALID_ARG, "W8 and scale must be non-NULL");
+    if (w->dtype != IDKM_F32 && w->dtype != IDKM_F16 && w->dtype != IDKM_BF16) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dtype must be an idkm_dtype");
+    if (w->rows < 1 || w->cols < 1) return refuse(ctx, IDKM_ERR_INVALID_ARG, "rows and cols must be >= 1");
+    if (w->ldw < w->cols || w->ldw % 128 != 0) return refuse(ctx, IDKM_ERR_INVALID_ARG, "ldw must be a multiple of 128 and >= cols");
+    if (!aligned_to(w->W8, 16) || !aligned_to(w->scale, 4)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "W8 must be 16-byte aligned and scale aligned to its type");
+    if (w->rows > MAX_SIDE || w->cols > MAX_INT8_COLS || w->ldw > MAX_SIDE) return refuse(ctx, IDKM_ERR_UNSUPPORTED, "the layer is too large");
+    if (n < 0) return refuse(ctx, IDKM_ERR_INVALID_ARG, "n must be >= 0");
+    if (n > MAX_SIDE) return refuse(ctx, IDKM_ERR_UNSUPPORTED, "too many tokens");
+    return IDKM_OK;
+}
+
+// Workspace of a product: the tokens' integers and scales, the parts' sums.
+struct Int8Layout {
+    bool few, fused;
+    int64_t pad, q, scale, parts, bytes;
+    TilePlan plan;
+};
+
+Int8Layout int8_layout(const idkm_int8_desc& w, int64_t n) {
+    Int8Layout l{};
+    l.pad = up_to(w.cols, 128);  // of the sum: what lies behind in W8's rows counts for nothing
+    l.few = n <= 64;
+    l.fused = n <= 4 && n * w.cols <= INT8_FUSED;
+    l.q = 0;
+    l.scale = l.fused ? 0 : buffer(n * l.pad, 1);
+    l.parts = l.scale + (l.fused ? 0 : buffer(n, 4));
+    l.bytes = l.parts;
+    if (!l.few) {
+        l.plan = tile_plan(n, w.rows, l.pad / TP_STEP, TP_INT8, 0);
+        if (l.plan.parts > 1) l.bytes += buffer(n * w.rows * l.plan.parts, 4);
+    }
+    return l;
+}
+
 const char* wrong_scale_shape(int64_t rows, int64_t cols, int64_t group) {
     if (rows < 0 || cols < 1) return "need rows >= 0 and cols >= 1";
     if (group < 1) return "group must be >= 1";
@@ -570,100 +729,123 @@ int64_t idkm_codes_linear_backward_workspace(const idkm_codes_desc* w, int64_t n
 idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, const void* X, int64_t ldx, const void* dY, int64_t lddy,
                                        int64_t n, void* dX, int64_t lddx, float* dC, float* dS, void* workspace, int64_t workspace_bytes,
                                        void* hip_stream) {
+    return gradients(ctx, w, Input{X, ldx, nullptr, false}, dY, lddy, n, dX, lddx, dC, dS, workspace, workspace_bytes, hip_stream);
+}
+
+idkm_status idkm_codes_linear_backward_kept(idkm_ctx* ctx, const idkm_codes_desc* w, const int8_t* Q, const uint8_t* E, const void* dY, int64_t lddy,
+                                            int64_t n, void* dX, int64_t lddx, float* dC, float* dS, void* workspace, int64_t workspace_bytes,
+                                            void* hip_stream) {
+    return gradients(ctx, w, Input{Q, w ? up_to(w->cols, KEEP_BLOCK) : 0, E, true}, dY, lddy, n, dX, lddx, dC, dS, workspace, workspace_bytes, hip_stream);
+}
+
+idkm_status idkm_keep8(idkm_ctx* ctx, const void* X, int64_t n, int64_t cols, int64_t ldx, idkm_dtype dtype, int8_t* Q, uint8_t* E, void* hip_stream) {
     return entry(ctx, [&]() -> idkm_status {
-        idkm_status st;
-        if (const char* e = wrong_layer(w, &st)) return refuse(ctx, st, e);
-        if (n < 0) return refuse(ctx, IDKM_ERR_INVALID_ARG, "n must be >= 0");
-        if (n > MAX_SIDE) return refuse(ctx, IDKM_ERR_UNSUPPORTED, "too many tokens");
-        if (dS && !w->S) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dS of a layer without scales");
-        if (!aligned_to(dC, 4) || !aligned_to(dS, 4)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dC and dS must be aligned to their type");
+        if (idkm_status st = wrong_kept(ctx, n, cols, dtype, X, ldx, Q, E)) return st;
+        if (n == 0) return IDKM_OK;
+        const KeepArgs a{const_cast<void*>(X), n, cols, ldx, Q, E, (cols + KEEP_BLOCK - 1) / KEEP_BLOCK};
+        return launched(ctx, [&] { launch_keep8(dtype, a, (hipStream_t)hip_stream); });
+    });
+}
+
+idkm_status idkm_restore8(idkm_ctx* ctx, const int8_t* Q, const uint8_t* E, int64_t n, int64_t cols, idkm_dtype dtype, void* X_out, int64_t ldx,
+                          void* hip_stream) {
+    return entry(ctx, [&]() -> idkm_status {
+        if (idkm_status st = wrong_kept(ctx, n, cols, dtype, X_out, ldx, Q, E)) return st;
+        if (n == 0) return IDKM_OK;
+        const KeepArgs a{X_out, n, cols, ldx, const_cast<int8_t*>(Q), const_cast<uint8_t*>(E), (cols + KEEP_BLOCK - 1) / KEEP_BLOCK};
+        return launched(ctx, [&] { launch_restore8(dtype, a, (hipStream_t)hip_stream); });
+    });
+}
+
+idkm_status idkm_int8_rows(idkm_ctx* ctx, const void* X, int64_t n, int64_t cols, int64_t ldx, idkm_dtype dtype, int8_t* Q, int64_t ldq,
+                           float* scale, void* hip_stream) {
+    return entry(ctx, [&]() -> idkm_status {
+        if (dtype != IDKM_F32 && dtype != IDKM_F16 && dtype != IDKM_BF16) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dtype must be an idkm_dtype");
+        if (n < 0 || cols < 1) return refuse(ctx, IDKM_ERR_INVALID_ARG, "need n >= 0 and cols >= 1");
+        if (n > MAX_SIDE || cols > MAX_SIDE || ldq > MAX_SIDE) return refuse(ctx, IDKM_ERR_UNSUPPORTED, "too many rows or columns");
+        if (ldq < cols || ldq % 16 != 0) return refuse(ctx, IDKM_ERR_INVALID_ARG, "ldq must be a multiple of 16 and >= cols");
+        if (n == 0) return IDKM_OK;
+        if (!X || !Q || !scale || ldx < cols) return refuse(ctx, IDKM_ERR_INVALID_ARG, "X, Q and scale must be non-NULL and ldx >= cols");
+        if (!aligned_to(X, esize_of(dtype)) || !aligned_to(Q, 16) || !aligned_to(scale, 4))
+            return refuse(ctx, IDKM_ERR_INVALID_ARG, "X and scale must be aligned to their types and Q to 16 bytes");
+        return launched(ctx, [&] { launch_int8_rows(dtype, Int8RowsArgs{X, n, cols, ldx, Q, ldq, scale}, (hipStream_t)hip_stream); });
+    });
+}
+
+int64_t idkm_int8_linear_workspace(const idkm_int8_desc* w, int64_t n) {
+    if (wrong_int8(nullptr, w, n)) return -1;
+    return n == 0 ? 0 : int8_layout(*w, n).bytes;
+}
+
+idkm_status idkm_int8_linear(idkm_ctx* ctx, const idkm_int8_desc* w, const void* X, int64_t n, int64_t ldx, void* Y, int64_t ldy, void* workspace,
+                             int64_t workspace_bytes, void* hip_stream) {
+    return entry(ctx, [&]() -> idkm_status {
+        if (idkm_status st = wrong_int8(ctx, w, n)) return st;
+        if (n == 0) return IDKM_OK;
+        const int es = esize_of(w->dtype);
+        if (!X || !Y) return refuse(ctx, IDKM_ERR_INVALID_ARG, "X and Y must be non-NULL");
+        if (ldx < w->cols || ldy < w->rows) return refuse(ctx, IDKM_ERR_INVALID_ARG, "ldx must be >= cols and ldy >= rows");
+        if (!aligned_to(X, es) || !aligned_to(Y, es)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "X and Y must be aligned to their type");
+        const Int8Layout l = int8_layout(*w, n);
+        if (const char* e = wrong_workspace(workspace, workspace_bytes, l.bytes)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
         hipStream_t s = (hipStream_t)hip_stream;
-        const int es = esize_of(w->dtype), groups = groups_of(*w);
-        if (n == 0)
-            return launched(ctx, [&] {
-                if (dC) launch_fill_zero(dC, (int64_t)w->k * w->d, s);
-                if (dS) launch_fill_zero(dS, w->rows * groups, s);
-            });
-        const bool layer = dC || dS;
-        if (!dX && !layer) return IDKM_OK;
-        if (!dY || lddy < w->rows) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dY must be non-NULL and lddy >= rows");
-        if (layer && (!X || ldx < w->cols)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "X must be non-NULL and ldx >= cols");
-        if (dX && lddx < w->cols) return refuse(ctx, IDKM_ERR_INVALID_ARG, "lddx must be >= cols");
-        if (!aligned_to(dY, es) || !aligned_to(X, es) || !aligned_to(dX, es))
-            return refuse(ctx, IDKM_ERR_INVALID_ARG, "X, dY and dX must be aligned to their type");
-        const GradLayout g = grad_layout(*w, n);
-        const bool together = g.together && dX && layer;
-        if (const char* e = wrong_workspace(workspace, workspace_bytes, g.bytes)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
+        unsigned char* ws = static_cast<unsigned char*>(workspace);
+        int8_t* q = reinterpret_cast<int8_t*>(ws + l.q);
+        float* scale = reinterpret_cast<float*>(ws + l.scale);
+        return launched(ctx, [&] {
+            if (!l.fused) launch_int8_rows(w->dtype, Int8RowsArgs{X, n, w->cols, ldx, q, l.pad, scale}, s);
+            if (l.few) {
+                launch_int8_few(w->dtype, Int8FewArgs{w->W8, w->rows, w->ldw, w->scale, l.fused ? nullptr : q, scale, X, w->cols, l.pad, ldx, n, Y, ldy}, s);
+                return;
+            }
+            TileArgs t{};
+            t.A = q;
+            t.lda = l.pad;
+            t.M = n;
+            t.B = w->W8;
+            t.ldb = w->ldw;
+            t.N = w->rows;
+            t.steps = (int)(l.pad / TP_STEP);
+            t.by_m = scale;
+            t.by_n = w->scale;
+            t.dtype = w->dtype;
+            set_out(l.plan, &t, Y, ldy, reinterpret_cast<float*>(ws + l.parts));
+            run_tiles(TP_INT8, l.plan, t, s);
+            if (l.plan.parts > 1)
+                launch_join_int8(w->dtype, reinterpret_cast<const int32_t*>(ws + l.parts), l.plan.parts, n, w->rows, scale, w->scale, Y, ldy, s);
+        });
+    });
+}
+
+int64_t idkm_int8_linear_backward_workspace(const idkm_int8_desc* w, int64_t n) {
+    if (wrong_int8(nullptr, w, n)) return -1;
+    return n == 0 ? 0 : product_layout(w->dtype, n, w->cols, w->rows).bytes;
+}
+
+idkm_status idkm_int8_linear_backward(idkm_ctx* ctx, const idkm_int8_desc* w, const void* dY, int64_t lddy, int64_t n, void* dX, int64_t lddx,
+                                      void* workspace, int64_t workspace_bytes, void* hip_stream) {
+    return entry(ctx, [&]() -> idkm_status {
+        if (idkm_status st = wrong_int8(ctx, w, n)) return st;
+        if (n == 0) return IDKM_OK;
+        const int es = esize_of(w->dtype);
+        if (!dY || !dX) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dY and dX must be non-NULL");
+        if (lddy < w->rows || lddx < w->cols) return refuse(ctx, IDKM_ERR_INVALID_ARG, "lddy must be >= rows and lddx >= cols");
+        if (!aligned_to(dY, es) || !aligned_to(dX, es)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dY and dX must be aligned to their type");
+        const ProductLayout l = product_layout(w->dtype, n, w->cols, w->rows);
+        if (const char* e = wrong_workspace(workspace, workspace_bytes, l.bytes)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
+        hipStream_t s = (hipStream_t)hip_stream;
         unsigned char* ws = static_cast<unsigned char*>(workspace);
         return launched(ctx, [&] {
-            const ProductLayout& d = g.d;
-            const LayerGradLayout& l = g.l;
-            TileArgs td{};
+            TileArgs t{};
             OperandArgs copies{};
-            if (dX) operand_of(w->dtype, dY, lddy, n, w->rows, d, ws, &td, &copies);
-            unsigned char* of_x = ws;
-            ws += d.bytes;
-            if (layer) {
-                add_operand(&copies, dY, lddy, n, w->rows, ws + l.dy, l.pad, true);
-                add_operand(&copies, X, ldx, n, w->cols, ws + l.x, l.pad, true);
+            operand_of(w->dtype, dY, lddy, n, w->rows, l, ws, &t, &copies);
+            for (int64_t c = 0; c < w->cols; c += l.panel) {
+                t.N = w->cols - c < l.panel ? w->cols - c : l.panel;
+                add_operand(&copies, w->W8 + c, w->ldw, w->rows, t.N, ws + l.matrix, l.pad, true, nullptr, w->scale);
+                launch_operands(w->dtype, copies, s);
+                copies.jobs = 0;
+                run_product(w->dtype, l.plan, t, static_cast<unsigned char*>(dX) + c * es, lddx, reinterpret_cast<float*>(ws + l.parts), s);
             }
-            launch_operands(w->dtype, copies, s);
-            if (dX) {
-                for (int64_t c = 0; c < w->cols; c += d.panel) {
-                    DenseArgs a = dense_of(*w);
-                    a.first = c;
-                    a.count = w->cols - c < d.panel ? w->cols - c : d.panel;
-                    a.pad = d.pad;
-                    a.out = of_x + d.matrix;
-                    launch_dense_cols(w->dtype, a, s);
-                    td.N = a.count;
-                    float* parts = reinterpret_cast<float*>(of_x + d.parts);
-                    if (together) set_out(d.plan, &td, dX, lddx, parts);
-                    else run_product(w->dtype, d.plan, td, static_cast<unsigned char*>(dX) + c * es, lddx, parts, s);
-                }
-            }
-            if (!layer) return;
-            float* bins = reinterpret_cast<float*>(ws + l.bins);
-            int64_t written = 0;
-            for (int64_t r = 0; r < w->rows; r += l.panel) {
-                const int64_t count = w->rows - r < l.panel ? w->rows - r : l.panel;
-                TileArgs t{};
-                t.A = ws + l.dy + r * l.pad * es;
-                t.lda = l.pad;
-                t.M = count;
-                t.B = ws + l.x;
-                t.ldb = l.pad;
-                t.N = w->cols;
-                t.steps = (int)(l.pad * es / TP_STEP);
-                t.wide = 1;
-                t.out = ws + l.p;
-                t.ldo = l.ldp;
-                if (!together) {
-                    run_tiles(w->dtype, l.plan, t, s);
-                } else {
-                    if ((td.steps + d.plan.parts - 1) / d.plan.parts > (t.steps + l.plan.parts - 1) / l.plan.parts)
-                        run_tiles(w->dtype, d.plan, td, s, &l.plan, &t);
-                    else
-                        run_tiles(w->dtype, l.plan, t, s, &d.plan, &td);
-                    if (d.plan.parts > 1)
-                        launch_join_parts(w->dtype, reinterpret_cast<const float*>(of_x + d.parts), d.plan.parts, n, w->cols, dX, lddx, s);
-                }
-                if (l.plan.parts > 1)
-                    launch_join_parts(IDKM_F32, reinterpret_cast<const float*>(ws + l.p), l.plan.parts, count, l.ldp, ws + l.p, l.ldp, s);
-                BinArgs b = bins_of(*w, l);
-                b.P = reinterpret_cast<const float*>(ws + l.p);
-                b.ldp = l.ldp;
-                b.pitch = l.panels * l.grid;
-                b.at = written;
-                b.first = r;
-                b.count = count;
-                b.bins = dC ? bins : nullptr;
-                b.segments = l.segmented && dS ? reinterpret_cast<float*>(ws + l.segments) : nullptr;
-                run_bins(w->dtype, l, b, dS, s);
-                written += l.grid;
-            }
-            launch_join_gradients(bins, written, w->k * w->d, dC, l.segmented && dS ? reinterpret_cast<const float*>(ws + l.segments) : nullptr, w->rows,
-                                  w->cols, l.group, l.groups, dS, s);
         });
     });
 }

@@ -22,14 +22,44 @@ struct TileArgs {
     int steps;         // steps of 128 bytes along the sum
     void* out;         // T [M, ldo], or float when `wide`
     int64_t ldo;
-    int wide;          // 1: float32 sums; the z-th of `parts` parts of the sum goes to out + z M ldo
+    int wide;          // 1: float32 sums (int32 ones of 8-bit integers); the z-th of `parts` parts of the sum goes to out + z M ldo
     int tiles_m, tiles_n, parts;
     // kernels with scales: B's element c of row n stands for scales[(c / group) scale_pitch + n] times itself
     const float* scales;  // its rows go on to a multiple of 128 rows of B
     int64_t scale_pitch;
     int groups;
     int group;  // in steps (SC = 1) or in half steps (SC = 2)
+    // 8-bit integers, not wide: out[m, n] = by_m[m] by_n[n] sum, in the type that `dtype` names
+    const float* by_m;
+    const float* by_n;
+    int dtype;
 };
+
+// Four consecutive results of a row, the last ones of it fewer.
+template <typename V, typename O>
+__device__ __forceinline__ void store_four(O* o, const V* v, bool quad, int64_t have) {
+    if (quad && have >= 4) {
+        struct alignas(4 * sizeof(O)) Quad { O v[4]; } w;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) w.v[r] = v[r];
+        *reinterpret_cast<Quad*>(o) = w;
+    } else {
+        for (int r = 0; r < 4 && r < have; ++r) o[r] = v[r];
+    }
+}
+
+// .. float32 ones, rounded to the type that dtype names; at: elements from `out` on.
+__device__ __forceinline__ void store_four_as(void* out, int64_t at, int dtype, const float* v, bool quad, int64_t have) {
+    if (dtype == 0) {
+        store_four(static_cast<float*>(out) + at, v, quad, have);
+    } else if (dtype == 1) {
+        const f16 w[4] = {Elem<f16>::down(v[0]), Elem<f16>::down(v[1]), Elem<f16>::down(v[2]), Elem<f16>::down(v[3])};
+        store_four(static_cast<f16*>(out) + at, w, quad, have);
+    } else {
+        const bf16 w[4] = {Elem<bf16>::down(v[0]), Elem<bf16>::down(v[1]), Elem<bf16>::down(v[2]), Elem<bf16>::down(v[3])};
+        store_four(static_cast<bf16*>(out) + at, w, quad, have);
+    }
+}
 
 // One product, or two that do not depend on each other in one launch: the workgroups of the first come first.
 struct TileJobs {
@@ -119,11 +149,11 @@ __global__ __launch_bounds__(64 * WM * WN, SC > 0 ? 2 : 1) void k_tile_product(c
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src[p] + off),
                                              (__attribute__((address_space(3))) void*)(to + (wave * PPW + p) * 1024), 16, 0, 0);
     };
-    floatx4 acc[TM][TN];
+    typename Sum<T>::four acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < TN; ++j) acc[i][j] = typename Sum<T>::four{0, 0, 0, 0};
 
     const int wm = wave / WN, wn = wave % WN;
     const int li = lane & 15, q = lane >> 4;
@@ -208,7 +238,18 @@ __global__ __launch_bounds__(64 * WM * WN, SC > 0 ? 2 : 1) void k_tile_product(c
         for (int j = 0; j < TN; ++j) {
             const int64_t n = n0 + wn * (BN / WN) + j * 16 + q * 4;
             if (n >= a.N) continue;
-            if (a.wide) {
+            if constexpr (sizeof(T) == 1) {
+                if (a.wide) {
+                    const int v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                    store_four(static_cast<int*>(a.out) + ((int64_t)z * a.M + m) * a.ldo + n, v, quad, a.N - n);
+                } else {
+                    const float by = a.by_m[m];
+                    float v[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v[r] = (float)acc[i][j][r] * by * a.by_n[min(n + r, a.N - 1)];
+                    store_four_as(a.out, m * a.ldo + n, a.dtype, v, quad, a.N - n);
+                }
+            } else if (a.wide) {
                 float* o = static_cast<float*>(a.out) + ((int64_t)z * a.M + m) * a.ldo + n;
                 if (quad && n + 4 <= a.N) {
                     *reinterpret_cast<floatx4*>(o) = acc[i][j];
