@@ -1,7 +1,7 @@
 // Host-side launches of the lookups in tables, stored and float32, and of their gradients.
 #pragma once
 #include "codes_gradient.hpp"
-#include "token_sort.hpp"
+#include "lookup_gradient.hpp"
 
 namespace idkm {
 
@@ -23,9 +23,10 @@ struct LookupArgs {
 void launch_lookup_table(int dtype, const LookupArgs& a, hipStream_t s);
 void launch_lookup_codes(int dtype, const LookupArgs& a, hipStream_t s);
 
-// Workspace of a sort, in int32: the order, a second one and counts where there are more than RANK_TOKENS tokens.
+// Workspace of a sort, in int32: the order, a second one and counts where there are more than GROUP_TOKENS tokens.
 int64_t sort_words(int64_t n);
-TokenOrder launch_sort(const TokenIds& ids, int32_t* workspace, hipStream_t s);
+// clear: `count` floats that are set to zero on the way.
+TokenOrder launch_sort(const TokenIds& ids, int32_t* workspace, float* clear, int64_t count, hipStream_t s);
 
 // The different rows among sorted tokens: index_at[p] of the row at place p, row_of[index], and their number.
 struct RowsOfTokens {
@@ -50,6 +51,18 @@ struct SumArgs {
     float* partial;    // [2 blocks][ldp]: of runs that go on beyond their wavefront's places
     int64_t ldp;
 };
+// dW of a table, up to FEW_TOKENS tokens.
+void launch_sums_of_few(int dtype, const TokenIds& ids, float alpha, const void* dY, int64_t ldy, int64_t cols, float* dW, hipStream_t s);
+
+// A stored table's gradient in one pass; grid: workgroups that sum, each with a column of `bins`.
+struct LookupGradPlan {
+    bool few;
+    int each, grid, waves;
+};
+LookupGradPlan lookup_grad_plan(int64_t n, int64_t cols, int esize, int kd);
+void launch_lookup_gradient(int dtype, int d, const LookupGradPlan& p, const LookupGradArgs& a, hipStream_t s);
+// dC from bins, dS of the rows that went to `parts`; of_group: segments of a group, or 1.
+void launch_join_lookup(const LookupGradPlan& p, const LookupGradArgs& a, int kd, float* dC, int of_group, hipStream_t s);
 int sum_places(int64_t n, int64_t cols);
 int64_t sum_partials(int64_t n, int64_t cols);  // floats
 void launch_sums(int dtype, const SumArgs& a, hipStream_t s);

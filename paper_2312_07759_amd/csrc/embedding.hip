@@ -8,9 +8,17 @@ namespace idkm {
 
 // ---- the order of the tokens
 
-__global__ __launch_bounds__(RANK_WAVES * 64) void k_rank_tokens(const TokenIds in, const TokenOrder out) {
-    extern __shared__ __align__(16) int rank_lds[];
-    rank_tokens(in, out, blockIdx.x, rank_lds);
+// .. and `count` floats cleared behind it.
+__global__ __launch_bounds__(GROUP_WAVES * 64) void k_group_tokens(const TokenIds in, const TokenOrder out, float* clear, int64_t count) {
+    extern __shared__ __align__(16) int group_lds_words[];
+    group_tokens(in, out, group_lds_words);
+    const int64_t t = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * blockDim.x;
+    if ((reinterpret_cast<uintptr_t>(clear) & 15) == 0) {
+        for (int64_t i = t; i < count / 4; i += step) reinterpret_cast<floatx4*>(clear)[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (t < (count & 3)) clear[count - 1 - t] = 0.f;
+    } else {
+        for (int64_t i = t; i < count; i += step) clear[i] = 0.f;
+    }
 }
 
 __global__ __launch_bounds__(256) void k_radix_count(const RadixPass a) {
@@ -101,19 +109,19 @@ __global__ __launch_bounds__(256) void k_radix_place(const RadixPass a) {
 }
 
 int64_t sort_words(int64_t n) {
-    if (n <= RANK_TOKENS) return 2 * n;
+    if (n <= GROUP_TOKENS) return 2 * n;
     return 4 * n + 256 * ((n + RADIX_BLOCK - 1) / RADIX_BLOCK);
 }
 
-TokenOrder launch_sort(const TokenIds& ids, int32_t* ws, hipStream_t s) {
+TokenOrder launch_sort(const TokenIds& ids, int32_t* ws, float* clear, int64_t count, hipStream_t s) {
     const int64_t n = ids.n;
     TokenOrder order{ws, ws + n};
-    if (n <= RANK_TOKENS) {
-        const size_t lds = 4 * (RANK_WAVES * 64 + (size_t)up_to(n, 4));
-        allow_lds(reinterpret_cast<const void*>(&k_rank_tokens), lds);
-        hipLaunchKernelGGL(k_rank_tokens, dim3((unsigned)((n + 63) / 64)), dim3(RANK_WAVES * 64), lds, s, ids, order);
+    if (n <= GROUP_TOKENS) {
+        allow_lds(reinterpret_cast<const void*>(&k_group_tokens), group_lds(n));
+        hipLaunchKernelGGL(k_group_tokens, dim3(257), dim3(GROUP_WAVES * 64), group_lds(n), s, ids, order, clear, count);
         return order;
     }
+    if (count > 0) launch_fill_zero(clear, count, s);
     TokenOrder other{ws + 2 * n, ws + 3 * n};
     RadixPass a{};
     a.ids = ids;
@@ -162,102 +170,88 @@ void launch_rows(const TokenOrder& order, int64_t n, int rows, const RowsOfToken
 
 // ---- sums by row
 
-// A wavefront takes `each` places of 64 x 8 columns: rows of dY in the order of their tokens, asked for eight ahead.  The sum of a
-// row that has all of its places there goes to `out`; the first and last rows' may go on before and behind: their parts go to `partial` (2 b: a row that
-// began before block b, 2 b + 1: one that begins in it and goes on), which the second kernel adds up in order.
-template <typename T>
-__global__ __launch_bounds__(256) void k_sums(const SumArgs a) {
-    constexpr int U = 8, FR = 8 / Elem<T>::PER16;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int strips = (int)((a.cols + 511) / 512);
-    const int64_t task = (int64_t)blockIdx.x * 4 + wave, b = task / strips;
-    const int strip = (int)(task - b * strips), c = strip * 512 + lane * 8;
-    const int64_t first = b * a.each, last = min(a.n, first + a.each);
-    if (first >= a.n || c >= a.cols) return;  // lanes behind the last column take no part: no exchanges between lanes follow
-    const bool whole = c + 8 <= a.cols;
-    const T* dY = static_cast<const T*>(a.dY) + c;
-    float sum[8];
+// Eight columns of a row's sum.
+__device__ __forceinline__ void store_sum(float* to, int c, int cols, float alpha, const float* sum) {
+    float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] = 0.f;
-    auto store = [&](float* to) {
+    for (int e = 0; e < 8; ++e) v[e] = alpha * sum[e];
+    if (c + 8 <= cols && (reinterpret_cast<uintptr_t>(to + c) & 15) == 0) {
+        reinterpret_cast<floatx4*>(to + c)[0] = floatx4{v[0], v[1], v[2], v[3]};
+        reinterpret_cast<floatx4*>(to + c)[1] = floatx4{v[4], v[5], v[6], v[7]};
+    } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] *= a.alpha;
-        if (whole && ((reinterpret_cast<uintptr_t>(to + c)) & 15) == 0) {
-            reinterpret_cast<floatx4*>(to + c)[0] = floatx4{sum[0], sum[1], sum[2], sum[3]};
-            reinterpret_cast<floatx4*>(to + c)[1] = floatx4{sum[4], sum[5], sum[6], sum[7]};
-        } else {
-            for (int e = 0; e < 8 && c + e < a.cols; ++e) to[c + e] = sum[e];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] = 0.f;
-    };
-    bool began = first > 0 && a.order.row_at[first - 1] == a.order.row_at[first];  // before this block
-    for (int64_t p0 = first; p0 < last; p0 += U) {
-        u32x4 raw[U][FR];
-        int row[U + 1];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t p = min(p0 + u, last - 1);
-            row[u] = a.order.row_at[p];
-            const T* from = dY + (int64_t)a.order.token_at[p] * a.ldy;
-            if (whole) {
-#pragma unroll
-                for (int f = 0; f < FR; ++f) raw[u][f] = reinterpret_cast<const u32x4_any*>(from)[f];
-            } else {
-                struct alignas(16) Eight { T v[8]; } y;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y.v[e] = c + e < a.cols ? from[e] : (T)0.f;
-                __builtin_memcpy(raw[u], &y, sizeof(y));
-            }
-        }
-        row[U] = p0 + U < a.n ? a.order.row_at[p0 + U] : a.rows;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t p = p0 + u;
-            if (p >= last || row[u] >= a.rows) break;
-            struct alignas(16) Eight { T v[8]; } y;
-            __builtin_memcpy(&y, raw[u], sizeof(y));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += Elem<T>::up(y.v[e]);
-            const int behind = p + 1 >= a.n ? a.rows : p + 1 < last || u == U - 1 ? row[u + 1] : a.order.row_at[p + 1];
-            const bool ends = behind != row[u];
-            if (ends && !began) {
-                store(a.out + (a.index_at ? (int64_t)a.index_at[p] : (int64_t)row[u]) * a.ldo);
-            } else if (ends || p + 1 == last) {
-                store(a.partial + (2 * b + (began ? 0 : 1)) * a.ldp);
-                began = false;
-            }
-        }
+        for (int e = 0; e < 8; ++e)
+            if (c + e < cols) to[c + e] = v[e];
     }
 }
 
-// Rows whose places lie in several blocks: the block in which such a row begins adds up its parts.
-__global__ __launch_bounds__(256) void k_join_sums(const SumArgs a) {
-    const int64_t b = blockIdx.x, behind = (b + 1) * a.each;  // a block follows
-    const int row = a.order.row_at[behind - 1];
-    if (row >= a.rows || a.order.row_at[behind] != row) return;
-    if (b > 0 && a.order.row_at[b * a.each] == row && a.order.row_at[b * a.each - 1] == row) return;  // it began before
-    int64_t inside = behind, outside = a.n;  // its last place, halving
-    while (outside - inside > 1) {
-        const int64_t p = (inside + outside) >> 1;
-        if (a.order.row_at[p] == row) inside = p;
-        else outside = p;
+// The sum of a row that has all of its places in a block goes to `out`; parts of others go to `partial` (2 b: of a row that began before block b,
+// 2 b + 1: of one that begins in it and goes on), which the next kernel adds up in order.
+template <typename T>
+__global__ __launch_bounds__(256) void k_sums(const SumArgs a) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int cols = (int)a.cols, strips = (cols + 511) / 512;
+    const int64_t task = (int64_t)blockIdx.x * 4 + wave, b = task / strips;
+    const int strip = (int)(task - b * strips), c = strip * 512 + lane * 8;
+    if (b * a.each >= a.n) return;
+    const Places places(a.order, a.n, a.rows, b, a.each);
+    struct None {};
+    auto begin = [&](None&, int) {};
+    auto end = [&](const None&, int row, int64_t place, bool complete, bool began, const float* sum) {
+        float* to = complete ? a.out + (a.index_at ? (int64_t)a.index_at[place] : (int64_t)row) * a.ldo : a.partial + (2 * b + (began ? 0 : 1)) * a.ldp;
+        if (c < cols) store_sum(to, c, cols, a.alpha, sum);
+    };
+    sum_places_of<T, None>(places, EightColumns<T>(a.dY, a.ldy, strip, cols), begin, end);
+}
+
+// Up to FEW_TOKENS tokens: the first workgroups sum, the ones behind them clear the rows of which there is no token.
+template <typename T>
+__global__ __launch_bounds__(256) void k_sums_of_few(const TokenIds ids, float alpha, const T* dY, int64_t ldy, int cols, float* dW, unsigned summing) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (blockIdx.x >= summing) {
+        clear_other_rows(ids, dW, cols, (int64_t)(blockIdx.x - summing) * 4 + wave, (int64_t)(gridDim.x - summing) * 4);
+        return;
     }
-    const int64_t end = inside / a.each;
+    const int strips = (cols + 511) / 512, task = blockIdx.x * 4 + wave, t = task / strips, strip = task - t * strips, c = strip * 512 + lane * 8;
+    if (t >= (int)ids.n) return;
+    const Mates::Rows rows(ids);
+    const int row = ids.row(t);
+    const Mates mates(rows, row);
+    if (row >= ids.rows || mates.first() != t) return;
+    float sum[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+    sum_of_mates<T>(sum, mates, EightColumns<T>(dY, ldy, strip, cols));
+    if (c < cols) store_sum(dW + (int64_t)row * cols, c, cols, alpha, sum);
+}
+
+void launch_sums_of_few(int dtype, const TokenIds& ids, float alpha, const void* dY, int64_t ldy, int64_t cols, float* dW, hipStream_t s) {
+    const unsigned summing = (unsigned)((ids.n * ((cols + 511) / 512) + 3) / 4), clearing = (unsigned)std::min<int64_t>(2048, (ids.rows + 3) / 4);
+    BY_TYPE(dtype, T, hipLaunchKernelGGL(k_sums_of_few<T>, dim3(summing + clearing), dim3(256), 0, s, ids, alpha, static_cast<const T*>(dY), ldy,
+                                         (int)cols, dW, summing));
+}
+
+// Rows whose places lie in several blocks: the block in which such a row ends adds up its parts, in order.
+__global__ __launch_bounds__(256) void k_join_sums(const SumArgs a) {
+    const int64_t b = blockIdx.x + 1, first = b * a.each, behind = min(first + a.each, a.n);
+    const int row = a.order.row_at[first];
+    if (row >= a.rows || a.order.row_at[first - 1] != row) return;
+    if (behind < a.n && a.order.row_at[behind - 1] == row && a.order.row_at[behind] == row) return;  // it goes on
+    const int64_t start = b - blocks_before(a.order, b, a.each, row);
     const int64_t c = (int64_t)blockIdx.y * 256 + threadIdx.x;
     if (c >= a.cols) return;
-    float sum = a.partial[(2 * b + 1) * a.ldp + c];
+    float sum = a.partial[(2 * start + 1) * a.ldp + c];
     const float* part = a.partial + c;
-    int64_t i = b + 1;
-    for (; i + 8 <= end + 1; i += 8) {
+    int64_t i = start + 1;
+    for (; i + 8 <= b + 1; i += 8) {
         float v[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) v[u] = part[2 * (i + u) * a.ldp];
 #pragma unroll
         for (int u = 0; u < 8; ++u) sum += v[u];
     }
-    for (; i <= end; ++i) sum += part[2 * i * a.ldp];
-    a.out[(a.index_at ? (int64_t)a.index_at[behind - 1] : (int64_t)row) * a.ldo + c] = sum;
+    for (; i <= b; ++i) sum += part[2 * i * a.ldp];
+    a.out[(a.index_at ? (int64_t)a.index_at[first] : (int64_t)row) * a.ldo + c] = sum;
 }
 
 // Places to a wavefront: some 4096 wavefronts, at most 64 places each.
@@ -279,6 +273,87 @@ void launch_sums(int dtype, const SumArgs& args, hipStream_t s) {
     const int64_t blocks = (a.n + a.each - 1) / a.each, tasks = blocks * ((a.cols + 511) / 512);
     BY_TYPE(dtype, T, hipLaunchKernelGGL(k_sums<T>, dim3((unsigned)((tasks + 3) / 4)), dim3(256), 0, s, a));
     if (blocks > 1) hipLaunchKernelGGL(k_join_sums, dim3((unsigned)(blocks - 1), (unsigned)((a.cols + 255) / 256)), dim3(256), 0, s, a);
+}
+
+// ---- gradients of stored tables
+
+// dC[e] = the sum of bins[e][..] in float64, a workgroup to an e; the workgroups behind them: dS of the rows whose sums went to `parts`, in the order
+// of their parts and segments.
+__global__ __launch_bounds__(256) void k_join_lookup(const LookupGradArgs a, int bins, int kd, float* dC, int of_group) {
+    if ((int)blockIdx.x < kd) {
+        __shared__ double waves[4];
+        const float* mine = a.bins + blockIdx.x * a.pitch;
+        double sum = 0.0;
+        for (int w = threadIdx.x; w < bins; w += 256) sum += (double)mine[w];
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+        if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = sum;
+        __syncthreads();
+        if (threadIdx.x == 0) dC[blockIdx.x] = (float)(waves[0] + waves[1] + waves[2] + waves[3]);
+        return;
+    }
+    const int64_t n = a.ids.n;
+    if (a.few) {  // a row is in one part
+        for (int64_t i = (int64_t)(blockIdx.x - kd) * 256 + threadIdx.x; i < n * a.groups; i += (int64_t)(gridDim.x - kd) * 256) {
+            const int64_t t = i / a.groups;
+            const int g = (int)(i - t * a.groups), row = a.order.row_at[t];
+            if (row >= a.ids.rows) continue;
+            float sum = 0.f;
+            for (int j = g * of_group; j < min(a.per_part, (g + 1) * of_group); ++j) sum += a.parts[t * a.per_part + j];
+            a.dS[(int64_t)row * a.groups + g] = sum;
+        }
+        return;
+    }
+    // a wavefront to the rows that end in a block
+    const int lane = threadIdx.x & 63;
+    const int64_t blocks = (n + a.each - 1) / a.each;
+    for (int64_t b = (int64_t)(blockIdx.x - kd) * 4 + (threadIdx.x >> 6); b < blocks; b += (int64_t)(gridDim.x - kd) * 4) {
+        const Places at(a.order, n, a.ids.rows, b, a.each);
+        uint64_t ends = at.row_ends;
+        if (!a.segmented) ends = at.began ? ends & (0 - ends) : 0;  // the others are in dS
+        for (bool began = at.began; ends; ends &= ends - 1, began = false) {
+            const int p = __builtin_ctzll(ends), row = __builtin_amdgcn_readlane(at.row, p);
+            const int64_t start = began ? b - blocks_before(a.order, b, a.each, row) : b;
+            for (int g = lane; g < a.groups; g += 64) {
+                float sum = 0.f;
+                for (int64_t q = start; q <= b; q += 8) {
+                    for (int j = g * of_group; j < min(a.per_part, (g + 1) * of_group); ++j) {
+                        float v[8];
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) {
+                            const int64_t place = min((q + u + 1) * a.each - 1, at.first + p);
+                            v[u] = a.parts[place * a.per_part + j];
+                        }
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) sum += q + u <= b ? v[u] : 0.f;
+                    }
+                }
+                a.dS[(int64_t)row * a.groups + g] = sum;
+            }
+        }
+    }
+}
+
+void launch_join_lookup(const LookupGradPlan& p, const LookupGradArgs& a, int kd, float* dC, int of_group, hipStream_t s) {
+    if (!dC) kd = 0;
+    const bool parts = a.dS && (a.segmented || (!p.few && a.ids.n > p.each));
+    const int64_t joining = p.few ? (a.ids.n * a.groups + 255) / 256 : ((a.ids.n + p.each - 1) / p.each + 3) / 4;
+    const unsigned grid = (unsigned)kd + (parts ? (unsigned)std::min<int64_t>(4096, joining) : 0u);
+    if (grid > 0) hipLaunchKernelGGL(k_join_lookup, dim3(grid), dim3(256), 0, s, a, p.grid, kd, dC, of_group);
+}
+
+// Bins take k d 256 bytes of LDS for every wavefront; as many workgroups as the compute units hold at once, and blocks of so few places that every wavefront
+// has one: 8192 tokens of 4096 columns 23.5 us with 24 wavefronts to a compute unit (as the registers allow) and 8 places, 30.5 with 16 places, 24.4 with 4.
+LookupGradPlan lookup_grad_plan(int64_t n, int64_t cols, int esize, int kd) {
+    LookupGradPlan p{};
+    const int64_t strips = (cols + 511) / 512;
+    p.few = n <= FEW_TOKENS;
+    p.each = (int)std::max<int64_t>(2, std::min<int64_t>(32, n * strips / 8192));
+    const int64_t tasks = (p.few ? n : (n + p.each - 1) / p.each) * strips;
+    p.waves = std::min(4, 128 * 1024 / (kd * 256));
+    const int64_t resident = std::max(1, std::min((esize == 4 ? 16 : 24) / p.waves, 152 * 1024 / (kd * 256 * p.waves + kd * 4)));
+    p.grid = (int)std::min<int64_t>((tasks + p.waves - 1) / p.waves, 256 * resident);
+    return p;
 }
 
 // ---- lookups

@@ -45,8 +45,11 @@ SumArgs sums_of(const TokenOrder& order, int64_t n, int64_t rows, float alpha, c
     return a;
 }
 
-// Workspace of a stored table's gradient.
+// Workspace of a stored table's gradient.  direct: see lookup_gradient.hpp; the others sum the rows first.
 struct CodesGradLayout : BinPlan {
+    bool direct;
+    LookupGradPlan plan;
+    int per_part;
     int64_t lines, ldp, order, index, partial, p, bins, segments, bytes;
 };
 
@@ -54,8 +57,17 @@ CodesGradLayout codes_grad_layout(const idkm_codes_desc& w, int64_t n) {
     CodesGradLayout l{};
     l.lines = n < w.rows ? n : w.rows;  // different rows, at most
     static_cast<BinPlan&>(l) = bin_plan(w, l.lines);
-    l.ldp = up_to(w.cols, 8);
     l.order = 0;
+    l.direct = l.runs && !l.wide;
+    if (l.direct) {
+        l.plan = lookup_grad_plan(n, w.cols, esize_of(w.dtype), w.k * w.d);
+        l.per_part = w.S ? l.segmented ? (int)((w.cols + 31) / 32) : l.groups : 0;
+        l.bins = buffer(sort_words(n), 4);
+        l.segments = l.bins + buffer((int64_t)l.plan.grid * w.k * w.d, 4);
+        l.bytes = l.segments + buffer(n * l.per_part, 4);
+        return l;
+    }
+    l.ldp = up_to(w.cols, 8);
     l.index = buffer(sort_words(n), 4);
     l.partial = l.index + buffer(2 * n + 1, 4);
     l.p = l.partial + buffer(sum_partials(n, w.cols), 4);
@@ -90,7 +102,7 @@ idkm_status idkm_embedding(idkm_ctx* ctx, const float* W, int64_t rows, int64_t 
 
 int64_t idkm_embedding_backward_workspace(int64_t rows, int64_t cols, int64_t n) {
     if (rows < 1 || cols < 1 || n < 0 || rows > MAX_SIDE || cols > MAX_SIDE || n > MAX_SIDE || rows * cols > ((int64_t)1 << 36)) return -1;
-    if (n == 0) return 0;
+    if (n <= FEW_TOKENS) return 0;
     return buffer(sort_words(n), 4) + buffer(sum_partials(n, cols), 4);
 }
 
@@ -108,9 +120,13 @@ idkm_status idkm_embedding_backward(idkm_ctx* ctx, int64_t rows, int64_t cols, c
         hipStream_t s = (hipStream_t)hip_stream;
         unsigned char* ws = static_cast<unsigned char*>(workspace);
         return launched(ctx, [&] {
-            launch_fill_zero(dW, rows * cols, s);
-            if (n == 0) return;
-            const TokenOrder order = launch_sort(tokens_of(ids, id_bytes, n, rows), reinterpret_cast<int32_t*>(ws), s);
+            const TokenIds tokens = tokens_of(ids, id_bytes, n, rows);
+            if (n <= FEW_TOKENS) {
+                if (n == 0) launch_fill_zero(dW, rows * cols, s);
+                else launch_sums_of_few(dtype, tokens, alpha, dY, lddy, cols, dW, s);
+                return;
+            }
+            const TokenOrder order = launch_sort(tokens, reinterpret_cast<int32_t*>(ws), dW, rows * cols, s);
             SumArgs a = sums_of(order, n, rows, alpha, dY, lddy, cols);
             a.out = dW;
             a.ldo = cols;
@@ -171,12 +187,46 @@ idkm_status idkm_codes_embedding_backward(idkm_ctx* ctx, const idkm_codes_desc* 
         hipStream_t s = (hipStream_t)hip_stream;
         unsigned char* ws = static_cast<unsigned char*>(workspace);
         return launched(ctx, [&] {
-            if (dS) launch_fill_zero(dS, w->rows * groups_of(*w), s);
+            const int64_t scales = dS ? w->rows * groups_of(*w) : 0;
             if (n == 0) {
+                if (dS) launch_fill_zero(dS, scales, s);
                 if (dC) launch_fill_zero(dC, (int64_t)w->k * w->d, s);
                 return;
             }
-            const TokenOrder order = launch_sort(tokens_of(ids, id_bytes, n, w->rows), reinterpret_cast<int32_t*>(ws), s);
+            const TokenIds tokens = tokens_of(ids, id_bytes, n, w->rows);
+            int32_t* sorted = reinterpret_cast<int32_t*>(ws);
+            const BinArgs bins = bins_of(*w, l);
+            if (l.direct) {
+                LookupGradArgs a{};
+                a.ids = tokens;
+                a.order = l.plan.few ? TokenOrder{sorted, nullptr} : launch_sort(tokens, sorted, dS, scales, s);
+                a.alpha = alpha;
+                a.dY = dY;
+                a.ldy = lddy;
+                a.cols = (int)w->cols;
+                a.words = w->words;
+                a.nwords = bins.nwords;
+                a.row_bits = w->cols / w->d * bins.bits;
+                a.C = w->C;
+                a.k = w->k;
+                a.bits = bins.bits;
+                a.S = w->S;
+                a.group = l.group;
+                a.groups = l.groups;
+                a.dS = dS;
+                a.parts = reinterpret_cast<float*>(ws + l.segments);
+                a.per_part = l.per_part;
+                a.segmented = l.segmented;
+                a.bins = reinterpret_cast<float*>(ws + l.bins);
+                a.pitch = l.plan.grid;
+                a.few = l.plan.few;
+                a.each = l.plan.each;
+                launch_lookup_gradient(w->dtype, w->d, l.plan, a, s);
+                // segments of a group; one where a part has a sum for each
+                launch_join_lookup(l.plan, a, w->k * w->d, dC, !l.segmented ? 1 : l.groups > 1 ? l.group / 32 : l.per_part, s);
+                return;
+            }
+            const TokenOrder order = launch_sort(tokens, sorted, dS, scales, s);
             int32_t* index = reinterpret_cast<int32_t*>(ws + l.index);
             const RowsOfTokens rows{index, index + n, index + 2 * n};
             launch_rows(order, n, (int)w->rows, rows, s);
@@ -187,7 +237,7 @@ idkm_status idkm_codes_embedding_backward(idkm_ctx* ctx, const idkm_codes_desc* 
             a.ldo = l.ldp;
             a.partial = reinterpret_cast<float*>(ws + l.partial);
             launch_sums(w->dtype, a, s);
-            BinArgs b = bins_of(*w, l);
+            BinArgs b = bins;
             b.P = P;
             b.ldp = l.ldp;
             b.pitch = l.grid;

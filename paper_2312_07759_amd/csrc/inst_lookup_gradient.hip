@@ -1,0 +1,29 @@
+// Gradients of lookups in stored tables: types and lengths of codewords.
+#include <algorithm>
+
+#include "embedding.h"
+#include "layers.h"
+
+namespace idkm {
+
+template <typename T, bool FEW>
+static void (*gradient_for(int d))(const LookupGradArgs) {
+    return d == 1 ? &k_lookup_gradient<T, 1, FEW> : d == 2 ? &k_lookup_gradient<T, 2, FEW> : d == 4 ? &k_lookup_gradient<T, 4, FEW> : &k_lookup_gradient<T, 8, FEW>;
+}
+
+void launch_lookup_gradient(int dtype, int d, const LookupGradPlan& p, const LookupGradArgs& args, hipStream_t s) {
+    LookupGradArgs a = args;
+    a.few = p.few;
+    a.each = p.each;
+    a.summing = (unsigned)p.grid;
+    const unsigned clearing = p.few && a.dS ? (unsigned)std::min<int64_t>(512, ((int64_t)a.ids.rows + 63) / 64) : 0u;
+    const int kd = a.k * d;
+    const size_t lds = 4 * ((size_t)p.waves * kd * 64 + kd);
+    BY_TYPE(dtype, T, {
+        void (*const fn)(const LookupGradArgs) = p.few ? gradient_for<T, true>(d) : gradient_for<T, false>(d);
+        allow_lds(reinterpret_cast<const void*>(fn), lds);
+        hipLaunchKernelGGL(fn, dim3(a.summing + clearing), dim3((unsigned)p.waves * 64), lds, s, a);
+    });
+}
+
+}  // namespace idkm
