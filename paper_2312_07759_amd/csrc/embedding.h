@@ -19,6 +19,7 @@ struct LookupArgs {
     const float* S;  // [rows, groups] or null
     int group, groups;
     int c_in_lds;
+    int each;  // tokens of a wavefront at a time
 };
 void launch_lookup_table(int dtype, const LookupArgs& a, hipStream_t s);
 void launch_lookup_codes(int dtype, const LookupArgs& a, hipStream_t s);

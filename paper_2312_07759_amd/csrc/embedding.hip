@@ -171,49 +171,51 @@ void launch_rows(const TokenOrder& order, int64_t n, int rows, const RowsOfToken
 // ---- sums by row
 
 // Eight columns of a row's sum.
-__device__ __forceinline__ void store_sum(float* to, int c, int cols, float alpha, const float* sum) {
+__device__ __forceinline__ void store_sum(float* to, const Columns& at, int cols, float alpha, const float* sum) {
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = alpha * sum[e];
-    if (c + 8 <= cols && (reinterpret_cast<uintptr_t>(to + c) & 15) == 0) {
-        reinterpret_cast<floatx4*>(to + c)[0] = floatx4{v[0], v[1], v[2], v[3]};
-        reinterpret_cast<floatx4*>(to + c)[1] = floatx4{v[4], v[5], v[6], v[7]};
+    if (at.skip == 0 && cols >= 8 && (reinterpret_cast<uintptr_t>(to + at.c) & 15) == 0) {
+        reinterpret_cast<floatx4*>(to + at.c)[0] = floatx4{v[0], v[1], v[2], v[3]};
+        reinterpret_cast<floatx4*>(to + at.c)[1] = floatx4{v[4], v[5], v[6], v[7]};
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (c + e < cols) to[c + e] = v[e];
+            if (e >= at.skip && at.c + e < cols) to[at.c + e] = v[e];
     }
 }
 
 // The sum of a row that has all of its places in a block goes to `out`; parts of others go to `partial` (2 b: of a row that began before block b,
 // 2 b + 1: of one that begins in it and goes on), which the next kernel adds up in order.
-template <typename T>
+template <typename T, bool NARROW>
 __global__ __launch_bounds__(256) void k_sums(const SumArgs a) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int cols = (int)a.cols, strips = (cols + 511) / 512;
     const int64_t task = (int64_t)blockIdx.x * 4 + wave, b = task / strips;
-    const int strip = (int)(task - b * strips), c = strip * 512 + lane * 8;
+    const Columns columns((int)(task - b * strips), cols);
     if (b * a.each >= a.n) return;
     const Places places(a.order, a.n, a.rows, b, a.each);
     struct None {};
     auto begin = [&](None&, int) {};
-    auto end = [&](const None&, int row, int64_t place, bool complete, bool began, const float* sum) {
-        float* to = complete ? a.out + (a.index_at ? (int64_t)a.index_at[place] : (int64_t)row) * a.ldo : a.partial + (2 * b + (began ? 0 : 1)) * a.ldp;
-        if (c < cols) store_sum(to, c, cols, a.alpha, sum);
+    auto end = [&](const None&, int p, bool complete, bool began, const float* sum) {
+        const int row = a.index_at ? a.index_at[places.first + p] : __builtin_amdgcn_readlane(places.row, p);
+        float* to = complete ? a.out + row * a.ldo : a.partial + (2 * b + (began ? 0 : 1)) * a.ldp;
+        if (columns.skip < 8) store_sum(to, columns, cols, a.alpha, sum);
     };
-    sum_places_of<T, None>(places, EightColumns<T>(a.dY, a.ldy, strip, cols), begin, end);
+    sum_places_of<T, NARROW, None>(places, static_cast<const T*>(a.dY), a.ldy, columns.c, cols, begin, end);
 }
 
 // Up to FEW_TOKENS tokens: the first workgroups sum, the ones behind them clear the rows of which there is no token.
-template <typename T>
+template <typename T, bool NARROW>
 __global__ __launch_bounds__(256) void k_sums_of_few(const TokenIds ids, float alpha, const T* dY, int64_t ldy, int cols, float* dW, unsigned summing) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (blockIdx.x >= summing) {
         clear_other_rows(ids, dW, cols, (int64_t)(blockIdx.x - summing) * 4 + wave, (int64_t)(gridDim.x - summing) * 4);
         return;
     }
-    const int strips = (cols + 511) / 512, task = blockIdx.x * 4 + wave, t = task / strips, strip = task - t * strips, c = strip * 512 + lane * 8;
+    const int strips = (cols + 511) / 512, task = blockIdx.x * 4 + wave, t = task / strips;
     if (t >= (int)ids.n) return;
+    const Columns columns(task - t * strips, cols);
     const Mates::Rows rows(ids);
     const int row = ids.row(t);
     const Mates mates(rows, row);
@@ -221,13 +223,13 @@ __global__ __launch_bounds__(256) void k_sums_of_few(const TokenIds ids, float a
     float sum[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] = 0.f;
-    sum_of_mates<T>(sum, mates, EightColumns<T>(dY, ldy, strip, cols));
-    if (c < cols) store_sum(dW + (int64_t)row * cols, c, cols, alpha, sum);
+    sum_of_mates<T, NARROW>(sum, mates, dY, ldy, columns.c, cols);
+    if (columns.skip < 8) store_sum(dW + (int64_t)row * cols, columns, cols, alpha, sum);
 }
 
 void launch_sums_of_few(int dtype, const TokenIds& ids, float alpha, const void* dY, int64_t ldy, int64_t cols, float* dW, hipStream_t s) {
     const unsigned summing = (unsigned)((ids.n * ((cols + 511) / 512) + 3) / 4), clearing = (unsigned)std::min<int64_t>(2048, (ids.rows + 3) / 4);
-    BY_TYPE(dtype, T, hipLaunchKernelGGL(k_sums_of_few<T>, dim3(summing + clearing), dim3(256), 0, s, ids, alpha, static_cast<const T*>(dY), ldy,
+    BY_TYPE(dtype, T, hipLaunchKernelGGL((cols < 8 ? &k_sums_of_few<T, true> : &k_sums_of_few<T, false>), dim3(summing + clearing), dim3(256), 0, s, ids, alpha, static_cast<const T*>(dY), ldy,
                                          (int)cols, dW, summing));
 }
 
@@ -271,7 +273,7 @@ void launch_sums(int dtype, const SumArgs& args, hipStream_t s) {
     a.each = sum_places(a.n, a.cols);
     a.ldp = up_to(a.cols, 4);
     const int64_t blocks = (a.n + a.each - 1) / a.each, tasks = blocks * ((a.cols + 511) / 512);
-    BY_TYPE(dtype, T, hipLaunchKernelGGL(k_sums<T>, dim3((unsigned)((tasks + 3) / 4)), dim3(256), 0, s, a));
+    BY_TYPE(dtype, T, hipLaunchKernelGGL((a.cols < 8 ? &k_sums<T, true> : &k_sums<T, false>), dim3((unsigned)((tasks + 3) / 4)), dim3(256), 0, s, a));
     if (blocks > 1) hipLaunchKernelGGL(k_join_sums, dim3((unsigned)(blocks - 1), (unsigned)((a.cols + 255) / 256)), dim3(256), 0, s, a);
 }
 
@@ -348,10 +350,11 @@ LookupGradPlan lookup_grad_plan(int64_t n, int64_t cols, int esize, int kd) {
     LookupGradPlan p{};
     const int64_t strips = (cols + 511) / 512;
     p.few = n <= FEW_TOKENS;
-    p.each = (int)std::max<int64_t>(2, std::min<int64_t>(32, n * strips / 8192));
+    p.each = (int)std::max<int64_t>(2, std::min<int64_t>(LOOKUP_PLACES, n * strips / 8192));
     const int64_t tasks = (p.few ? n : (n + p.each - 1) / p.each) * strips;
-    p.waves = std::min(4, 128 * 1024 / (kd * 256));
-    const int64_t resident = std::max(1, std::min((esize == 4 ? 16 : 24) / p.waves, 152 * 1024 / (kd * 256 * p.waves + kd * 4)));
+    const int wave_bytes = kd * 256 + LOOKUP_KEPT * 4;
+    p.waves = std::min(4, 144 * 1024 / wave_bytes);
+    const int64_t resident = std::max(1, std::min((esize == 4 ? 16 : 24) / p.waves, 156 * 1024 / (wave_bytes * p.waves + kd * 4)));
     p.grid = (int)std::min<int64_t>((tasks + p.waves - 1) / p.waves, 256 * resident);
     return p;
 }
@@ -441,6 +444,97 @@ __global__ __launch_bounds__(256) void k_lookup_codes(const LookupArgs a) {
     }
 }
 
+// The same for codes of up to 8 bits, D in {1, 2, 4, 8} and rows of at least eight columns: a wavefront takes 512 columns of some tokens' rows, whose codes
+// are asked for one token ahead.  The codebook lies in LDS, once: lanes that meet in a bank wait for each other, which the stores cover.
+// 8192 tokens of 4096 columns, k = 256, d = 4, float16: 18 us (a fill of Y takes 10; 43 with one code read at a time, 64-bit divisions for every eight columns).
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_lookup_codes_fast(const LookupArgs a) {
+    constexpr int NC = 8 / D;
+    extern __shared__ __align__(16) unsigned char lds[];
+    struct alignas(D * sizeof(T) > 16 ? 16 : D * sizeof(T)) Entry { T v[D]; };
+    T* book = reinterpret_cast<T*>(lds);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int cols = (int)a.cols, strips = (cols + 511) / 512, blocks = (int)((a.ids.n + a.each - 1) / a.each);
+    const uint32_t mask = (1u << a.bits) - 1u;
+    const int entries = (int)mask + 1;  // codes that are none give NaN
+    const float* S = a.S ? a.S : reinterpret_cast<const float*>(a.words);  // without scales some word, which is not used
+    const int groups = a.S ? a.groups : 0;
+    struct Item {
+        uint32_t w[3];
+        int sh;
+        float s;
+    };
+    bool built = false;
+    for (int task = blockIdx.x * 4 + wave;; task += gridDim.x * 4) {
+        const bool there = task < blocks * strips;
+        const int b = there ? task / strips : 0, strip = there ? task - b * strips : 0;
+        const Columns columns(strip, cols);
+        const int c = columns.c, at_bit = c / D * a.bits, g = a.S ? min(c + columns.skip, cols - 1) / a.group : 0;
+        const int64_t first = (int64_t)b * a.each;
+        const int count = there ? (int)min((int64_t)a.each, a.ids.n - first) : 0;
+        const int64_t id = a.ids.raw(first + min(lane, max(count, 1) - 1));
+        const int row = id < 0 || id >= a.ids.rows ? 0 : (int)id, kind = id < 0 ? 1 : id >= a.ids.rows ? 2 : 0;
+        const int64_t row_bit = row * a.row_bits;
+        const uint64_t word = reinterpret_cast<uint64_t>(a.words + (row_bit >> 5)), scale = reinterpret_cast<uint64_t>(S + (int64_t)row * groups);
+        // the row's bit, whether its last word but two ends behind the stream, and what its token is
+        const int start = (int)(row_bit & 31) | ((row_bit + a.row_bits + 31) / 32 + 3 > a.nwords ? 32 : 0) | kind << 6;
+        auto ask = [&](Item& t, int p) {
+            const int of = __builtin_amdgcn_readlane(start, p);
+            const uint32_t* words = reinterpret_cast<const uint32_t*>(of_lane(word, p));
+            const int bit = (of & 31) + at_bit;
+            int from = bit >> 5;
+            if (of & 32) from = min(from, (int)(a.words + (a.nwords - 3) - words));
+            t.sh = bit - from * 32;
+            const u32x3_word w = *reinterpret_cast<const u32x3_word*>(words + from);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) t.w[i] = w[i];
+            t.s = reinterpret_cast<const float*>(of_lane(scale, p))[g];
+        };
+        Item now, next;
+        ask(now, 0);
+        if (!built) {  // the same for the whole workgroup
+            for (int i = threadIdx.x; i < entries * D; i += 256) book[i] = i < a.k * D ? static_cast<const T*>(a.C)[i] : Elem<T>::nan();
+            __syncthreads();
+            built = true;
+        }
+        if (!there) break;
+        for (int p = 0; p < count; ++p) {
+            ask(next, min(p + 1, count - 1));
+            uint32_t b0 = now.w[0], b1 = now.w[1], b2 = now.w[2];
+            if (__any(now.sh >= 32)) {  // only near the stream's end
+                const bool two = now.sh >= 64, one = now.sh >= 32;
+                b0 = two ? b2 : one ? b1 : b0;
+                b1 = two ? 0u : one ? b2 : b1;
+                b2 = one ? 0u : b2;
+            }
+            uint32_t low = __builtin_amdgcn_alignbit(b1, b0, now.sh & 31), high = __builtin_amdgcn_alignbit(b2, b1, now.sh & 31);
+            const float by = a.S ? a.alpha * now.s : a.alpha;
+            EightOut<T> out;
+#pragma unroll
+            for (int e = 0; e < NC; ++e) {
+                const Entry entry = *reinterpret_cast<const Entry*>(book + (low & mask) * D);
+                low = __builtin_amdgcn_alignbit(high, low, a.bits);
+                high >>= a.bits;
+#pragma unroll
+                for (int i = 0; i < D; ++i) out.y.v[e * D + i] = Elem<T>::down(Elem<T>::up(entry.v[i]) * by);
+            }
+            const int of = __builtin_amdgcn_readlane(start, p) >> 6;
+            if (of != 0) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) out.y.v[e] = of == 1 ? (T)0.f : Elem<T>::nan();
+            }
+            // the row's last lanes write some columns twice, the same values
+            if (columns.skip < 8) out.store(static_cast<T*>(a.Y) + (first + p) * a.ldy + c, 8);
+            now = next;
+        }
+    }
+}
+
+template <typename T>
+static void (*lookup_for(int d))(const LookupArgs) {
+    return d == 1 ? &k_lookup_codes_fast<T, 1> : d == 2 ? &k_lookup_codes_fast<T, 2> : d == 4 ? &k_lookup_codes_fast<T, 4> : &k_lookup_codes_fast<T, 8>;
+}
+
 static unsigned grid_of(int64_t threads, int64_t most) {
     const int64_t g = (threads + 255) / 256;
     return (unsigned)(g < 1 ? 1 : g > most ? most : g);
@@ -452,6 +546,14 @@ void launch_lookup_table(int dtype, const LookupArgs& a, hipStream_t s) {
 
 void launch_lookup_codes(int dtype, const LookupArgs& args, hipStream_t s) {
     LookupArgs a = args;
+    if (a.bits <= 8 && (a.d == 1 || a.d == 2 || a.d == 4 || a.d == 8) && a.nwords >= 3 && a.cols >= 8) {
+        const int64_t strips = (a.cols + 511) / 512;
+        a.each = (int)std::max<int64_t>(1, std::min<int64_t>(16, a.ids.n * strips / 8192));
+        const int64_t tasks = (a.ids.n + a.each - 1) / a.each * strips;
+        const unsigned grid = (unsigned)std::min<int64_t>((tasks + 3) / 4, 2048);
+        BY_TYPE(dtype, T, hipLaunchKernelGGL(lookup_for<T>(a.d), dim3(grid), dim3(256), ((size_t)a.d << a.bits) * sizeof(T), s, a));
+        return;
+    }
     const size_t book = (size_t)a.k * a.d * (dtype == 0 ? 4 : 2);
     a.c_in_lds = book <= 32 * 1024;
     BY_TYPE(dtype, T, hipLaunchKernelGGL(k_lookup_codes<T>, dim3(grid_of(a.ids.n * ((a.cols + 7) / 8), 2048)), dim3(256), a.c_in_lds ? book : 0, s, a));

@@ -58,7 +58,7 @@ CodesGradLayout codes_grad_layout(const idkm_codes_desc& w, int64_t n) {
     l.lines = n < w.rows ? n : w.rows;  // different rows, at most
     static_cast<BinPlan&>(l) = bin_plan(w, l.lines);
     l.order = 0;
-    l.direct = l.runs && !l.wide;
+    l.direct = l.runs && !l.wide && w.cols >= 8;
     if (l.direct) {
         l.plan = lookup_grad_plan(n, w.cols, esize_of(w.dtype), w.k * w.d);
         l.per_part = w.S ? l.segmented ? (int)((w.cols + 31) / 32) : l.groups : 0;

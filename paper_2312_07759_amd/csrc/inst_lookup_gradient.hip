@@ -18,7 +18,10 @@ void launch_lookup_gradient(int dtype, int d, const LookupGradPlan& p, const Loo
     a.summing = (unsigned)p.grid;
     const unsigned clearing = p.few && a.dS ? (unsigned)std::min<int64_t>(512, ((int64_t)a.ids.rows + 63) / 64) : 0u;
     const int kd = a.k * d;
-    const size_t lds = 4 * ((size_t)p.waves * kd * 64 + kd);
+    // a stored group shorter than a row is a multiple of 32
+    const int sums = a.segmented ? 16 : a.groups > 1 ? 512 / a.group : 1;
+    for (a.sums_log = 0; 1 << a.sums_log < sums;) ++a.sums_log;
+    const size_t lds = 4 * ((size_t)p.waves * (kd * 64 + LOOKUP_KEPT) + kd);
     BY_TYPE(dtype, T, {
         void (*const fn)(const LookupGradArgs) = p.few ? gradient_for<T, true>(d) : gradient_for<T, false>(d);
         allow_lds(reinterpret_cast<const void*>(fn), lds);

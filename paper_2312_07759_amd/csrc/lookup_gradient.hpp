@@ -3,7 +3,7 @@
 //   S P  to its bins of the codebook's components (in LDS, 64 for each, one to a lane: no two lanes add to the same word, and the order of every sum is fixed)
 //   P C[code]  over the lanes of a group: dS of the row, or of its part where the row's tokens lie in several blocks.
 // For codes of up to 8 bits, D in {1, 2, 4, 8} and codebooks of up to 256 components; the others write the sums P out and go through the kernels of the
-// gradient of a product.
+// gradient of a product, as do rows of fewer than eight columns.
 #pragma once
 #include "codes_gradient.hpp"
 #include "token_sums.hpp"
@@ -30,10 +30,33 @@ struct LookupGradArgs {
     int segmented;  // every row's go to `parts`: a group is not a power of two of lanes
     float* bins;    // [k D][pitch]
     int64_t pitch;
-    int each;          // places to a block
+    int each;          // places to a block, at most LOOKUP_PLACES
+    int sums_log;      // sums of groups (segments) that a row has in a strip of 512 columns: 1 << sums_log, at most 16
     unsigned summing;  // few: workgroups that sum; the ones behind them clear the other rows of dS
 };
 
+// The sum over a lane's aligned neighbours, `lanes` of them, a power of two.  Up to 16 without LDS: once the lanes of a half agree, a mirrored one is as good
+// as the other half's.
+__device__ __forceinline__ float sum_of_lanes(float v, int lanes) {
+    auto moved = [&](auto control) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, true));
+    };
+    if (lanes >= 2) v += moved(std::integral_constant<int, 0xb1>());   // lanes 1 0 3 2 of four
+    if (lanes >= 4) v += moved(std::integral_constant<int, 0x4e>());   // 2 3 0 1
+    if (lanes >= 8) v += moved(std::integral_constant<int, 0x141>());  // eight, mirrored
+    if (lanes >= 16) v += moved(std::integral_constant<int, 0x140>()); // sixteen, mirrored
+    if (lanes >= 32) v += __shfl_xor(v, 16);
+    if (lanes >= 64) v += __shfl_xor(v, 32);
+    return v;
+}
+
+constexpr int LOOKUP_PLACES = 32;
+constexpr int LOOKUP_KEPT = LOOKUP_PLACES * 17;  // words of LDS for a wavefront: sums of groups, and whose they are
+
+// 8192 tokens of 4096 columns, 4 bits, groups of 128, bfloat16: 24 us, where dY alone is 13 at the rate of a copy.  Bound by issue and by the turns of the bins: some
+// 5,100 sums of rows and parts of rows, 42,000 strips of 512 columns at about 100 vector and as many scalar instructions, and eight LDS updates one after
+// another in each.  Beginning and end take 6 us (bins cleared and added up), as many wavefronts as the registers allow the rest.
+// A strip's sums of groups are kept in LDS and stored at the block's end, so that no load waits behind a store.
 template <typename T, int D, bool FEW>
 __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a) {
     constexpr int NC = 8 / D;
@@ -46,13 +69,18 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
     const int kd = a.k * D;
     float* mine = bin_lds + wave * kd * 64 + lane;
     float* book = bin_lds + nw * kd * 64;
+    float* kept = book + kd + wave * LOOKUP_KEPT;
+    int* kept_for = reinterpret_cast<int*>(kept + LOOKUP_PLACES * 16);  // a row of dS, or ~ a place of `parts`
     for (int j = 0; j < kd; ++j) mine[j * 64] = 0.f;
     for (int i = threadIdx.x; i < kd; i += blockDim.x) book[i] = Elem<T>::up(static_cast<const T*>(a.C)[i]);
     __syncthreads();
     const int strips = (a.cols + 511) / 512, n = (int)a.ids.n;
     const int blocks = FEW ? n : (n + a.each - 1) / a.each;
     const uint32_t mask = (1u << a.bits) - 1u;
-    const int group_lanes = a.group / 8;
+    // without scales some word is read in their place, so that every row makes the same loads
+    const float* S = a.S ? a.S : reinterpret_cast<const float*>(a.words);
+    const int groups = a.S ? a.groups : 0;
+    const int sum_lanes = a.segmented ? 4 : min(64, a.group / 8), lanes_log = 31 - __builtin_clz(sum_lanes);
     // a row's codes and scale of the lane's columns
     struct Item {
         uint32_t w[3];
@@ -61,17 +89,24 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
     };
     for (int task = blockIdx.x * nw + wave; task < blocks * strips; task += (int)a.summing * nw) {
         const int b = task / strips, strip = task - b * strips;
-        const EightColumns<T> columns(a.dY, a.ldy, strip, a.cols);
-        const int c = columns.c, at = min(c, (a.cols - 1) & ~7), g = at / a.group;
-        const bool there = c < a.cols, sure = strip * 512 + 512 <= a.cols && a.k > (int)mask;
-        auto ask = [&](Item& t, int row) {
-            const int64_t bit = row * a.row_bits + (unsigned)(at / D * a.bits), from = min(bit >> 5, a.nwords - 3);
-            t.sh = (int)(bit - (from << 5));
+        const Columns columns(strip, a.cols);
+        const int skip = columns.skip, at_bit = columns.c / D * a.bits, g = a.S ? min(columns.c + skip, a.cols - 1) / a.group : 0;
+        const int g_first = strip * 512 / a.group;
+        int held = 0;
+        const bool sure = strip * 512 + 512 <= a.cols && a.k > (int)mask;
+        // word: of the stream, where the row's words begin; row_sh: its codes' bit there; near: three words from a lane's first one on may not be there, and
+        // are taken from further ahead
+        auto ask = [&](Item& t, const uint32_t* word, int row_sh, bool near, const float* scale) {
+            const int bit = row_sh + at_bit;
+            int from = bit >> 5;
+            if (near) from = min(from, (int)(a.words + (a.nwords - 3) - word));
+            t.sh = bit - from * 32;
+            const u32x3_word w = *reinterpret_cast<const u32x3_word*>(word + from);
 #pragma unroll
-            for (int i = 0; i < 3; ++i) t.w[i] = a.words[from + i];
-            t.s = a.S ? a.S[(int64_t)row * a.groups + g] : 1.f;
+            for (int i = 0; i < 3; ++i) t.w[i] = w[i];
+            t.s = scale[g];
         };
-        auto finish = [&](const Item& t, int row, int64_t place, bool complete, const float* p) {
+        auto finish = [&](const Item& t, int who, const float* p) {
             uint32_t b0 = t.w[0], b1 = t.w[1], b2 = t.w[2];
             if (__any(t.sh >= 32)) {  // only near the stream's end
                 const bool two = t.sh >= 64, one = t.sh >= 32;
@@ -80,21 +115,23 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
                 b2 = one ? 0u : b2;
             }
             uint32_t low = __builtin_amdgcn_alignbit(b1, b0, t.sh & 31), high = __builtin_amdgcn_alignbit(b2, b1, t.sh & 31);
-            const float by = a.alpha * t.s;
+            const float by = a.S ? a.alpha * t.s : a.alpha;
             float sum = 0.f;
-            auto add = [&](auto sure_) {  // sure: all eight columns are there and every code is one
-                constexpr bool sure = decltype(sure_)::value;
-                const int have = there ? min(8, a.cols - c) : 0;
+            // sure: all eight columns are there and every code is one; word: the codes lie in 32 bits
+            auto add = [&](auto sure_, auto word_) {
+                constexpr bool sure = decltype(sure_)::value, word = decltype(word_)::value;
 #pragma unroll
                 for (int e = 0; e < NC; ++e) {
-                    const uint32_t code = low & mask;
-                    low = __builtin_amdgcn_alignbit(high, low, a.bits);
-                    high >>= a.bits;
+                    const uint32_t code = word ? __builtin_amdgcn_ubfe(low, e * a.bits, a.bits) : low & mask;
+                    if (!word) {
+                        low = __builtin_amdgcn_alignbit(high, low, a.bits);
+                        high >>= a.bits;
+                    }
                     const bool none = !sure && code >= (uint32_t)a.k;
                     const int j = none ? 0 : (int)code * D;
 #pragma unroll
                     for (int i = 0; i < D; ++i) {
-                        const bool counts = sure || e * D + i < have;
+                        const bool counts = sure || e * D + i >= skip;
                         const float w = none ? __builtin_nanf("") : book[j + i];
                         sum = counts ? fmaf(p[e * D + i], w, sum) : sum;
                         float& bin = mine[(j + i) * 64];
@@ -102,18 +139,24 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
                     }
                 }
             };
-            if (sure) add(std::true_type());
-            else add(std::false_type());
+            if (sure && NC * a.bits <= 32) add(std::true_type(), std::true_type());
+            else if (sure) add(std::true_type(), std::false_type());
+            else add(std::false_type(), std::false_type());
             if (!a.dS) return;
             sum *= a.alpha;
-            if (a.segmented) {
-                sum += __shfl_xor(sum, 1);
-                sum += __shfl_xor(sum, 2);
-                if (there && (lane & 3) == 0) a.parts[place * a.per_part + (c >> 5)] = sum;
-            } else {
-                for (int o = 1; o < group_lanes; o <<= 1) sum += __shfl_xor(sum, o);
-                if (there && (lane & (group_lanes - 1)) == 0) (complete ? a.dS + (int64_t)row * a.groups : a.parts + place * a.per_part)[g] = sum;
+            sum = sum_of_lanes(sum, sum_lanes);
+            if ((lane & (sum_lanes - 1)) == 0 && lane >> lanes_log < 1 << a.sums_log) kept[held << a.sums_log | lane >> lanes_log] = sum;
+            if (lane == 0) kept_for[held] = who;
+            ++held;
+        };
+        auto store_kept = [&] {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const int g0 = (a.segmented ? strip * 16 : g_first), all = a.segmented ? a.per_part : a.groups;
+            for (int i = lane; i < held << a.sums_log; i += 64) {
+                const int f = i >> a.sums_log, of = g0 + (i & ((1 << a.sums_log) - 1)), who = kept_for[f];
+                if (of < all) (who >= 0 ? a.dS + (int64_t)who * a.groups : a.parts + (int64_t)~who * a.per_part)[of] = kept[i];
             }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         };
         if constexpr (FEW) {
             const Mates::Rows rows(a.ids);
@@ -123,16 +166,31 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
             if (strip == 0 && lane == 0) a.order.row_at[b] = first ? row : a.ids.rows;
             if (!first) continue;
             Item t;
-            ask(t, row);
+            const int64_t row_bit = row * a.row_bits;
+            ask(t, a.words + (row_bit >> 5), (int)(row_bit & 31), true, S + (int64_t)row * groups);
             float sum[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] = 0.f;
-            sum_of_mates<T>(sum, mates, columns);
-            finish(t, row, b, true, sum);
+            sum_of_mates<T, false>(sum, mates, static_cast<const T*>(a.dY), a.ldy, columns.c, a.cols);
+            finish(t, a.segmented ? ~b : row, sum);
+            if (a.dS) store_kept();
         } else {
             const Places places(a.order, n, a.ids.rows, b, a.each);
-            sum_places_of<T, Item>(places, columns, ask,
-                                   [&](const Item& t, int row, int64_t place, bool complete, bool, const float* p) { finish(t, row, place, complete, p); });
+            const int row = min(places.row, a.ids.rows - 1);
+            const int64_t row_bit = row * a.row_bits;
+            const uint64_t word = reinterpret_cast<uint64_t>(a.words + (row_bit >> 5)), scale = reinterpret_cast<uint64_t>(S + (int64_t)row * groups);
+            // the row's bit, and whether its last word but two ends behind the stream
+            const int start = (int)(row_bit & 31) | ((row_bit + a.row_bits + 31) / 32 + 3 > a.nwords ? 32 : 0);
+            sum_places_of<T, false, Item>(
+                places, static_cast<const T*>(a.dY), a.ldy, columns.c, a.cols,
+                [&](Item& t, int p) {
+                    const int at = __builtin_amdgcn_readlane(start, p);
+                    ask(t, reinterpret_cast<const uint32_t*>(of_lane(word, p)), at & 31, at & 32, reinterpret_cast<const float*>(of_lane(scale, p)));
+                },
+                [&](const Item& t, int p, bool complete, bool, const float* sum) {
+                    finish(t, complete && !a.segmented ? __builtin_amdgcn_readlane(places.row, p) : ~(int)(places.first + p), sum);
+                });
+            if (a.dS) store_kept();
         }
     }
     __syncthreads();

@@ -10,34 +10,33 @@ namespace idkm {
 
 constexpr int FEW_TOKENS = 256;
 
-// A lane's eight columns of rows of dY.
-template <typename T>
-struct EightColumns {
-    const T* dY;
-    int64_t ldy;
-    int c, cols;
-    bool clean;  // every lane of the wavefront has all eight columns or none (those read the row's first ones)
-    __device__ __forceinline__ EightColumns(const void* dY_, int64_t ldy_, int strip, int cols_) : ldy(ldy_), c(strip * 512 + (threadIdx.x & 63) * 8), cols(cols_) {
-        clean = (cols & 7) == 0 || strip * 512 + 512 <= cols;
-        dY = static_cast<const T*>(dY_) + (c < cols ? c : 0);
+// A lane's eight columns of rows of dY, from column c on.  The last lane of a row whose length is no multiple of eight takes the last eight columns, of which
+// the first `skip` are its neighbour's: all rows are read in the same way, 16 bytes at a time.  Lanes behind the row's end skip all eight.  NARROW: rows of
+// fewer than eight columns, element by element.
+struct Columns {
+    int c, skip;
+    __device__ __forceinline__ Columns(int strip, int cols) {
+        const int from = strip * 512 + (int)(threadIdx.x & 63) * 8;
+        c = max(0, min(from, cols - 8));
+        skip = from >= cols ? 8 : from - c;
     }
 };
 
-// .. of four rows on their way.
-template <typename T>
+// .. of a few rows on their way.
+template <typename T, int U, bool NARROW>
 struct RowsAhead {
-    static constexpr int U = 4, FR = 8 / Elem<T>::PER16;
+    static constexpr int FR = 8 / Elem<T>::PER16;
     u32x4 raw[U][FR];
-    __device__ __forceinline__ void ask(int u, const EightColumns<T>& at, int token) {
-        const T* row = at.dY + (int64_t)token * at.ldy;
-        if (at.clean) {
-#pragma unroll
-            for (int f = 0; f < FR; ++f) raw[u][f] = reinterpret_cast<const u32x4_any*>(row)[f];
-        } else {
+    // row: the same for all lanes
+    __device__ __forceinline__ void ask(int u, const T* row, unsigned c, int cols) {
+        if constexpr (NARROW) {
             struct alignas(16) Eight { T v[8]; } y;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y.v[e] = at.c + e < at.cols ? row[e] : (T)0.f;
+            for (int e = 0; e < 8; ++e) y.v[e] = e < cols ? row[e] : (T)0.f;
             __builtin_memcpy(raw[u], &y, sizeof(y));
+        } else {
+#pragma unroll
+            for (int f = 0; f < FR; ++f) raw[u][f] = *reinterpret_cast<const u32x4_any*>(reinterpret_cast<const char*>(row) + (c * (unsigned)sizeof(T) + f * 16));
         }
     }
     __device__ __forceinline__ void add(int u, float* sum) const {
@@ -45,6 +44,12 @@ struct RowsAhead {
         __builtin_memcpy(&y, raw[u], sizeof(y));
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum[e] += Elem<T>::up(y.v[e]);
+    }
+    __device__ __forceinline__ void begin(int u, float* sum) const {
+        struct alignas(16) Eight { T v[8]; } y;
+        __builtin_memcpy(&y, raw[u], sizeof(y));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] = Elem<T>::up(y.v[e]);
     }
 };
 
@@ -89,30 +94,23 @@ struct Mates {
     }
 };
 
-// The sum over all mates, four of them asked for ahead.
-template <typename T>
-__device__ __forceinline__ void sum_of_mates(float* sum, Mates mates, const EightColumns<T>& at) {
-    struct Step {
-        RowsAhead<T> rows;
-        int count;
-    };
-    auto ask = [&](Step& s) {
-        s.count = 0;
+// The sum over all mates, four of them asked for at a time.
+template <typename T, bool NARROW>
+__device__ __forceinline__ void sum_of_mates(float* sum, Mates mates, const T* dY, int64_t ldy, unsigned c, int cols) {
+    while (mates.any()) {
+        RowsAhead<T, 4, NARROW> rows;
+        int have = 0, token = 0;
 #pragma unroll
-        for (int u = 0; u < RowsAhead<T>::U; ++u)
+        for (int u = 0; u < 4; ++u) {
             if (mates.any()) {
-                s.rows.ask(u, at, mates.next());
-                s.count = u + 1;
+                token = mates.next();
+                have = u + 1;
             }
-    };
-    Step now, next;
-    ask(now);
-    while (now.count > 0) {
-        ask(next);
+            rows.ask(u, dY + (int64_t)token * ldy, c, cols);  // the last one again where there are fewer
+        }
 #pragma unroll
-        for (int u = 0; u < RowsAhead<T>::U; ++u)
-            if (u < now.count) now.rows.add(u, sum);
-        now = next;
+        for (int u = 0; u < 4; ++u)
+            if (u < have) rows.add(u, sum);
     }
 }
 
@@ -138,49 +136,59 @@ struct Places {
     }
 };
 
-// Sums the places of a block, one row after another, and calls finish(item, row, place, complete, began, sum) with its last place there; begin(item, row) where
-// that place is asked for, to ask for what finish takes.  complete: the row has all of its places there; began: it has places before them.
-// Most rows have one token or two, so a step is up to four places of one row, and the next step is asked for before this one is added.
-template <typename T, class Item, class Begin, class Finish>
-__device__ __forceinline__ void sum_places_of(const Places& at, const EightColumns<T>& columns, Begin begin, Finish finish) {
+__device__ __forceinline__ uint64_t of_lane(uint64_t v, int lane) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+
+// Sums the places of a block, one row after another, and calls finish(item, p, complete, began, sum) with a row's last place there, the p-th; begin(item, p)
+// where that row is asked for, to ask for what finish takes.  complete: the row has all of its places there; began: it has places before them.
+// Most rows have one token or two, so a step is up to two places of one row, and the next step is asked for before this one is added.  Every step makes the
+// same loads, its last place's again where it has fewer: how many are on their way has to be known for a wait that leaves the next step's alone.
+// Addresses are formed for all places at once, a lane to each: formed for one place after another they took as many scalar instructions as the sums take
+// vector ones.
+template <typename T, bool NARROW, class Item, class Begin, class Finish>
+__device__ __forceinline__ void sum_places_of(const Places& at, const T* dY, int64_t ldy, unsigned c, int cols, Begin begin, Finish finish) {
     struct Step {
-        RowsAhead<T> rows;
+        RowsAhead<T, 2, NARROW> rows;
         Item item;
-        int row, count, last;  // last: the row's last place here if that is in the step, or -1
+        int count, last;  // last: the row's last place here if that is in the step, or -1
     };
+    if (at.count == 0) return;
+    const int lane = threadIdx.x & 63;
+    const uint64_t from_lane = reinterpret_cast<uint64_t>(dY + (int64_t)at.token * ldy), left = lane < at.count ? at.row_ends >> lane : 0;
+    const int last_of_lane = left ? lane + (int)__builtin_ctzll(left) : at.count - 1;
+    const bool open = !(at.row_ends >> (at.count - 1) & 1);  // the last row goes on
     int p = 0;
     auto ask = [&](Step& s) {
-        s.count = 0;
-        if (p >= at.count) return;
-        s.row = __builtin_amdgcn_readlane(at.row, p);
-        const uint64_t left = at.row_ends >> p;
-        const int last = left ? min(p + (int)__builtin_ctzll(left), at.count - 1) : at.count - 1;
-        s.count = min(RowsAhead<T>::U, last - p + 1);
-        s.last = p + s.count > last ? last : -1;
-        if (s.last >= 0) begin(s.item, s.row);
-#pragma unroll
-        for (int u = 0; u < RowsAhead<T>::U; ++u)
-            if (u < s.count) s.rows.ask(u, columns, __builtin_amdgcn_readlane(at.token, p + u));
+        const int from = min(p, at.count - 1), last = __builtin_amdgcn_readlane(last_of_lane, from), to = min(from + 1, last);
+        begin(s.item, from);
+        s.rows.ask(0, reinterpret_cast<const T*>(of_lane(from_lane, from)), c, cols);
+        s.rows.ask(1, reinterpret_cast<const T*>(of_lane(from_lane, to)), c, cols);
+        s.count = p < at.count ? to - from + 1 : 0;
+        s.last = to == last ? last : -1;
         p += s.count;
     };
     float sum[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] = 0.f;
-    bool began = at.began;
-    Step now, next;
-    ask(now);
-    while (now.count > 0) {
-        ask(next);
-#pragma unroll
-        for (int u = 0; u < RowsAhead<T>::U; ++u)
-            if (u < now.count) now.rows.add(u, sum);
-        if (now.last >= 0) {
-            finish(now.item, now.row, at.first + now.last, (at.row_ends >> now.last & 1) && !began, began, sum);
+    bool began = at.began, fresh = true;
+    auto use = [&](const Step& s) {
+        if (fresh) s.rows.begin(0, sum);
+        else s.rows.add(0, sum);
+        if (s.count > 1) s.rows.add(1, sum);
+        fresh = s.last >= 0;
+        if (fresh) {
+            finish(s.item, s.last, !began && !(open && s.last == at.count - 1), began, sum);
             began = false;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] = 0.f;
         }
-        now = next;
+    };
+    Step one, two;  // taken in turns: a copy would cost as much as the sum
+    ask(one);
+    for (;;) {
+        ask(two);
+        use(one);
+        if (two.count == 0) break;
+        ask(one);
+        use(two);
+        if (one.count == 0) break;
     }
 }
 
