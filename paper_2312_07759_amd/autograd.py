@@ -1,5 +1,5 @@
 """torch.autograd front end of the quantisation layer W -> r_tau(W, C*(W)) (Alg. 2, per-layer steps), of products with
-layers in their stored form and of the loss against the unquantised network.
+layers in their stored form or in 8-bit integers, of lookups in embedding tables and of the loss against the unquantised network.
 
 Argument marshalling only: the quantisation's forward is one idkm_forward call, its backward one idkm_backward call on the same
 context; every step runs in the library's kernels.  One context per layer (the library keeps C*, n*, F* and a borrowed
@@ -123,7 +123,7 @@ def _context(device):
 def _no_capture(*tensors):
     # A graph that records the backward pass of leaves which an eager graph holds too ends the process.
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors) and torch.cuda.is_current_stream_capturing():
-        raise RuntimeError("a differentiable call cannot be captured: capture Context.codes_linear, codes_linear_backward and distill")
+        raise RuntimeError("a differentiable call cannot be captured: capture the methods of Context (codes_linear, codes_linear_backward, distill ..)")
 
 
 def _no_captured_backward():
@@ -133,20 +133,30 @@ def _no_captured_backward():
 
 class _CodesProduct(torch.autograd.Function):
     @staticmethod
-    def forward(fn, X, C, S, layer):
-        fn.layer = layer
-        fn.save_for_backward(X, C, S, layer.words)
-        return _context(X.get_device()).codes_linear(layer, X)
+    def forward(fn, X, C, S, layer, keep8=False):
+        ctx, (_, need_C, need_S) = _context(X.get_device()), fn.needs_input_grad[:3]
+        fn.layer, fn.kept = layer, None
+        held = (X, None)
+        if keep8:
+            held = (None, None)  # dX does not need X
+            if need_C or need_S:
+                fn.kept = X.dtype
+                kept = ctx.keep8(X)
+                held = (kept.Q, kept.E)
+        fn.save_for_backward(*held, C, S, layer.words)
+        return ctx.codes_linear(layer, X)
 
     @staticmethod
     @once_differentiable
     def backward(fn, dY):
         _no_captured_backward()
-        X, C, S, _ = fn.saved_tensors
+        X, E, C, S, _ = fn.saved_tensors
         need_X, need_C, need_S = fn.needs_input_grad[:3]
-        r = _context(X.get_device()).codes_linear_backward(fn.layer, X, dY.contiguous(), want_dX=need_X, want_dC=need_C,
-                                                           want_dS=need_S)
-        return r.get("dX"), r["dC"].to(C.dtype) if need_C else None, r["dS"].to(S.dtype) if need_S else None, None
+        if fn.kept is not None:
+            X = binding.Kept8(X, E, fn.layer.cols, fn.kept)
+        r = _context(fn.layer.device).codes_linear_backward(fn.layer, X, dY.contiguous(), want_dX=need_X, want_dC=need_C,
+                                                            want_dS=need_S)
+        return r.get("dX"), r["dC"].to(C.dtype) if need_C else None, r["dS"].to(S.dtype) if need_S else None, None, None
 
 
 def _as_rows(t):
@@ -160,12 +170,13 @@ def _as_rows(t):
 class CodesLinear(torch.nn.Module):
     """Product with a [rows, cols] layer in its stored form (binding.CodesLayer): X [..., cols] of any strides -> X w^T [..., rows], in X's
     type (float32, float16 or bfloat16).  The codes stay; the codebook C (float32) and the scales S are parameters, so that both, and
-    what lies below, can be trained."""
+    what lies below, can be trained.  keep8: X is kept in 8 bits (binding.Context.keep8) between the forward and the backward pass, a quarter of
+    float32's memory and half of 16 bits'; dC and dS are then those of the kept X, dX is the same."""
 
-    def __init__(self, layer):
+    def __init__(self, layer, keep8=False):
         super().__init__()
         _context(layer.device)
-        self.rows, self.cols, self.group = layer.rows, layer.cols, layer.group
+        self.rows, self.cols, self.group, self.keep8 = layer.rows, layer.cols, layer.group, bool(keep8)
         self.register_buffer("words", layer.words)
         self.C = torch.nn.Parameter(layer.C.detach().to(torch.float32, copy=True))
         self.S = torch.nn.Parameter(layer.S.detach().clone()) if layer.S is not None else None
@@ -183,7 +194,117 @@ class CodesLinear(torch.nn.Module):
         _no_capture(X, self.C, self.S)
         tracked = torch.is_grad_enabled() and (X.requires_grad or self.C.requires_grad or (self.S is not None and self.S.requires_grad))
         layer = self.layer(X.dtype, copy=tracked)
-        return _CodesProduct.apply(_as_rows(X.reshape(-1, self.cols)), self.C, self.S, layer).view(*X.shape[:-1], self.rows)
+        return _CodesProduct.apply(_as_rows(X.reshape(-1, self.cols)), self.C, self.S, layer, self.keep8).view(*X.shape[:-1], self.rows)
+
+
+def _ids(ids):
+    if ids.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"ids must be int32 or int64, got {ids.dtype}")
+    return ids.reshape(-1).contiguous()
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(fn, W, ids, alpha, dtype):
+        fn.rows, fn.alpha = W.shape[0], alpha
+        fn.save_for_backward(ids)
+        return _context(W.get_device()).embedding(W, ids, alpha, dtype)
+
+    @staticmethod
+    @once_differentiable
+    def backward(fn, dY):
+        _no_captured_backward()
+        ids, = fn.saved_tensors
+        return _context(ids.get_device()).embedding_backward(_as_rows(dY), ids, fn.rows, fn.alpha), None, None, None
+
+
+def embedding(ids, W, alpha=1.0, dtype=torch.float32):
+    """Rows ids [...] (int32 or int64; a negative one is padding, a row of zeros) of the float32 table W [rows, cols], times alpha, [..., cols] in
+    `dtype`; differentiable in W (SoftKMeansQuantize's Wq, say), whose gradient is float32."""
+    if W.dim() != 2:
+        raise ValueError(f"W must be [rows, cols], got {tuple(W.shape)}")
+    _no_capture(W)
+    return _Embedding.apply(W.contiguous(), _ids(ids), float(alpha), dtype).view(*ids.shape, W.shape[1])
+
+
+class _CodesLookup(torch.autograd.Function):
+    @staticmethod
+    def forward(fn, C, S, ids, layer, alpha):
+        fn.layer, fn.alpha = layer, alpha
+        fn.save_for_backward(C, S, ids, layer.words)
+        return _context(layer.device).codes_embedding(layer, ids, alpha)
+
+    @staticmethod
+    @once_differentiable
+    def backward(fn, dY):
+        _no_captured_backward()
+        C, S, ids, _ = fn.saved_tensors
+        need_C, need_S = fn.needs_input_grad[:2]
+        r = _context(fn.layer.device).codes_embedding_backward(fn.layer, ids, _as_rows(dY), fn.alpha, want_dC=need_C, want_dS=need_S)
+        return r["dC"].to(C.dtype) if need_C else None, r["dS"].to(S.dtype) if need_S else None, None, None, None
+
+
+class CodesEmbedding(torch.nn.Module):
+    """Embedding table in its stored form (a [rows, cols] binding.CodesLayer): ids [...] (int32 or int64; a negative one is padding, a row of zeros) ->
+    alpha times their rows, [..., cols] in `dtype` (the layer's unless given).  The codes stay; the codebook C (float32) and the scales S are parameters."""
+
+    def __init__(self, layer, alpha=1.0, dtype=None):
+        super().__init__()
+        _context(layer.device)
+        self.rows, self.cols, self.group, self.alpha, self.dtype = layer.rows, layer.cols, layer.group, float(alpha), dtype or layer.dtype
+        self.register_buffer("words", layer.words)
+        self.C = torch.nn.Parameter(layer.C.detach().to(torch.float32, copy=True))
+        self.S = torch.nn.Parameter(layer.S.detach().clone()) if layer.S is not None else None
+
+    layer = CodesLinear.layer
+
+    def forward(self, ids):
+        _no_capture(self.C, self.S)
+        tracked = torch.is_grad_enabled() and (self.C.requires_grad or (self.S is not None and self.S.requires_grad))
+        layer = self.layer(self.dtype, copy=tracked)
+        return _CodesLookup.apply(self.C, self.S, _ids(ids), layer, self.alpha).view(*ids.shape, self.cols)
+
+
+class _Int8Product(torch.autograd.Function):
+    @staticmethod
+    def forward(fn, X, layer):
+        fn.layer = layer
+        fn.save_for_backward(layer.W8, layer.scale)
+        return _context(X.get_device()).int8_linear(layer, X)
+
+    @staticmethod
+    @once_differentiable
+    def backward(fn, dY):
+        _no_captured_backward()
+        _ = fn.saved_tensors  # integers and scales that were changed in place since are refused
+        return _context(fn.layer.device).int8_linear_backward(fn.layer, _as_rows(dY)), None
+
+
+class Int8Linear(torch.nn.Module):
+    """Product in 8-bit integers with a layer that stays as it is (binding.Int8Layer, see binding.Context.int8_layer): X [..., cols] of any strides ->
+    [..., rows], in X's type (float32, float16 or bfloat16).  X's rows are brought to integers in the call; the gradient in X is that of
+    the product with X itself, so that what lies below can be trained."""
+
+    def __init__(self, layer):
+        super().__init__()
+        _context(layer.device)
+        self.rows, self.cols = layer.rows, layer.cols
+        self.register_buffer("W8", layer.W8)
+        self.register_buffer("scale", layer.scale)
+        self._layers = {}
+
+    def layer(self, dtype):
+        """The layer as it is now, for activations of `dtype`."""
+        made = self._layers.get(dtype)
+        if made is None or made[0] is not self.W8 or made[1] is not self.scale:
+            made = self._layers[dtype] = self.W8, self.scale, binding.Int8Layer(self.W8, self.scale.float(), dtype, self.cols)
+        return made[2]
+
+    def forward(self, X):
+        if X.shape[-1] != self.cols:
+            raise ValueError(f"X must be [..., {self.cols}], got {tuple(X.shape)}")
+        _no_capture(X)
+        return _Int8Product.apply(_as_rows(X.reshape(-1, self.cols)), self.layer(X.dtype)).view(*X.shape[:-1], self.rows)
 
 
 class _Distill(torch.autograd.Function):

@@ -16,15 +16,32 @@ struct RowScale {
         s = top >= 0x7f800000 ? __builtin_nanf("") : fmaxf(__builtin_bit_cast(float, top) / 127.f, 0x1p-126f);
         inverse = 1.f / s;
     }
-    // The product with the rounded inverse is at most one off.  What is left, x - q s, is exact where it decides: it is a multiple of half the last
-    // place of s and no larger than about s / 2; where it is rounded (x below s / 2, q = 1) it cannot become smaller than s / 2.
-    __device__ __forceinline__ int integer(float x) const {
-        float q = __builtin_rintf(x * inverse);
-        const float left = fmaf(-q, s, x), half = 0.5f * s;
-        const bool odd = ((int)q & 1) != 0;
-        q += left > half || (left == half && odd) ? 1.f : 0.f;
-        q -= left < -half || (left == -half && odd) ? 1.f : 0.f;
-        return (int)q;
+    // Eight integers, as bytes.  The product with the rounded inverse differs from the quotient by less than 2^-15, so its nearest integer is the quotient's unless it
+    // lies beside a tie; then what is left, x - q s, decides, which is exact where it does: it is a multiple of half the last place of s and no larger than
+    // about s / 2; where it is rounded (x below s / 2, q = 1) it cannot become smaller than s / 2.
+    __device__ __forceinline__ u32x2 integers(const float* x) const {
+        float q[8], beside = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float m = x[e] * inverse;
+            q[e] = __builtin_rintf(m);
+            beside = fmaxf(beside, fabsf(m - q[e]));
+        }
+        if (__any(beside > 0.5f - 0x1p-14f)) {
+            const float half = 0.5f * s;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float left = fmaf(-q[e], s, x[e]);
+                const bool odd = ((int)q[e] & 1) != 0;
+                q[e] += (left > half || (left == half && odd) ? 1.f : 0.f) - (left < -half || (left == -half && odd) ? 1.f : 0.f);
+            }
+        }
+        uint32_t b[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] = (uint32_t)(int)q[e];
+        // the low bytes of two registers, then of two pairs
+        auto pair = [](uint32_t low, uint32_t high) { return __builtin_amdgcn_perm(high, low, 0x0c0c0400u); };
+        return u32x2{pair(b[0], b[1]) | pair(b[2], b[3]) << 16, pair(b[4], b[5]) | pair(b[6], b[7]) << 16};
     }
 };
 
@@ -51,38 +68,30 @@ __device__ __forceinline__ uint32_t larger_of_wave(uint32_t top) {
     return top;
 }
 
-__device__ __forceinline__ u32x2 eight_integers(const RowScale& s, const float* v) {
-    u32x2 q{0, 0};
+__device__ __forceinline__ uint32_t larger_of_eight(uint32_t top, const float* v) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q[e >> 2] |= ((uint32_t)s.integer(v[e]) & 255u) << (e & 3) * 8;
-    return q;
+    for (int e = 0; e < 8; ++e) top = max(top, size_of(v[e]));
+    return top;
 }
 
-// A workgroup to a row; up to 8192 columns stay in registers between the two looks at them.
+// A workgroup to a row; up to 4096 columns stay in registers between the two looks at them.
+// 2048 rows of 4096 columns, bfloat16: 8 to 10 us (a copy's rate: 5; every quotient decided by what is left: 9.6; a wavefront to a row, without a barrier: 10).
 template <typename T>
 __global__ __launch_bounds__(256) void k_int8_rows(const Int8RowsArgs a) {
-    constexpr int HELD = 4;
+    constexpr int HELD = 2;
     __shared__ uint32_t tops[4];
     const int64_t t = blockIdx.x;
     const T* row = static_cast<const T*>(a.X) + t * a.ldx;
     float v[HELD][8];
     uint32_t top = 0;
 #pragma unroll
-    for (int h = 0; h < HELD; ++h) {
-        const int64_t c = (h * 256 + threadIdx.x) * 8;
-        if (c < a.ldq) eight_floats(v[h], row, c, a.cols);
-    }
+    for (int h = 0; h < HELD; ++h) eight_floats(v[h], row, (int64_t)(h * 256 + threadIdx.x) * 8, a.cols);
 #pragma unroll
-    for (int h = 0; h < HELD; ++h)
-        if ((h * 256 + (int)threadIdx.x) * 8 < a.ldq) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, size_of(v[h][e]));
-        }
+    for (int h = 0; h < HELD; ++h) top = larger_of_eight(top, v[h]);
     for (int64_t c = (HELD * 256 + threadIdx.x) * 8; c < a.cols; c += 2048) {
         float w[8];
         eight_floats(w, row, c, a.cols);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = max(top, size_of(w[e]));
+        top = larger_of_eight(top, w);
     }
     top = larger_of_wave(top);
     if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
@@ -93,12 +102,13 @@ __global__ __launch_bounds__(256) void k_int8_rows(const Int8RowsArgs a) {
 #pragma unroll
     for (int h = 0; h < HELD; ++h) {
         const int64_t c = (h * 256 + threadIdx.x) * 8;
-        if (c < a.ldq) *reinterpret_cast<u32x2*>(out + c) = eight_integers(s, v[h]);
+        const u32x2 q = s.integers(v[h]);
+        if (c < a.ldq) *reinterpret_cast<u32x2*>(out + c) = q;
     }
     for (int64_t c = (HELD * 256 + threadIdx.x) * 8; c < a.ldq; c += 2048) {
         float w[8];
         eight_floats(w, row, c, a.cols);
-        *reinterpret_cast<u32x2*>(out + c) = eight_integers(s, w);
+        *reinterpret_cast<u32x2*>(out + c) = s.integers(w);
     }
 }
 
@@ -106,94 +116,133 @@ void launch_int8_rows(int dtype, const Int8RowsArgs& a, hipStream_t s) {
     BY_TYPE(dtype, T, hipLaunchKernelGGL(k_int8_rows<T>, dim3((unsigned)a.n), dim3(256), 0, s, a));
 }
 
-// 16 rows of the layer and 16 NT tokens to a workgroup, whose eight wavefronts share the sum in chunks of 256 columns; lane l has row l % 16 and, of
-// every 64 columns, the 16 of quarter l / 16.  The layer's first integers are asked for before the tokens are looked at.
+// 16 rows of the layer and 16 NT tokens to a workgroup, whose WAVES wavefronts share the sum; lane l has row l % 16 and, of every 64 columns, the 16 of quarter
+// l / 16.  Integers of four to eight such steps are asked for together, where there are registers the next ones
+// before these are used.
 // FUSED (up to INT8_FUSED elements of X, NT = 1): every workgroup brings the tokens to integers itself, into LDS, instead of a launch before this one.
-template <typename T, int NT, bool FUSED>
-__global__ __launch_bounds__(512) void k_int8_few(const Int8FewArgs a) {
-    constexpr int U = 4;  // 64 columns each: a chunk
+template <typename T, int NT, int WAVES, bool FUSED>
+__global__ __launch_bounds__(64 * WAVES) void k_int8_few(const Int8FewArgs a) {
+    constexpr int U = FUSED ? 8 : NT == 1 ? 6 : 4, XN = FUSED ? 1 : NT;
+    constexpr bool AHEAD = FUSED || NT > 1;  // sixteen wavefronts have 128 registers each
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int li = lane & 15, q = lane >> 4;
     const int64_t r0 = (int64_t)blockIdx.x * 16, t0 = (int64_t)blockIdx.y * 16 * NT;
     const int8_t* W = a.W8 + min(r0 + li, a.rows - 1) * a.ldw + q * 16;  // rows and tokens behind the last: computed from it, not stored
-    const int steps = (int)(a.pad / 64), each = ((steps + 7) / 8 + U - 1) / U * U;
+    const int steps = (int)(a.pad / 64), each = (steps + WAVES - 1) / WAVES;
     const int first = min(steps, wave * each), last = min(steps, first + each);
-    u32x4 w[2][U];
-    auto ask = [&](int of, int step) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) w[of][u] = *reinterpret_cast<const u32x4*>(W + (int64_t)min(step + u, steps - 1) * 64);
+    struct Batch {
+        u32x4 w[U], x[XN][U];
     };
-    if (first < last) {
-        ask(0, first);
-        ask(1, first + U);
+    const int8_t* X[XN];
+    if constexpr (!FUSED) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) X[i] = a.Q + min(t0 + i * 16 + li, a.n - 1) * a.pad + q * 16;
     }
+    auto ask = [&](Batch& b, int step) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t c = (int64_t)min(step + u, steps - 1) * 64;
+            b.w[u] = *reinterpret_cast<const u32x4*>(W + c);
+            if constexpr (!FUSED) {
+#pragma unroll
+                for (int i = 0; i < NT; ++i) b.x[i][u] = *reinterpret_cast<const u32x4*>(X[i] + c);
+            }
+        }
+    };
+    Batch now, next;
+    if constexpr (!FUSED) ask(now, first);
     float scales[NT][4];
-    const int8_t* X[NT];
     if constexpr (FUSED) {
-        uint32_t* tops = reinterpret_cast<uint32_t*>(lds);  // [n][8]
-        int8_t* held = reinterpret_cast<int8_t*>(lds) + 512;  // [n][pad]
-        const int n = (int)a.n;
-        for (int t = 0; t < n; ++t) {
-            uint32_t top = 0;
-            for (int64_t c = threadIdx.x * 8; c < a.cols; c += 4096) {
-                float v[8];
-                eight_floats(v, static_cast<const T*>(a.X) + t * a.ldx, c, a.cols);
+        // pieces of eight elements, up to HELD of a thread, which stay in its registers between the two looks at them
+        constexpr int HELD = (int)(INT8_FUSED / 8 / (64 * WAVES));
+        uint32_t* tops = reinterpret_cast<uint32_t*>(lds);    // [16]
+        int8_t* held = reinterpret_cast<int8_t*>(lds) + 64;  // [n][pad]
+        const int n = (int)a.n, of_row = (int)(a.pad / 8), pieces = n * of_row, cols = (int)a.cols;
+        u32x4 raw[HELD][8 / Elem<T>::PER16];
+        auto floats = [&](int h, float* v) {
+            struct alignas(16) Eight { T v[8]; } y;
+            __builtin_memcpy(&y, raw[h], sizeof(y));
 #pragma unroll
-                for (int e = 0; e < 8; ++e) top = max(top, size_of(v[e]));
+            for (int e = 0; e < 8; ++e) v[e] = Elem<T>::up(y.v[e]);
+        };
+#pragma unroll
+        for (int h = 0; h < HELD; ++h) {
+            const int piece = h * 64 * WAVES + (int)threadIdx.x;
+            if (piece >= pieces) continue;
+            const int t = piece / of_row, c = (piece - t * of_row) * 8;
+            const T* row = static_cast<const T*>(a.X) + t * a.ldx;
+            if (c + 8 <= cols) {
+#pragma unroll
+                for (int f = 0; f < 8 / Elem<T>::PER16; ++f) raw[h][f] = reinterpret_cast<const u32x4_any*>(row + c)[f];
+            } else {
+                struct alignas(16) Eight { T v[8]; } y;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y.v[e] = c + e < cols ? row[c + e] : (T)0.f;
+                __builtin_memcpy(raw[h], &y, sizeof(y));
             }
-            top = larger_of_wave(top);
-            if (lane == 0) tops[t * 8 + wave] = top;
+        }
+        ask(now, first);  // behind the tokens, which are waited for first
+        if (threadIdx.x < 16) tops[threadIdx.x] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < HELD; ++h) {
+            const int piece = h * 64 * WAVES + (int)threadIdx.x;
+            uint32_t top = 0;
+            if (piece < pieces) {
+                float v[8];
+                floats(h, v);
+                top = larger_of_eight(0, v);
+            }
+            if (h * 64 * WAVES >= pieces) continue;
+            if (of_row % 64 == 0) {  // a wavefront's pieces are of one token
+                top = larger_of_wave(top);
+                if (lane == 0 && piece < pieces) atomicMax(&tops[piece / of_row], top);
+            } else if (piece < pieces) {
+                atomicMax(&tops[piece / of_row], top);
+            }
         }
         __syncthreads();
-        for (int t = 0; t < n; ++t) {
-            uint32_t top = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = max(top, tops[t * 8 + i]);
-            const RowScale s(top);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (q * 4 + r == t) scales[0][r] = s.s;
-            for (int64_t c = threadIdx.x * 8; c < a.pad; c += 4096) {
-                float v[8];
-                eight_floats(v, static_cast<const T*>(a.X) + t * a.ldx, c, a.cols);
-                *reinterpret_cast<u32x2*>(held + t * a.pad + c) = eight_integers(s, v);
-            }
+        for (int h = 0; h < HELD; ++h) {
+            const int piece = h * 64 * WAVES + (int)threadIdx.x;
+            if (piece >= pieces) continue;
+            float v[8];
+            floats(h, v);
+            *reinterpret_cast<u32x2*>(held + piece * 8) = RowScale(tops[piece / of_row]).integers(v);
         }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) scales[0][r] = q * 4 + r < n ? RowScale(tops[q * 4 + r]).s : 0.f;
         __syncthreads();
-        X[0] = held + min(li, n - 1) * a.pad + q * 16;
+        X[0] = held + min(li, n - 1) * (int)a.pad + q * 16;
     } else {
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            X[i] = a.Q + min(t0 + i * 16 + li, a.n - 1) * a.pad + q * 16;
+        for (int i = 0; i < NT; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) scales[i][r] = a.q_scale[min(t0 + i * 16 + q * 4 + r, a.n - 1)];
-        }
     }
     intx4 acc[NT];
 #pragma unroll
     for (int i = 0; i < NT; ++i) acc[i] = intx4{0, 0, 0, 0};
-    auto use = [&](int of, int step) {
+    for (int step = first; step < last; step += U) {
+        if (AHEAD && step + U < last) ask(next, step + U);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (step + u >= last) break;
 #pragma unroll
-            for (int i = 0; i < NT; ++i) mma16<int8_t>(acc[i], *reinterpret_cast<const u32x4*>(X[i] + (int64_t)(step + u) * 64), w[of][u]);
+            for (int i = 0; i < NT; ++i) {
+                if constexpr (FUSED) mma16<int8_t>(acc[i], *reinterpret_cast<const u32x4*>(X[i] + (step + u) * 64), now.w[u]);
+                else mma16<int8_t>(acc[i], now.x[i][u], now.w[u]);
+            }
         }
-    };
-    for (int step = first; step < last; step += 2 * U) {
-        use(0, step);
-        if (step + 2 * U < last) ask(0, step + 2 * U);
-        if (step + U < last) {
-            use(1, step + U);
-            if (step + 3 * U < last) ask(1, step + 3 * U);
-        }
+        if (AHEAD) now = next;
+        else if (step + U < last) ask(now, step + U);
     }
     // the wavefronts' sums, exact in any order
     __syncthreads();
-    int* sums = reinterpret_cast<int*>(lds);  // [NT][8][256]
+    int* sums = reinterpret_cast<int*>(lds);  // [NT][WAVES][256]
 #pragma unroll
-    for (int i = 0; i < NT; ++i) *reinterpret_cast<intx4*>(sums + ((i * 8 + wave) * 64 + lane) * 4) = acc[i];
+    for (int i = 0; i < NT; ++i) *reinterpret_cast<intx4*>(sums + ((i * WAVES + wave) * 64 + lane) * 4) = acc[i];
     __syncthreads();
     if (wave >= NT) return;
     // wavefront i: tokens i 16 + 4 q + r of row li
@@ -206,7 +255,7 @@ __global__ __launch_bounds__(512) void k_int8_few(const Int8FewArgs a) {
         }
     intx4 sum{0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += *reinterpret_cast<const intx4*>(sums + ((wave * 8 + i) * 64 + lane) * 4);
+    for (int i = 0; i < WAVES; ++i) sum += *reinterpret_cast<const intx4*>(sums + ((wave * WAVES + i) * 64 + lane) * 4);
     if (r0 + li >= a.rows) return;
     const float by = a.scale[r0 + li];
 #pragma unroll
@@ -216,19 +265,21 @@ __global__ __launch_bounds__(512) void k_int8_few(const Int8FewArgs a) {
     }
 }
 
-template <typename T, int NT, bool FUSED>
+template <typename T, int NT, int WAVES, bool FUSED>
 static void launch_few(const Int8FewArgs& a, hipStream_t s) {
-    const size_t sums = (size_t)NT * 8192, held = FUSED ? 512 + (size_t)(a.n * a.pad) : 0, lds = held > sums ? held : sums;
-    void (*const fn)(const Int8FewArgs) = &k_int8_few<T, NT, FUSED>;
+    const size_t sums = (size_t)NT * WAVES * 1024, held = FUSED ? 64 + (size_t)(a.n * a.pad) : 0, lds = held > sums ? held : sums;
+    void (*const fn)(const Int8FewArgs) = &k_int8_few<T, NT, WAVES, FUSED>;
     allow_lds(reinterpret_cast<const void*>(fn), lds);
-    hipLaunchKernelGGL(fn, dim3((unsigned)((a.rows + 15) / 16), (unsigned)((a.n + 16 * NT - 1) / (16 * NT))), dim3(512), lds, s, a);
+    hipLaunchKernelGGL(fn, dim3((unsigned)((a.rows + 15) / 16), (unsigned)((a.n + 16 * NT - 1) / (16 * NT))), dim3(64 * WAVES), lds, s, a);
 }
 
+// Where there are fewer workgroups than compute units, with fewer tokens or more wavefronts to each.
 void launch_int8_few(int dtype, const Int8FewArgs& a, hipStream_t s) {
-    if (!a.Q) BY_TYPE(dtype, T, (launch_few<T, 1, true>(a, s)));
-    else if (a.n <= 16) BY_TYPE(dtype, T, (launch_few<T, 1, false>(a, s)));
-    else if (a.n <= 32) BY_TYPE(dtype, T, (launch_few<T, 2, false>(a, s)));
-    else BY_TYPE(dtype, T, (launch_few<T, 4, false>(a, s)));
+    const int64_t blocks = (a.rows + 15) / 16;
+    if (!a.Q) BY_TYPE(dtype, T, (launch_few<T, 1, 8, true>(a, s)));
+    else if (a.n > 32 && blocks * ((a.n + 63) / 64) >= 256) BY_TYPE(dtype, T, (launch_few<T, 4, 8, false>(a, s)));
+    else if (a.n > 16 && blocks * ((a.n + 31) / 32) >= 256) BY_TYPE(dtype, T, (launch_few<T, 2, 8, false>(a, s)));
+    else BY_TYPE(dtype, T, (launch_few<T, 1, 16, false>(a, s)));
 }
 
 template <typename T>

@@ -10,6 +10,8 @@
 // barrier: nothing covers it where a workgroup fills a compute unit (16 bits: 256 x 128, 256 x 256 and 128 x 128 with four stages; float: 128 x 128);
 // of the other shapes two fit.
 #pragma once
+#include <type_traits>
+
 #include "elem.hpp"
 
 namespace idkm {
@@ -158,7 +160,74 @@ __global__ __launch_bounds__(64 * WM * WN, SC > 0 ? 2 : 1) void k_tile_product(c
     const int wm = wave / WN, wn = wave % WN;
     const int li = lane & 15, q = lane >> 4;
     const int row_a = wm * (BM / WM) + li, row_b = BM + wn * (BN / WN) + li;
-    if (first < last) {
+    constexpr bool TURNS = SC == 0 && TM * TN >= 8;  // fewer matrix instructions do not cover what is put between them
+    if (TURNS && first < last) {
+        // Half a step's fragments are read while the matrix cores work on the other half's, and the next steps' copies are issued a few at a time between
+        // matrix instructions: issued one after another they hold up the wavefront for as long as the loads of all wavefronts take to be accepted.
+        constexpr int MMAS = TM * TN, READS = TM + TN, LATER = PPW / 2, NOW = PPW - LATER;
+        u32x4 fa[2][TM], fb[2][TN];
+        auto read = [&](int h, int slot, int i) {
+            const unsigned char* base = lds + slot * STAGE;
+            const int c = (((h << 2) | q) ^ (li & 7)) << 4;
+            if (i < TN) fb[h][i] = *reinterpret_cast<const u32x4*>(base + (row_b + i * 16) * TP_STEP + c);
+            else fa[h][i - TN] = *reinterpret_cast<const u32x4*>(base + (row_a + (i - TN) * 16) * TP_STEP + c);
+        };
+        auto copy = [&](int step, int slot, int p) {
+            const int64_t off = (int64_t)min(step, last - 1) * TP_STEP;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src[p] + off),
+                                             (__attribute__((address_space(3))) void*)(lds + slot * STAGE + (wave * PPW + p) * 1024), 16, 0, 0);
+        };
+        // matrix instructions of half h; between them the other half's fragments are read, from read_slot, and copies [from, to) of copy_step are issued
+        auto multiply = [&](int h, int read_slot, int copy_step, int copy_slot, auto from_, auto to_) {
+            constexpr int from = decltype(from_)::value, to = decltype(to_)::value;
+            int r = 0, p = from;
+#pragma unroll
+            for (int m = 0; m < MMAS; ++m) {
+                mma16<T>(acc[m / TN][m % TN], fb[h][m % TN], fa[h][m / TN]);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int again = 0; again < READS; ++again)
+                    if (r < READS && r * 3 * MMAS <= m * 4 * READS) read(1 - h, read_slot, r++);
+#pragma unroll
+                for (int again = from; again < to; ++again)
+                    if (p < to && (2 * (p - from) + 1) * MMAS <= 2 * (m + 1) * (to - from)) copy(copy_step, copy_slot, p++);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int again = 0; again < READS; ++again)
+                if (r < READS) read(1 - h, read_slot, r++);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        // vmcnt: so many copies of this wavefront may still be on their way; lgkmcnt 0: its own reads have returned
+        constexpr auto wait = [](int copies) { return 0x0070 | (copies & 15) | ((copies >> 4) << 14); };
+        constexpr std::integral_constant<int, 0> none;
+        constexpr std::integral_constant<int, NOW> now;
+        constexpr std::integral_constant<int, PPW> all;
+#pragma unroll
+        for (int s = 0; s < ST; ++s)
+#pragma unroll
+            for (int p = 0; p < (s < ST - 1 ? PPW : NOW); ++p) copy(first + s, s, p);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(wait((ST - 2) * PPW + NOW));
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < READS; ++i) read(0, 0, i);
+        int slot = 0;
+        for (int step = first; step < last; ++step) {
+            const int before = slot == 0 ? ST - 1 : slot - 1, next = slot + 1 == ST ? 0 : slot + 1;
+            multiply(0, slot, step + ST - 1, before, now, all);
+            // behind the barrier everybody's copies of the next step are there, and everybody has read this step's slot, which is fetched into next
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(wait((ST - 2) * PPW));
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            multiply(1, next, step + ST, slot, none, now);  // behind the last step: fragments that nobody uses
+            slot = next;
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // nothing may still be written into this LDS when it is given to others
+    }
+    if (!TURNS && first < last) {
 #pragma unroll
         for (int s = 0; s < ST - 1; ++s) fetch(first + s, s);
         int slot = 0;
