@@ -523,8 +523,14 @@ __global__ __launch_bounds__(256) void k_lookup_codes_fast(const LookupArgs a) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) out.y.v[e] = of == 1 ? (T)0.f : Elem<T>::nan();
             }
-            // the row's last lanes write some columns twice, the same values
-            if (columns.skip < 8) out.store(static_cast<T*>(a.Y) + (first + p) * a.ldy + c, 8);
+            T* to = static_cast<T*>(a.Y) + (first + p) * a.ldy + c;
+            if (columns.skip == 0) {
+                out.store(to, 8);
+            } else if (columns.skip < 8) {  // its scale is that of the columns that are its own
+#pragma unroll
+                for (int e = 1; e < 8; ++e)
+                    if (e >= columns.skip) to[e] = out.y.v[e];
+            }
             now = next;
         }
     }
