@@ -599,11 +599,13 @@ class Context:
         code, (n, cols) = _dtype(X, "X"), X.shape
         ldx = _rows(X, X.dtype, cols, self.device, "X")
         blocks = -(-cols // 32)
-        Q, E = X.new_empty(n, 32 * blocks, dtype=torch.int8), X.new_empty(n, blocks, dtype=torch.uint8)
+        kept = Kept8.__new__(Kept8)
+        kept.Q, kept.E = Q, E = X.new_empty(n, 32 * blocks, dtype=torch.int8), X.new_empty(n, blocks, dtype=torch.uint8)
+        kept.cols, kept.dtype, kept.code, kept.device, kept.shape = cols, X.dtype, code, self.device, (n, cols)
         st = self._lib.idkm_keep8(self._h, X.data_ptr(), n, cols, ldx, code, Q.data_ptr(), E.data_ptr(), self._raw_stream())
         if st:
             self._check(st)
-        return Kept8(Q, E, cols, X.dtype)
+        return kept
 
     def restore8(self, kept, out=None):
         """idkm_restore8: the activations [n, cols] that `kept` stands for, in their type."""

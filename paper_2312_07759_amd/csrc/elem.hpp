@@ -16,6 +16,7 @@ typedef u32x2 u32x2_word __attribute__((aligned(4)));
 typedef u32x4 u32x4_word __attribute__((aligned(4)));
 typedef uint32_t u32x3_word __attribute__((ext_vector_type(3), aligned(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));  // 16 bytes from any even address: global memory allows it
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 

@@ -8,11 +8,15 @@ namespace idkm {
 
 // ---- the order of the tokens
 
-// .. and `count` floats cleared behind it.
+// The workgroups behind the first GROUPS clear `count` floats, beside them.
+constexpr unsigned GROUPS = 257;
 __global__ __launch_bounds__(GROUP_WAVES * 64) void k_group_tokens(const TokenIds in, const TokenOrder out, float* clear, int64_t count) {
     extern __shared__ __align__(16) int group_lds_words[];
-    group_tokens(in, out, group_lds_words);
-    const int64_t t = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * blockDim.x;
+    if (blockIdx.x < GROUPS) {
+        group_tokens(in, out, group_lds_words);
+        return;
+    }
+    const int64_t t = (int64_t)(blockIdx.x - GROUPS) * blockDim.x + threadIdx.x, step = (int64_t)(gridDim.x - GROUPS) * blockDim.x;
     if ((reinterpret_cast<uintptr_t>(clear) & 15) == 0) {
         for (int64_t i = t; i < count / 4; i += step) reinterpret_cast<floatx4*>(clear)[i] = floatx4{0.f, 0.f, 0.f, 0.f};
         if (t < (count & 3)) clear[count - 1 - t] = 0.f;
@@ -118,7 +122,8 @@ TokenOrder launch_sort(const TokenIds& ids, int32_t* ws, float* clear, int64_t c
     TokenOrder order{ws, ws + n};
     if (n <= GROUP_TOKENS) {
         allow_lds(reinterpret_cast<const void*>(&k_group_tokens), group_lds(n));
-        hipLaunchKernelGGL(k_group_tokens, dim3(257), dim3(GROUP_WAVES * 64), group_lds(n), s, ids, order, clear, count);
+        const unsigned clearing = (unsigned)std::min<int64_t>(512, (count + 4095) / 4096);
+        hipLaunchKernelGGL(k_group_tokens, dim3(GROUPS + clearing), dim3(GROUP_WAVES * 64), group_lds(n), s, ids, order, clear, count);
         return order;
     }
     if (count > 0) launch_fill_zero(clear, count, s);
@@ -259,7 +264,7 @@ __global__ __launch_bounds__(256) void k_join_sums(const SumArgs a) {
 // Places to a wavefront: some 4096 wavefronts, at most 64 places each.
 int sum_places(int64_t n, int64_t cols) {
     const int64_t strips = (cols + 511) / 512, each = n * strips / 4096;
-    return each < 8 ? 8 : each > 64 ? 64 : (int)each;
+    return each < 4 ? 4 : each > 64 ? 64 : (int)each;
 }
 
 int64_t sum_partials(int64_t n, int64_t cols) {
@@ -295,43 +300,46 @@ __global__ __launch_bounds__(256) void k_join_lookup(const LookupGradArgs a, int
         return;
     }
     const int64_t n = a.ids.n;
-    if (a.few) {  // a row is in one part
-        for (int64_t i = (int64_t)(blockIdx.x - kd) * 256 + threadIdx.x; i < n * a.groups; i += (int64_t)(gridDim.x - kd) * 256) {
-            const int64_t t = i / a.groups;
-            const int g = (int)(i - t * a.groups), row = a.order.row_at[t];
-            if (row >= a.ids.rows) continue;
+    // Lanes to a group's segments, a power of two; a wavefront takes as many groups at a time as it has room for.
+    const int lane = threadIdx.x & 63;
+    int share = 1;
+    while (share < 64 && share < of_group) share <<= 1;
+    const int part = lane & (share - 1), own = lane / share, at_once = 64 / share;
+    // the sums of a row whose parts end with blocks `start` .. `last` (the last one's at place p) to dS
+    auto join = [&](int row, int64_t start, int64_t last, int64_t p) {
+        for (int g = own; g - own < a.groups; g += at_once) {  // all lanes take part in the exchanges
             float sum = 0.f;
-            for (int j = g * of_group; j < min(a.per_part, (g + 1) * of_group); ++j) sum += a.parts[t * a.per_part + j];
-            a.dS[(int64_t)row * a.groups + g] = sum;
+            const int from = g * of_group, to = g < a.groups ? min(a.per_part, from + of_group) : from;
+            for (int64_t q = start; q <= last; q += 8) {
+                for (int j = from + part; j < to; j += share) {
+                    float v[8];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) v[u] = q + u <= last ? a.parts[(a.few ? p : min((q + u + 1) * a.each - 1, p)) * a.per_part + j] : 0.f;
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) sum += v[u];
+                }
+            }
+            for (int o = 1; o < share; o <<= 1) sum += __shfl_xor(sum, o);
+            if (part == 0 && g < a.groups) a.dS[(int64_t)row * a.groups + g] = sum;
+        }
+    };
+    const int64_t wave = (int64_t)(blockIdx.x - kd) * 4 + (threadIdx.x >> 6), waves = (int64_t)(gridDim.x - kd) * 4;
+    if (a.few) {  // a wavefront to a token, whose row is in one part if it is the row's first
+        for (int64_t t = wave; t < n; t += waves) {
+            const int row = a.order.row_at[t];
+            if (row < a.ids.rows) join(row, 0, 0, t);
         }
         return;
     }
-    // a wavefront to the rows that end in a block
-    const int lane = threadIdx.x & 63;
+    // .. to the rows that end in a block
     const int64_t blocks = (n + a.each - 1) / a.each;
-    for (int64_t b = (int64_t)(blockIdx.x - kd) * 4 + (threadIdx.x >> 6); b < blocks; b += (int64_t)(gridDim.x - kd) * 4) {
+    for (int64_t b = wave; b < blocks; b += waves) {
         const Places at(a.order, n, a.ids.rows, b, a.each);
         uint64_t ends = at.row_ends;
         if (!a.segmented) ends = at.began ? ends & (0 - ends) : 0;  // the others are in dS
         for (bool began = at.began; ends; ends &= ends - 1, began = false) {
             const int p = __builtin_ctzll(ends), row = __builtin_amdgcn_readlane(at.row, p);
-            const int64_t start = began ? b - blocks_before(a.order, b, a.each, row) : b;
-            for (int g = lane; g < a.groups; g += 64) {
-                float sum = 0.f;
-                for (int64_t q = start; q <= b; q += 8) {
-                    for (int j = g * of_group; j < min(a.per_part, (g + 1) * of_group); ++j) {
-                        float v[8];
-#pragma unroll
-                        for (int u = 0; u < 8; ++u) {
-                            const int64_t place = min((q + u + 1) * a.each - 1, at.first + p);
-                            v[u] = a.parts[place * a.per_part + j];
-                        }
-#pragma unroll
-                        for (int u = 0; u < 8; ++u) sum += q + u <= b ? v[u] : 0.f;
-                    }
-                }
-                a.dS[(int64_t)row * a.groups + g] = sum;
-            }
+            join(row, began ? b - blocks_before(a.order, b, a.each, row) : b, b, at.first + p);
         }
     }
 }
@@ -339,7 +347,7 @@ __global__ __launch_bounds__(256) void k_join_lookup(const LookupGradArgs a, int
 void launch_join_lookup(const LookupGradPlan& p, const LookupGradArgs& a, int kd, float* dC, int of_group, hipStream_t s) {
     if (!dC) kd = 0;
     const bool parts = a.dS && (a.segmented || (!p.few && a.ids.n > p.each));
-    const int64_t joining = p.few ? (a.ids.n * a.groups + 255) / 256 : ((a.ids.n + p.each - 1) / p.each + 3) / 4;
+    const int64_t joining = ((p.few ? a.ids.n : (a.ids.n + p.each - 1) / p.each) + 3) / 4;
     const unsigned grid = (unsigned)kd + (parts ? (unsigned)std::min<int64_t>(4096, joining) : 0u);
     if (grid > 0) hipLaunchKernelGGL(k_join_lookup, dim3(grid), dim3(256), 0, s, a, p.grid, kd, dC, of_group);
 }

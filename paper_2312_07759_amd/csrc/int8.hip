@@ -282,6 +282,62 @@ void launch_int8_few(int dtype, const Int8FewArgs& a, hipStream_t s) {
     else BY_TYPE(dtype, T, (launch_few<T, 1, 16, false>(a, s)));
 }
 
+// dX of float32: x = dY scale is the sum of three numbers of bfloat16, its upper, middle and lower eight bits (cut off, so that no part becomes infinite;
+// below 2^-110 the lowest may be lost), and integers of eight bits are numbers of bfloat16.  The float32 product is thus one of bfloat16 with three times the rows, exact but
+// for its float32 sums, three of which make a result.  1001 x 1000 x 512: 22 us; by float32 matrix instructions, a ninth as many a second, 26.7.
+__global__ __launch_bounds__(256) void k_int8_split(const Int8SplitArgs a) {
+    __shared__ __align__(16) uint32_t lds[TransposeTile<bf16>::WORDS];
+    if (blockIdx.x < a.splitting) {
+        const int64_t per_row = a.pad / 8, pieces = a.n * per_row;
+        for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < pieces; at += (int64_t)a.splitting * 256) {
+            const int64_t t = pieces >> 31 ? at / per_row : (unsigned)at / (unsigned)per_row, r = (at - t * per_row) * 8;
+            float x[8];
+            float by[8];
+            eight_floats(x, a.dY + t * a.ldy, r, a.rows);
+            eight_floats(by, a.scale, r, a.rows);
+            u32x4 part[3];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] *= by[e];
+                const bool finite = size_of(x[e]) < 0x7f800000;
+#pragma unroll
+                for (int i = 0; i < 3; ++i) {
+                    uint32_t bits = __builtin_bit_cast(uint32_t, x[e]);
+                    if (!finite && (bits & 0x7fffff)) bits |= 0x10000;  // a NaN stays one
+                    if (!finite && i > 0) bits = 0;                     // .. and is one part
+                    const uint32_t high = bits >> 16;
+                    part[i][e / 2] = e & 1 ? part[i][e / 2] | high << 16 : high;
+                    x[e] -= __builtin_bit_cast(float, bits & 0xffff0000);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 3; ++i) *reinterpret_cast<u32x4*>(static_cast<bf16*>(a.A) + (i * a.n + t) * a.pad + r) = part[i];
+        }
+        return;
+    }
+    const int64_t tiles_c = (a.cols + 63) / 64, tile_at = blockIdx.x - a.splitting, tr = tile_at / tiles_c, r0 = tr * 64, c0 = (tile_at - tr * tiles_c) * 64;
+    const int64_t r = r0 + (threadIdx.x >> 3) * 2, c = c0 + (threadIdx.x & 7) * 8;
+    bf16 v[2][8];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        const bool there = r + b < a.rows && c < a.cols;
+        const u32x2 q = *reinterpret_cast<const u32x2*>(a.W8 + (there ? (r + b) * a.ldw + c : 0));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[b][e] = there ? (bf16)(float)(int8_t)(q[e >> 2] >> (e & 3) * 8) : (bf16)0.f;
+    }
+    const TransposeTile<bf16> tile{lds};
+    tile.put(v[0], v[1]);
+    __syncthreads();
+    tile.emit(static_cast<bf16*>(a.B) + c0 * a.pad + r0, a.cols - c0, a.pad, a.pad - r0);
+}
+
+void launch_int8_split(const Int8SplitArgs& args, bool dY, hipStream_t s) {
+    Int8SplitArgs a = args;
+    const int64_t groups = (a.n * (a.pad / 8) + 255) / 256, tiles = ((a.cols + 63) / 64) * ((a.pad + 63) / 64);
+    a.splitting = dY ? (unsigned)(groups < 4096 ? groups : 4096) : 0u;
+    hipLaunchKernelGGL(k_int8_split, dim3(a.splitting + (unsigned)tiles), dim3(256), 0, s, a);
+}
+
 template <typename T>
 __global__ __launch_bounds__(256) void k_join_int8(const int32_t* __restrict__ parts, int nz, int64_t M, int64_t N, const float* __restrict__ by_m,
                                                    const float* __restrict__ by_n, T* __restrict__ out, int64_t ldo) {

@@ -11,8 +11,6 @@ namespace idkm {
 
 constexpr int KEEP_BLOCK = 32;
 
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-
 template <typename T>
 struct Keep8 {
     // the last exponent field of T's finite numbers, as float32's

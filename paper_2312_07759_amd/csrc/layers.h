@@ -89,6 +89,19 @@ struct Int8FewArgs {
 };
 constexpr int64_t INT8_FUSED = 4 * 8192;  // elements of X that a workgroup brings to integers itself, at most
 void launch_int8_few(int dtype, const Int8FewArgs& a, hipStream_t s);
+// Operands of the gradient of a float32 product: dY times the scales in three parts of 16 bits, and columns of W8 in 16 bits.
+struct Int8SplitArgs {
+    const float* dY;  // [n, ldy]
+    int64_t n, ldy, rows;
+    const float* scale;  // [rows]
+    const int8_t* W8;    // [rows, ldw], from the first column that is wanted on
+    int64_t ldw, cols;
+    void* A;      // bf16 [3, n, pad], zero behind column `rows`
+    void* B;      // bf16 [cols, pad]
+    int64_t pad;  // a multiple of 64
+    unsigned splitting;  // workgroups, set by the launch
+};
+void launch_int8_split(const Int8SplitArgs& a, bool dY, hipStream_t s);  // dY: A too, or B alone
 // out[M, N] in the type of dtype = by_m by_n times the sum of the parts [nz][M, N].
 void launch_join_int8(int dtype, const int32_t* parts, int nz, int64_t M, int64_t N, const float* by_m, const float* by_n, void* out, int64_t ldo,
                       hipStream_t s);

@@ -610,6 +610,23 @@ Int8Layout int8_layout(const idkm_int8_desc& w, int64_t n) {
     return l;
 }
 
+// .. of the gradient of a float32 product (see k_int8_split).
+struct SplitLayout {
+    int64_t pad, panel, matrix, parts, bytes;
+    TilePlan plan;
+};
+
+SplitLayout split_layout(const idkm_int8_desc& w, int64_t n) {
+    SplitLayout l{};
+    l.pad = up_to(w.rows, TP_STEP / 2);
+    l.panel = panel_of(w.cols, l.pad);
+    l.plan = tile_plan(3 * n, l.panel, l.pad * 2 / TP_STEP, IDKM_BF16, 0);
+    l.matrix = buffer(n * 3 * l.pad, 2);
+    l.parts = l.matrix + buffer(l.panel * l.pad, 2);
+    l.bytes = l.parts + buffer(3 * n * l.panel * l.plan.parts, 4);
+    return l;
+}
+
 const char* wrong_scale_shape(int64_t rows, int64_t cols, int64_t group) {
     if (rows < 0 || cols < 1) return "need rows >= 0 and cols >= 1";
     if (group < 1) return "group must be >= 1";
@@ -819,7 +836,7 @@ idkm_status idkm_int8_linear(idkm_ctx* ctx, const idkm_int8_desc* w, const void*
 
 int64_t idkm_int8_linear_backward_workspace(const idkm_int8_desc* w, int64_t n) {
     if (wrong_int8(nullptr, w, n)) return -1;
-    return n == 0 ? 0 : product_layout(w->dtype, n, w->cols, w->rows).bytes;
+    return n == 0 ? 0 : w->dtype == IDKM_F32 ? split_layout(*w, n).bytes : product_layout(w->dtype, n, w->cols, w->rows).bytes;
 }
 
 idkm_status idkm_int8_linear_backward(idkm_ctx* ctx, const idkm_int8_desc* w, const void* dY, int64_t lddy, int64_t n, void* dX, int64_t lddx,
@@ -831,10 +848,34 @@ idkm_status idkm_int8_linear_backward(idkm_ctx* ctx, const idkm_int8_desc* w, co
         if (!dY || !dX) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dY and dX must be non-NULL");
         if (lddy < w->rows || lddx < w->cols) return refuse(ctx, IDKM_ERR_INVALID_ARG, "lddy must be >= rows and lddx >= cols");
         if (!aligned_to(dY, es) || !aligned_to(dX, es)) return refuse(ctx, IDKM_ERR_INVALID_ARG, "dY and dX must be aligned to their type");
-        const ProductLayout l = product_layout(w->dtype, n, w->cols, w->rows);
-        if (const char* e = wrong_workspace(workspace, workspace_bytes, l.bytes)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
         hipStream_t s = (hipStream_t)hip_stream;
         unsigned char* ws = static_cast<unsigned char*>(workspace);
+        if (w->dtype == IDKM_F32) {
+            const SplitLayout l = split_layout(*w, n);
+            if (const char* e = wrong_workspace(workspace, workspace_bytes, l.bytes)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
+            return launched(ctx, [&] {
+                TileArgs t{};
+                t.A = ws;
+                t.lda = l.pad;
+                t.M = 3 * n;  // 12,000,000 at most
+                t.B = ws + l.matrix;
+                t.ldb = l.pad;
+                t.steps = (int)(l.pad * 2 / TP_STEP);
+                t.wide = 1;
+                float* parts = reinterpret_cast<float*>(ws + l.parts);
+                t.out = parts;
+                for (int64_t c = 0; c < w->cols; c += l.panel) {
+                    t.N = t.ldo = w->cols - c < l.panel ? w->cols - c : l.panel;
+                    launch_int8_split(Int8SplitArgs{static_cast<const float*>(dY), n, lddy, w->rows, w->scale, w->W8 + c, w->ldw, t.N, ws, ws + l.matrix, l.pad, 0},
+                                      c == 0, s);
+                    run_tiles(IDKM_BF16, l.plan, t, s);
+                    // the parts of the sum, three of each
+                    launch_join_parts(IDKM_F32, parts, 3 * l.plan.parts, n, t.N, static_cast<float*>(dX) + c, lddx, s);
+                }
+            });
+        }
+        const ProductLayout l = product_layout(w->dtype, n, w->cols, w->rows);
+        if (const char* e = wrong_workspace(workspace, workspace_bytes, l.bytes)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
         return launched(ctx, [&] {
             TileArgs t{};
             OperandArgs copies{};

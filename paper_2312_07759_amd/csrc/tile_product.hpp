@@ -40,11 +40,21 @@ struct TileArgs {
 // Four consecutive results of a row, the last ones of it fewer.
 template <typename V, typename O>
 __device__ __forceinline__ void store_four(O* o, const V* v, bool quad, int64_t have) {
-    if (quad && have >= 4) {
+    if (have >= 4) {
         struct alignas(4 * sizeof(O)) Quad { O v[4]; } w;
 #pragma unroll
         for (int r = 0; r < 4; ++r) w.v[r] = v[r];
-        *reinterpret_cast<Quad*>(o) = w;
+        if (quad) {
+            *reinterpret_cast<Quad*>(o) = w;
+        } else if constexpr (sizeof(O) == 2) {  // rows that begin anywhere: still one store, which global memory allows
+            u32x2_any raw;
+            __builtin_memcpy(&raw, &w, sizeof(raw));
+            *reinterpret_cast<u32x2_any*>(o) = raw;
+        } else {
+            u32x4 raw;
+            __builtin_memcpy(&raw, &w, sizeof(raw));
+            *reinterpret_cast<u32x4_word*>(o) = raw;
+        }
     } else {
         for (int r = 0; r < 4 && r < have; ++r) o[r] = v[r];
     }
@@ -318,22 +328,13 @@ __global__ __launch_bounds__(64 * WM * WN, SC > 0 ? 2 : 1) void k_tile_product(c
                     for (int r = 0; r < 4; ++r) v[r] = (float)acc[i][j][r] * by * a.by_n[min(n + r, a.N - 1)];
                     store_four_as(a.out, m * a.ldo + n, a.dtype, v, quad, a.N - n);
                 }
-            } else if (a.wide) {
-                float* o = static_cast<float*>(a.out) + ((int64_t)z * a.M + m) * a.ldo + n;
-                if (quad && n + 4 <= a.N) {
-                    *reinterpret_cast<floatx4*>(o) = acc[i][j];
-                } else {
-                    for (int r = 0; r < 4 && n + r < a.N; ++r) o[r] = acc[i][j][r];
-                }
             } else {
-                T* o = static_cast<T*>(a.out) + m * a.ldo + n;
-                if (quad && n + 4 <= a.N) {
-                    struct alignas(4 * sizeof(T)) Quad { T v[4]; } w;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) w.v[r] = Elem<T>::down(acc[i][j][r]);
-                    *reinterpret_cast<Quad*>(o) = w;
+                const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                if (a.wide) {
+                    store_four(static_cast<float*>(a.out) + ((int64_t)z * a.M + m) * a.ldo + n, v, quad, a.N - n);
                 } else {
-                    for (int r = 0; r < 4 && n + r < a.N; ++r) o[r] = Elem<T>::down(acc[i][j][r]);
+                    const T w[4] = {Elem<T>::down(v[0]), Elem<T>::down(v[1]), Elem<T>::down(v[2]), Elem<T>::down(v[3])};
+                    store_four(static_cast<T*>(a.out) + m * a.ldo + n, w, quad, a.N - n);
                 }
             }
         }

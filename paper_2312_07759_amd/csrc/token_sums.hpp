@@ -94,14 +94,14 @@ struct Mates {
     }
 };
 
-// The sum over all mates, four of them asked for at a time.
+// The sum over all mates, eight of them asked for at a time.
 template <typename T, bool NARROW>
 __device__ __forceinline__ void sum_of_mates(float* sum, Mates mates, const T* dY, int64_t ldy, unsigned c, int cols) {
     while (mates.any()) {
-        RowsAhead<T, 4, NARROW> rows;
+        RowsAhead<T, 8, NARROW> rows;
         int have = 0, token = 0;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < 8; ++u) {
             if (mates.any()) {
                 token = mates.next();
                 have = u + 1;
@@ -109,7 +109,7 @@ __device__ __forceinline__ void sum_of_mates(float* sum, Mates mates, const T* d
             rows.ask(u, dY + (int64_t)token * ldy, c, cols);  // the last one again where there are fewer
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < 8; ++u)
             if (u < have) rows.add(u, sum);
     }
 }
