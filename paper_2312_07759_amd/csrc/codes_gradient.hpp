@@ -29,12 +29,34 @@ struct BinArgs {
     int lanes;         // of a wavefront that take part: a multiple of d
     int run;           // groups of a row that a wavefront takes at a time
     int c_in_lds;
+    unsigned group_magic;  // ceil(2^31 / (group / 32)) where a row has several groups, which are multiples of 32; 0 for one
+    __device__ __forceinline__ int group_of(int c) const {  // a division would be half of a column's instructions
+        const unsigned x = (unsigned)c >> 5;
+        unsigned g = __umulhi(2u * x, group_magic);
+        if (__umul24(g, (unsigned)group >> 5) > x) --g;  // the rounded-up inverse is off by one at most, and then too large; both below 2^17
+        return (int)g;
+    }
     // LISTED: P's row i belongs to the layer's row listed[i], for *listed_count rows; `segments` has a row for each of them
     const int32_t* listed;
     const int32_t* listed_count;
     __device__ __forceinline__ int64_t row_of(int64_t rr, bool of_list) const { return of_list ? (int64_t)listed[rr] : first + rr; }
     __device__ __forceinline__ int64_t rows_here(bool of_list) const { return of_list ? (int64_t)*listed_count : count; }
 };
+
+// The sum over a lane's aligned neighbours, `lanes` of them, a power of two.  Up to 16 without LDS: once the lanes of a half agree, a mirrored one is as good
+// as the other half's.
+__device__ __forceinline__ float sum_of_lanes(float v, int lanes) {
+    auto moved = [&](auto control) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, true));
+    };
+    if (lanes >= 2) v += moved(std::integral_constant<int, 0xb1>());   // lanes 1 0 3 2 of four
+    if (lanes >= 4) v += moved(std::integral_constant<int, 0x4e>());   // 2 3 0 1
+    if (lanes >= 8) v += moved(std::integral_constant<int, 0x141>());  // eight, mirrored
+    if (lanes >= 16) v += moved(std::integral_constant<int, 0x140>()); // sixteen, mirrored
+    if (lanes >= 32) v += __shfl_xor(v, 16);
+    if (lanes >= 64) v += __shfl_xor(v, 32);
+    return v;
+}
 
 template <typename T, bool LISTED>
 __global__ __launch_bounds__(256) void k_codes_bins(const BinArgs a) {
@@ -169,7 +191,7 @@ __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {
         t.sh = (int)(bit - (from << 5));
 #pragma unroll
         for (int i = 0; i < 3; ++i) t.w[i] = a.words[from + i];
-        t.s = a.S ? a.S[r * a.groups + at / a.group] : 1.f;
+        t.s = a.S ? a.S[r * a.groups + a.group_of(at)] : 1.f;
     };
     Item now, next;
     if (rr < count) ask(now, rr, strip);
@@ -190,13 +212,18 @@ __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {
         const int sh = now.sh;
         const uint32_t b0 = sh < 32 ? now.w[0] : sh < 64 ? now.w[1] : now.w[2], b1 = sh < 32 ? now.w[1] : sh < 64 ? now.w[2] : 0u,
                        b2 = sh < 32 ? now.w[2] : 0u;
-        const uint64_t codes = (uint64_t)__builtin_amdgcn_alignbit(b2, b1, sh & 31) << 32 | __builtin_amdgcn_alignbit(b1, b0, sh & 31);
+        uint32_t low = __builtin_amdgcn_alignbit(b1, b0, sh & 31), high = __builtin_amdgcn_alignbit(b2, b1, sh & 31);
         float sum = 0.f;
-        auto add = [&](auto sure_) {  // sure: all eight columns are there and every code is one
-            constexpr bool sure = decltype(sure_)::value;
+        // sure: all eight columns are there and every code is one; word: the codes lie in 32 bits
+        auto add = [&](auto sure_, auto word_) {
+            constexpr bool sure = decltype(sure_)::value, word = decltype(word_)::value;
 #pragma unroll
             for (int e = 0; e < NC; ++e) {
-                const uint32_t code = (uint32_t)(codes >> (e * a.bits)) & mask;
+                const uint32_t code = word ? __builtin_amdgcn_ubfe(low, e * a.bits, a.bits) : low & mask;
+                if (!word) {
+                    low = __builtin_amdgcn_alignbit(high, low, a.bits);
+                    high >>= a.bits;
+                }
                 const bool none = !sure && code >= (uint32_t)a.k;
                 const int j = none ? 0 : (int)code * D;
 #pragma unroll
@@ -210,15 +237,16 @@ __global__ __launch_bounds__(256) void k_codes_bins_runs(const BinArgs a) {
                 }
             }
         };
-        if (strip * 512 + 512 <= a.cols && a.k > (int)mask) add(std::true_type());
-        else add(std::false_type());
+        const bool sure = strip * 512 + 512 <= a.cols && a.k > (int)mask;
+        if (sure && NC * a.bits <= 32) add(std::true_type(), std::true_type());
+        else if (sure) add(std::true_type(), std::false_type());
+        else add(std::false_type(), std::false_type());
         if (a.segments) {
-            sum += __shfl_xor(sum, 1);
-            sum += __shfl_xor(sum, 2);
+            sum = sum_of_lanes(sum, 4);
             if (there && (lane & 3) == 0) a.segments[(LISTED ? rr : r) * ((a.cols + 31) / 32) + (c >> 5)] = sum;
         } else if (a.dS) {
-            for (int o = 1; o < group_lanes; o <<= 1) sum += __shfl_xor(sum, o);
-            if (there && (lane & (group_lanes - 1)) == 0) a.dS[r * a.groups + c / a.group] = sum;
+            sum = sum_of_lanes(sum, group_lanes);
+            if (there && (lane & (group_lanes - 1)) == 0) a.dS[r * a.groups + a.group_of(c)] = sum;
         }
         now = next;
         rr = rn;
@@ -285,7 +313,7 @@ __global__ __launch_bounds__(256) void k_codes_bins_wide(const BinArgs a) {
         for (int u = 0; u < STEPS; ++u) {
             const int c = min(at * 512 + u * 64 + lane, (int)a.cols - 1);  // columns behind the last: read as it, not counted
             t.p[u] = P[c];
-            t.s[u] = S ? S[c / a.group] : 1.f;
+            t.s[u] = S ? S[a.group_of(c)] : 1.f;
             const int bit = (int)(bit0 & 31) + min(u * (64 / D) + lane / D, per_row - 1 - at * (512 / D)) * a.bits;
             const int from = min(bit >> 5, limit);
             t.sh[u] = bit - from * 32;

@@ -109,6 +109,7 @@ BinArgs bins_of(const idkm_codes_desc& w, const BinPlan& l) {
     b.groups = l.groups;
     b.run = l.run;
     b.lanes = l.lanes;
+    if (l.runs && l.groups > 1) b.group_magic = (unsigned)((((int64_t)1 << 31) + l.group / 32 - 1) / (l.group / 32));
     return b;
 }
 

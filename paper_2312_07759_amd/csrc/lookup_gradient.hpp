@@ -35,21 +35,6 @@ struct LookupGradArgs {
     unsigned summing;  // few: workgroups that sum; the ones behind them clear the other rows of dS
 };
 
-// The sum over a lane's aligned neighbours, `lanes` of them, a power of two.  Up to 16 without LDS: once the lanes of a half agree, a mirrored one is as good
-// as the other half's.
-__device__ __forceinline__ float sum_of_lanes(float v, int lanes) {
-    auto moved = [&](auto control) {
-        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, true));
-    };
-    if (lanes >= 2) v += moved(std::integral_constant<int, 0xb1>());   // lanes 1 0 3 2 of four
-    if (lanes >= 4) v += moved(std::integral_constant<int, 0x4e>());   // 2 3 0 1
-    if (lanes >= 8) v += moved(std::integral_constant<int, 0x141>());  // eight, mirrored
-    if (lanes >= 16) v += moved(std::integral_constant<int, 0x140>()); // sixteen, mirrored
-    if (lanes >= 32) v += __shfl_xor(v, 16);
-    if (lanes >= 64) v += __shfl_xor(v, 32);
-    return v;
-}
-
 constexpr int LOOKUP_PLACES = 32;
 constexpr int LOOKUP_KEPT = LOOKUP_PLACES * 17;  // words of LDS for a wavefront: sums of groups, and whose they are
 
