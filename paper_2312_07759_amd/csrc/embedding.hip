@@ -360,7 +360,10 @@ LookupGradPlan lookup_grad_plan(int64_t n, int64_t cols, int esize, int kd) {
     p.few = n <= FEW_TOKENS;
     p.each = (int)std::max<int64_t>(2, std::min<int64_t>(LOOKUP_PLACES, n * strips / 8192));
     const int64_t tasks = (p.few ? n : (n + p.each - 1) / p.each) * strips;
-    const int wave_bytes = kd * 256 + LOOKUP_KEPT * 4;
+    // 8192 tokens of 4096 columns, bfloat16: 128 components 62 us with bins for each lane, 40 with bins for two lanes, 100 components 77 and 71; 64 and 32
+    // components, whose bins leave room for all wavefronts either way: 40 and 31 with both
+    p.share = kd > 64 ? 2 : 1;
+    const int wave_bytes = kd * 256 / p.share + LOOKUP_KEPT * 4;
     p.waves = std::min(4, 144 * 1024 / wave_bytes);
     const int64_t resident = std::max(1, std::min((esize == 4 ? 16 : 24) / p.waves, 156 * 1024 / (wave_bytes * p.waves + kd * 4)));
     p.grid = (int)std::min<int64_t>((tasks + p.waves - 1) / p.waves, 256 * resident);

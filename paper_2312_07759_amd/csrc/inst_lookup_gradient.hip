@@ -6,9 +6,9 @@
 
 namespace idkm {
 
-template <typename T, bool FEW>
+template <typename T, bool FEW, int SHARE>
 static void (*gradient_for(int d))(const LookupGradArgs) {
-    return d == 1 ? &k_lookup_gradient<T, 1, FEW> : d == 2 ? &k_lookup_gradient<T, 2, FEW> : d == 4 ? &k_lookup_gradient<T, 4, FEW> : &k_lookup_gradient<T, 8, FEW>;
+    return d == 1 ? &k_lookup_gradient<T, 1, FEW, SHARE> : d == 2 ? &k_lookup_gradient<T, 2, FEW, SHARE> : d == 4 ? &k_lookup_gradient<T, 4, FEW, SHARE> : &k_lookup_gradient<T, 8, FEW, SHARE>;
 }
 
 void launch_lookup_gradient(int dtype, int d, const LookupGradPlan& p, const LookupGradArgs& args, hipStream_t s) {
@@ -21,9 +21,11 @@ void launch_lookup_gradient(int dtype, int d, const LookupGradPlan& p, const Loo
     // a stored group shorter than a row is a multiple of 32
     const int sums = a.segmented ? 16 : a.groups > 1 ? 512 / a.group : 1;
     for (a.sums_log = 0; 1 << a.sums_log < sums;) ++a.sums_log;
-    const size_t lds = 4 * ((size_t)p.waves * (kd * 64 + LOOKUP_KEPT) + kd);
+    const size_t lds = 4 * ((size_t)p.waves * (kd * (64 / p.share) + LOOKUP_KEPT) + kd);
     BY_TYPE(dtype, T, {
-        void (*const fn)(const LookupGradArgs) = p.few ? gradient_for<T, true>(d) : gradient_for<T, false>(d);
+        void (*fn)(const LookupGradArgs) = nullptr;
+        if (p.share > 1) fn = p.few ? gradient_for<T, true, 2>(d) : gradient_for<T, false, 2>(d);
+        else fn = p.few ? gradient_for<T, true, 1>(d) : gradient_for<T, false, 1>(d);
         allow_lds(reinterpret_cast<const void*>(fn), lds);
         hipLaunchKernelGGL(fn, dim3(a.summing + clearing), dim3((unsigned)p.waves * 64), lds, s, a);
     });

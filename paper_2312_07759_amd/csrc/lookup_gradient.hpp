@@ -1,6 +1,6 @@
 // Gradients of a lookup in a stored table, in the codebook and the group scales, in one pass over dY: a row's sum P[c] = alpha sum dY[t, c] stays in the
 // registers of the wavefront that forms it, which reads the row's codes and scales and adds
-//   S P  to its bins of the codebook's components (in LDS, 64 for each, one to a lane: no two lanes add to the same word, and the order of every sum is fixed)
+//   S P  to its bins of the codebook's components (in LDS, one to a lane or to two lanes that take turns: the order of every sum is fixed)
 //   P C[code]  over the lanes of a group: dS of the row, or of its part where the row's tokens lie in several blocks.
 // For codes of up to 8 bits, D in {1, 2, 4, 8} and codebooks of up to 256 components; the others write the sums P out and go through the kernels of the
 // gradient of a product, as do rows of fewer than eight columns.
@@ -42,21 +42,23 @@ constexpr int LOOKUP_KEPT = LOOKUP_PLACES * 17;  // words of LDS for a wavefront
 // 5,100 sums of rows and parts of rows, 42,000 strips of 512 columns at about 100 vector and as many scalar instructions, and eight LDS updates one after
 // another in each.  Beginning and end take 6 us (bins cleared and added up), as many wavefronts as the registers allow the rest.
 // A strip's sums of groups are kept in LDS and stored at the block's end, so that no load waits behind a store.
-template <typename T, int D, bool FEW>
+// SHARE lanes have the same bins and add to them one after another: the bins of larger codebooks leave room for more wavefronts then, see lookup_grad_plan.
+template <typename T, int D, bool FEW, int SHARE>
 __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a) {
-    constexpr int NC = 8 / D;
-    extern __shared__ __align__(16) float bin_lds[];  // [wave][k D][64], then the codebook
+    constexpr int NC = 8 / D, WIDTH = 64 / SHARE;
+    extern __shared__ __align__(16) float bin_lds[];  // [wave][k D][WIDTH], then the codebook
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
     if (FEW && blockIdx.x >= a.summing) {
         if (a.dS) clear_other_rows(a.ids, a.dS, a.groups, (int64_t)(blockIdx.x - a.summing) * nw + wave, (int64_t)(gridDim.x - a.summing) * nw);
         return;
     }
     const int kd = a.k * D;
-    float* mine = bin_lds + wave * kd * 64 + lane;
-    float* book = bin_lds + nw * kd * 64;
+    float* mine = bin_lds + wave * kd * WIDTH + lane % WIDTH;
+    float* book = bin_lds + nw * kd * WIDTH;
+    const int turn = lane / WIDTH;
     float* kept = book + kd + wave * LOOKUP_KEPT;
     int* kept_for = reinterpret_cast<int*>(kept + LOOKUP_PLACES * 16);  // a row of dS, or ~ a place of `parts`
-    for (int j = 0; j < kd; ++j) mine[j * 64] = 0.f;
+    for (int j = 0; j < kd; ++j) mine[j * WIDTH] = 0.f;
     for (int i = threadIdx.x; i < kd; i += blockDim.x) book[i] = Elem<T>::up(static_cast<const T*>(a.C)[i]);
     __syncthreads();
     const int strips = (a.cols + 511) / 512, n = (int)a.ids.n;
@@ -105,6 +107,7 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
             // sure: all eight columns are there and every code is one; word: the codes lie in 32 bits
             auto add = [&](auto sure_, auto word_) {
                 constexpr bool sure = decltype(sure_)::value, word = decltype(word_)::value;
+                int place[8];
 #pragma unroll
                 for (int e = 0; e < NC; ++e) {
                     const uint32_t code = word ? __builtin_amdgcn_ubfe(low, e * a.bits, a.bits) : low & mask;
@@ -119,8 +122,25 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
                         const bool counts = sure || e * D + i >= skip;
                         const float w = none ? __builtin_nanf("") : book[j + i];
                         sum = counts ? fmaf(p[e * D + i], w, sum) : sum;
-                        float& bin = mine[(j + i) * 64];
-                        bin = counts && !none ? fmaf(by, p[e * D + i], bin) : bin;
+                        if constexpr (SHARE == 1) {
+                            float& bin = mine[(j + i) * 64];
+                            bin = counts && !none ? fmaf(by, p[e * D + i], bin) : bin;
+                        } else {
+                            place[e * D + i] = counts && !none ? (j + i) * WIDTH : -1;
+                        }
+                    }
+                }
+                if constexpr (SHARE > 1) {
+#pragma unroll
+                    for (int t = 0; t < SHARE; ++t) {
+                        if (turn == t) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (sure || place[e] >= 0) mine[place[e]] = fmaf(by, p[e], mine[place[e]]);
+                        }
+                        // one turn after another
+                        __builtin_amdgcn_wave_barrier();
+                        asm volatile("" ::: "memory");
                     }
                 }
             };
@@ -180,18 +200,18 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
     }
     __syncthreads();
     // A component's bins to as many lanes as there are, see k_codes_bins_runs
-    int split = 64;
+    int split = WIDTH;
     while (split > 1 && split * kd > (int)blockDim.x) split >>= 1;
-    const int part = threadIdx.x & (split - 1), count = 64 / split;
+    const int part = threadIdx.x & (split - 1), count = WIDTH / split;
     for (int e0 = 0; e0 < kd; e0 += blockDim.x / split) {
         const int e = e0 + threadIdx.x / split;
         double sum = 0.0;
         for (int w = 0; w < nw && e < kd; ++w) {
-            const float* of = bin_lds + (w * kd + e) * 64;
+            const float* of = bin_lds + (w * kd + e) * WIDTH;
             for (int i = 0; i < count; i += 8) {
                 float v[8];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) v[u] = of[((i + u) * split + part + e * split) & 63];
+                for (int u = 0; u < 8; ++u) v[u] = of[((i + u) * split + part + e * split) & (WIDTH - 1)];
 #pragma unroll
                 for (int u = 0; u < 8; ++u) sum += i + u < count ? (double)v[u] : 0.0;
             }
