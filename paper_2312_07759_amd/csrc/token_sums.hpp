@@ -8,7 +8,10 @@
 
 namespace idkm {
 
-constexpr int FEW_TOKENS = 256;
+// 301 tokens of a text, as these measure and sorted: float32, 734 columns, k = 100, d = 2 15.9 us and 19.4; bfloat16, 4096 columns, k = 16 14.7 and 18; a
+// table of 32000 x 1024 22.7 and 29.  512 tokens: 17.5 and 20.5, 18.1 and 18.2, 24.5 and 30; 1024: 29 and 21, 33 and 21, 27 and 31.  One row's tokens follow
+// one another here, 0.07 us each: 512 of the same row take 51 us, and 20 to 34 sorted.
+constexpr int FEW_TOKENS = 512;
 
 // A lane's eight columns of rows of dY, from column c on.  The last lane of a row whose length is no multiple of eight takes the last eight columns, of which
 // the first `skip` are its neighbour's: all rows are read in the same way, 16 bytes at a time.  Lanes behind the row's end skip all eight.  NARROW: rows of
@@ -75,16 +78,38 @@ struct Mates {
         for (int j = 0; j < FEW_TOKENS / 64; ++j) all |= word[j];
         return all != 0;
     }
-    // the lowest token, taken out; only where any()
-    __device__ __forceinline__ int next() {
+    __device__ __forceinline__ int count() const {
+        int n = 0;
 #pragma unroll
-        for (int j = 0; j < FEW_TOKENS / 64; ++j)
-            if (word[j]) {
-                const int at = __builtin_ctzll(word[j]);
-                word[j] &= word[j] - 1;
-                return j * 64 + at;
-            }
-        return 0;
+        for (int j = 0; j < FEW_TOKENS / 64; ++j) n += __popcll(word[j]);
+        return n;
+    }
+    // the i-th token, another one for each lane; i < count()
+    __device__ __forceinline__ int at(int i) const {
+        uint64_t of = word[0];
+        int base = 0;
+#pragma unroll
+        for (int j = 0; j + 1 < FEW_TOKENS / 64; ++j) {
+            const int before = __popcll(word[j]);
+            const bool on = base == j * 64 && i >= before;
+            i -= on ? before : 0;
+            of = on ? word[j + 1] : of;
+            base += on ? 64 : 0;
+        }
+        const int low = __popc((uint32_t)of);
+        const bool high = i >= low;
+        uint32_t bits = high ? (uint32_t)(of >> 32) : (uint32_t)of;
+        i -= high ? low : 0;
+        base += high ? 32 : 0;
+#pragma unroll
+        for (int half = 16; half > 0; half >>= 1) {
+            const int before = __popc(bits & ((1u << half) - 1u));
+            const bool on = i >= before;
+            i -= on ? before : 0;
+            bits = on ? bits >> half : bits;
+            base += on ? half : 0;
+        }
+        return base;
     }
     __device__ __forceinline__ int first() const {
 #pragma unroll
@@ -94,23 +119,43 @@ struct Mates {
     }
 };
 
-// The sum over all mates, eight of them asked for at a time.
+// The sum over all mates, eight of them asked for at a time, where there are more the next eight before these are added.  Each lane finds one of 64 mates'
+// tokens first: found one after another by scalar instructions they took longer than their rows.
 template <typename T, bool NARROW>
-__device__ __forceinline__ void sum_of_mates(float* sum, Mates mates, const T* dY, int64_t ldy, unsigned c, int cols) {
-    while (mates.any()) {
-        RowsAhead<T, 8, NARROW> rows;
-        int have = 0, token = 0;
+__device__ __forceinline__ void sum_of_mates(float* sum, const Mates& mates, const T* dY, int64_t ldy, unsigned c, int cols) {
+    const int all = mates.count(), lane = threadIdx.x & 63;
+    using Rows = RowsAhead<T, 8, NARROW>;
+    for (int first = 0; first < all; first += 64) {
+        const int there = min(64, all - first), tokens = mates.at(first + min(lane, there - 1));
+        auto ask = [&](Rows& rows, int i) {
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            if (mates.any()) {
-                token = mates.next();
-                have = u + 1;
+            for (int u = 0; u < 8; ++u) {  // the last one again where there are fewer
+                const int token = __builtin_amdgcn_readlane(tokens, min(i + u, there - 1));
+                rows.ask(u, dY + (int64_t)token * ldy, c, cols);
             }
-            rows.ask(u, dY + (int64_t)token * ldy, c, cols);  // the last one again where there are fewer
-        }
+        };
+        auto add = [&](const Rows& rows, int i) {
+            if (i + 8 <= there) {
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-            if (u < have) rows.add(u, sum);
+                for (int u = 0; u < 8; ++u) rows.add(u, sum);
+            } else {
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (i + u < there) rows.add(u, sum);
+            }
+        };
+        Rows now, next;
+        ask(now, 0);
+        if (there > 8) {
+            for (int i = 0; i < there; i += 16) {
+                ask(next, i + 8);
+                add(now, i);
+                ask(now, i + 16);
+                add(next, i + 8);
+            }
+        } else {
+            add(now, 0);
+        }
     }
 }
 

@@ -189,7 +189,7 @@ def test_arguments_that_the_library_refuses(ctx):
     refused("idkm_codes_embedding_backward", w, p, 8, 4, f(1.0), p, 64, p, p, p, 8, None)          # a workspace that is too small
     refused("idkm_codes_embedding_backward", w, p, 8, 4, f(1.0), p, 64, p, p, p + 8, big, None)    # .. not aligned
     refused("idkm_codes_embedding_backward", w, p, 8, 4, f(1.0), p, 64, p + 2, p, p, big, None)
-    refused("idkm_embedding_backward", 8, 64, p, 8, 300, f(1.0), p, 64, 2, p, p, 16, None)
+    refused("idkm_embedding_backward", 8, 64, p, 8, 600, f(1.0), p, 64, 2, p, p, 16, None)
     refused("idkm_embedding_backward", 8, 64, p, 8, 4, f(1.0), p, 64, 2, None, None, 0, None)
     refused("idkm_embedding", p, 0, 64, p, 8, 4, f(1.0), p, 64, 2, None)
     refused("idkm_embedding", p, 8, 64, p, 8, 4, f(1.0), p, 64, 5, None)
