@@ -58,7 +58,7 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
     const int turn = lane / WIDTH;
     float* kept = book + kd + wave * LOOKUP_KEPT;
     int* kept_for = reinterpret_cast<int*>(kept + LOOKUP_PLACES * 16);  // a row of dS, or ~ a place of `parts`
-    for (int j = 0; j < kd; ++j) mine[j * WIDTH] = 0.f;
+    for (int i = lane; i < kd * (WIDTH / 4); i += 64) reinterpret_cast<floatx4*>(bin_lds + wave * kd * WIDTH)[i] = floatx4{0.f, 0.f, 0.f, 0.f};
     for (int i = threadIdx.x; i < kd; i += blockDim.x) book[i] = Elem<T>::up(static_cast<const T*>(a.C)[i]);
     __syncthreads();
     const int strips = (a.cols + 511) / 512, n = (int)a.ids.n;
@@ -199,22 +199,22 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
         }
     }
     __syncthreads();
-    // A component's bins to as many lanes as there are, see k_codes_bins_runs
-    int split = WIDTH;
+    // A component's bins to as many lanes as there are, four at a time; neighbours begin with other ones, in other banks
+    constexpr int QUADS = WIDTH / 4;
+    int split = QUADS;
     while (split > 1 && split * kd > (int)blockDim.x) split >>= 1;
-    const int part = threadIdx.x & (split - 1), count = WIDTH / split;
+    const int part = threadIdx.x & (split - 1), count = QUADS / split;
     for (int e0 = 0; e0 < kd; e0 += blockDim.x / split) {
         const int e = e0 + threadIdx.x / split;
         double sum = 0.0;
-        for (int w = 0; w < nw && e < kd; ++w) {
-            const float* of = bin_lds + (w * kd + e) * WIDTH;
-            for (int i = 0; i < count; i += 8) {
-                float v[8];
+        for (int i = 0; i < count; ++i) {
+            floatx4 v[4];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) v[u] = of[((i + u) * split + part + e * split) & (WIDTH - 1)];
+            for (int w = 0; w < 4; ++w)
+                if (w < nw && e < kd) v[w] = reinterpret_cast<const floatx4*>(bin_lds + (w * kd + e) * WIDTH)[(i * split + part + e) & (QUADS - 1)];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) sum += i + u < count ? (double)v[u] : 0.0;
-            }
+            for (int w = 0; w < 4; ++w)
+                if (w < nw && e < kd) sum += ((double)v[w][0] + (double)v[w][1]) + ((double)v[w][2] + (double)v[w][3]);
         }
         for (int o = split / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
         if (e < kd && part == 0) a.bins[e * a.pitch + blockIdx.x] = (float)sum;
