@@ -58,7 +58,7 @@ void launch_sums_of_few(int dtype, const TokenIds& ids, float alpha, const void*
 // A stored table's gradient in one pass; grid: workgroups that sum, each with a column of `bins`.
 struct LookupGradPlan {
     bool few;
-    int each, grid, waves, share;  // share: lanes with the same bins
+    int each, grid, waves, width_log;  // width_log: see LookupGradArgs
 };
 LookupGradPlan lookup_grad_plan(int64_t n, int64_t cols, int esize, int kd);
 void launch_lookup_gradient(int dtype, int d, const LookupGradPlan& p, const LookupGradArgs& a, hipStream_t s);

@@ -352,18 +352,20 @@ void launch_join_lookup(const LookupGradPlan& p, const LookupGradArgs& a, int kd
     if (grid > 0) hipLaunchKernelGGL(k_join_lookup, dim3(grid), dim3(256), 0, s, a, p.grid, kd, dC, of_group);
 }
 
-// Bins take k d 256 bytes of LDS for every wavefront; as many workgroups as the compute units hold at once, and blocks of so few places that every wavefront
-// has one: 8192 tokens of 4096 columns 23.5 us with 24 wavefronts to a compute unit (as the registers allow) and 8 places, 30.5 with 16 places, 24.4 with 4.
+// As many workgroups as the compute units hold at once, and blocks of so few places that every wavefront has one: 8192 tokens of 4096 columns, bfloat16,
+// k = 16 21.5 us with 24 wavefronts to a compute unit (as the registers allow) and 8 places; when it took 23.5, 30.5 with 16 places and 24.4 with 4.
+// A wavefront's bins take 8 KB of LDS at most, 16 for codebooks of more than 256 components: lanes that share bins take turns, and more room for each means
+// fewer wavefronts.  The same tokens with 8, 16 and 32 KB: 100 components (d = 1) 52 us, 65 and 80; 128 (d = 8) 34, 35 and 49; in all 400 (d = 4) 82, 72 and 92;
+// 512 (d = 2) 95, 79 and 101.
 LookupGradPlan lookup_grad_plan(int64_t n, int64_t cols, int esize, int kd) {
     LookupGradPlan p{};
     const int64_t strips = (cols + 511) / 512;
     p.few = n <= FEW_TOKENS;
     p.each = (int)std::max<int64_t>(2, std::min<int64_t>(LOOKUP_PLACES, n * strips / 8192));
     const int64_t tasks = (p.few ? n : (n + p.each - 1) / p.each) * strips;
-    // 8192 tokens of 4096 columns, bfloat16: 128 components 62 us with bins for each lane, 40 with bins for two lanes, 100 components 77 and 71; 64 and 32
-    // components, whose bins leave room for all wavefronts either way: 40 and 31 with both
-    p.share = kd > 64 ? 2 : 1;
-    const int wave_bytes = kd * 256 / p.share + LOOKUP_KEPT * 4;
+    p.width_log = 6;
+    while (p.width_log > 2 && kd * 4 << p.width_log > (kd > 256 ? 16384 : 8192)) --p.width_log;
+    const int wave_bytes = (kd * 4 << p.width_log) + LOOKUP_KEPT * 4;
     p.waves = std::min(4, 144 * 1024 / wave_bytes);
     const int64_t resident = std::max(1, std::min((esize == 4 ? 16 : 24) / p.waves, 156 * 1024 / (wave_bytes * p.waves + kd * 4)));
     p.grid = (int)std::min<int64_t>((tasks + p.waves - 1) / p.waves, 256 * resident);
@@ -491,7 +493,7 @@ __global__ __launch_bounds__(256) void k_lookup_codes_fast(const LookupArgs a) {
         const int start = (int)(row_bit & 31) | ((row_bit + a.row_bits + 31) / 32 + 3 > a.nwords ? 32 : 0) | kind << 6;
         auto ask = [&](Item& t, int p) {
             const int of = __builtin_amdgcn_readlane(start, p);
-            const uint32_t* words = reinterpret_cast<const uint32_t*>(of_lane(word, p));
+            const uint32_t* words = of_lane<uint32_t>(word, p);
             const int bit = (of & 31) + at_bit;
             int from = bit >> 5;
             if (of & 32) from = min(from, (int)(a.words + (a.nwords - 3) - words));
@@ -499,7 +501,7 @@ __global__ __launch_bounds__(256) void k_lookup_codes_fast(const LookupArgs a) {
             const u32x3_word w = *reinterpret_cast<const u32x3_word*>(words + from);
 #pragma unroll
             for (int i = 0; i < 3; ++i) t.w[i] = w[i];
-            t.s = reinterpret_cast<const float*>(of_lane(scale, p))[g];
+            t.s = of_lane<float>(scale, p)[g];
         };
         Item now, next;
         ask(now, 0);

@@ -58,9 +58,13 @@ CodesGradLayout codes_grad_layout(const idkm_codes_desc& w, int64_t n) {
     l.lines = n < w.rows ? n : w.rows;  // different rows, at most
     static_cast<BinPlan&>(l) = bin_plan(w, l.lines);
     l.order = 0;
-    l.direct = l.runs && !l.wide && w.cols >= 8;
+    // Many strips of 512 columns and a large codebook: the turns of lanes with the same bins take longer than sums written out and read again.  k = 256, d = 8,
+    // bfloat16, scales of groups of 128: 2000 tokens of 2048 columns 50.5 us in one pass and 53, 8192 of 4096 146 and 125; d = 4, half the components: 38.5
+    // and 51.5, 120 and 123.
+    l.direct = l.runs && w.cols >= 8 && (w.k * w.d <= 1024 || n * ((w.cols + 511) / 512) <= 16384);
     if (l.direct) {
         l.plan = lookup_grad_plan(n, w.cols, esize_of(w.dtype), w.k * w.d);
+        l.segmented = w.S && (l.group > 512 || l.group % 8 != 0 || (l.group & (l.group - 1)) != 0);
         l.per_part = w.S ? l.segmented ? (int)((w.cols + 31) / 32) : l.groups : 0;
         l.bins = buffer(sort_words(n), 4);
         l.segments = l.bins + buffer((int64_t)l.plan.grid * w.k * w.d, 4);

@@ -1,8 +1,8 @@
 // Gradients of a lookup in a stored table, in the codebook and the group scales, in one pass over dY: a row's sum P[c] = alpha sum dY[t, c] stays in the
 // registers of the wavefront that forms it, which reads the row's codes and scales and adds
-//   S P  to its bins of the codebook's components (in LDS, one to a lane or to two lanes that take turns: the order of every sum is fixed)
+//   S P  to its bins of the codebook's components (in LDS, those of a lane or of some lanes that take turns: the order of every sum is fixed)
 //   P C[code]  over the lanes of a group: dS of the row, or of its part where the row's tokens lie in several blocks.
-// For codes of up to 8 bits, D in {1, 2, 4, 8} and codebooks of up to 256 components; the others write the sums P out and go through the kernels of the
+// For codes of up to 8 bits and D in {1, 2, 4, 8}, but for the largest codebooks with many tokens; the others write the sums P out and go through the kernels of the
 // gradient of a product, as do rows of fewer than eight columns.
 #pragma once
 #include "codes_gradient.hpp"
@@ -32,33 +32,37 @@ struct LookupGradArgs {
     int64_t pitch;
     int each;          // places to a block, at most LOOKUP_PLACES
     int sums_log;      // sums of groups (segments) that a row has in a strip of 512 columns: 1 << sums_log, at most 16
+    int width_log;     // lanes with bins of their own: 1 << width_log
     unsigned summing;  // few: workgroups that sum; the ones behind them clear the other rows of dS
 };
 
 constexpr int LOOKUP_PLACES = 32;
 constexpr int LOOKUP_KEPT = LOOKUP_PLACES * 17;  // words of LDS for a wavefront: sums of groups, and whose they are
 
-// 8192 tokens of 4096 columns, 4 bits, groups of 128, bfloat16: 24 us, where dY alone is 13 at the rate of a copy.  Bound by issue and by the turns of the bins: some
+// 8192 tokens of 4096 columns, 4 bits, groups of 128, bfloat16: 21.5 us, where dY alone is 13 at the rate of a copy.  Bound by issue and by the turns of the bins: some
 // 5,100 sums of rows and parts of rows, 42,000 strips of 512 columns at about 100 vector and as many scalar instructions, and eight LDS updates one after
 // another in each.  Beginning and end take 6 us (bins cleared and added up), as many wavefronts as the registers allow the rest.
 // A strip's sums of groups are kept in LDS and stored at the block's end, so that no load waits behind a store.
-// SHARE lanes have the same bins and add to them one after another: the bins of larger codebooks leave room for more wavefronts then, see lookup_grad_plan.
-template <typename T, int D, bool FEW, int SHARE>
+// SHARED: 64 >> width_log lanes have the same bins and add to them one after another: the bins of larger codebooks leave room for more wavefronts then, see
+// lookup_grad_plan.  A code's D bins of a lane lie together and are read and written at once.
+template <typename T, int D, bool FEW, bool SHARED>
 __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a) {
-    constexpr int NC = 8 / D, WIDTH = 64 / SHARE;
-    extern __shared__ __align__(16) float bin_lds[];  // [wave][k D][WIDTH], then the codebook
+    constexpr int NC = 8 / D, WORD = 1, SURE = 2, SCALED = 4, SUMS = 8;
+    struct alignas(4 * D) Code { float part[D]; };
+    extern __shared__ __align__(16) float bin_lds[];  // [wave][k][width][D], then the codebook
+    const int width_log = SHARED ? a.width_log : 6, width = 1 << width_log;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
     if (FEW && blockIdx.x >= a.summing) {
         if (a.dS) clear_other_rows(a.ids, a.dS, a.groups, (int64_t)(blockIdx.x - a.summing) * nw + wave, (int64_t)(gridDim.x - a.summing) * nw);
         return;
     }
     const int kd = a.k * D;
-    float* mine = bin_lds + wave * kd * WIDTH + lane % WIDTH;
-    float* book = bin_lds + nw * kd * WIDTH;
-    const int turn = lane / WIDTH;
+    Code* mine = reinterpret_cast<Code*>(bin_lds + (wave * kd << width_log)) + (lane & (width - 1));
+    float* book = bin_lds + (nw * kd << width_log);
+    const int turn = lane >> width_log;
     float* kept = book + kd + wave * LOOKUP_KEPT;
     int* kept_for = reinterpret_cast<int*>(kept + LOOKUP_PLACES * 16);  // a row of dS, or ~ a place of `parts`
-    for (int i = lane; i < kd * (WIDTH / 4); i += 64) reinterpret_cast<floatx4*>(bin_lds + wave * kd * WIDTH)[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int i = lane; i < kd << (width_log - 2); i += 64) reinterpret_cast<floatx4*>(bin_lds + (wave * kd << width_log))[i] = floatx4{0.f, 0.f, 0.f, 0.f};
     for (int i = threadIdx.x; i < kd; i += blockDim.x) book[i] = Elem<T>::up(static_cast<const T*>(a.C)[i]);
     __syncthreads();
     const int strips = (a.cols + 511) / 512, n = (int)a.ids.n;
@@ -80,7 +84,9 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
         const int skip = columns.skip, at_bit = columns.c / D * a.bits, g = a.S ? min(columns.c + skip, a.cols - 1) / a.group : 0;
         const int g_first = strip * 512 / a.group;
         int held = 0;
+        // sure: all eight columns are there and every code is one; word: the codes lie in 32 bits
         const bool sure = strip * 512 + 512 <= a.cols && a.k > (int)mask;
+        const int form = (sure ? NC * a.bits <= 32 ? WORD : SURE : 0) | (a.S ? SCALED : 0) | (a.dS ? SUMS : 0);
         // word: of the stream, where the row's words begin; row_sh: its codes' bit there; near: three words from a lane's first one on may not be there, and
         // are taken from further ahead
         auto ask = [&](Item& t, const uint32_t* word, int row_sh, bool near, const float* scale) {
@@ -94,6 +100,9 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
             t.s = scale[g];
         };
         auto finish = [&](const Item& t, int who, const float* p) {
+            // looked at anew for every row: the conditions and shifts that follow from them would take more scalar registers than there are
+            int how = form, bits = a.bits, lanes = sum_lanes;
+            asm volatile("" : "+s"(how), "+s"(bits), "+s"(lanes));
             uint32_t b0 = t.w[0], b1 = t.w[1], b2 = t.w[2];
             if (__any(t.sh >= 32)) {  // only near the stream's end
                 const bool two = t.sh >= 64, one = t.sh >= 32;
@@ -102,41 +111,46 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
                 b2 = one ? 0u : b2;
             }
             uint32_t low = __builtin_amdgcn_alignbit(b1, b0, t.sh & 31), high = __builtin_amdgcn_alignbit(b2, b1, t.sh & 31);
-            const float by = a.S ? a.alpha * t.s : a.alpha;
+            const float by = how & SCALED ? a.alpha * t.s : a.alpha;
             float sum = 0.f;
-            // sure: all eight columns are there and every code is one; word: the codes lie in 32 bits
             auto add = [&](auto sure_, auto word_) {
                 constexpr bool sure = decltype(sure_)::value, word = decltype(word_)::value;
-                int place[8];
+                int place[NC];
 #pragma unroll
                 for (int e = 0; e < NC; ++e) {
-                    const uint32_t code = word ? __builtin_amdgcn_ubfe(low, e * a.bits, a.bits) : low & mask;
+                    const uint32_t code = word ? __builtin_amdgcn_ubfe(low, e * bits, bits) : low & mask;
                     if (!word) {
-                        low = __builtin_amdgcn_alignbit(high, low, a.bits);
-                        high >>= a.bits;
+                        low = __builtin_amdgcn_alignbit(high, low, bits);
+                        high >>= bits;
                     }
-                    const bool none = !sure && code >= (uint32_t)a.k;
-                    const int j = none ? 0 : (int)code * D;
+                    const bool none = !sure && code >= (uint32_t)a.k, counts = sure || e * D >= skip;  // skip is a multiple of D
+                    const int j = none ? 0 : (int)code;
+                    const Code w = reinterpret_cast<const Code*>(book)[j];
 #pragma unroll
-                    for (int i = 0; i < D; ++i) {
-                        const bool counts = sure || e * D + i >= skip;
-                        const float w = none ? __builtin_nanf("") : book[j + i];
-                        sum = counts ? fmaf(p[e * D + i], w, sum) : sum;
-                        if constexpr (SHARE == 1) {
-                            float& bin = mine[(j + i) * 64];
-                            bin = counts && !none ? fmaf(by, p[e * D + i], bin) : bin;
-                        } else {
-                            place[e * D + i] = counts && !none ? (j + i) * WIDTH : -1;
-                        }
+                    for (int i = 0; i < D; ++i) sum = counts ? fmaf(p[e * D + i], none ? __builtin_nanf("") : w.part[i], sum) : sum;
+                    place[e] = counts && !none ? j << width_log : -1;
+                }
+                if constexpr (!SHARED) {
+#pragma unroll
+                    for (int e = 0; e < NC; ++e) {
+                        const bool there = sure || place[e] >= 0;
+                        Code bin = mine[there ? place[e] : 0];
+#pragma unroll
+                        for (int i = 0; i < D; ++i) bin.part[i] = there ? fmaf(by, p[e * D + i], bin.part[i]) : bin.part[i];
+                        mine[there ? place[e] : 0] = bin;
                     }
                 }
-                if constexpr (SHARE > 1) {
-#pragma unroll
-                    for (int t = 0; t < SHARE; ++t) {
+                if constexpr (SHARED) {
+                    for (int t = 0; t < 64 >> width_log; ++t) {
                         if (turn == t) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (sure || place[e] >= 0) mine[place[e]] = fmaf(by, p[e], mine[place[e]]);
+                            for (int e = 0; e < NC; ++e) {
+                                if (!sure && place[e] < 0) continue;
+                                Code bin = mine[place[e]];
+#pragma unroll
+                                for (int i = 0; i < D; ++i) bin.part[i] = fmaf(by, p[e * D + i], bin.part[i]);
+                                mine[place[e]] = bin;
+                            }
                         }
                         // one turn after another
                         __builtin_amdgcn_wave_barrier();
@@ -144,12 +158,12 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
                     }
                 }
             };
-            if (sure && NC * a.bits <= 32) add(std::true_type(), std::true_type());
-            else if (sure) add(std::true_type(), std::false_type());
+            if (how & WORD) add(std::true_type(), std::true_type());
+            else if (how & SURE) add(std::true_type(), std::false_type());
             else add(std::false_type(), std::false_type());
-            if (!a.dS) return;
+            if (!(how & SUMS)) return;
             sum *= a.alpha;
-            sum = sum_of_lanes(sum, sum_lanes);
+            sum = sum_of_lanes(sum, lanes);
             if ((lane & (sum_lanes - 1)) == 0 && lane >> lanes_log < 1 << a.sums_log) kept[held << a.sums_log | lane >> lanes_log] = sum;
             if (lane == 0) kept_for[held] = who;
             ++held;
@@ -190,7 +204,7 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
                 places, static_cast<const T*>(a.dY), a.ldy, columns.c, a.cols,
                 [&](Item& t, int p) {
                     const int at = __builtin_amdgcn_readlane(start, p);
-                    ask(t, reinterpret_cast<const uint32_t*>(of_lane(word, p)), at & 31, at & 32, reinterpret_cast<const float*>(of_lane(scale, p)));
+                    ask(t, of_lane<uint32_t>(word, p), at & 31, at & 32, of_lane<float>(scale, p));
                 },
                 [&](const Item& t, int p, bool complete, bool, const float* sum) {
                     finish(t, complete && !a.segmented ? __builtin_amdgcn_readlane(places.row, p) : ~(int)(places.first + p), sum);
@@ -199,24 +213,26 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
         }
     }
     __syncthreads();
-    // A component's bins to as many lanes as there are, four at a time; neighbours begin with other ones, in other banks
-    constexpr int QUADS = WIDTH / 4;
-    int split = QUADS;
-    while (split > 1 && split * kd > (int)blockDim.x) split >>= 1;
-    const int part = threadIdx.x & (split - 1), count = QUADS / split;
-    for (int e0 = 0; e0 < kd; e0 += blockDim.x / split) {
-        const int e = e0 + threadIdx.x / split;
+    // A component's bins to as many lanes as there are; components of different codes begin with different lanes' bins
+    int split_log = width_log;
+    while (split_log > 0 && kd << split_log > (int)blockDim.x) --split_log;
+    const int part = threadIdx.x & ((1 << split_log) - 1), count = width >> split_log;
+    for (int e0 = 0; e0 < kd; e0 += blockDim.x >> split_log) {
+        const int e = e0 + (threadIdx.x >> split_log), j = e / D;
         double sum = 0.0;
-        for (int i = 0; i < count; ++i) {
-            floatx4 v[4];
+        for (int i = 0; i < count && e < kd; i += 4) {
+            float v[4][4];
 #pragma unroll
-            for (int w = 0; w < 4; ++w)
-                if (w < nw && e < kd) v[w] = reinterpret_cast<const floatx4*>(bin_lds + (w * kd + e) * WIDTH)[(i * split + part + e) & (QUADS - 1)];
+            for (int u = 0; u < 4; ++u) {
+                const int at = (((j << width_log) + ((((i + u) << split_log) + part + j) & (width - 1))) * D) + (e - j * D);
 #pragma unroll
-            for (int w = 0; w < 4; ++w)
-                if (w < nw && e < kd) sum += ((double)v[w][0] + (double)v[w][1]) + ((double)v[w][2] + (double)v[w][3]);
+                for (int w = 0; w < 4; ++w) v[u][w] = w < nw ? bin_lds[(w * kd << width_log) + at] : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (i + u < count) sum += ((double)v[u][0] + (double)v[u][1]) + ((double)v[u][2] + (double)v[u][3]);
         }
-        for (int o = split / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+        for (int o = 1 << split_log >> 1; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
         if (e < kd && part == 0) a.bins[e * a.pitch + blockIdx.x] = (float)sum;
     }
 }

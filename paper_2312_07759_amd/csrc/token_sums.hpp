@@ -181,8 +181,12 @@ struct Places {
     }
 };
 
-__device__ __forceinline__ uint64_t of_lane(uint64_t v, int lane) {
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+// An address in the card's memory, of one lane.  Said to be there: a load from any address counts as one of LDS too, and every wait for LDS, of the bins or
+// the codebook, then waits for the rows asked for ahead (8192 tokens, k = 16: 24 us against 21.5).
+template <typename P>
+__device__ __forceinline__ const P* of_lane(uint64_t v, int lane) {
+    const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+    return (const P*)reinterpret_cast<const __attribute__((address_space(1))) P*>(at);
 }
 
 // Sums the places of a block, one row after another, and calls finish(item, p, complete, began, sum) with a row's last place there, the p-th; begin(item, p)
@@ -207,8 +211,8 @@ __device__ __forceinline__ void sum_places_of(const Places& at, const T* dY, int
     auto ask = [&](Step& s) {
         const int from = min(p, at.count - 1), last = __builtin_amdgcn_readlane(last_of_lane, from), to = min(from + 1, last);
         begin(s.item, from);
-        s.rows.ask(0, reinterpret_cast<const T*>(of_lane(from_lane, from)), c, cols);
-        s.rows.ask(1, reinterpret_cast<const T*>(of_lane(from_lane, to)), c, cols);
+        s.rows.ask(0, of_lane<T>(from_lane, from), c, cols);
+        s.rows.ask(1, of_lane<T>(from_lane, to), c, cols);
         s.count = p < at.count ? to - from + 1 : 0;
         s.last = to == last ? last : -1;
         p += s.count;

@@ -112,6 +112,14 @@ def test_stored_many_tokens(ctx, n, kind):
     run_codes(ctx, Layer(700, 64, 16, 1, 32, torch.bfloat16, seed=n), tokens(kind, n, 700, 3), n)
 
 
+@pytest.mark.parametrize("n,cols,k,d", [(17000, 16, 256, 8), (6000, 1496, 256, 8), (16384, 16, 256, 8), (3000, 1032, 256, 4), (3000, 1032, 100, 8), (2000, 520, 64, 1),
+                                        (2000, 520, 65, 1), (2000, 520, 100, 4), (2000, 520, 256, 2), (450, 1030, 100, 2), (513, 1032, 256, 8), (700, 9, 129, 1)])
+def test_stored_codebooks_of_many_tokens(ctx, n, cols, k, d):
+    """Bins of a lane's own, of two to sixteen lanes in turn, and sums written out, on both sides of where they change."""
+    for group, dtype, kind in ((0, torch.float32, "text"), (32, torch.bfloat16, "runs"), (cols, torch.float16, "any")):
+        run_codes(ctx, Layer(500, cols, k, d, group, dtype, seed=n), tokens(kind, n, 500, 4), n)
+
+
 @pytest.mark.parametrize("dtype", sorted(DTYPES))
 @pytest.mark.parametrize("rows,cols", [(1, 1), (50, 7), (300, 512), (333, 1001), (70000, 24)])
 @pytest.mark.parametrize("n", [1, 33, 700, 20000])
