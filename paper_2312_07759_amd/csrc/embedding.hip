@@ -191,7 +191,8 @@ __device__ __forceinline__ void store_sum(float* to, const Columns& at, int cols
 }
 
 // The sum of a row that has all of its places in a block goes to `out`; parts of others go to `partial` (2 b: of a row that began before block b,
-// 2 b + 1: of one that begins in it and goes on), which the next kernel adds up in order.
+// 2 b + 1: of one that begins in it and goes on), which the next kernel adds up in order.  4096 tokens of 1024 columns, bfloat16: 6 us, and 5 to join the parts; latency of
+// the order, the rows and, in the other launch, the parts.
 template <typename T, bool NARROW>
 __global__ __launch_bounds__(256) void k_sums(const SumArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -210,7 +211,7 @@ __global__ __launch_bounds__(256) void k_sums(const SumArgs a) {
     sum_places_of<T, NARROW, None>(places, static_cast<const T*>(a.dY), a.ldy, columns.c, cols, begin, end);
 }
 
-// Up to FEW_TOKENS tokens: the first workgroups sum, the ones behind them clear the rows of which there is no token.
+// Up to FEW_TOKENS tokens: the first workgroups sum, the ones behind them clear the rows of which there is no token.  33 tokens, 1000 rows of 512: 3.8 us.
 template <typename T, bool NARROW>
 __global__ __launch_bounds__(256) void k_sums_of_few(const TokenIds ids, float alpha, const T* dY, int64_t ldy, int cols, float* dW, unsigned summing) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -391,7 +392,7 @@ struct EightOut {
     }
 };
 
-// A thread takes 8 columns of a token's row.
+// A thread takes 8 columns of a token's row.  Bound by memory: 4096 tokens of 1024 columns to bfloat16, 17 MB read and 8 written, 5.3 us, 4.7 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void k_lookup_table(const LookupArgs a) {
     const int64_t per_row = (a.cols + 7) / 8, total = a.ids.n * per_row;
@@ -459,7 +460,7 @@ __global__ __launch_bounds__(256) void k_lookup_codes(const LookupArgs a) {
 
 // The same for codes of up to 8 bits, D in {1, 2, 4, 8} and rows of at least eight columns: a wavefront takes 512 columns of some tokens' rows, whose codes
 // are asked for one token ahead.  The codebook lies in LDS, once: lanes that meet in a bank wait for each other, which the stores cover.
-// 8192 tokens of 4096 columns, k = 256, d = 4, float16: 18 us (a fill of Y takes 10; 43 with one code read at a time, 64-bit divisions for every eight columns).
+// 8192 tokens of 4096 columns, k = 256, d = 4, float16: 18.5 us (a fill of Y takes 10; 43 with one code read at a time, 64-bit divisions for every eight columns).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_lookup_codes_fast(const LookupArgs a) {
     constexpr int NC = 8 / D;

@@ -118,7 +118,8 @@ void launch_int8_rows(int dtype, const Int8RowsArgs& a, hipStream_t s) {
 
 // 16 rows of the layer and 16 NT tokens to a workgroup, whose WAVES wavefronts share the sum; lane l has row l % 16 and, of every 64 columns, the 16 of quarter
 // l / 16.  Integers of four to eight such steps are asked for together, where there are registers the next ones
-// before these are used.
+// before these are used.  The layer is read once for 16 NT tokens: 4096 x 4096 at one token 5.6 us, 3.0 TB/s (a copy's rate: 3.3 us); 41 tokens of 512 x 4608 7 us, the
+// latency of four or five batches of loads, one after another, and of the joining of sixteen sums.
 // FUSED (up to INT8_FUSED elements of X, NT = 1): every workgroup brings the tokens to integers itself, into LDS, instead of a launch before this one.
 template <typename T, int NT, int WAVES, bool FUSED>
 __global__ __launch_bounds__(64 * WAVES) void k_int8_few(const Int8FewArgs a) {

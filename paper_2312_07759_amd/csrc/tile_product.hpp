@@ -5,8 +5,8 @@
 // the order c ^ (r mod 8), so that the eight lanes that LDS serves together read eight different bank groups.
 // Operands are padded: a row's elements up to the next whole step are there (and zero in one of the two), rows begin at
 // multiples of 16 bytes.  Rows behind the last one are read from the last one and not stored.
-// 2048 x 4096 x 4096 in bfloat16: 62 us, 1100 TFLOP/s (the library's 61.9); 4096 x 4096 x 2048 with float32 results: 63 (the library's 52.8, with
-// results of 16 bits); 512 x 4608 x 1024 in float32: 57 (the library's 64).  Bound by the matrix cores and, between two steps, by the
+// 2048 x 4096 x 4096 in bfloat16: 62 us, 1100 TFLOP/s (the library's 61.9); 4096 x 4096 x 2048 with float32 results: 62 to 65 (the library's 52.8, with
+// results of 16 bits); 512 x 4608 x 1024 in float32: 57 (the library's 64); 2048 x 4096 x 4096 in 8-bit integers: 38 (the library's 45.7).  Bound by the matrix cores and, between two steps, by the
 // barrier: nothing covers it where a workgroup fills a compute unit (16 bits: 256 x 128, 256 x 256 and 128 x 128 with four stages; float: 128 x 128);
 // of the other shapes two fit.
 #pragma once
