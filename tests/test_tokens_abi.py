@@ -23,14 +23,14 @@ def test_workspace_sizes():
     for kw in ({}, {"S": 16, "group": 64}, {"S": 16, "group": 96}, {"dtype": binding.F32}, {"k": 1000, "d": 4}, {"k": 256, "d": 4}, {"rows": 1, "cols": 1}):
         w = codes(**kw)
         assert lib.idkm_codes_embedding_backward_workspace(ctypes.byref(w), 0) == 0
-        for n in (1, 256, 257, 16384, 16385, 4_000_000):
+        for n in (1, 256, 257, 512, 513, 16384, 16385, 4_000_000):
             b = lib.idkm_codes_embedding_backward_workspace(ctypes.byref(w), n)
             assert b > 0 and b % 256 == 0
     # the sums of rows are as many as there are rows, not tokens
     small = lib.idkm_codes_embedding_backward_workspace(ctypes.byref(codes(k=256, d=4)), 4_000_000)
     assert small < 4_000_000 * 24 + 2 ** 30
-    assert lib.idkm_embedding_backward_workspace(1000, 64, 0) == 0 and lib.idkm_embedding_backward_workspace(1000, 64, 256) == 0
-    assert lib.idkm_embedding_backward_workspace(1000, 64, 257) > 0
+    assert lib.idkm_embedding_backward_workspace(1000, 64, 0) == 0 and lib.idkm_embedding_backward_workspace(1000, 64, 512) == 0
+    assert lib.idkm_embedding_backward_workspace(1000, 64, 513) > 0
     for n in (1, 4, 5, 64, 65, 4096):
         f, b = (getattr(lib, name)(ctypes.byref(int8()), n) for name in ("idkm_int8_linear_workspace", "idkm_int8_linear_backward_workspace"))
         assert f >= 0 and b > 0 and f % 16 == 0 and b % 16 == 0
