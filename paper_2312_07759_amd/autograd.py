@@ -291,14 +291,10 @@ class Int8Linear(torch.nn.Module):
         self.rows, self.cols = layer.rows, layer.cols
         self.register_buffer("W8", layer.W8)
         self.register_buffer("scale", layer.scale)
-        self._layers = {}
 
     def layer(self, dtype):
         """The layer as it is now, for activations of `dtype`."""
-        made = self._layers.get(dtype)
-        if made is None or made[0] is not self.W8 or made[1] is not self.scale:
-            made = self._layers[dtype] = self.W8, self.scale, binding.Int8Layer(self.W8, self.scale.float(), dtype, self.cols)
-        return made[2]
+        return binding.Int8Layer(self.W8, self.scale.float(), dtype, self.cols)
 
     def forward(self, X):
         if X.shape[-1] != self.cols:

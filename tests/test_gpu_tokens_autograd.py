@@ -1,4 +1,6 @@
 """The differentiable front ends of embedding tables, of inputs kept in 8 bits and of layers in 8-bit integers, alone and one after another."""
+import copy
+
 import pytest
 import torch
 
@@ -242,4 +244,22 @@ def test_differentiable_calls_cannot_be_captured():
             graph.replay()
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(out, ref))
+    ctx.close()
+
+
+def test_copies_and_casts_of_an_integer_layer():
+    """After a call: a copy, another type of the scales, and what is loaded into them is what the next call uses."""
+    ctx = binding.Context(0)
+    m = autograd.Int8Linear(ctx.int8_layer(draw((50, 200), torch.float32, 1).cuda(), torch.float32))
+    X = draw((7, 200), torch.float32, 2).cuda()
+    Y = m(X)
+    twin = copy.deepcopy(m)
+    assert torch.equal(twin(X), Y)
+    twin.half()
+    Z = twin(X)
+    with torch.no_grad():
+        twin.scale.mul_(2)
+    assert torch.equal(twin(X), 2 * Z) and torch.equal(m(X), Y)
+    m.load_state_dict({"W8": torch.zeros_like(m.W8), "scale": m.scale.clone()})
+    assert not bool(m(X).any())
     ctx.close()
