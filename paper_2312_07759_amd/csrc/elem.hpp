@@ -78,4 +78,12 @@ __device__ __forceinline__ void mma16(typename Sum<T>::four& acc, u32x4 a, u32x4
     }
 }
 
+// A token's scale in a product of 8-bit integers: sum s by, in this order, for |sum| < 2^31 and s as the tokens' are, at most 2^122.  sum s alone may be too large for a float32
+// number where the result is none too large: the largest scales take part in two steps, of which the second is a power of two.
+struct TokenScale {
+    float s, rest;
+    __device__ __forceinline__ explicit TokenScale(float scale) : s(scale < 0x1p96f ? scale : scale * 0x1p-64f), rest(scale < 0x1p96f ? 1.f : 0x1p64f) {}
+    __device__ __forceinline__ float result(int sum, float by) const { return (float)sum * s * by * rest; }
+};
+
 }  // namespace idkm

@@ -262,7 +262,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_int8_few(const Int8FewArgs a) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const int64_t t = t0 + wave * 16 + q * 4 + r;
-        if (t < a.n) static_cast<T*>(a.Y)[t * a.ldy + r0 + li] = Elem<T>::down((float)sum[r] * s[r] * by);
+        if (t < a.n) static_cast<T*>(a.Y)[t * a.ldy + r0 + li] = Elem<T>::down(TokenScale(s[r]).result(sum[r], by));
     }
 }
 
@@ -347,7 +347,7 @@ __global__ __launch_bounds__(256) void k_join_int8(const int32_t* __restrict__ p
         int sum = parts[at];
         for (int z = 1; z < nz; ++z) sum += parts[z * total + at];
         const int64_t m = at / N, n = at - m * N;
-        out[m * ldo + n] = Elem<T>::down((float)sum * by_m[m] * by_n[n]);
+        out[m * ldo + n] = Elem<T>::down(TokenScale(by_m[m]).result(sum, by_n[n]));
     }
 }
 

@@ -322,10 +322,10 @@ __global__ __launch_bounds__(64 * WM * WN, SC > 0 ? 2 : 1) void k_tile_product(c
                     const int v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
                     store_four(static_cast<int*>(a.out) + ((int64_t)z * a.M + m) * a.ldo + n, v, quad, a.N - n);
                 } else {
-                    const float by = a.by_m[m];
+                    const TokenScale by(a.by_m[m]);
                     float v[4];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) v[r] = (float)acc[i][j][r] * by * a.by_n[min(n + r, a.N - 1)];
+                    for (int r = 0; r < 4; ++r) v[r] = by.result(acc[i][j][r], a.by_n[min(n + r, a.N - 1)]);
                     store_four_as(a.out, m * a.ldo + n, a.dtype, v, quad, a.N - n);
                 }
             } else {

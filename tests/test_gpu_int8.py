@@ -183,3 +183,15 @@ def test_none_and_refusals(ctx):
                     (W8.cuda(), scale.cuda(), torch.int8), (W8.cuda().t(), scale.cuda(), torch.float32), (W8, scale, torch.float32)):
         with pytest.raises(TypeError):
             binding.Int8Layer(W, s, t)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,rows,cols", [(1, 40, 512), (3, 40, 512), (20, 40, 700), (300, 200, 512), (70, 64, 8192)])
+def test_tokens_near_the_largest_number(ctx, n, rows, cols, dtype):
+    """A sum times the token's scale has no float32 number here, the result has one."""
+    X = (draw((n, cols), torch.float32, 1).clamp(-3, 3) * 1e38).to(DTYPES[dtype])
+    W8, scale, _ = layer_of(rows, cols, X.dtype, 2)
+    scale *= 1e-8
+    got = ctx.int8_linear(binding.Int8Layer(W8.cuda(), scale.cuda(), X.dtype), X.cuda())
+    assert bool(got.isfinite().all()) and float(got.abs().max()) > 1e30
+    check_product(got.cpu(), X, W8, scale)
