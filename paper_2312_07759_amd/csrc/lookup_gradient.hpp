@@ -186,7 +186,7 @@ __global__ __launch_bounds__(256) void k_lookup_gradient(const LookupGradArgs a)
             if (!first) continue;
             Item t;
             const int64_t row_bit = row * a.row_bits;
-            ask(t, a.words + (row_bit >> 5), (int)(row_bit & 31), true, S + (int64_t)row * groups);
+            ask(t, a.words + (row_bit >> 5), (int)(row_bit & 31), (row_bit + a.row_bits + 31) / 32 + 3 > a.nwords, S + (int64_t)row * groups);
             float sum[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] = 0.f;

@@ -100,6 +100,22 @@ def test_tables_beyond_32_bits(ctx):
     assert torch.equal(dC[:, 0], torch.bincount(codes.reshape(-1), minlength=16).float())
 
 
+def test_stored_tables_of_more_than_2_31_words(ctx):
+    """Rows whose words lie further from the stream's end than 32 bits tell."""
+    rows, cols = 3_600_000, 2400
+    ids = torch.tensor([0, rows - 1, 5, rows - 2, rows - 1, -1, 1_700_000], device="cuda")
+    words = torch.zeros(rows, cols // 4, dtype=torch.int32, device="cuda")
+    held = ids[ids >= 0]
+    words[held] = torch.randint(-2 ** 31, 2 ** 31 - 1, (6, cols // 4), generator=torch.Generator().manual_seed(1)).int().cuda()
+    C = torch.linspace(-1, 1, 256, device="cuda")[:, None].contiguous()
+    layer = binding.CodesLayer(words.view(-1), rows, cols, C)
+    codes = ((words[held][:, :, None] >> torch.arange(0, 32, 8, device="cuda", dtype=torch.int32)) & 255).reshape(6, cols).long()
+    assert torch.equal(ctx.codes_embedding(layer, ids)[ids >= 0], C[:, 0][codes])
+    for n in (7, 700):
+        dC = ctx.codes_embedding_backward(layer, ids.repeat(n // 7), torch.ones(n, cols, device="cuda"))["dC"]
+        assert torch.equal(dC[:, 0], n // 7 * torch.bincount(codes.reshape(-1), minlength=256).float())
+
+
 def test_activations_beyond_32_bits(ctx):
     """More than 2^31 elements of activations: kept, brought back, in integers, looked up and summed."""
     n, cols = 600_000, 4096
