@@ -87,7 +87,7 @@ struct Int8FewArgs {
     void* Y;  // T [n, ldy]
     int64_t ldy;
 };
-constexpr int64_t INT8_FUSED = 4 * 8192;  // elements of X that a workgroup brings to integers itself, at most
+constexpr int64_t INT8_FUSED = 4 * 8192;  // elements of X, in whole steps of 128 columns, that a workgroup brings to integers itself, at most
 void launch_int8_few(int dtype, const Int8FewArgs& a, hipStream_t s);
 // Operands of the gradient of a float32 product: dY times the scales in three parts of 16 bits, and columns of W8 in 16 bits.
 struct Int8SplitArgs {

@@ -600,7 +600,7 @@ Int8Layout int8_layout(const idkm_int8_desc& w, int64_t n) {
     l.pad = up_to(w.cols, 128);  // of the sum: what lies behind in W8's rows counts for nothing
     // Both forms at 64 and 65 tokens, bfloat16: 512 x 4608 10.7 us and 13.8, 1000 x 512 9.9 and 9.7, 4096 x 4096 15.6 and 15.1.
     l.few = n <= 64;
-    l.fused = n <= 4 && n * w.cols <= INT8_FUSED;
+    l.fused = n <= 4 && n * l.pad <= INT8_FUSED;
     l.q = 0;
     l.scale = l.fused ? 0 : buffer(n * l.pad, 1);
     l.parts = l.scale + (l.fused ? 0 : buffer(n, 4));

@@ -195,3 +195,11 @@ def test_tokens_near_the_largest_number(ctx, n, rows, cols, dtype):
     got = ctx.int8_linear(binding.Int8Layer(W8.cuda(), scale.cuda(), X.dtype), X.cuda())
     assert bool(got.isfinite().all()) and float(got.abs().max()) > 1e30
     check_product(got.cpu(), X, W8, scale)
+
+
+@pytest.mark.parametrize("n,cols", [(3, 10_900), (3, 10_880), (2, 16_384), (2, 16_300), (1, 32_700), (4, 8192), (4, 8100), (1, 32_769)])
+def test_as_many_columns_as_a_workgroup_holds(ctx, n, cols):
+    """Tokens brought to integers by the product's own workgroups, up to the last column that fits, and by a launch before it."""
+    X = draw((n, cols), torch.bfloat16, 1)
+    W8, scale, layer = layer_of(20, cols, torch.bfloat16, 3)
+    check_product(ctx.int8_linear(layer, X.cuda()).cpu(), X, W8, scale)
