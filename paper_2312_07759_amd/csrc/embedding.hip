@@ -251,14 +251,13 @@ __global__ __launch_bounds__(256) void k_join_sums(const SumArgs a) {
     float sum = a.partial[(2 * start + 1) * a.ldp + c];
     const float* part = a.partial + c;
     int64_t i = start + 1;
-    for (; i + 8 <= b + 1; i += 8) {
-        float v[8];
+    for (; i <= b; i += 16) {  // the last part again where there are fewer
+        float v[16];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = part[2 * (i + u) * a.ldp];
+        for (int u = 0; u < 16; ++u) v[u] = part[2 * min(i + u, b) * a.ldp];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) sum += v[u];
+        for (int u = 0; u < 16; ++u) sum += i + u <= b ? v[u] : 0.f;
     }
-    for (; i <= b; ++i) sum += part[2 * i * a.ldp];
     a.out[(a.index_at ? (int64_t)a.index_at[first] : (int64_t)row) * a.ldo + c] = sum;
 }
 
@@ -311,15 +310,19 @@ __global__ __launch_bounds__(256) void k_join_lookup(const LookupGradArgs a, int
         for (int g = own; g - own < a.groups; g += at_once) {  // all lanes take part in the exchanges
             float sum = 0.f;
             const int from = g * of_group, to = g < a.groups ? min(a.per_part, from + of_group) : from;
-            for (int64_t q = start; q <= last; q += 8) {
+            auto batch = [&](int64_t q, auto many) {  // the last part again where there are fewer
+                constexpr int U = decltype(many)::value;
                 for (int j = from + part; j < to; j += share) {
-                    float v[8];
+                    float v[U];
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) v[u] = q + u <= last ? a.parts[(a.few ? p : min((q + u + 1) * a.each - 1, p)) * a.per_part + j] : 0.f;
+                    for (int u = 0; u < U; ++u) v[u] = a.parts[(a.few ? p : min((min(q + u, last) + 1) * a.each - 1, p)) * a.per_part + j];
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) sum += v[u];
+                    for (int u = 0; u < U; ++u) sum += q + u <= last ? v[u] : 0.f;
                 }
-            }
+            };
+            int64_t q = start;
+            for (; q + 8 <= last; q += 16) batch(q, std::integral_constant<int, 16>());
+            if (q <= last) batch(q, std::integral_constant<int, 8>());
             for (int o = 1; o < share; o <<= 1) sum += __shfl_xor(sum, o);
             if (part == 0 && g < a.groups) a.dS[(int64_t)row * a.groups + g] = sum;
         }
