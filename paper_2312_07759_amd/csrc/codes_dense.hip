@@ -61,9 +61,17 @@ void allow_lds(const void* fn, size_t bytes) {
     if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess) slot.store(key, std::memory_order_relaxed);
 }
 
-// The kernels with lookups, for the codes that they take; a run's words (three at most) have to be there.
+static int64_t operand_tiles(const OperandArgs& a) {
+    int64_t tiles = 0;
+    for (int j = 0; j < a.jobs; ++j) tiles += a.job[j].tiles;
+    return tiles;
+}
+
+// The kernels with lookups take these; a run's words (three at most) have to be there.
+static bool fast_codes(const DenseArgs& a) { return a.bits <= 8 && (a.d == 1 || a.d == 2 || a.d == 4 || a.d == 8) && a.nwords >= 4; }
+
 static bool launch_fast(int dtype, const DenseArgs& a, bool columns, hipStream_t s) {
-    if (a.bits > 8 || (a.d != 1 && a.d != 2 && a.d != 4 && a.d != 8) || a.nwords < 4) return false;
+    if (!fast_codes(a)) return false;
     const int at_once = codes_at_once(a.bits, a.d), IB = at_once * a.bits, W = at_once * a.d;
     const DenseFn fn = codes_dense_kernel(dtype, IB, W, columns, a.row_bits % 32 == 0);
     const size_t table = (size_t)128 << IB, tile = columns ? (dtype == 0 ? TransposeTile<float>::WORDS : TransposeTile<bf16>::WORDS) * 4 : 0;
@@ -71,7 +79,9 @@ static bool launch_fast(int dtype, const DenseArgs& a, bool columns, hipStream_t
     // as many workgroups as the compute units hold at once, each with one table
     const int64_t most = columns ? 768 : 1024;
     if (grid > most) grid = most;
-    hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(256), table + tile, s, a);
+    DenseArgs b = a;
+    b.dense = (unsigned)grid;
+    hipLaunchKernelGGL(fn, dim3((unsigned)(grid + operand_tiles(a.also))), dim3(256), table + tile, s, b);
     return true;
 }
 
@@ -84,9 +94,16 @@ void launch_dense_rows(int dtype, const DenseArgs& args, hipStream_t s) {
     });
 }
 
-void launch_dense_cols(int dtype, const DenseArgs& args, hipStream_t s) {
+void launch_dense_cols(int dtype, const DenseArgs& args, hipStream_t s, const OperandArgs& also) {
     DenseArgs a = args;
-    if (launch_fast(dtype, a, true, s)) return;
+    // One launch for both: gradients of 512 tokens of 2048 x 2048 in bfloat16 57.5 us in two launches and 55, 500 of 1000 x 1000 in float32 57 and 54, as long where
+    // either fills the device by itself (2048 tokens of 4096 x 4096).
+    if (fast_codes(a)) {
+        a.also = also;
+        launch_fast(dtype, a, true, s);
+        return;
+    }
+    launch_operands(dtype, also, s);
     const dim3 grid((unsigned)((a.count + 63) / 64), (unsigned)((a.pad + 63) / 64));
     BY_TYPE(dtype, T, {
         const size_t lds = codebook_lds(a, sizeof(T));
@@ -103,8 +120,7 @@ void add_operand(OperandArgs* a, const void* in, int64_t ldi, int64_t M, int64_t
 }
 
 void launch_operands(int dtype, const OperandArgs& a, hipStream_t s) {
-    int64_t tiles = 0;
-    for (int j = 0; j < a.jobs; ++j) tiles += a.job[j].tiles;
+    const int64_t tiles = operand_tiles(a);
     if (tiles > 0) BY_TYPE(dtype, T, hipLaunchKernelGGL(k_operands<T>, dim3((unsigned)tiles), dim3(256), 0, s, a));
 }
 

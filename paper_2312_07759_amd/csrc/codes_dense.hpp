@@ -5,6 +5,27 @@
 
 namespace idkm {
 
+// Operands brought to the form in which the tile product takes them, several in one launch.
+//   rows        out[M, pad] = in[M, N], zero behind column N
+//   transposed  out[N, pad] = in[M, N]^T, zero behind column M
+// E: `in` is kept in 8 bits, rows ldi apart (see keep8.hpp), and brought back on the way.
+// scale: `in` holds 8-bit integers (rows ldi apart, a multiple of 16, zero behind column N), and comes out times its row's scale, rounded to T: an operand of the
+// matrix instruction, with the relative error, eps / 2 at most, of a weight stored in T.
+struct Operand {
+    const void* in;
+    int64_t ldi, M, N;
+    void* out;
+    int64_t pad;
+    int transposed;
+    int64_t tiles, tiles_n;  // of 64 x 64, and along N (rows: along pad)
+    const uint8_t* E;        // [M, ldi / 32] or null
+    const float* scale;      // [M] or null
+};
+struct OperandArgs {
+    Operand job[3];
+    int jobs;
+};
+
 // A layer's rows [r0, r0 + nr) or columns [c0, c0 + nc), as the tile product takes them.
 struct DenseArgs {
     const uint32_t* words;
@@ -25,6 +46,9 @@ struct DenseArgs {
     // rows only: the codewords go out as they are, and S transposed to scales_out [groups, scale_pitch], row `first` its first
     float* scales_out;  // or null
     int64_t scale_pitch;
+    // columns only: workgroups behind the first `dense` bring operands
+    unsigned dense;
+    OperandArgs also;
 };
 
 // Group of column c: the product with the rounded-up inverse is off by one at most, and then too large.
@@ -66,6 +90,54 @@ struct TransposeTile {
         }
     }
 };
+
+// The t-th 64 x 64 tile of all operands, by a workgroup.
+template <typename T>
+__device__ __forceinline__ void bring_operand(const OperandArgs& a, int64_t t, const TransposeTile<T>& tile) {
+    int j = 0;
+    while (j + 1 < a.jobs && t >= a.job[j].tiles) t -= a.job[j++].tiles;
+    const Operand& o = a.job[j];
+    const int64_t tm = t / o.tiles_n, m0 = tm * 64, n0 = (t - tm * o.tiles_n) * 64;
+    const int64_t m = m0 + (threadIdx.x >> 3) * 2, n = n0 + (threadIdx.x & 7) * 8;
+    struct alignas(16) Eight { T v[8]; } v[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        const T* row = static_cast<const T*>(o.in) + (m + b) * o.ldi;
+        if (o.scale) {
+            const bool there = m + b < o.M && n < o.N;
+            const u32x2 q = *reinterpret_cast<const u32x2*>(static_cast<const int8_t*>(o.in) + (there ? (m + b) * o.ldi + n : 0));
+            const float by = o.scale[there ? m + b : 0];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[b].v[e] = there ? Elem<T>::down((float)(int8_t)(q[e >> 2] >> (e & 3) * 8) * by) : (T)0.f;
+        } else if (o.E) {
+            const bool there = m + b < o.M && n < o.N;
+            const int64_t at = there ? (m + b) * o.ldi + n : 0;
+            const u32x2 q = *reinterpret_cast<const u32x2*>(static_cast<const int8_t*>(o.in) + at);
+            const int field = o.E[at / KEEP_BLOCK];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[b].v[e] = there ? Keep8<T>::value((int8_t)(q[e >> 2] >> (e & 3) * 8), field) : (T)0.f;
+        } else if (m + b < o.M && n + 8 <= o.N) {
+            u32x4 raw[8 / Elem<T>::PER16];
+#pragma unroll
+            for (int f = 0; f < 8 / Elem<T>::PER16; ++f) raw[f] = reinterpret_cast<const u32x4_any*>(row + n)[f];
+            __builtin_memcpy(v[b].v, raw, sizeof(raw));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[b].v[e] = m + b < o.M && n + e < o.N ? row[n + e] : (T)0.f;
+        }
+    }
+    if (o.transposed) {  // the same for the whole workgroup
+        tile.put(v[0].v, v[1].v);
+        __syncthreads();
+        tile.emit(static_cast<T*>(o.out) + n0 * o.pad + m0, o.N - n0, o.pad, o.pad - m0);
+    } else {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+            if (m + b < o.M && n < o.pad) *reinterpret_cast<Eight*>(static_cast<T*>(o.out) + (m + b) * o.pad + n) = v[b];
+    }
+}
 
 // Eight columns of a row of the layer on their way: asked for, and brought to T.  Where the weights are scaled here (columns, for dX, along
 // whose sum every weight has another scale; and float32) each is rounded once: it is an operand of the matrix instruction, and the
@@ -172,13 +244,17 @@ __global__ __launch_bounds__(256) void k_dense_rows_fast(const DenseArgs a) {
 }
 
 // The layer's columns: out[c, r] = w[r, c], 64 x 64 weights at a time, the next tile's asked for before this one goes through LDS.
-// 4096 x 4096 in 16 bits: 17 us (24 with nothing asked for ahead); bound by the lookups and the LDS traffic of the transposition.
+// 4096 x 4096 in 16 bits: 14 us (24 with nothing asked for ahead); bound by the lookups and the LDS traffic of the transposition.
 template <typename T, int IB, int W, bool ALIGNED>
 __global__ __launch_bounds__(256) void k_dense_cols_fast(const DenseArgs a) {
     extern __shared__ __align__(128) unsigned char lds[];
     const Table<T, IB, W> entries(a.C, a.k, a.bits, a.d);
     const unsigned char* table = Table<T, IB, W>::own(lds);
     const TransposeTile<T> tile{reinterpret_cast<uint32_t*>(lds + Table<T, IB, W>::BYTES)};
+    if (blockIdx.x >= a.dense) {
+        bring_operand(a.also, blockIdx.x - a.dense, tile);
+        return;
+    }
     const int tiles_c = (int)((a.count + 63) / 64), tiles_r = (int)((a.pad + 63) / 64);
     const int lr = (threadIdx.x >> 3) * 2, lc = (threadIdx.x & 7) * 8;
     EightOfLayer<T, IB, W, ALIGNED> eight[2];
@@ -191,7 +267,7 @@ __global__ __launch_bounds__(256) void k_dense_cols_fast(const DenseArgs a) {
     int t = blockIdx.x;
     if (t < tiles_c * tiles_r) ask(t);
     entries.build(lds, a.C, a.k, a.bits, a.d);
-    for (; t < tiles_c * tiles_r; t += gridDim.x) {
+    for (; t < tiles_c * tiles_r; t += a.dense) {
         const int tr = t / tiles_c, tc = t - tr * tiles_c;
         const int c0 = (int)a.first + tc * 64 + lc;
         T w[2][8];
@@ -205,7 +281,7 @@ __global__ __launch_bounds__(256) void k_dense_cols_fast(const DenseArgs a) {
                 for (int e = 0; e < 8; ++e) w[b][e] = (T)0.f;
             }
         }
-        if (t + (int)gridDim.x < tiles_c * tiles_r) ask(t + gridDim.x);
+        if (t + (int)a.dense < tiles_c * tiles_r) ask(t + a.dense);
         tile.put(w[0], w[1]);
         __syncthreads();
         tile.emit(static_cast<T*>(a.out) + (int64_t)tc * 64 * a.pad + tr * 64, a.count - tc * 64, a.pad, a.pad - tr * 64);
@@ -325,75 +401,10 @@ __global__ __launch_bounds__(256) void k_dense_cols(const DenseArgs a) {
     }
 }
 
-// Operands brought to the form in which the tile product takes them, several in one launch.
-//   rows        out[M, pad] = in[M, N], zero behind column N
-//   transposed  out[N, pad] = in[M, N]^T, zero behind column M
-// E: `in` is kept in 8 bits, rows ldi apart (see keep8.hpp), and brought back on the way.
-// scale: `in` holds 8-bit integers (rows ldi apart, a multiple of 16, zero behind column N), and comes out times its row's scale, rounded to T: an operand of the
-// matrix instruction, with the relative error, eps / 2 at most, of a weight stored in T.
-struct Operand {
-    const void* in;
-    int64_t ldi, M, N;
-    void* out;
-    int64_t pad;
-    int transposed;
-    int64_t tiles, tiles_n;  // of 64 x 64, and along N (rows: along pad)
-    const uint8_t* E;        // [M, ldi / 32] or null
-    const float* scale;      // [M] or null
-};
-struct OperandArgs {
-    Operand job[3];
-    int jobs;
-};
-
 template <typename T>
 __global__ __launch_bounds__(256) void k_operands(const OperandArgs a) {
     __shared__ __align__(16) uint32_t lds[TransposeTile<T>::WORDS];
-    int64_t t = blockIdx.x;
-    int j = 0;
-    while (j + 1 < a.jobs && t >= a.job[j].tiles) t -= a.job[j++].tiles;
-    const Operand& o = a.job[j];
-    const int64_t tm = t / o.tiles_n, m0 = tm * 64, n0 = (t - tm * o.tiles_n) * 64;
-    const int64_t m = m0 + (threadIdx.x >> 3) * 2, n = n0 + (threadIdx.x & 7) * 8;
-    struct alignas(16) Eight { T v[8]; } v[2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const T* row = static_cast<const T*>(o.in) + (m + b) * o.ldi;
-        if (o.scale) {
-            const bool there = m + b < o.M && n < o.N;
-            const u32x2 q = *reinterpret_cast<const u32x2*>(static_cast<const int8_t*>(o.in) + (there ? (m + b) * o.ldi + n : 0));
-            const float by = o.scale[there ? m + b : 0];
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                v[b].v[e] = there ? Elem<T>::down((float)(int8_t)(q[e >> 2] >> (e & 3) * 8) * by) : (T)0.f;
-        } else if (o.E) {
-            const bool there = m + b < o.M && n < o.N;
-            const int64_t at = there ? (m + b) * o.ldi + n : 0;
-            const u32x2 q = *reinterpret_cast<const u32x2*>(static_cast<const int8_t*>(o.in) + at);
-            const int field = o.E[at / KEEP_BLOCK];
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                v[b].v[e] = there ? Keep8<T>::value((int8_t)(q[e >> 2] >> (e & 3) * 8), field) : (T)0.f;
-        } else if (m + b < o.M && n + 8 <= o.N) {
-            u32x4 raw[8 / Elem<T>::PER16];
-#pragma unroll
-            for (int f = 0; f < 8 / Elem<T>::PER16; ++f) raw[f] = reinterpret_cast<const u32x4_any*>(row + n)[f];
-            __builtin_memcpy(v[b].v, raw, sizeof(raw));
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[b].v[e] = m + b < o.M && n + e < o.N ? row[n + e] : (T)0.f;
-        }
-    }
-    if (o.transposed) {  // the same for the whole workgroup
-        const TransposeTile<T> tile{lds};
-        tile.put(v[0].v, v[1].v);
-        __syncthreads();
-        tile.emit(static_cast<T*>(o.out) + n0 * o.pad + m0, o.N - n0, o.pad, o.pad - m0);
-    } else {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-            if (m + b < o.M && n < o.pad) *reinterpret_cast<Eight*>(static_cast<T*>(o.out) + (m + b) * o.pad + n) = v[b];
-    }
+    bring_operand(a, blockIdx.x, TransposeTile<T>{lds});
 }
 
 // out[M, N] (rows ldo apart) = the sum over z, in order, of parts[z, M, N].  out may be the first part.

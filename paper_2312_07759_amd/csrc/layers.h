@@ -47,7 +47,8 @@ constexpr int TP_INT8 = 3;  // beside idkm_dtype's
 TileShape tile_shape(int dtype, int which, int scaled);
 
 void launch_dense_rows(int dtype, const DenseArgs& a, hipStream_t s);
-void launch_dense_cols(int dtype, const DenseArgs& a, hipStream_t s);
+// also: operands to bring, in the same launch or in one before it
+void launch_dense_cols(int dtype, const DenseArgs& a, hipStream_t s, const OperandArgs& also);
 void allow_lds(const void* fn, size_t bytes);  // before a launch of fn with so much dynamic LDS
 // Up to three operands to a launch.
 void add_operand(OperandArgs* a, const void* in, int64_t ldi, int64_t M, int64_t N, void* out, int64_t pad, bool transposed,

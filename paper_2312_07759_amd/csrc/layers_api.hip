@@ -500,15 +500,15 @@ idkm_status gradients(idkm_ctx* ctx, const idkm_codes_desc* w, const Input& x, c
                 add_operand(&copies, dY, lddy, n, w->rows, ws + l.dy, l.pad, true);
                 add_operand(&copies, x.X, x.ld, n, w->cols, ws + l.x, l.pad, true, x.kept ? x.E : nullptr);
             }
-            launch_operands(w->dtype, copies, s);
+            if (!dX) launch_operands(w->dtype, copies, s);
             if (dX) {
-                for (int64_t c = 0; c < w->cols; c += d.panel) {
+                for (int64_t c = 0; c < w->cols; c += d.panel, copies.jobs = 0) {
                     DenseArgs a = dense_of(*w);
                     a.first = c;
                     a.count = w->cols - c < d.panel ? w->cols - c : d.panel;
                     a.pad = d.pad;
                     a.out = of_x + d.matrix;
-                    launch_dense_cols(w->dtype, a, s);
+                    launch_dense_cols(w->dtype, a, s, copies);
                     td.N = a.count;
                     float* parts = reinterpret_cast<float*>(of_x + d.parts);
                     if (together) set_out(d.plan, &td, dX, lddx, parts);
