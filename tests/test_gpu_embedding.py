@@ -133,6 +133,21 @@ def test_table(ctx, rows, cols, n, dtype):
     check(got, P, error(A, most))
 
 
+@pytest.mark.parametrize("kind", ["any", "text", "one", "none", "runs"])
+@pytest.mark.parametrize("rows,cols,n", [(40_001, 260, 600), (40_001, 260, 16_384), (9_001, 1001, 5000), (32_768, 256, 513), (40_001, 260, 16_385), (300, 32_000, 700)])
+def test_large_tables(ctx, rows, cols, n, kind):
+    """Rows without a token are zero in memory that held something else."""
+    torch.cuda.empty_cache()
+    held = torch.full((rows, cols), float("nan"), device="cuda")
+    del held
+    ids, dY = tokens(kind, n, rows, 2), draw((n, cols), torch.bfloat16, 3)
+    got = ctx.embedding_backward(dY.cuda(), ids.cuda(), rows, ALPHA)
+    some = ((ids >= 0) & (ids < rows)).nonzero()[:, 0]
+    P, A, most = by_row(ids, dY, rows)
+    check(got, P, error(A, most))
+    assert bool(got[ids[some].cuda()].isfinite().all())
+
+
 def test_rows_beyond_16_bits_of_the_sort(ctx):
     """Ids that differ in their high bits only, more than one launch ranks."""
     ids = torch.arange(20_000) % 5 * 65_536
