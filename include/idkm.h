@@ -319,7 +319,7 @@ idkm_status idkm_codes_linear_backward_kept(idkm_ctx* ctx, const idkm_codes_desc
  *   idkm_codes_embedding_backward  with P[v,c] = alpha sum of dY[t,c] over the tokens of v: dS[v,g] = sum over the group's columns of P[v,c]
  *                                  C[code, c mod d] (all rows are written) and dC[j,i] = the sum of S P over the components i of all sub-vectors
  *                                  with code j.  dC, dS may each be NULL (not wanted).
- * Tokens are sorted by row, and a row's sum is taken in the order of the tokens (in parts, in order, where there are many): results repeat.
+ * A row's sum is taken in the order of its tokens (in parts, in order, where there are many): results repeat.
  * n = 0 writes zeros to the gradients.  Types, strides, alignment, workspace, limits and enqueueing as for idkm_codes_linear; n <= 4,000,000.
  */
 idkm_status idkm_embedding(idkm_ctx* ctx, const float* W, int64_t rows, int64_t cols, const void* ids, int32_t id_bytes, int64_t n,
