@@ -8,9 +8,9 @@
 
 namespace idkm {
 
-// 301 tokens of a text, as these measure and sorted: float32, 734 columns, k = 100, d = 2 15.9 us and 19.4; bfloat16, 4096 columns, k = 16 14.7 and 18; a
-// table of 32000 x 1024 22.7 and 29.  512 tokens: 17.5 and 20.5, 18.1 and 18.2, 24.5 and 30; 1024: 29 and 21, 33 and 21, 27 and 31.  One row's tokens follow
-// one another here, 0.07 us each: 512 of the same row take 51 us, and 20 to 34 sorted.
+// Tokens of a text, taken so and sorted: 301 of float32, 734 columns, k = 100, d = 2 13.6 us and 17.9; bfloat16, 4096 columns, k = 16 16 and 17.7; a table of
+// 32000 x 1024 22.6 and 29.3.  512 of them: 15.2 and 18.5, 18.1 and 17.7, 24.2 and 29.9; 1024, when that was measured, 29 and 21, 33 and 21, 27 and 31.  One row's
+// tokens follow one another here, 0.07 us each: 512 of the same row take 49 us, and 17 to 33 sorted.
 constexpr int FEW_TOKENS = 512;
 
 // A lane's eight columns of rows of dY, from column c on.  The last lane of a row whose length is no multiple of eight takes the last eight columns, of which
