@@ -342,8 +342,10 @@ idkm_status idkm_codes_embedding_backward(idkm_ctx* ctx, const idkm_codes_desc* 
  *                              holds an infinity or NaN has scale NaN and integers 0.  (The layer's rows are made by it, too, from float32 weights.)
  *   idkm_int8_linear           Y[t,r] = s[t] scale[r] sum_c q[t,c] W8[r,c], with q and s what idkm_int8_rows gives for X.  The sum is exact; it is rounded to
  *                              float32, multiplied by s[t], by scale[r], and rounded to the type.
- *   idkm_int8_linear_backward  dX[t,c] = sum_r dY[t,r] scale[r] W8[r,c]: as if the tokens' integers were the tokens.  with 16-bit types
- *                              scale W8, with float32 dY scale is rounded to the type; sums are float32, results are rounded once.
+ *   idkm_int8_linear_backward  dX[t,c] = sum_r dY[t,r] scale[r] W8[r,c]: as if the tokens' integers were the tokens.  With bfloat16 scale W8 is
+ *                              rounded to the type, with float32 and float16 dY scale, with float16 after the token has been multiplied by a power of two
+ *                              (so that neither small nor large scales matter; terms below 2^-28 of the token's largest dY scale keep fewer bits).
+ *                              Sums are float32, results are rounded once.
  * W8 [rows, ldw]: rows a multiple of 128 elements apart, 16-byte aligned; what lies from column cols on counts for nothing.
  * Limits: rows, n <= 4,000,000, cols <= 131072 (sums of more would not fit 32 bits).  Types, strides, alignment, workspace and enqueueing as for idkm_codes_linear.
  */

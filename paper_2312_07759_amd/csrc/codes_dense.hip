@@ -124,8 +124,9 @@ void launch_operands(int dtype, const OperandArgs& a, hipStream_t s) {
     if (tiles > 0) BY_TYPE(dtype, T, hipLaunchKernelGGL(k_operands<T>, dim3((unsigned)tiles), dim3(256), 0, s, a));
 }
 
-void launch_join_parts(int dtype, const float* parts, int nz, int64_t M, int64_t N, void* out, int64_t ldo, hipStream_t s) {
-    BY_TYPE(dtype, T, hipLaunchKernelGGL(k_join_parts<T>, dim3(grid_for(M * N)), dim3(256), 0, s, parts, nz, M, N, static_cast<T*>(out), ldo));
+void launch_join_parts(int dtype, const float* parts, int nz, int64_t M, int64_t N, void* out, int64_t ldo, hipStream_t s,
+                       const float* by_m) {
+    BY_TYPE(dtype, T, hipLaunchKernelGGL(k_join_parts<T>, dim3(grid_for(M * N)), dim3(256), 0, s, parts, nz, M, N, static_cast<T*>(out), ldo, by_m));
 }
 
 void launch_codes_bins(int dtype, const BinArgs& args, int grid, int waves, hipStream_t s) {

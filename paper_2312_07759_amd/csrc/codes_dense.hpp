@@ -9,8 +9,8 @@ namespace idkm {
 //   rows        out[M, pad] = in[M, N], zero behind column N
 //   transposed  out[N, pad] = in[M, N]^T, zero behind column M
 // E: `in` is kept in 8 bits, rows ldi apart (see keep8.hpp), and brought back on the way.
-// scale: `in` holds 8-bit integers (rows ldi apart, a multiple of 16, zero behind column N), and comes out times its row's scale, rounded to T: an operand of the
-// matrix instruction, with the relative error, eps / 2 at most, of a weight stored in T.
+// scale (T bfloat16): `in` holds 8-bit integers (rows ldi apart, a multiple of 16), and comes out times its row's scale, rounded to T: an operand of the
+// matrix instruction, with the relative error, eps / 2 at most, of a weight stored in T, whose exponents are float32's.
 struct Operand {
     const void* in;
     int64_t ldi, M, N;
@@ -103,7 +103,7 @@ __device__ __forceinline__ void bring_operand(const OperandArgs& a, int64_t t, c
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
         const T* row = static_cast<const T*>(o.in) + (m + b) * o.ldi;
-        if (o.scale) {
+        if (__is_same(T, bf16) && o.scale) {
             const bool there = m + b < o.M && n < o.N;
             const u32x2 q = *reinterpret_cast<const u32x2*>(static_cast<const int8_t*>(o.in) + (there ? (m + b) * o.ldi + n : 0));
             const float by = o.scale[there ? m + b : 0];
@@ -407,15 +407,15 @@ __global__ __launch_bounds__(256) void k_operands(const OperandArgs a) {
     bring_operand(a, blockIdx.x, TransposeTile<T>{lds});
 }
 
-// out[M, N] (rows ldo apart) = the sum over z, in order, of parts[z, M, N].  out may be the first part.
+// out[M, N] (rows ldo apart) = the sum over z, in order, of parts[z, M, N], times by_m[m] if that is not null.  out may be the first part.
 template <typename T>
-__global__ __launch_bounds__(256) void k_join_parts(const float* parts, int nz, int64_t M, int64_t N, T* out, int64_t ldo) {
+__global__ __launch_bounds__(256) void k_join_parts(const float* parts, int nz, int64_t M, int64_t N, T* out, int64_t ldo, const float* by_m) {
     const int64_t total = M * N;
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += (int64_t)gridDim.x * 256) {
         float sum = parts[at];
         for (int z = 1; z < nz; ++z) sum += parts[z * total + at];
         const int64_t m = at / N;
-        out[m * ldo + (at - m * N)] = Elem<T>::down(sum);
+        out[m * ldo + (at - m * N)] = Elem<T>::down(by_m ? sum * by_m[m] : sum);
     }
 }
 

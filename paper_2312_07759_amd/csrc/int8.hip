@@ -283,6 +283,25 @@ void launch_int8_few(int dtype, const Int8FewArgs& a, hipStream_t s) {
     else BY_TYPE(dtype, T, (launch_few<T, 1, 16, false>(a, s)));
 }
 
+// The tile_at-th 64 x 64 tile of W8's columns, as numbers of T, which holds integers of eight bits.
+template <typename T>
+__device__ __forceinline__ void integer_columns(const Int8SplitArgs& a, int64_t tile_at, uint32_t* lds) {
+    const int64_t tiles_c = (a.cols + 63) / 64, tr = tile_at / tiles_c, r0 = tr * 64, c0 = (tile_at - tr * tiles_c) * 64;
+    const int64_t r = r0 + (threadIdx.x >> 3) * 2, c = c0 + (threadIdx.x & 7) * 8;
+    T v[2][8];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        const bool there = r + b < a.rows && c < a.cols;
+        const u32x2 q = *reinterpret_cast<const u32x2*>(a.W8 + (there ? (r + b) * a.ldw + c : 0));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[b][e] = there ? (T)(float)(int8_t)(q[e >> 2] >> (e & 3) * 8) : (T)0.f;
+    }
+    const TransposeTile<T> tile{lds};
+    tile.put(v[0], v[1]);
+    __syncthreads();
+    tile.emit(static_cast<T*>(a.B) + c0 * a.pad + r0, a.cols - c0, a.pad, a.pad - r0);
+}
+
 // dX of float32: x = dY scale is the sum of three numbers of bfloat16, its upper, middle and lower eight bits (cut off, so that no part becomes infinite;
 // below 2^-110 the lowest may be lost), and integers of eight bits are numbers of bfloat16.  The float32 product is thus one of bfloat16 with three times the rows, exact but
 // for its float32 sums, three of which make a result.  1001 x 1000 x 512: 22 us; by float32 matrix instructions, a ninth as many a second, 26.7.
@@ -294,7 +313,7 @@ __global__ __launch_bounds__(256) void k_int8_split(const Int8SplitArgs a) {
             const int64_t t = pieces >> 31 ? at / per_row : (unsigned)at / (unsigned)per_row, r = (at - t * per_row) * 8;
             float x[8];
             float by[8];
-            eight_floats(x, a.dY + t * a.ldy, r, a.rows);
+            eight_floats(x, static_cast<const float*>(a.dY) + t * a.ldy, r, a.rows);
             eight_floats(by, a.scale, r, a.rows);
             u32x4 part[3];
 #pragma unroll
@@ -316,20 +335,7 @@ __global__ __launch_bounds__(256) void k_int8_split(const Int8SplitArgs a) {
         }
         return;
     }
-    const int64_t tiles_c = (a.cols + 63) / 64, tile_at = blockIdx.x - a.splitting, tr = tile_at / tiles_c, r0 = tr * 64, c0 = (tile_at - tr * tiles_c) * 64;
-    const int64_t r = r0 + (threadIdx.x >> 3) * 2, c = c0 + (threadIdx.x & 7) * 8;
-    bf16 v[2][8];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const bool there = r + b < a.rows && c < a.cols;
-        const u32x2 q = *reinterpret_cast<const u32x2*>(a.W8 + (there ? (r + b) * a.ldw + c : 0));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[b][e] = there ? (bf16)(float)(int8_t)(q[e >> 2] >> (e & 3) * 8) : (bf16)0.f;
-    }
-    const TransposeTile<bf16> tile{lds};
-    tile.put(v[0], v[1]);
-    __syncthreads();
-    tile.emit(static_cast<bf16*>(a.B) + c0 * a.pad + r0, a.cols - c0, a.pad, a.pad - r0);
+    integer_columns<bf16>(a, blockIdx.x - a.splitting, lds);
 }
 
 void launch_int8_split(const Int8SplitArgs& args, bool dY, hipStream_t s) {
@@ -337,6 +343,71 @@ void launch_int8_split(const Int8SplitArgs& args, bool dY, hipStream_t s) {
     const int64_t groups = (a.n * (a.pad / 8) + 255) / 256, tiles = ((a.cols + 63) / 64) * ((a.pad + 63) / 64);
     a.splitting = dY ? (unsigned)(groups < 4096 ? groups : 4096) : 0u;
     hipLaunchKernelGGL(k_int8_split, dim3(a.splitting + (unsigned)tiles), dim3(256), 0, s, a);
+}
+
+// dX of float16: x = dY scale times a power of two 2^f of its token's, with which the token's largest is 2^14 to 2^15, rounded to float16, and integers as numbers of
+// float16; the product's epilogue (or its join) multiplies by 2^-f.  Scale W8 in float16 would be none at all for layers of small weights, and infinite beyond 65504.
+// Rounded by half a step, so are x down to 2^-28 of the token's largest; smaller ones by 2^-39 of it.  A workgroup to a token, as in k_int8_rows.
+// f <= 126, so that 2^-f is a normal number: of smaller tokens the results are zero.
+// 2048 x 4096 x 4096: 81 us in all, 1001 x 1000 x 512 13.7 (with dY as it is and scale W8 78; two parts of bfloat16 instead of one of float16
+// 142 and 17.7).
+__global__ __launch_bounds__(256) void k_int8_half(const Int8SplitArgs a) {
+    constexpr int HELD = 2;
+    __shared__ __align__(16) uint32_t lds[TransposeTile<f16>::WORDS];
+    if (blockIdx.x >= a.splitting) {
+        integer_columns<f16>(a, blockIdx.x - a.splitting, lds);
+        return;
+    }
+    const int64_t t = blockIdx.x;
+    const f16* row = static_cast<const f16*>(a.dY) + t * a.ldy;
+    uint32_t top = 0;  // bits of the largest finite size
+    auto ask = [&](float* x, int64_t r) {
+        float by[8];
+        eight_floats(x, row, r, a.rows);
+        eight_floats(by, a.scale, r, a.rows);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= by[e];
+    };
+    auto look = [&](const float* x) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = size_of(x[e]) < 0x7f800000 ? max(top, size_of(x[e])) : top;
+    };
+    float x[HELD][8];
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) ask(x[h], (h * 256 + threadIdx.x) * 8);
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) look(x[h]);
+    for (int64_t r = (HELD * 256 + threadIdx.x) * 8; r < a.rows; r += 2048) {
+        float y[8];
+        ask(y, r);
+        look(y);
+    }
+    top = larger_of_wave(top);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = max(max(lds[0], lds[1]), max(lds[2], lds[3]));
+    const int f = min(127 + 14 - (int)(top >> 23), 126);
+    if (threadIdx.x == 0) a.by[t] = ldexpf(1.f, -f);
+    f16* out = static_cast<f16*>(a.A) + t * a.pad;
+    auto put = [&](const float* v, int64_t r) {
+        struct alignas(16) Eight { f16 v[8]; } y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y.v[e] = Elem<f16>::down(ldexpf(v[e], f));
+        if (r < a.pad) *reinterpret_cast<Eight*>(out + r) = y;
+    };
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) put(x[h], (h * 256 + threadIdx.x) * 8);
+    for (int64_t r = (HELD * 256 + threadIdx.x) * 8; r < a.pad; r += 2048) {
+        float y[8];
+        ask(y, r);
+        put(y, r);
+    }
+}
+
+void launch_int8_half(const Int8SplitArgs& args, bool dY, hipStream_t s) {
+    Int8SplitArgs a = args;
+    a.splitting = dY ? (unsigned)a.n : 0u;
+    hipLaunchKernelGGL(k_int8_half, dim3(a.splitting + (unsigned)(((a.cols + 63) / 64) * ((a.pad + 63) / 64))), dim3(256), 0, s, a);
 }
 
 template <typename T>

@@ -54,7 +54,8 @@ void allow_lds(const void* fn, size_t bytes);  // before a launch of fn with so 
 void add_operand(OperandArgs* a, const void* in, int64_t ldi, int64_t M, int64_t N, void* out, int64_t pad, bool transposed,
                  const uint8_t* E = nullptr, const float* scale = nullptr);
 void launch_operands(int dtype, const OperandArgs& a, hipStream_t s);
-void launch_join_parts(int dtype, const float* parts, int nz, int64_t M, int64_t N, void* out, int64_t ldo, hipStream_t s);
+// by_m: factors [M] of the rows, or null.
+void launch_join_parts(int dtype, const float* parts, int nz, int64_t M, int64_t N, void* out, int64_t ldo, hipStream_t s, const float* by_m = nullptr);
 void launch_codes_bins(int dtype, const BinArgs& a, int grid, int waves, hipStream_t s);
 int bins_shared_by(int k);
 void launch_codes_bins_runs(int dtype, const BinArgs& a, bool wide, int grid, int waves, hipStream_t s);
@@ -90,19 +91,22 @@ struct Int8FewArgs {
 };
 constexpr int64_t INT8_FUSED = 4 * 8192;  // elements of X, in whole steps of 128 columns, that a workgroup brings to integers itself, at most
 void launch_int8_few(int dtype, const Int8FewArgs& a, hipStream_t s);
-// Operands of the gradient of a float32 product: dY times the scales in three parts of 16 bits, and columns of W8 in 16 bits.
+// Operands of the gradient of a product, float32: dY times the scales in three parts of 16 bits, and columns of W8 in 16 bits; float16: the same in one part,
+// every token divided by a power of two.
 struct Int8SplitArgs {
-    const float* dY;  // [n, ldy]
+    const void* dY;  // T [n, ldy]
     int64_t n, ldy, rows;
     const float* scale;  // [rows]
     const int8_t* W8;    // [rows, ldw], from the first column that is wanted on
     int64_t ldw, cols;
-    void* A;      // bf16 [3, n, pad], zero behind column `rows`
-    void* B;      // bf16 [cols, pad]
+    void* A;      // bf16 [3, n, pad] or f16 [n, pad], zero behind column `rows`
+    void* B;      // [cols, pad], A's type
     int64_t pad;  // a multiple of 64
+    float* by;    // float16: [n], the powers of two
     unsigned splitting;  // workgroups, set by the launch
 };
 void launch_int8_split(const Int8SplitArgs& a, bool dY, hipStream_t s);  // dY: A too, or B alone
+void launch_int8_half(const Int8SplitArgs& a, bool dY, hipStream_t s);   // .. of float16
 // out[M, N] in the type of dtype = by_m by_n times the sum of the parts [nz][M, N].
 void launch_join_int8(int dtype, const int32_t* parts, int nz, int64_t M, int64_t N, const float* by_m, const float* by_n, void* out, int64_t ldo,
                       hipStream_t s);

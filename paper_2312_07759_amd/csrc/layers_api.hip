@@ -288,7 +288,7 @@ void set_out(const TilePlan& p, TileArgs* a, void* out, int64_t ldo, float* part
 void run_product(int dtype, const TilePlan& p, TileArgs a, void* out, int64_t ldo, float* parts, hipStream_t s) {
     set_out(p, &a, out, ldo, parts);
     run_tiles(dtype, p, a, s);
-    if (p.parts > 1) launch_join_parts(dtype, parts, p.parts, a.M, a.N, out, ldo, s);
+    if (p.parts > 1) launch_join_parts(dtype, parts, p.parts, a.M, a.N, out, ldo, s, a.by_m);
 }
 
 int64_t panel_of(int64_t lines, int64_t length) {
@@ -629,6 +629,16 @@ SplitLayout split_layout(const idkm_int8_desc& w, int64_t n) {
     return l;
 }
 
+// .. of a product in 16 bits: with float16 the tokens' powers of two behind it (see k_int8_half).
+ProductLayout narrow_layout(const idkm_int8_desc& w, int64_t n) {
+    ProductLayout l = product_layout(w.dtype, n, w.cols, w.rows);
+    if (w.dtype == IDKM_F16) {
+        l.scales = l.bytes;
+        l.bytes += buffer(n, 4);
+    }
+    return l;
+}
+
 const char* wrong_scale_shape(int64_t rows, int64_t cols, int64_t group) {
     if (rows < 0 || cols < 1) return "need rows >= 0 and cols >= 1";
     if (group < 1) return "group must be >= 1";
@@ -838,7 +848,7 @@ idkm_status idkm_int8_linear(idkm_ctx* ctx, const idkm_int8_desc* w, const void*
 
 int64_t idkm_int8_linear_backward_workspace(const idkm_int8_desc* w, int64_t n) {
     if (wrong_int8(nullptr, w, n)) return -1;
-    return n == 0 ? 0 : w->dtype == IDKM_F32 ? split_layout(*w, n).bytes : product_layout(w->dtype, n, w->cols, w->rows).bytes;
+    return n == 0 ? 0 : w->dtype == IDKM_F32 ? split_layout(*w, n).bytes : narrow_layout(*w, n).bytes;
 }
 
 idkm_status idkm_int8_linear_backward(idkm_ctx* ctx, const idkm_int8_desc* w, const void* dY, int64_t lddy, int64_t n, void* dX, int64_t lddx,
@@ -868,7 +878,7 @@ idkm_status idkm_int8_linear_backward(idkm_ctx* ctx, const idkm_int8_desc* w, co
                 t.out = parts;
                 for (int64_t c = 0; c < w->cols; c += l.panel) {
                     t.N = t.ldo = w->cols - c < l.panel ? w->cols - c : l.panel;
-                    launch_int8_split(Int8SplitArgs{static_cast<const float*>(dY), n, lddy, w->rows, w->scale, w->W8 + c, w->ldw, t.N, ws, ws + l.matrix, l.pad, 0},
+                    launch_int8_split(Int8SplitArgs{dY, n, lddy, w->rows, w->scale, w->W8 + c, w->ldw, t.N, ws, ws + l.matrix, l.pad, nullptr, 0},
                                       c == 0, s);
                     run_tiles(IDKM_BF16, l.plan, t, s);
                     // the parts of the sum, three of each
@@ -876,17 +886,28 @@ idkm_status idkm_int8_linear_backward(idkm_ctx* ctx, const idkm_int8_desc* w, co
                 }
             });
         }
-        const ProductLayout l = product_layout(w->dtype, n, w->cols, w->rows);
+        const ProductLayout l = narrow_layout(*w, n);
         if (const char* e = wrong_workspace(workspace, workspace_bytes, l.bytes)) return refuse(ctx, IDKM_ERR_INVALID_ARG, e);
+        const bool half = w->dtype == IDKM_F16;
         return launched(ctx, [&] {
             TileArgs t{};
             OperandArgs copies{};
             operand_of(w->dtype, dY, lddy, n, w->rows, l, ws, &t, &copies);
+            float* by = reinterpret_cast<float*>(ws + l.scales);
+            if (half) {
+                t.A = ws + l.operand;
+                t.lda = l.pad;
+                t.by_m = by;
+            }
             for (int64_t c = 0; c < w->cols; c += l.panel) {
                 t.N = w->cols - c < l.panel ? w->cols - c : l.panel;
-                add_operand(&copies, w->W8 + c, w->ldw, w->rows, t.N, ws + l.matrix, l.pad, true, nullptr, w->scale);
-                launch_operands(w->dtype, copies, s);
-                copies.jobs = 0;
+                if (half) {
+                    launch_int8_half(Int8SplitArgs{dY, n, lddy, w->rows, w->scale, w->W8 + c, w->ldw, t.N, ws + l.operand, ws + l.matrix, l.pad, by, 0}, c == 0, s);
+                } else {
+                    add_operand(&copies, w->W8 + c, w->ldw, w->rows, t.N, ws + l.matrix, l.pad, true, nullptr, w->scale);
+                    launch_operands(w->dtype, copies, s);
+                    copies.jobs = 0;
+                }
                 run_product(w->dtype, l.plan, t, static_cast<unsigned char*>(dX) + c * es, lddx, reinterpret_cast<float*>(ws + l.parts), s);
             }
         });

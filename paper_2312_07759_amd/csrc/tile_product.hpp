@@ -32,6 +32,7 @@ struct TileArgs {
     int groups;
     int group;  // in steps (SC = 1) or in half steps (SC = 2)
     // 8-bit integers, not wide: out[m, n] = by_m[m] by_n[n] sum, in the type that `dtype` names
+    // float16 without scales, not wide: out[m, n] = by_m[m] sum where by_m is not null
     const float* by_m;
     const float* by_n;
     int dtype;
@@ -333,7 +334,8 @@ __global__ __launch_bounds__(64 * WM * WN, SC > 0 ? 2 : 1) void k_tile_product(c
                 if (a.wide) {
                     store_four(static_cast<float*>(a.out) + ((int64_t)z * a.M + m) * a.ldo + n, v, quad, a.N - n);
                 } else {
-                    const T w[4] = {Elem<T>::down(v[0]), Elem<T>::down(v[1]), Elem<T>::down(v[2]), Elem<T>::down(v[3])};
+                    const float by = __is_same(T, f16) && SC == 0 && a.by_m ? a.by_m[m] : 1.f;
+                    const T w[4] = {Elem<T>::down(v[0] * by), Elem<T>::down(v[1] * by), Elem<T>::down(v[2] * by), Elem<T>::down(v[3] * by)};
                     store_four(static_cast<T*>(a.out) + m * a.ldo + n, w, quad, a.N - n);
                 }
             }
