@@ -194,7 +194,7 @@ class CodesLinear(torch.nn.Module):
         _no_capture(X, self.C, self.S)
         tracked = torch.is_grad_enabled() and (X.requires_grad or self.C.requires_grad or (self.S is not None and self.S.requires_grad))
         layer = self.layer(X.dtype, copy=tracked)
-        return _CodesProduct.apply(_as_rows(X.reshape(-1, self.cols)), self.C, self.S, layer, self.keep8).view(*X.shape[:-1], self.rows)
+        return _CodesProduct.apply(_as_rows(X.reshape(-1, self.cols)), self.C, self.S, layer, self.keep8 and tracked).view(*X.shape[:-1], self.rows)
 
 
 def _ids(ids):
