@@ -290,9 +290,10 @@ idkm_status idkm_codes_linear_backward(idkm_ctx* ctx, const idkm_codes_desc* w, 
 
 /*
  * Activations kept in 8 bits between a forward and a backward pass.  Every 32 columns of a row (the last ones of a row may be fewer) share a
- * power of two 2^e: x is kept as q 2^e with whole q in [-127, 127], which is a number of x's own type.  e is the smallest with which the 32 largest
- * size, rounded to the nearest (ties to even), is at most 127, so that no error is larger than 2^e / 2 (1/128 of that size); e >= -132, and in the
- * last binade of the type, where a larger power could round to infinity, larger quotients are cut to 127 (an error of 2^e at most).
+ * power of two 2^e: x is kept as q 2^e with whole q in [-127, 127], which is a number of x's own type.  e is the smallest with which the block's
+ * largest size, divided by 2^e and rounded to the nearest (ties to even), is at most 127, so that no error is larger than 2^e / 2, at most 1/127.5 of that
+ * size.  e >= -132: in blocks below 2^-126 errors are up to 2^-133, however small the numbers.  In the last binade of the type, where a larger power could
+ * round to infinity, larger quotients are cut to 127 (an error of 2^e at most).
  * q = -128 stands for an infinity or NaN of x, which has no part in e and comes back as NaN.
  *   idkm_keep8      X [n, cols] (rows ldx apart) -> Q int8 [n, 32 b] (zero behind column cols), 8-byte aligned, and E [n, b], e + 133, b = ceil(cols / 32)
  *   idkm_restore8   X_out = q 2^e, exactly
