@@ -96,3 +96,24 @@ def test_nan_with_only_low_bits(ctx):
     dY.view(torch.int32)[1, 5] = 0x7f800001
     dX = ctx.int8_linear_backward(binding.Int8Layer(torch.ones(20, 130, dtype=torch.int8, device="cuda"), torch.ones(20, device="cuda"), torch.float32), dY)
     assert bool(dX[1].isnan().all()) and bool((dX[[0, 2]] == 20).all())
+
+
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+@pytest.mark.parametrize("n,rows,cols", [(5, 4097, 70), (3, 8200, 130), (2, 300_000, 520), (70_001, 40, 24)])
+def test_long_layers_and_many_tokens(ctx, n, rows, cols, dtype):
+    """More rows than a workgroup holds of a token, layers that are written out in panels of columns, tokens beyond 16 bits."""
+    t = DTYPES[dtype]
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    W8 = torch.randint(-127, 128, (rows, cols), generator=g, device="cuda", dtype=torch.int8)
+    scale = torch.exp(torch.randn(rows, generator=g, device="cuda") - 5)
+    dY = torch.randn(n, rows, generator=g, device="cuda").to(t)
+    got = ctx.int8_linear_backward(binding.Int8Layer(W8, scale, t), dY)
+    ref = torch.zeros(n, cols, dtype=torch.float64, device="cuda")
+    terms = torch.zeros_like(ref)
+    for r in range(0, rows, 50_000):
+        w, y = W8[r:r + 50_000].double() * scale[r:r + 50_000].double()[:, None], dY[:, r:r + 50_000].double()
+        ref += y @ w
+        terms += y.abs() @ w.abs()
+    half = HALF_STEP[t]
+    bound = half * ref.abs() + (half + 2.0 ** -23) * terms + 2 * sum_error(terms, rows)
+    check(got, ref.cpu(), (bound + (2.0 ** -25 if t == torch.float16 else 0.0)).cpu())
