@@ -140,8 +140,8 @@ __device__ __forceinline__ void bring_operand(const OperandArgs& a, int64_t t, c
 }
 
 // Eight columns of a row of the layer on their way: asked for, and brought to T.  Where the weights are scaled here (columns, for dX, along
-// whose sum every weight has another scale; and float32) each is rounded once: it is an operand of the matrix instruction, and the
-// relative error, eps / 2 at most, is that of a weight stored in T.  Zeros behind the last column.
+// whose sum every weight has another scale; and float32) each is rounded once: it is an operand of the matrix instruction, and its
+// error is that of a weight stored in T: eps / 2 of it at most, in float16 half a subnormal step below 2^-14, and infinite beyond 65504.  Zeros behind the last column.
 template <typename T, int IB, int W, bool ALIGNED>
 struct EightOfLayer {
     static constexpr int NB = 8 / W * IB;
